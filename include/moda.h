@@ -524,6 +524,71 @@ int moda_depth_slot_mass(const void* Q, const void* depth_kv, const float* LSE,
                          int B, int T, int H, int H_kv, int d, int l, float scale,
                          float* mass, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * ---- Serving: the attention weight of cached keys, eviction by it, and a prefix that a batch shares ----
+ *
+ * The sequence cache of a serving program grows by a row per token and is read whole for each.  These calls measure which of its keys
+ * the queries use, cut a cache to the keys that are used most, and let the sequences of a batch that continue one prompt read its
+ * cache once.  A weight ("mass") is a probability of the operator's one softmax over sequence and depth keys, summed over
+ * the query rows and over the query heads of a group: fp32 [B][H_kv][T_cap], beside a cache K, V of [B][T_cap][H_kv][d].
+ *
+ * moda_attn_key_mass      after a forward of T_q rows at the end of T_kv keys (moda_attn_fwd_prefill; T_q = T_kv: any forward), with its LSE:
+ *
+ *     mass[b, hk, j] = old + sum_{h in group hk} sum_{i : i + T_kv - T_q >= j} exp( scale <Q[b,i,h,:], K[b,j,hk,:]> - LSE[b,h,i] )
+ *
+ *     Q        : bf16 [B][T_q][H][d]        K : bf16 [B][T_cap][H_kv][d], rows [0, T_kv) read
+ *     LSE      : fp32 [B][H][T_q], of the forward of these rows; a row whose LSE is -inf (it saw no key) has no weight
+ *     mass_in  : NULL, or the weights before the call, of which the positions before the T_q new ones (j < T_kv - T_q) are read: `old`; may be `mass`
+ *     mass     : positions [0, T_kv) written
+ *     workspace: moda_key_mass_workspace_bytes
+ *   To rate the keys by the last rows of a prompt only, pass those rows of Q and LSE.  Sums in a fixed order (bit-reproducible).  Two launches.
+ *
+ * moda_attn_decode_mass   moda_attn_decode (seq_lens NULL) or moda_attn_decode_varlen that also writes
+ *
+ *     mass[b, hk, j] = (j < len - 1 ? mass_in[b, hk, j] : 0) + sum_{h in group hk} exp( scale <q[b,h,:], K[b,j,hk,:]> - LSE[b,h] )     j < len
+ *
+ *   (the last key is the token's own, which the accumulator does not hold yet).  mass_in may be NULL (all 0) or `mass`.
+ *   workspace: moda_decode_mass_workspace_bytes.  O and LSE as from the plain call.
+ *
+ * moda_kv_evict           the cut.  Of the len = seq_lens[b] (NULL: T; each 0 .. T) keys of (b, hk), kept = min(n_keep, len) stay: the last
+ *                         min(n_recent, kept), and of the others those of largest weight (equal weights: the lower position; NaN
+ *                         counts as less than any number).  They keep their order.
+ *     K, V     : bf16 [B][T_cap][H_kv][d]       mass : fp32 [B][H_kv][T_cap]; neither is changed
+ *     K_out, V_out : bf16 [B][T_out][H_kv][d], T_out >= n_keep; rows [0, kept) written; must not overlap K, V (MODA_ERR_BAD_SHAPE)
+ *     mass_out : fp32 [B][H_kv][T_out], rows [0, kept) written, or NULL       index : int32 [B][H_kv][n_keep], old positions of the kept rows, -1 behind them
+ *     lens_out : int32 [B], kept, or NULL
+ *   1 <= n_keep, 0 <= n_recent <= n_keep.  The positions of a head differ from another's: positional information has to be in the keys.  Two launches.
+ *
+ * moda_attn_decode_shared decode step of B sequences over a prefix that all share, each sequence's own cache, and the token's depth pairs, under
+ *                         one softmax; the prefix is read once for the batch.
+ *     K_prefix, V_prefix : bf16 [T_prefix][H_kv][d], T_prefix >= 0
+ *     K, V     : bf16 [B][T_cap][H_kv][d], the sequences' own positions; seq_lens : int32 [B], each 0 .. max_seq_len, or NULL: max_seq_len for all.
+ *                max_seq_len may be 0 (K, V are not read then)
+ *     depth_kv_token : as for moda_attn_decode
+ *   A token without any key (T_prefix = 0, len = 0, l = 0) has O = 0 and LSE = -inf.  workspace: moda_decode_shared_workspace_bytes.
+ *   At most three launches.
+ *
+ * Supported heads, widths, depths and scales, ownership, asynchrony and error codes as for moda_attn_decode.  The workspace queries are host
+ * arithmetic and return 0 for an unsupported shape.
+ */
+size_t moda_key_mass_workspace_bytes(int B, int T_q, int T_kv, int H, int H_kv, int d);
+int moda_attn_key_mass(const void* Q, const void* K, const float* LSE, const float* mass_in,
+                       int B, int T_q, int T_kv, int T_cap, int H, int H_kv, int d, float scale,
+                       float* mass, void* workspace, size_t workspace_bytes, void* stream);
+size_t moda_decode_mass_workspace_bytes(int B, int max_seq_len, int H, int H_kv, int d);
+int moda_attn_decode_mass(const void* q, const void* K, const void* V, const int* seq_lens,
+                          const void* depth_kv_token, const float* mass_in,
+                          int B, int max_seq_len, int T_cap, int H, int H_kv, int d, int l, float scale,
+                          void* O, float* LSE, float* mass, void* workspace, size_t workspace_bytes, void* stream);
+int moda_kv_evict(const void* K, const void* V, const float* mass, const int* seq_lens,
+                  int B, int T, int T_cap, int H_kv, int d, int n_keep, int n_recent, int T_out,
+                  void* K_out, void* V_out, float* mass_out, int* index, int* lens_out, void* stream);
+size_t moda_decode_shared_workspace_bytes(int B, int T_prefix, int H, int H_kv, int d);
+int moda_attn_decode_shared(const void* q, const void* K_prefix, const void* V_prefix,
+                            const void* K, const void* V, const int* seq_lens, const void* depth_kv_token,
+                            int B, int T_prefix, int max_seq_len, int T_cap, int H, int H_kv, int d, int l, float scale,
+                            void* O, float* LSE, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -418,3 +418,57 @@ def depth_slot_mass(Q, Kd, LSE, scale):
             u = scale * np.einsum("btd,btd->bt", Q[:, :, hq, :], Kd[i, :, :, hq // G, :])      # [B, T]
             mass[:, hq, i] = np.exp(u - LSE[:, hq, :]).sum(axis=1)
     return mass
+
+
+# ---------------------------------------------------------------------------------------
+# Serving: attention weight of the sequence keys, eviction by it, and a decode step over a shared prefix.  Definitions
+# written out in numpy float64.
+# ---------------------------------------------------------------------------------------
+def key_mass(Q, K, LSE, scale):
+    """mass [B, Hk, T_kv] from Q [B, T_q, Hq, d] (the last T_q positions), K [B, T_kv, Hk, d] and LSE [B, Hq, T_q]: the probability that the
+    rows which see a key, and the heads of its group, give to it.  A row whose LSE is -inf has no key and no weight."""
+    Q, K, LSE = (np.asarray(x, dtype=np.float64) for x in (Q, K, LSE))
+    B, T_q, Hq, d = Q.shape
+    T_kv, Hk = K.shape[1], K.shape[2]
+    if K.shape != (B, T_kv, Hk, d) or Hq % Hk or T_kv < T_q or LSE.shape != (B, Hq, T_q):
+        raise ValueError("K must be [B, T_kv >= T_q, Hk, d] with Hk dividing Hq, LSE [B, Hq, T_q]")
+    G, off = Hq // Hk, T_kv - T_q
+    mass = np.zeros((B, Hk, T_kv))
+    for b in range(B):
+        for h in range(Hq):
+            for i in range(T_q):
+                if LSE[b, h, i] == -np.inf:
+                    continue
+                s = (K[b, :i + off + 1, h // G] @ Q[b, i, h]) * float(scale)
+                mass[b, h // G, :i + off + 1] += np.exp(s - LSE[b, h, i])
+    return mass
+
+
+def kept_positions(mass, n_keep, n_recent):
+    """Positions, ascending, that stay of a sequence's keys with the weights `mass` [len]: the last min(n_recent, kept), and the others by weight
+    (ties: the lower position; NaN below every number), kept = min(n_keep, len) in all."""
+    mass = np.asarray(mass, dtype=np.float64)
+    n = mass.shape[0]
+    kept = min(int(n_keep), n)
+    recent = min(int(n_recent), kept)
+    old = sorted(range(n - recent), key=lambda j: (np.isnan(mass[j]), 0.0 if np.isnan(mass[j]) else -mass[j], j))
+    return sorted(old[:kept - recent]) + list(range(n - recent, n))
+
+
+def decode_shared(q, Kp, Vp, K, V, lens, kd, vd, scale):
+    """o [B,Hq,d] and lse [B,Hq] for q [B,Hq,d]: one softmax over Kp [P,Hk,d], the first lens[b] rows of K [B,T,Hk,d] and kd [l,B,Hk,d].  A row
+    without keys has o = 0, lse = -inf."""
+    q, Kp, Vp, K, V = (np.asarray(x, dtype=np.float64) for x in (q, Kp, Vp, K, V))
+    B, Hq, d = q.shape
+    o, lse = np.zeros((B, Hq, d)), np.full((B, Hq), -np.inf)
+    for b in range(B):
+        keys = np.concatenate([Kp, K[b, :lens[b]]])[None]
+        values = np.concatenate([Vp, V[b, :lens[b]]])[None]
+        own = [None if x is None or len(x) == 0 else np.asarray(x)[:, b:b + 1] for x in (kd, vd)]
+        if keys.shape[1] == 0:                       # the depth pairs alone: one of them takes the place of the sequence keys
+            if own[0] is None:
+                continue
+            keys, values = own[0][:1, 0][None], own[1][:1, 0][None]
+            own = [x[1:] if len(x) > 1 else None for x in own]
+        o[b:b + 1], lse[b:b + 1] = decode_gqa(q[b:b + 1], keys, values, own[0], own[1], scale)
+    return o, lse

@@ -37,6 +37,10 @@ SYMBOLS = (
     "moda_attn_fwd_append_e4m3",
     "moda_depth_slot_mass_workspace_bytes",
     "moda_depth_slot_mass",
+    "moda_key_mass_workspace_bytes", "moda_attn_key_mass",
+    "moda_decode_mass_workspace_bytes", "moda_attn_decode_mass",
+    "moda_kv_evict",
+    "moda_decode_shared_workspace_bytes", "moda_attn_decode_shared",
 )
 MODA_STATIC_SCRATCH_ROWS = 1 << 20
 MODA_BWD_STAGE_ROWTERMS, MODA_BWD_STAGE_DQ, MODA_BWD_STAGE_DKDV, MODA_BWD_ALL_STAGES = 1, 2, 4, 7
@@ -142,6 +146,20 @@ def load() -> ctypes.CDLL:
     lib.moda_depth_slot_mass.argtypes = [vp, vp, vp, ci, ci, ci, ci, ci, ci, ctypes.c_float, vp, vp, ctypes.c_size_t, vp]
     lib.moda_kv_project_append_e4m3.restype = ci
     lib.moda_kv_project_append_e4m3.argtypes = [vp, vp, vp, ci, ci, ci, ci, ci, vp, vp, vp, ci, vp]
+    lib.moda_key_mass_workspace_bytes.restype = sz
+    lib.moda_key_mass_workspace_bytes.argtypes = [ci] * 6
+    lib.moda_attn_key_mass.restype = ci
+    lib.moda_attn_key_mass.argtypes = [vp] * 4 + [ci] * 7 + [cf] + [vp] * 2 + [sz, vp]
+    lib.moda_decode_mass_workspace_bytes.restype = sz
+    lib.moda_decode_mass_workspace_bytes.argtypes = [ci] * 5
+    lib.moda_attn_decode_mass.restype = ci
+    lib.moda_attn_decode_mass.argtypes = [vp] * 6 + [ci] * 7 + [cf] + [vp] * 4 + [sz, vp]
+    lib.moda_kv_evict.restype = ci
+    lib.moda_kv_evict.argtypes = [vp] * 4 + [ci] * 8 + [vp] * 6
+    lib.moda_decode_shared_workspace_bytes.restype = sz
+    lib.moda_decode_shared_workspace_bytes.argtypes = [ci] * 5
+    lib.moda_attn_decode_shared.restype = ci
+    lib.moda_attn_decode_shared.argtypes = [vp] * 7 + [ci] * 8 + [cf] + [vp] * 3 + [sz, vp]
     _lib = lib
     return lib
 
@@ -766,4 +784,134 @@ def moda_attn_decode_paged(q, K_pages, V_pages, block_table, seq_lens, depth_kv_
                                          float(scale), _ptr(O), _ptr(LSE), _ptr(workspace),
                                          workspace.numel() * workspace.element_size(), _stream(stream)),
            "moda_attn_decode_paged")
+    return O, LSE
+
+
+def moda_key_mass_workspace_bytes(B, T_q, T_kv, H, H_kv, d) -> int:
+    return int(load().moda_key_mass_workspace_bytes(B, T_q, T_kv, H, H_kv, d))
+
+
+def _mass(t, name, shape):
+    if t.dtype != torch.float32 or tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be an fp32 tensor of shape {shape}")
+    return t
+
+
+def moda_attn_key_mass(Q, K, LSE, scale, T_kv=None, mass_in=None, mass=None, workspace=None, stream=None):
+    """Attention weight of the cached keys: mass [B,H_kv,T_cap] fp32, what the rows Q [B,T_q,H,d] at the end of the first T_kv (None: all)
+    rows of K [B,T_cap,H_kv,d] gave to each of those keys, summed over the rows and the heads of a group, with the LSE [B,H,T_q] of their
+    forward; added to ``mass_in`` (which may be ``mass``) for the positions before the T_q rows.  Positions past T_kv are not touched."""
+    B, T_q, H, d = _bthd(Q, "Q")
+    Bk, T_cap, Hk, dk = _bthd(K, "K")
+    if (Bk, dk) != (B, d):
+        raise ValueError("K must be a bf16 [B, T_cap, H_kv, d] tensor matching Q's B and d")
+    T_kv = T_cap if T_kv is None else int(T_kv)
+    if tuple(LSE.shape) != (B, H, T_q):
+        raise ValueError("LSE must be an fp32 [B, H, T_q] tensor")
+    mass = _new((B, Hk, T_cap), torch.float32, Q.device, stream) if mass is None else _mass(mass, "mass", (B, Hk, T_cap))
+    if mass_in is not None:
+        _mass(mass_in, "mass_in", (B, Hk, T_cap))
+    if workspace is None:
+        workspace = _new((max(moda_key_mass_workspace_bytes(B, T_q, T_kv, H, Hk, d), 16),), torch.uint8, Q.device, stream)
+    _check(load().moda_attn_key_mass(_ptr(Q), _ptr(K), _f32(LSE, B * H * T_q), _ptr(mass_in), B, T_q, T_kv, T_cap, H, Hk, d, float(scale),
+                                     _ptr(mass), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
+           "moda_attn_key_mass")
+    return mass
+
+
+def moda_decode_mass_workspace_bytes(B, max_seq_len, H, H_kv, d) -> int:
+    return int(load().moda_decode_mass_workspace_bytes(B, max_seq_len, H, H_kv, d))
+
+
+def _decode_shapes(q, K, V, seq_lens, depth_kv_token, l):
+    if q.dtype != torch.bfloat16 or q.dim() != 3:
+        raise ValueError("q must be a bf16 [B, H, d] tensor")
+    B, H, d = q.shape
+    Bk, T_cap, Hk, dk = _bthd(K, "K")
+    if (Bk, dk) != (B, d) or _bthd(V, "V") != (B, T_cap, Hk, d):
+        raise ValueError("K and V must be bf16 [B, T_cap, H_kv, d] tensors matching q's B and d")
+    if seq_lens is not None:
+        _int32(seq_lens, "seq_lens", (B,))
+    if l > 0 and depth_kv_token is None:
+        raise ValueError("depth_kv_token must be a bf16 [l, B, H_kv, 2, d] tensor")
+    return B, H, d, T_cap, Hk
+
+
+def moda_attn_decode_mass(q, K, V, depth_kv_token, max_seq_len, l, scale, seq_lens=None, mass_in=None, mass=None, O=None, LSE=None,
+                          workspace=None, stream=None):
+    """Decode step that also adds its weights to an accumulator per cached key: O [B,H,d], LSE [B,H] as from ``moda_attn_decode`` (or, with
+    ``seq_lens``, ``moda_attn_decode_varlen``) and mass [B,H_kv,T_cap] fp32 = ``mass_in`` (0 for the token's own key, the last; None: 0 for all) + the
+    probabilities of this step, summed over the heads of a group.  ``mass_in`` may be ``mass``; positions past a length are not touched."""
+    B, H, d, T_cap, Hk = _decode_shapes(q, K, V, seq_lens, depth_kv_token, l)
+    mass = _new((B, Hk, T_cap), torch.float32, q.device, stream) if mass is None else _mass(mass, "mass", (B, Hk, T_cap))
+    if mass_in is not None:
+        _mass(mass_in, "mass_in", (B, Hk, T_cap))
+    O = _new_like(q, stream) if O is None else _given(O, B * H * d, torch.bfloat16)
+    LSE = _new((B, H), torch.float32, q.device, stream) if LSE is None else _given(LSE, B * H, torch.float32)
+    if workspace is None:
+        workspace = _new((max(moda_decode_mass_workspace_bytes(B, int(max_seq_len), H, Hk, d), 16),), torch.uint8, q.device, stream)
+    _check(load().moda_attn_decode_mass(_ptr(q), _ptr(K), _ptr(V), _ptr(seq_lens), _token(depth_kv_token, l, B, Hk, d), _ptr(mass_in),
+                                        B, int(max_seq_len), T_cap, H, Hk, d, int(l), float(scale), _ptr(O), _ptr(LSE), _ptr(mass),
+                                        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
+           "moda_attn_decode_mass")
+    return O, LSE, mass
+
+
+def moda_kv_evict(K, V, mass, T, n_keep, n_recent=0, seq_lens=None, K_out=None, V_out=None, mass_out=None, index=None, lens_out=None,
+                  stream=None):
+    """Cuts a cache to its most used keys: of the T (or, with ``seq_lens`` int32 [B], fewer) rows of K, V [B,T_cap,H_kv,d], per (sequence, key/value head) the
+    last ``n_recent`` and those of largest ``mass`` [B,H_kv,T_cap] stay, ``n_keep`` in all, in their order.  Returns K_out, V_out [B,T_out,H_kv,d] (T_out =
+    n_keep where they are allocated here), mass_out [B,H_kv,T_out], the old positions index int32 [B,H_kv,n_keep] (-1 behind the last one kept) and the
+    new lengths lens_out int32 [B]."""
+    B, T_cap, Hk, d = _bthd(K, "K")
+    if _bthd(V, "V") != (B, T_cap, Hk, d):
+        raise ValueError("V must be a bf16 tensor of K's shape")
+    _mass(mass, "mass", (B, Hk, T_cap))
+    if seq_lens is not None:
+        _int32(seq_lens, "seq_lens", (B,))
+    n_keep = int(n_keep)
+    n = max(n_keep, 1)                                                      # what the C call refuses is allocated all the same
+    K_out = _new((B, n, Hk, d), torch.bfloat16, K.device, stream) if K_out is None else K_out
+    V_out = _new(tuple(K_out.shape), torch.bfloat16, K.device, stream) if V_out is None else V_out
+    Bo, T_out, Ho, do = _bthd(K_out, "K_out")
+    if (Bo, Ho, do) != (B, Hk, d) or _bthd(V_out, "V_out") != (B, T_out, Hk, d):
+        raise ValueError("K_out and V_out must be bf16 [B, T_out, H_kv, d] tensors matching K")
+    mass_out = _new((B, Hk, T_out), torch.float32, K.device, stream) if mass_out is None else _mass(mass_out, "mass_out", (B, Hk, T_out))
+    index = _new((B, Hk, n), torch.int32, K.device, stream) if index is None else _int32(index, "index", (B, Hk, n))
+    lens_out = _new((B,), torch.int32, K.device, stream) if lens_out is None else _int32(lens_out, "lens_out", (B,))
+    _check(load().moda_kv_evict(_ptr(K), _ptr(V), _ptr(mass), _ptr(seq_lens), B, int(T), T_cap, Hk, d, n_keep, int(n_recent), T_out,
+                                _ptr(K_out), _ptr(V_out), _ptr(mass_out), _ptr(index), _ptr(lens_out), _stream(stream)), "moda_kv_evict")
+    return K_out, V_out, mass_out, index, lens_out
+
+
+def moda_decode_shared_workspace_bytes(B, T_prefix, H, H_kv, d) -> int:
+    return int(load().moda_decode_shared_workspace_bytes(B, T_prefix, H, H_kv, d))
+
+
+def moda_attn_decode_shared(q, K_prefix, V_prefix, K, V, seq_lens, depth_kv_token, max_seq_len, l, scale, O=None, LSE=None, workspace=None,
+                            stream=None):
+    """Decode step of a batch that shares a prefix: q [B,H,d] attends, under one softmax, to K_prefix, V_prefix [T_prefix,H_kv,d] (read once for the
+    batch), to the first seq_lens[b] (int32 [B], 0 .. max_seq_len; None: max_seq_len) rows of its own K, V [B,T_cap,H_kv,d] and to its
+    depth pairs [l,B,H_kv,2,d].  K, V may be None where max_seq_len is 0.  Returns O [B,H,d] bf16 and LSE [B,H] fp32."""
+    if K_prefix.dtype != torch.bfloat16 or K_prefix.dim() != 3 or V_prefix.dtype != torch.bfloat16 or V_prefix.shape != K_prefix.shape:
+        raise ValueError("K_prefix and V_prefix must be bf16 [T_prefix, H_kv, d] tensors")
+    P, Hk, dp = K_prefix.shape
+    if K is None and int(max_seq_len) == 0:
+        if q.dtype != torch.bfloat16 or q.dim() != 3:
+            raise ValueError("q must be a bf16 [B, H, d] tensor")
+        (B, H, d), T_cap = q.shape, 0
+    else:
+        B, H, d, T_cap, Hs = _decode_shapes(q, K, V, seq_lens, depth_kv_token, l)
+        if Hs != Hk:
+            raise ValueError("K and K_prefix must have the same heads")
+    if dp != d or (l > 0 and depth_kv_token is None):
+        raise ValueError("the prefix's width must be q's, and l depth pairs need depth_kv_token")
+    O = _new_like(q, stream) if O is None else _given(O, B * H * d, torch.bfloat16)
+    LSE = _new((B, H), torch.float32, q.device, stream) if LSE is None else _given(LSE, B * H, torch.float32)
+    if workspace is None:
+        workspace = _new((max(moda_decode_shared_workspace_bytes(B, P, H, Hk, d), 16),), torch.uint8, q.device, stream)
+    _check(load().moda_attn_decode_shared(_ptr(q), _ptr(K_prefix), _ptr(V_prefix), _ptr(K), _ptr(V), _ptr(seq_lens),
+                                          _token(depth_kv_token, l, B, Hk, d), B, P, int(max_seq_len), T_cap, H, Hk, d, int(l), float(scale),
+                                          _ptr(O), _ptr(LSE), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
+           "moda_attn_decode_shared")
     return O, LSE

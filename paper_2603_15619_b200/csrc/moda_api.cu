@@ -15,8 +15,11 @@
 #include "moda_fwd.cuh"
 #include "moda_fwd_wide.cuh"
 #include "moda_fwd_wide128.cuh"
+#include "moda_evict.cuh"
+#include "moda_keymass.cuh"
 #include "moda_mass.cuh"
 #include "moda_kvproj.cuh"
+#include "moda_shared.cuh"
 #include "sm100_ptx.cuh"
 
 namespace {
@@ -90,6 +93,21 @@ bool make_bthd_map(CUtensorMap* map, const void* base, int B, int T, int H, int 
     const cuuint64_t dims[4] = {cuuint64_t(d), cuuint64_t(H), cuuint64_t(T), cuuint64_t(B)};
     const cuuint64_t strides[3] = {cuuint64_t(d) * 2, cuuint64_t(H) * d * 2, cuuint64_t(T) * H * d * 2};
     const cuuint32_t box[4] = {64, 1, cuuint32_t(box_rows), 1};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) { tl_last_cuda_error = static_cast<int>(cudaErrorInvalidValue); return false; }
+    return true;
+}
+
+// The same tensor in boxes of `heads` adjacent heads x `rows` positions: row (position, head) after row, 64 features each.
+bool make_box_map(CUtensorMap* map, const void* base, int B, int T, int H, int d, int heads, int rows) {
+    EncodeTiledFn enc = get_encode_fn();
+    if (!enc) { tl_last_cuda_error = static_cast<int>(cudaErrorNotSupported); return false; }
+    const cuuint64_t dims[4] = {cuuint64_t(d), cuuint64_t(H), cuuint64_t(T), cuuint64_t(B)};
+    const cuuint64_t strides[3] = {cuuint64_t(d) * 2, cuuint64_t(H) * d * 2, cuuint64_t(T) * H * d * 2};
+    const cuuint32_t box[4] = {64, cuuint32_t(heads), cuuint32_t(rows), 1};
     const cuuint32_t estr[4] = {1, 1, 1, 1};
     const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
@@ -683,10 +701,10 @@ inline size_t decode_merge_reserve(long long ctas, int sms) {
     return ctas <= 4ll * sms ? 44000 : ctas <= 8ll * sms ? 24000 : ctas <= 12ll * sms ? 16000 : 0;
 }
 
-// Decode step: a split kernel over the KV cache and a merge kernel that adds the depth pairs.
-template <int D, int G>
-int launch_decode_g(const DecodeParams& p, cudaStream_t stream) {
-    using L = DecodeSmem<D, G>;
+// The split kernel of a decode step over the KV cache.  GF: heads of a group (+ kDecodeKeepScores).
+template <int D, int GF>
+int launch_decode_split(const DecodeParams& p, cudaStream_t stream) {
+    using L = DecodeSmem<D, GF % kDecodeKeepScores>;
     CUtensorMap mK, mV;
     // contiguous cache: [B][T_cap][Hk][d]; paged cache: [num_pages][page_size][Hk][d] (p.T_cap holds num_pages then)
     const int outer = p.block_table ? p.T_cap : p.B, rows = p.block_table ? p.page_size : p.T_cap;
@@ -697,7 +715,7 @@ int launch_decode_g(const DecodeParams& p, cudaStream_t stream) {
     int dev = 0;
     if (!cuda_ok(cudaGetDevice(&dev))) return MODA_ERR_CUDA;
     if (configured_dev != dev) {
-        if (!set_smem_limit(decode_split_tma_kernel<D, G>, L::kDynamic)) return MODA_ERR_CUDA;
+        if (!set_smem_limit(decode_split_tma_kernel<D, GF>, L::kDynamic)) return MODA_ERR_CUDA;
         configured_dev = dev;
     }
     // one CTA per SM, or per run when there are fewer (with lengths: at least as many as there can be runs)
@@ -706,8 +724,14 @@ int launch_decode_g(const DecodeParams& p, cudaStream_t stream) {
     const long long runs = !p.seq_lens && !p.cut.aligned ? (groups * units + shortest - 1) / shortest
                                                          : groups * ((units + shortest - 1) / shortest);
     const unsigned grid = unsigned((runs < p.teams ? runs : p.teams) * p.team);
-    decode_split_tma_kernel<D, G><<<grid, kDecodeTmaThreads, L::kDynamic, stream>>>(mK, mV, p);
-    if (!cuda_ok(cudaGetLastError())) return MODA_ERR_CUDA;
+    decode_split_tma_kernel<D, GF><<<grid, kDecodeTmaThreads, L::kDynamic, stream>>>(mK, mV, p);
+    return cuda_ok(cudaGetLastError()) ? MODA_OK : MODA_ERR_CUDA;
+}
+
+// Decode step: the split kernel and a merge kernel that adds the depth pairs.
+template <int D, int GF>
+int launch_decode_g(const DecodeParams& p, cudaStream_t stream) {
+    if (int rc = launch_decode_split<D, GF>(p, stream)) return rc;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(p.H), unsigned(p.B), 1);
     cfg.blockDim = dim3(kDecodeMergeThreads, 1, 1);
@@ -721,46 +745,26 @@ int launch_decode_g(const DecodeParams& p, cudaStream_t stream) {
     if (!cuda_ok(cudaLaunchKernelEx(&cfg, decode_merge_kernel<D>, p))) return MODA_ERR_CUDA;
     return MODA_OK;
 }
-template <int D>
+template <int D, int MORE = 0>
 int launch_decode(const DecodeParams& p, cudaStream_t stream) {
     switch (p.H / p.Hk) {
-        case 1: return launch_decode_g<D, 1>(p, stream);
-        case 2: return launch_decode_g<D, 2>(p, stream);
-        case 3: return launch_decode_g<D, 3>(p, stream);
-        case 4: return launch_decode_g<D, 4>(p, stream);
-        case 5: return launch_decode_g<D, 5>(p, stream);
-        case 6: return launch_decode_g<D, 6>(p, stream);
-        case 7: return launch_decode_g<D, 7>(p, stream);
-        case 8: return launch_decode_g<D, 8>(p, stream);
+        case 1: return launch_decode_g<D, 1 + MORE>(p, stream);
+        case 2: return launch_decode_g<D, 2 + MORE>(p, stream);
+        case 3: return launch_decode_g<D, 3 + MORE>(p, stream);
+        case 4: return launch_decode_g<D, 4 + MORE>(p, stream);
+        case 5: return launch_decode_g<D, 5 + MORE>(p, stream);
+        case 6: return launch_decode_g<D, 6 + MORE>(p, stream);
+        case 7: return launch_decode_g<D, 7 + MORE>(p, stream);
+        case 8: return launch_decode_g<D, 8 + MORE>(p, stream);
         default: return MODA_ERR_BAD_GROUP;
     }
 }
 
-// The decode step behind its three entry points: contiguous cache with one length, contiguous cache with a
-// length per sequence, paged cache (T_cap then counts pages).
-int decode_common(const void* q, const void* K, const void* V, const int* seq_lens, const int* block_table,
-                  const void* depth_kv_token, int B, int T_kv, int T_cap, int page_size, int max_blocks,
-                  int H, int H_kv, int d, int l, float scale,
-                  void* O, float* LSE, void* workspace, size_t workspace_bytes, void* stream) {
-    const bool paged = block_table != nullptr;
-    if (B < 1 || T_kv < 1 || H < 1 || (!paged && T_cap < T_kv)) return MODA_ERR_BAD_SHAPE;
-    if (d != 64 && d != 128) return MODA_ERR_BAD_HEAD_DIM;
-    if (int rc = check_scale(scale)) return rc;
-    if ((long long)(paged ? page_size : B) * T_cap > 0x7fffffffLL / H) return MODA_ERR_BAD_SHAPE;
-    if (int rc = check_groups(H, H_kv)) return rc;
-    if ((long long)B * H * kDecodeMaxSplits > 0x7fffffffLL || B > 65535) return MODA_ERR_BAD_SHAPE;
-    if (l < 0 || l > MODA_MAX_DEPTH) return MODA_ERR_BAD_DEPTH;
-    if (!q || !K || !V || !O || !LSE || (l > 0 && !depth_kv_token)) return MODA_ERR_NULL_POINTER;
-    if ((seq_lens && (reinterpret_cast<uintptr_t>(seq_lens) & 3u)) || (block_table && (reinterpret_cast<uintptr_t>(block_table) & 3u)))
-        return MODA_ERR_MISALIGNED;
-    if (!aligned16(q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned16(LSE) ||
-        (l > 0 && !aligned16(depth_kv_token)))
-        return MODA_ERR_MISALIGNED;
-    if (!workspace || !aligned16(workspace) || workspace_bytes < decode_workspace_bytes(B, H, d)) return MODA_ERR_WORKSPACE;
-    if (int rc = check_device()) return rc;
-    int sms = 0;
-    if (int rc = device_sm_count(&sms)) return rc;
-    DecodeParams p;
+// What the kernels of a decode step are launched with, for arguments that have been checked.
+DecodeParams decode_params(const void* q, const void* K, const void* V, const int* seq_lens, const int* block_table,
+                           const void* depth_kv_token, int B, int T_kv, int T_cap, int page_size, int max_blocks,
+                           int H, int H_kv, int d, int l, float scale, void* O, float* LSE, void* workspace, int sms) {
+    DecodeParams p = {};
     p.q = static_cast<const __nv_bfloat16*>(q);
     p.K = static_cast<const __nv_bfloat16*>(K);
     p.V = static_cast<const __nv_bfloat16*>(V);
@@ -788,6 +792,35 @@ int decode_common(const void* q, const void* K, const void* V, const int* seq_le
     p.stride = DecodeWalk::stride_of(decode_units(T_kv, p.unit_log2), p.cut);
     p.max_pieces = std::min(kDecodeMaxSplits - 1, decode_units(T_kv, p.unit_log2) / p.min_run + 2);
     p.scale_log2 = scale * kDecodeLog2e;
+    return p;
+}
+
+// The decode step behind its three entry points: contiguous cache with one length, contiguous cache with a
+// length per sequence, paged cache (T_cap then counts pages).
+int decode_common(const void* q, const void* K, const void* V, const int* seq_lens, const int* block_table,
+                  const void* depth_kv_token, int B, int T_kv, int T_cap, int page_size, int max_blocks,
+                  int H, int H_kv, int d, int l, float scale,
+                  void* O, float* LSE, void* workspace, size_t workspace_bytes, void* stream) {
+    const bool paged = block_table != nullptr;
+    if (B < 1 || T_kv < 1 || H < 1 || (!paged && T_cap < T_kv)) return MODA_ERR_BAD_SHAPE;
+    if (d != 64 && d != 128) return MODA_ERR_BAD_HEAD_DIM;
+    if (int rc = check_scale(scale)) return rc;
+    if ((long long)(paged ? page_size : B) * T_cap > 0x7fffffffLL / H) return MODA_ERR_BAD_SHAPE;
+    if (int rc = check_groups(H, H_kv)) return rc;
+    if ((long long)B * H * kDecodeMaxSplits > 0x7fffffffLL || B > 65535) return MODA_ERR_BAD_SHAPE;
+    if (l < 0 || l > MODA_MAX_DEPTH) return MODA_ERR_BAD_DEPTH;
+    if (!q || !K || !V || !O || !LSE || (l > 0 && !depth_kv_token)) return MODA_ERR_NULL_POINTER;
+    if ((seq_lens && (reinterpret_cast<uintptr_t>(seq_lens) & 3u)) || (block_table && (reinterpret_cast<uintptr_t>(block_table) & 3u)))
+        return MODA_ERR_MISALIGNED;
+    if (!aligned16(q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned16(LSE) ||
+        (l > 0 && !aligned16(depth_kv_token)))
+        return MODA_ERR_MISALIGNED;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < decode_workspace_bytes(B, H, d)) return MODA_ERR_WORKSPACE;
+    if (int rc = check_device()) return rc;
+    int sms = 0;
+    if (int rc = device_sm_count(&sms)) return rc;
+    const DecodeParams p = decode_params(q, K, V, seq_lens, block_table, depth_kv_token, B, T_kv, T_cap, page_size, max_blocks, H, H_kv, d, l,
+                                         scale, O, LSE, workspace, sms);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return d == 128 ? launch_decode<128>(p, st) : launch_decode<64>(p, st);
 }
@@ -1364,3 +1397,5 @@ extern "C" int moda_attn_bwd_static_scratch(const void* Q, const void* K, const 
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return d == 128 ? launch_bwd<128>(a, MODA_BWD_ALL_STAGES, st) : launch_bwd<64>(a, MODA_BWD_ALL_STAGES, st);
 }
+
+#include "moda_api_serving.cuh"

@@ -1,0 +1,277 @@
+// The entry points that measure, bound and share the sequence cache of a serving program (include/moda.h): argument checks and
+// launches.  Part of moda_api.cu, whose helpers it uses.
+#pragma once
+
+namespace {
+
+// ------------------------------------------------------------------------------------------ attention weight of the keys
+constexpr int kKeyMassCtas = 148;                 // most runs of a call: partial sums of that many fit the workspace
+
+inline int key_mass_positions(int G) { return 128 / G; }
+
+template <int D>
+int launch_key_mass(const void* Q, const void* K, int B, KeyMassParams p, unsigned ctas, cudaStream_t stream) {
+    using L = KeyMassSmem<D>;
+    // query rows of a unit: P positions of the G heads, position after position
+    CUtensorMap mQ, mK;
+    if (!make_box_map(&mQ, Q, B, p.T_q, p.H, D, p.G, p.P) || !make_bthd_map(&mK, K, B, p.T_cap, p.Hk, D)) return MODA_ERR_CUDA;
+    static thread_local int configured_dev = -1;
+    int dev = 0;
+    if (!cuda_ok(cudaGetDevice(&dev))) return MODA_ERR_CUDA;
+    if (configured_dev != dev) {
+        if (!set_smem_limit(key_mass_kernel<D>, L::kDynamic)) return MODA_ERR_CUDA;
+        configured_dev = dev;
+    }
+    key_mass_kernel<D><<<ctas, kKmThreads, L::kDynamic, stream>>>(mQ, mK, p);
+    if (!cuda_ok(cudaGetLastError())) return MODA_ERR_CUDA;
+    key_mass_join_kernel<<<ctas, 128, 0, stream>>>(p);
+    return cuda_ok(cudaGetLastError()) ? MODA_OK : MODA_ERR_CUDA;
+}
+
+// ------------------------------------------------------------------------------------------------------ shared prefix
+constexpr int kSharedCtas = 148;
+
+// How the prefix of a call is cut, for `ctas` CTAs.
+SharedParams shared_plan(int B, int P, int H, int H_kv, int ctas) {
+    SharedParams p = {};
+    p.B = B; p.P = P; p.H = H; p.Hk = H_kv; p.G = H / H_kv;
+    if (P == 0) return p;
+    p.S = 128 / p.G;
+    p.row_tiles = (B + p.S - 1) / p.S;
+    p.pairs = (p.row_tiles + 1) / 2;
+    p.key_tiles = (P + 127) / 128;
+    p.total = H_kv * p.pairs * p.key_tiles;
+    p.run = (p.total + ctas - 1) / ctas;
+    p.pieces = ((p.key_tiles + p.run - 2) / p.run + 1) * (p.row_tiles > 1 ? 1 : 2);
+    return p;
+}
+size_t shared_prefix_bytes(const SharedParams& p, int d) {
+    return (size_t(p.pieces) * p.B * p.H * (size_t(d) * 4 + 8) + 15) / 16 * 16;
+}
+
+template <int D>
+int launch_shared_prefix(const void* q, const void* Kp, const void* Vp, const SharedParams& p, cudaStream_t stream) {
+    using L = SharedSmem<D>;
+    CUtensorMap mQ, mK, mV;
+    if (!make_box_map(&mQ, q, 1, p.B, p.H, D, p.G, p.S) || !make_bthd_map(&mK, Kp, 1, p.P, p.Hk, D) || !make_bthd_map(&mV, Vp, 1, p.P, p.Hk, D))
+        return MODA_ERR_CUDA;
+    static thread_local int configured_dev = -1;
+    int dev = 0;
+    if (!cuda_ok(cudaGetDevice(&dev))) return MODA_ERR_CUDA;
+    if (configured_dev != dev) {
+        if (!set_smem_limit(shared_prefix_kernel<D>, L::kDynamic)) return MODA_ERR_CUDA;
+        configured_dev = dev;
+    }
+    shared_prefix_kernel<D><<<unsigned((p.total + p.run - 1) / p.run), kSpThreads, L::kDynamic, stream>>>(mQ, mK, mV, p);
+    return cuda_ok(cudaGetLastError()) ? MODA_OK : MODA_ERR_CUDA;
+}
+
+template <int D>
+int launch_own_cache(const DecodeParams& p, cudaStream_t stream) {
+    switch (p.H / p.Hk) {
+        case 1: return launch_decode_split<D, 1>(p, stream);
+        case 2: return launch_decode_split<D, 2>(p, stream);
+        case 3: return launch_decode_split<D, 3>(p, stream);
+        case 4: return launch_decode_split<D, 4>(p, stream);
+        case 5: return launch_decode_split<D, 5>(p, stream);
+        case 6: return launch_decode_split<D, 6>(p, stream);
+        case 7: return launch_decode_split<D, 7>(p, stream);
+        case 8: return launch_decode_split<D, 8>(p, stream);
+        default: return MODA_ERR_BAD_GROUP;
+    }
+}
+
+template <int D>
+int launch_shared(const void* q, const void* Kp, const void* Vp, const SharedMergeParams& p, cudaStream_t stream) {
+    if (p.pre.P > 0)
+        if (int rc = launch_shared_prefix<D>(q, Kp, Vp, p.pre, stream)) return rc;
+    if (p.dec.T_kv > 0)
+        if (int rc = launch_own_cache<D>(p.dec, stream)) return rc;
+    shared_merge_kernel<D><<<dim3(unsigned(p.dec.H), unsigned(p.dec.B)), kSharedMergeThreads, 0, stream>>>(p);
+    return cuda_ok(cudaGetLastError()) ? MODA_OK : MODA_ERR_CUDA;
+}
+
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+size_t decode_mass_stride(int T_kv) { return (size_t(T_kv) + 7) / 8 * 8; }
+
+}  // namespace
+
+extern "C" {
+
+size_t moda_key_mass_workspace_bytes(int B, int T_q, int T_kv, int H, int H_kv, int d) {
+    if (B < 1 || T_q < 1 || T_kv < T_q || H < 1 || check_groups(H, H_kv) || (d != 64 && d != 128)) return 0;
+    return size_t(kKeyMassCtas) * (2 * 128 * 4 + 2 * 8);
+}
+
+int moda_attn_key_mass(const void* Q, const void* K, const float* LSE, const float* mass_in,
+                       int B, int T_q, int T_kv, int T_cap, int H, int H_kv, int d, float scale,
+                       float* mass, void* workspace, size_t workspace_bytes, void* stream) {
+    if (int rc = check_shape(B, T_q, H, d)) return rc;
+    if (T_kv < T_q || T_cap < T_kv) return MODA_ERR_BAD_SHAPE;
+    if (int rc = check_scale(scale)) return rc;
+    if (int rc = check_groups(H, H_kv)) return rc;
+    if ((long long)B * T_cap > 0x7fffffffLL / H) return MODA_ERR_BAD_SHAPE;
+    if (!Q || !K || !LSE || !mass) return MODA_ERR_NULL_POINTER;
+    if (!aligned16(Q) || !aligned16(K) || !aligned16(LSE) || !aligned16(mass) || !aligned16(mass_in)) return MODA_ERR_MISALIGNED;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < moda_key_mass_workspace_bytes(B, T_q, T_kv, H, H_kv, d)) return MODA_ERR_WORKSPACE;
+    KeyMassParams p = {};
+    p.LSE = LSE; p.mass_in = mass_in; p.mass = mass; p.part = static_cast<float*>(workspace);
+    p.T_q = T_q; p.T_kv = T_kv; p.T_cap = T_cap; p.H = H; p.Hk = H_kv; p.G = H / H_kv;
+    p.P = key_mass_positions(p.G);
+    p.n_units = (T_q + p.P - 1) / p.P;
+    p.tiles = (T_kv + 127) / 128;
+    for (int j = 0; j < p.tiles; ++j) {
+        const int i = j * 128 - (T_kv - T_q);
+        p.per_head += p.n_units - (i > 0 ? i / p.P : 0);
+    }
+    if (p.per_head > 0x3fffffffLL) return MODA_ERR_BAD_SHAPE;
+    p.total = p.per_head * B * H_kv;
+    if (int rc = check_device()) return rc;
+    int sms = 0;
+    if (int rc = device_sm_count(&sms)) return rc;
+    const long long most = std::min(sms, kKeyMassCtas);
+    const long long run = (p.total + most - 1) / most;
+    if (run > 0x3fffffffLL || (long long)B * H_kv * p.tiles > 0x7fffffffLL) return MODA_ERR_BAD_SHAPE;
+    p.run = int(run);
+    p.scale_log2 = scale * kLog2e;
+    const unsigned ctas = unsigned((p.total + run - 1) / run);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return d == 128 ? launch_key_mass<128>(Q, K, B, p, ctas, st) : launch_key_mass<64>(Q, K, B, p, ctas, st);
+}
+
+size_t moda_decode_mass_workspace_bytes(int B, int T_kv, int H, int H_kv, int d) {
+    if (B < 1 || T_kv < 1 || H < 1 || check_groups(H, H_kv) || (d != 64 && d != 128)) return 0;
+    return decode_workspace_bytes(B, H, d) + size_t(B) * H * decode_mass_stride(T_kv) * 4;
+}
+
+int moda_attn_decode_mass(const void* q, const void* K, const void* V, const int* seq_lens,
+                          const void* depth_kv_token, const float* mass_in,
+                          int B, int T_kv, int T_cap, int H, int H_kv, int d, int l, float scale,
+                          void* O, float* LSE, float* mass, void* workspace, size_t workspace_bytes, void* stream) {
+    if (B < 1 || T_kv < 1 || H < 1 || T_cap < T_kv) return MODA_ERR_BAD_SHAPE;
+    if (d != 64 && d != 128) return MODA_ERR_BAD_HEAD_DIM;
+    if (int rc = check_scale(scale)) return rc;
+    if ((long long)B * T_cap > 0x7fffffffLL / H) return MODA_ERR_BAD_SHAPE;
+    if (int rc = check_groups(H, H_kv)) return rc;
+    if ((long long)B * H * kDecodeMaxSplits > 0x7fffffffLL || B > 65535 || H_kv > 65535) return MODA_ERR_BAD_SHAPE;
+    if (l < 0 || l > MODA_MAX_DEPTH) return MODA_ERR_BAD_DEPTH;
+    if (!q || !K || !V || !O || !LSE || !mass || (l > 0 && !depth_kv_token)) return MODA_ERR_NULL_POINTER;
+    if (!aligned4(seq_lens) || !aligned16(q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned16(LSE) || !aligned16(mass) ||
+        !aligned16(mass_in) || (l > 0 && !aligned16(depth_kv_token)))
+        return MODA_ERR_MISALIGNED;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < moda_decode_mass_workspace_bytes(B, T_kv, H, H_kv, d)) return MODA_ERR_WORKSPACE;
+    if (int rc = check_device()) return rc;
+    int sms = 0;
+    if (int rc = device_sm_count(&sms)) return rc;
+    DecodeParams p = decode_params(q, K, V, seq_lens, nullptr, depth_kv_token, B, T_kv, T_cap, 0, 0, H, H_kv, d, l, scale, O, LSE, workspace, sms);
+    p.scores = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + decode_workspace_bytes(B, H, d));
+    p.score_stride = decode_mass_stride(T_kv);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (int rc = d == 128 ? launch_decode<128, kDecodeKeepScores>(p, st) : launch_decode<64, kDecodeKeepScores>(p, st)) return rc;
+    DecodeKeyMassParams m = {};
+    m.scores = p.scores; m.LSE = LSE; m.mass_in = mass_in; m.mass = mass; m.seq_lens = seq_lens;
+    m.stride = p.score_stride; m.T_kv = T_kv; m.T_cap = T_cap; m.H = H; m.Hk = H_kv;
+    const unsigned blocks = unsigned((T_kv + 4 * kDecodeMassThreads - 1) / (4 * kDecodeMassThreads));
+    decode_key_mass_kernel<<<dim3(blocks, unsigned(H_kv), unsigned(B)), kDecodeMassThreads, 0, st>>>(m);
+    return cuda_ok(cudaGetLastError()) ? MODA_OK : MODA_ERR_CUDA;
+}
+
+int moda_kv_evict(const void* K, const void* V, const float* mass, const int* seq_lens,
+                  int B, int T, int T_cap, int H_kv, int d, int n_keep, int n_recent, int T_out,
+                  void* K_out, void* V_out, float* mass_out, int* index, int* lens_out, void* stream) {
+    if (B < 1 || T < 1 || H_kv < 1 || T_cap < T || n_keep < 1 || T_out < n_keep || n_recent < 0 || n_recent > n_keep) return MODA_ERR_BAD_SHAPE;
+    if (d != 64 && d != 128) return MODA_ERR_BAD_HEAD_DIM;
+    if ((long long)B * T_cap > 0x7fffffffLL / H_kv || (long long)B * T_out > 0x7fffffffLL / H_kv || B > 65535 || H_kv > 4096) return MODA_ERR_BAD_SHAPE;
+    if (!K || !V || !mass || !K_out || !V_out || !index) return MODA_ERR_NULL_POINTER;
+    if (!aligned16(K) || !aligned16(V) || !aligned16(K_out) || !aligned16(V_out) || !aligned4(mass) || !aligned4(mass_out) || !aligned4(index) ||
+        !aligned4(seq_lens) || !aligned4(lens_out))
+        return MODA_ERR_MISALIGNED;
+    const size_t row = size_t(H_kv) * d * 2;
+    auto apart = [&](const void* in, const void* out) {
+        const auto a = reinterpret_cast<uintptr_t>(in), b = reinterpret_cast<uintptr_t>(out);
+        return b >= a + size_t(B) * T_cap * row || a >= b + size_t(B) * T_out * row;
+    };
+    if (!apart(K, K_out) || !apart(V, V_out) || !apart(K, V_out) || !apart(V, K_out)) return MODA_ERR_BAD_SHAPE;
+    if (int rc = check_device()) return rc;
+    EvictParams p = {};
+    p.K = static_cast<const __nv_bfloat16*>(K); p.V = static_cast<const __nv_bfloat16*>(V); p.mass = mass; p.seq_lens = seq_lens;
+    p.K_out = static_cast<__nv_bfloat16*>(K_out); p.V_out = static_cast<__nv_bfloat16*>(V_out); p.mass_out = mass_out; p.index = index;
+    p.lens_out = lens_out;
+    p.B = B; p.T = T; p.T_cap = T_cap; p.T_out = T_out; p.Hk = H_kv; p.n_keep = n_keep; p.n_recent = n_recent;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    static thread_local int configured_dev = -1;
+    int dev = 0;
+    if (!cuda_ok(cudaGetDevice(&dev))) return MODA_ERR_CUDA;
+    if (configured_dev != dev) {
+        if (!set_smem_limit(evict_select_kernel, evict_select_smem(kEvictKeys))) return MODA_ERR_CUDA;
+        configured_dev = dev;
+    }
+    int ranks = 1;
+    while (ranks < 8 && T > 4096 * ranks) ranks *= 2;
+    const int share = ((T + ranks - 1) / ranks + kEvictThreads - 1) / kEvictThreads * kEvictThreads;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(ranks), unsigned(H_kv), unsigned(B));
+    cfg.blockDim = dim3(kEvictThreads, 1, 1);
+    cfg.dynamicSmemBytes = size_t(evict_select_smem(share));
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = unsigned(ranks);
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (!cuda_ok(cudaLaunchKernelEx(&cfg, evict_select_kernel, p))) return MODA_ERR_CUDA;
+    int rows = std::max(1, kEvictGatherRows * 8 * 8 / (H_kv * (d / 8)));
+    const int longest = std::min(n_keep, T);
+    cfg.gridDim = dim3(unsigned((longest + rows - 1) / rows), unsigned(B), 1);
+    cfg.blockDim = dim3(kEvictGatherThreads, 1, 1);
+    cfg.dynamicSmemBytes = size_t(rows) * H_kv * 4;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    const bool ok = d == 128 ? cuda_ok(cudaLaunchKernelEx(&cfg, evict_gather_kernel<128>, p, rows))
+                             : cuda_ok(cudaLaunchKernelEx(&cfg, evict_gather_kernel<64>, p, rows));
+    return ok ? MODA_OK : MODA_ERR_CUDA;
+}
+
+size_t moda_decode_shared_workspace_bytes(int B, int T_prefix, int H, int H_kv, int d) {
+    if (B < 1 || T_prefix < 0 || H < 1 || check_groups(H, H_kv) || (d != 64 && d != 128)) return 0;
+    return decode_workspace_bytes(B, H, d) + shared_prefix_bytes(shared_plan(B, T_prefix, H, H_kv, kSharedCtas), d);
+}
+
+int moda_attn_decode_shared(const void* q, const void* K_prefix, const void* V_prefix, const void* K, const void* V, const int* seq_lens,
+                            const void* depth_kv_token,
+                            int B, int T_prefix, int max_seq_len, int T_cap, int H, int H_kv, int d, int l, float scale,
+                            void* O, float* LSE, void* workspace, size_t workspace_bytes, void* stream) {
+    if (B < 1 || T_prefix < 0 || max_seq_len < 0 || H < 1 || T_cap < max_seq_len) return MODA_ERR_BAD_SHAPE;
+    if (d != 64 && d != 128) return MODA_ERR_BAD_HEAD_DIM;
+    if (int rc = check_scale(scale)) return rc;
+    if ((long long)B * T_cap > 0x7fffffffLL / H || T_prefix > 0x7fffffffLL / H) return MODA_ERR_BAD_SHAPE;
+    if (int rc = check_groups(H, H_kv)) return rc;
+    if ((long long)B * H * kDecodeMaxSplits > 0x7fffffffLL || B > 65535) return MODA_ERR_BAD_SHAPE;
+    if (l < 0 || l > MODA_MAX_DEPTH) return MODA_ERR_BAD_DEPTH;
+    if (!q || !O || !LSE || (l > 0 && !depth_kv_token) || (T_prefix > 0 && (!K_prefix || !V_prefix)) || (max_seq_len > 0 && (!K || !V)))
+        return MODA_ERR_NULL_POINTER;
+    if (!aligned4(seq_lens) || !aligned16(q) || !aligned16(O) || !aligned16(LSE) || (l > 0 && !aligned16(depth_kv_token)) ||
+        (T_prefix > 0 && (!aligned16(K_prefix) || !aligned16(V_prefix))) || (max_seq_len > 0 && (!aligned16(K) || !aligned16(V))))
+        return MODA_ERR_MISALIGNED;
+    const SharedParams most = shared_plan(B, T_prefix, H, H_kv, kSharedCtas);
+    if ((long long)H_kv * most.pairs * most.key_tiles > 0x3fffffffLL) return MODA_ERR_BAD_SHAPE;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < moda_decode_shared_workspace_bytes(B, T_prefix, H, H_kv, d)) return MODA_ERR_WORKSPACE;
+    if (int rc = check_device()) return rc;
+    int sms = 0;
+    if (int rc = device_sm_count(&sms)) return rc;
+    SharedMergeParams p = {};
+    p.dec = decode_params(q, K, V, seq_lens, nullptr, depth_kv_token, B, std::max(max_seq_len, 1), T_cap, 0, 0, H, H_kv, d, l, scale, O, LSE,
+                          workspace, sms);
+    p.dec.T_kv = max_seq_len;
+    p.pre = shared_plan(B, T_prefix, H, H_kv, std::min(sms, kSharedCtas));
+    uint8_t* at = static_cast<uint8_t*>(workspace) + decode_workspace_bytes(B, H, d);
+    p.pre.o = reinterpret_cast<float*>(at);
+    p.pre.ml = reinterpret_cast<float2*>(at + size_t(p.pre.pieces) * B * H * d * 4);
+    p.pre.scale_log2 = scale * kDecodeLog2e;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return d == 128 ? launch_shared<128>(q, K_prefix, V_prefix, p, st) : launch_shared<64>(q, K_prefix, V_prefix, p, st);
+}
+
+}  // extern "C"

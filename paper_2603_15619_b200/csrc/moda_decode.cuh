@@ -61,7 +61,12 @@ struct DecodeParams {
     const int* block_table;       // paged cache: [B][max_blocks] page of every block of page_size positions, or null
     int page_size, max_blocks;    // paged cache: K, V are [num_pages][page_size][Hk][d]; page_size is a multiple of 64
     float scale_log2;             // scale * log2(e)
+    float* scores;                // [B][Hk][G][score_stride]: scores of the cached keys, times log2(e) (kDecodeKeepScores only)
+    size_t score_stride;
 };
+
+// Added to the group size in the split kernel's second parameter: the form that keeps the scores, for moda_attn_decode_mass.
+constexpr int kDecodeKeepScores = 16;
 
 inline size_t decode_workspace_bytes(int B, int H, int d) {
     return size_t(B) * H * kDecodeMaxSplits * (d + 2) * 4;
@@ -128,10 +133,12 @@ __device__ __forceinline__ void decode_wait(uint32_t bar, uint32_t parity, volat
     }
 }
 
-template <int D, int G>
+template <int D, int GF>
 __global__ void __launch_bounds__(kDecodeTmaThreads, 1)
 decode_split_tma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV,
                         const DecodeParams p) {
+    constexpr int G = GF % kDecodeKeepScores;
+    constexpr bool kScores = GF >= kDecodeKeepScores;
     using L = DecodeSmem<D, G>;
     constexpr int CH = D / 8, NH = D / 64;                                    // NH 64-feature boxes per row
     constexpr int kBoxBytes = kDecodeStageKeys * 128;
@@ -314,12 +321,15 @@ decode_split_tma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_c
         while (!k.done()) {
             int k_begin, k_end, n_stage;
             bool has_next;
+            float* scores = nullptr;                                     // of head g, keys 2t and 2t + 1 of a block of 8
             uint4 qnext = make_uint4(0u, 0u, 0u, 0u);
             {
                 const DecodePiece w = k.piece(cut, my_team, p.unit_log2, len_of);
                 k_begin = w.k_begin;
                 k_end = w.k_end;
                 n_stage = stages_of(w);
+                if constexpr (kScores)
+                    scores = p.scores + ((size_t(w.b) * p.Hk + head_of(w.head_team)) * G + min(g, G - 1)) * p.score_stride + 2 * t;
                 DecodeWalk next = k;
                 next.next(cut, heads, p.unit_log2, len_of);
                 has_next = !next.done();
@@ -373,6 +383,14 @@ decode_split_tma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_c
                         }
                         sc[nb][0] = (8 * nb + 2 * t < n) ? c[0] * p.scale_log2 : -INFINITY;       // rows past T_kv may hold anything
                         sc[nb][1] = (8 * nb + 2 * t + 1 < n) ? c[1] * p.scale_log2 : -INFINITY;
+                    }
+                    if constexpr (kScores) {
+                        // rows are padded to whole blocks of 8 keys: what lies past the last key is -inf and not read again
+                        if (g < G) {
+#pragma unroll
+                            for (int nb = 0; nb < 4; ++nb)
+                                if (8 * nb < n) *reinterpret_cast<float2*>(scores + k0 + 8 * nb) = make_float2(sc[nb][0], sc[nb][1]);
+                        }
                     }
                     // ---- online softmax of head g over these 32 keys (8 per lane, 4 lanes per head) ----
                     float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[1][0], sc[1][1])),
