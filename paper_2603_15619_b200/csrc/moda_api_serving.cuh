@@ -9,12 +9,20 @@ constexpr int kKeyMassCtas = 148;                 // most runs of a call: partia
 
 inline int key_mass_positions(int G) { return 128 / G; }
 
+// CTAs that take adjacent heads at the same time.
+inline int key_mass_team(int H_kv, int n_units) {
+    if (n_units > 4) return 1;
+    int team = 8;
+    while (H_kv % team != 0) --team;
+    return team;
+}
+
 template <int D>
-int launch_key_mass(const void* Q, const void* K, int B, KeyMassParams p, unsigned ctas, cudaStream_t stream) {
+int launch_key_mass(const void* Q, const void* K, int B, const KeyMassParams& p, unsigned ctas, bool join, cudaStream_t stream) {
     using L = KeyMassSmem<D>;
     // query rows of a unit: P positions of the G heads, position after position
     CUtensorMap mQ, mK;
-    if (!make_box_map(&mQ, Q, B, p.T_q, p.H, D, p.G, p.P) || !make_bthd_map(&mK, K, B, p.T_cap, p.Hk, D)) return MODA_ERR_CUDA;
+    if (!make_box_map(&mQ, Q, B, p.T_q, p.Hk * p.G, D, p.G, p.P) || !make_bthd_map(&mK, K, B, p.T_cap, p.Hk, D)) return MODA_ERR_CUDA;
     static thread_local int configured_dev = -1;
     int dev = 0;
     if (!cuda_ok(cudaGetDevice(&dev))) return MODA_ERR_CUDA;
@@ -24,8 +32,17 @@ int launch_key_mass(const void* Q, const void* K, int B, KeyMassParams p, unsign
     }
     key_mass_kernel<D><<<ctas, kKmThreads, L::kDynamic, stream>>>(mQ, mK, p);
     if (!cuda_ok(cudaGetLastError())) return MODA_ERR_CUDA;
-    key_mass_join_kernel<<<ctas, 128, 0, stream>>>(p);
-    return cuda_ok(cudaGetLastError()) ? MODA_OK : MODA_ERR_CUDA;
+    if (!join) return MODA_OK;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ctas, 1, 1);
+    cfg.blockDim = dim3(kKmTile, 1, 1);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cuda_ok(cudaLaunchKernelEx(&cfg, key_mass_join_kernel, p)) ? MODA_OK : MODA_ERR_CUDA;
 }
 
 // ------------------------------------------------------------------------------------------------------ shared prefix
@@ -101,7 +118,7 @@ extern "C" {
 
 size_t moda_key_mass_workspace_bytes(int B, int T_q, int T_kv, int H, int H_kv, int d) {
     if (B < 1 || T_q < 1 || T_kv < T_q || H < 1 || check_groups(H, H_kv) || (d != 64 && d != 128)) return 0;
-    return size_t(kKeyMassCtas) * (2 * 128 * 4 + 2 * 8);
+    return size_t(kKeyMassCtas) * (2 * kKmTile * 4 + 2 * 8);
 }
 
 int moda_attn_key_mass(const void* Q, const void* K, const float* LSE, const float* mass_in,
@@ -117,27 +134,33 @@ int moda_attn_key_mass(const void* Q, const void* K, const float* LSE, const flo
     if (!workspace || !aligned16(workspace) || workspace_bytes < moda_key_mass_workspace_bytes(B, T_q, T_kv, H, H_kv, d)) return MODA_ERR_WORKSPACE;
     KeyMassParams p = {};
     p.LSE = LSE; p.mass_in = mass_in; p.mass = mass; p.part = static_cast<float*>(workspace);
-    p.T_q = T_q; p.T_kv = T_kv; p.T_cap = T_cap; p.H = H; p.Hk = H_kv; p.G = H / H_kv;
+    p.T_q = T_q; p.T_kv = T_kv; p.T_cap = T_cap; p.Hk = H_kv; p.G = H / H_kv;
     p.P = key_mass_positions(p.G);
     p.n_units = (T_q + p.P - 1) / p.P;
-    p.tiles = (T_kv + 127) / 128;
-    for (int j = 0; j < p.tiles; ++j) {
-        const int i = j * 128 - (T_kv - T_q);
-        p.per_head += p.n_units - (i > 0 ? i / p.P : 0);
-    }
+    p.tiles = (T_kv + kKmTile - 1) / kKmTile;
+    for (int j = 0; j < p.tiles; ++j) p.per_head += p.n_units - key_mass_first_unit(j, T_kv - T_q, p.P);
     if (p.per_head > 0x3fffffffLL) return MODA_ERR_BAD_SHAPE;
-    p.total = p.per_head * B * H_kv;
     if (int rc = check_device()) return rc;
     int sms = 0;
     if (int rc = device_sm_count(&sms)) return rc;
-    const long long most = std::min(sms, kKeyMassCtas);
-    const long long run = (p.total + most - 1) / most;
+    const bool all_see_all = key_mass_first_unit(p.tiles - 1, T_kv - T_q, p.P) == 0;
+    p.team = key_mass_team(H_kv, p.n_units);
+    const long long teams = std::min(sms, kKeyMassCtas) / p.team;
+    p.total = p.per_head * B * (H_kv / p.team);
+    long long run = (p.total + teams - 1) / teams;
+    // whole tiles where they cost little: nothing to join then
+    if (all_see_all && (run + p.n_units - 1) / p.n_units * p.n_units <= run + run / 16) run = (run + p.n_units - 1) / p.n_units * p.n_units;
+    const bool join = !(all_see_all && run % p.n_units == 0);
     if (run > 0x3fffffffLL || (long long)B * H_kv * p.tiles > 0x7fffffffLL) return MODA_ERR_BAD_SHAPE;
     p.run = int(run);
     p.scale_log2 = scale * kLog2e;
-    const unsigned ctas = unsigned((p.total + run - 1) / run);
+    p.inv_scale = 1.f / scale;
+    p.least = -127.f / p.scale_log2;
+    key_mass_slots(d, p.n_units, p.k_slots, p.q_slots);
+    p.stay = p.q_slots % p.n_units == 0 && all_see_all;
+    const unsigned ctas = unsigned((p.total + run - 1) / run) * unsigned(p.team);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return d == 128 ? launch_key_mass<128>(Q, K, B, p, ctas, st) : launch_key_mass<64>(Q, K, B, p, ctas, st);
+    return d == 128 ? launch_key_mass<128>(Q, K, B, p, ctas, join, st) : launch_key_mass<64>(Q, K, B, p, ctas, join, st);
 }
 
 size_t moda_decode_mass_workspace_bytes(int B, int T_kv, int H, int H_kv, int d) {

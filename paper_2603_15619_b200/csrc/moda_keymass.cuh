@@ -6,19 +6,20 @@
 // decode_key_mass_kernel   T_q = 1, behind the decode step's merge: the split kernel has left its scores, which are G floats a key beside
 //                          the 4 d bytes of the key's K and V rows; reading K a second time would be 2 d bytes.
 //
-// key_mass_kernel          T_q rows: one product S^T = K Q^T per (key tile, unit), the keys as the 128 rows of the tcgen05 tile, so that
-//                          a thread holds a key and the sum over the query rows stays in one register.  A unit is up to 128 query
-//                          rows: P = 128 / G positions with the G heads of the group (row = position in the unit * G + head), as one TMA box
-//                          of the [T][H][d] tensor leaves them.
+// key_mass_kernel          T_q rows: products S^T = K Q^T of a tile, two adjacent 128-key tiles, and a unit, up to 128 query rows.  The keys are the rows of the
+//                          tcgen05 products, so that a thread holds a key and the sum over the query rows stays in a register.  A
+//                          unit is P = 128 / G positions with the G heads of the group (row = position in the unit * G + head), as one TMA box of the
+//                          [T][H][d] tensor leaves them.  One more step of 16 contraction elements subtracts LSE / scale (three bf16 terms a row,
+//                          whose sum is the fp32 value, against ones), so the weight is exp2(scale log2(e) S) as it comes.
 //
-//   Every CTA takes an equal run of the units of all (b, hk, key tile) in this order (within a key tile only the units that see it), so
-//   all SMs end together whatever the causal triangle looks like; the part of a key tile that a run covers is a piece.  A piece that is its whole key
-//   tile is stored at once; the others leave partial sums, at most two a CTA, that key_mass_join_kernel adds in order of the units
-//   (no atomics: the result is reproducible bit for bit).
+//   Every CTA takes an equal run of the units of all (b, hk, tile) in this order (within a tile only the units that see it), so all SMs end
+//   together whatever the causal triangle looks like; the part of a tile that a run covers is a piece.  With few units a tile, where the
+//   bytes of K set the pace, the runs are those of teams of CTAs that take adjacent heads, whose rows are adjacent in memory, at the same time.  A piece that is its whole tile
+//   is stored at once; the others leave partial sums, at most two a CTA, that key_mass_join_kernel adds in order of the units (no
+//   atomics: the result is reproducible bit for bit).
 //
-//   20 warps: 0-15 four warpgroups on the units in turn (weights of a 128 x 128 tile: thread = key), 16 TMA producer, 17 issues the
-//   products and owns TMEM, 18 loads the LSE of a unit's rows.  Unit n uses stage n % 4 of the Q ring, of the LSE ring and of the four
-//   score buffers in tensor memory.
+//   20 warps: 0-15 four warpgroups (even units: tiles' first and second 128 keys, odd units: likewise), 16 TMA producer, 17 and 19 issue the
+//   products of the two halves (17 owns TMEM), 18 prepares the LSE terms.
 #pragma once
 
 #include <cstdint>
@@ -79,73 +80,107 @@ decode_key_mass_kernel(const DecodeKeyMassParams p) {
 
 // ------------------------------------------------------------------------------------------------------------ T_q rows
 constexpr int kKmThreads = 640;
-constexpr int kKmStages = 4;
-
+constexpr int kKmTile = 256;          // keys of a tile
 struct KeyMassParams {
     const float* LSE;             // [B][H][T_q]
     const float* mass_in;         // [B][Hk][T_cap], or null
     float* mass;                  // [B][Hk][T_cap]
-    float* part;                  // [CTA][2][128] partial sums, then [CTA][2] int2 {key tile of all, kPieceStart | kPieceEnd}
-    int T_q, T_kv, T_cap, H, Hk, G;
+    float* part;                  // [CTA][2][kKmTile] partial sums, then [CTA][2] int2 {tile of all, kPieceStart | kPieceEnd}
+    int T_q, T_kv, T_cap, Hk, G;
     int P, n_units;               // positions of a unit; units that cover T_q
-    int tiles;                    // key tiles of a (b, hk)
-    long long per_head, total;    // units of a (b, hk), of all
-    int run;                      // units of a CTA
-    float scale_log2;
+    int tiles;                    // tiles of a (b, hk)
+    int team;                     // CTAs of a team (divides Hk): CTA c takes the heads c % team of the groups of `team` heads
+    long long per_head, total;    // units of a (b, hk), of all groups of heads
+    int run;                      // units of a team
+    int k_slots, q_slots;         // of shared memory: halves of tiles, units
+    int stay;                     // every tile sees every unit, and a unit comes round to its slot again with every tile: it stays there
+    float scale_log2, inv_scale, least;   // least: -127 / scale_log2
 };
 enum : int { kPieceStart = 1, kPieceEnd = 2, kPieceNone = 4 };
 
+// Slots of 128 rows: the ring of tile halves takes the first k_slots, the ring of units the next q_slots.
 template <int D>
 struct KeyMassSmem {
-    static constexpr int kTileBytes = 128 * D * 2;
+    static constexpr int kSlotBytes = 128 * D * 2;
     static constexpr int kSubBytes = 128 * 128;
-    static constexpr int kK = 0;                                   // 2 stages
-    static constexpr int kQ = kK + 2 * kTileBytes;                 // kKmStages
-    static constexpr int kLse = kQ + kKmStages * kTileBytes;       // [stage][128]
-    static constexpr int kAcc = kLse + kKmStages * 512;            // [2][4][128]
+    static constexpr int kSlots = D == 128 ? 6 : 10;
+    static constexpr int kMaxUnits = 6;
+    static constexpr int kTermBytes = 128 * 16;                    // 8 contraction elements of 128 rows
+    static constexpr int kOnes = kSlots * kSlotBytes;              // the keys' side of the LSE step
+    static constexpr int kTerms = kOnes + kTermBytes;              // [unit slot]
+    static constexpr int kZero = kTerms + kMaxUnits * kTermBytes;  // the second 8 elements, of both sides
+    static constexpr int kAcc = kZero + kTermBytes;                // [2][4][128]
     static constexpr int kBars = kAcc + 2 * 4 * 512;
-    static constexpr int kNumBars = 24;
+    static constexpr int kNumBars = 48;
     static constexpr int kMisc = kBars + kNumBars * 8;             // tmem base, abort word, start of the run
     static constexpr int kTotal = kMisc + 32;
     static constexpr int kDynamic = kTotal + 1024;
     static_assert(kDynamic <= 232448, "shared memory");
 };
+// Few units a tile (the last rows of a prompt): they stay in their slots, and the tiles stream.  Many: two units on their way while one is used.
+inline void key_mass_slots(int d, int n_units, int& k_slots, int& q_slots) {
+    if (d == 64) { k_slots = 4; q_slots = 6; return; }
+    k_slots = n_units <= 2 ? 4 : 3;
+    q_slots = 6 - k_slots;
+}
 
 enum KeyMassBar : int {
-    kKmKFull = 0,      // +(piece & 1)
-    kKmKEmpty = 2,     // +(piece & 1): every product of the piece is complete
-    kKmQFull = 4,      // +stage
-    kKmLFull = 8,      // +stage
-    kKmSFull = 12,     // +stage: the scores are there, the Q stage is free
-    kKmSEmpty = 16,    // +stage: the scores and the LSE have been read
-    kKmDone = 20,      // +(piece & 1): the four warpgroups' sums of a piece are in shared memory
-    kKmDrain = 22,
+    kKmKFull = 0,      // +slot of a tile's half (<= 4)
+    kKmKEmpty = 4,     // +slot: every product with it is complete
+    kKmQFull = 8,      // +slot of a unit (<= 6): its rows and their LSE terms
+    kKmQEmpty = 14,    // +slot: the products of both halves with it are complete
+    kKmSFull = 26,     // +(n % 2) * 2 + half: the scores are there
+    kKmSEmpty = 30,    // +(n % 2) * 2 + half: the scores have been read
+    kKmDone = 34,      // +(piece % 2): the warpgroups' sums of a piece are in shared memory
+    kKmDrain = 36,     // +half
+};
+
+// A place in a ring of `slots` slots and how often the ring has gone round.
+struct RingAt {
+    int slot = 0, round = 0;
+    __device__ __forceinline__ void next(int slots) {
+        if (++slot == slots) { slot = 0; ++round; }
+    }
 };
 
 // A wait of the kernels for serving: mbar_wait, as a call that takes the CTA's abort word along.
 struct PipeWait {
     volatile int* abort_flag;
     __device__ __forceinline__ void operator()(uint32_t bar, uint32_t parity, int site) const { mbar_wait(bar, parity, abort_flag, site); }
+    __device__ __forceinline__ void both(uint32_t bar_a, uint32_t parity_a, uint32_t bar_b, uint32_t parity_b, int site_a, int site_b) const {
+        mbar_wait2(bar_a, parity_a, bar_b, parity_b, abort_flag, site_a, site_b);
+    }
 };
 
-// First unit that sees key tile `jt`: the one of the first position i with i + off >= 128 jt.
-__device__ __forceinline__ int key_mass_first_unit(int jt, int off, int P) {
-    const int i = jt * 128 - off;
+// First unit that sees tile `jt`: the one of the first position i with i + off >= 256 jt.
+__host__ __device__ __forceinline__ int key_mass_first_unit(int jt, int off, int P) {
+    const int i = jt * kKmTile - off;
     return i > 0 ? i / P : 0;
 }
 
-// The units of a CTA's run, piece by piece.
+// The pieces of a CTA's run.
 struct KeyMassWalk {
-    int bh, jt, u;                // of the next unit
-    int left;                     // units of the run that are left
-    __device__ __forceinline__ bool last_of_tile(const KeyMassParams& p) const { return u + 1 == p.n_units; }
-    __device__ __forceinline__ bool last_of_piece(const KeyMassParams& p) const { return left == 1 || u + 1 == p.n_units; }
+    int bh, jt, u0, u1;           // (b, kv head), tile, units of the piece
+    int left;                     // units of the run from u0 on
+    bool starts;                  // the piece starts its tile
+    __device__ __forceinline__ void begin(const KeyMassParams& p, const int* start) {
+        bh = start[0] * p.team + int(blockIdx.x) % p.team;
+        jt = start[1];
+        u0 = start[2];
+        left = int(min((long long)p.run, p.total - (long long)(int(blockIdx.x) / p.team) * p.run));
+        u1 = min(p.n_units, u0 + left);
+        starts = u0 == key_mass_first_unit(jt, p.T_kv - p.T_q, p.P);
+    }
+    __device__ __forceinline__ bool ends(const KeyMassParams& p) const { return u1 == p.n_units; }
     __device__ __forceinline__ void next(const KeyMassParams& p) {
-        --left;
-        if (++u == p.n_units) {
-            if (++jt == p.tiles) { jt = 0; ++bh; }
-            u = key_mass_first_unit(jt, p.T_kv - p.T_q, p.P);
+        left -= u1 - u0;
+        if (++jt == p.tiles) {
+            jt = 0;
+            bh += p.team;
         }
+        u0 = key_mass_first_unit(jt, p.T_kv - p.T_q, p.P);
+        u1 = min(p.n_units, u0 + left);
+        starts = true;
     }
 };
 
@@ -166,22 +201,23 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int off = p.T_kv - p.T_q;
     const int rows = p.P * p.G;                       // query rows of a unit, at most 128
+    int2* dir = reinterpret_cast<int2*>(p.part + size_t(gridDim.x) * 2 * kKmTile) + blockIdx.x * 2;
 
-    if (tid < 2) reinterpret_cast<int2*>(p.part + size_t(gridDim.x) * 256)[blockIdx.x * 2 + tid] = make_int2(0, kPieceNone);
+    if (tid < 2) dir[tid] = make_int2(0, kPieceNone);
     if (tid == 0) {
         *abort_flag = 0;
-        for (int s = 0; s < 2; ++s) {
+        for (int s = 0; s < 4; ++s) {
             mbar_init(bar(kKmKFull + s), 1);
             mbar_init(bar(kKmKEmpty + s), 1);
-            mbar_init(bar(kKmDone + s), 512);
-        }
-        for (int s = 0; s < kKmStages; ++s) {
-            mbar_init(bar(kKmQFull + s), 1);
-            mbar_init(bar(kKmLFull + s), 32);
             mbar_init(bar(kKmSFull + s), 1);
             mbar_init(bar(kKmSEmpty + s), 128);
         }
-        mbar_init(bar(kKmDrain), 1);
+        for (int s = 0; s < L::kMaxUnits; ++s) {
+            mbar_init(bar(kKmQFull + s), 2);
+            mbar_init(bar(kKmQEmpty + s), 2);
+        }
+        for (int s = 0; s < 2; ++s) mbar_init(bar(kKmDone + s), 512);
+        for (int s = 0; s < 2; ++s) mbar_init(bar(kKmDrain + s), 1);
         fence_mbar_init();
     }
     if (warp == 17) {
@@ -189,10 +225,10 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
         tmem_relinquish();
     }
     if (warp == 16) {
-        // where the run starts: (b, hk), then its key tile by the lanes' sums over equal shares of the tiles
-        const long long at = (long long)blockIdx.x * p.run;
-        const int bh = int(at / p.per_head);
-        const int in_head = int(at - bh * p.per_head);
+        // where the run starts: (b, group of heads), then its tile by the lanes' sums over equal shares of the tiles
+        const long long at = (long long)(int(blockIdx.x) / p.team) * p.run;
+        const int group = int(at / p.per_head);
+        const int in_head = int(at - group * p.per_head);
         const int per_lane = (p.tiles + 31) / 32;
         const int j0 = min(lane * per_lane, p.tiles), j1 = min(j0 + per_lane, p.tiles);
         int sum = 0;
@@ -210,207 +246,239 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                 if (in_head < before + n) break;
                 before += n;
             }
-            s_start[0] = bh;
+            s_start[0] = group;
             s_start[1] = j;
             s_start[2] = key_mass_first_unit(j, off, p.P) + in_head - before;
         }
     }
-    // rows of the Q stages that no box covers stay zero (their LSE is +inf: weight 0)
+    // rows of the unit slots that no box covers stay zero (their LSE terms make their weights 0)
     if (rows < 128) {
-        for (int e = tid; e < kKmStages * NSUB * (128 - rows) * 8; e += kKmThreads) {
+        for (int e = tid; e < p.q_slots * NSUB * (128 - rows) * 8; e += kKmThreads) {
             const int piece = e & 7, r = rows + (e >> 3) % (128 - rows), sub = (e >> 3) / (128 - rows);
-            *reinterpret_cast<uint4*>(smem + L::kQ + sub * L::kSubBytes + r * 128 + piece * 16) = make_uint4(0u, 0u, 0u, 0u);
+            *reinterpret_cast<uint4*>(smem + p.k_slots * L::kSlotBytes + sub * L::kSubBytes + r * 128 + piece * 16) = make_uint4(0u, 0u, 0u, 0u);
         }
-        fence_proxy_async_smem();
     }
+    // the keys' side of the LSE step: 1, 1, 1, 0 ...
+    if (tid < 128) {
+        *reinterpret_cast<uint4*>(smem + L::kOnes + tid * 16) = make_uint4(0x3f803f80u, 0x00003f80u, 0u, 0u);
+        *reinterpret_cast<uint4*>(smem + L::kZero + tid * 16) = make_uint4(0u, 0u, 0u, 0u);
+    }
+    fence_proxy_async_smem();
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = *tmem_slot;
-    const long long begin = (long long)blockIdx.x * p.run;
     KeyMassWalk w;
-    w.bh = s_start[0];
-    w.jt = s_start[1];
-    w.u = s_start[2];
-    w.left = int(min((long long)p.run, p.total - begin));
+    w.begin(p, s_start);
 
     if (warp < 16) {
         // =========================== weights and their sums: thread = key ===========================
+        setmaxnreg_inc<104>();
         const int wg = warp >> 2, r = tid & 127;
-        const uint32_t tS = tmem + (uint32_t((warp & 3) * 32) << 16) + wg * 128;
+        const int half = wg & 1, st = wg >> 1;                           // half of the tile; the units n % 2 == st are this warpgroup's
+        const uint32_t tS = tmem + (uint32_t((warp & 3) * 32) << 16) + st * 256 + half * 128;
         float* s_acc = reinterpret_cast<float*>(smem + L::kAcc);
-        const float4* s_lse = reinterpret_cast<const float4*>(smem + L::kLse + wg * 512);
-        float acc = 0.f;
-        int n = 0, piece = 0;
-        bool starts = w.u == key_mass_first_unit(w.jt, off, p.P);        // the piece starts its key tile
+        int n0 = 0;                                                      // units before the piece
+        int q_slot = st;                                                 // of this warpgroup's next unit
 #pragma unroll 1
-        for (; w.left > 0; ++n) {
-            if ((n & 3) == wg) {
-                const int par = (n >> 2) & 1;
-                wait(bar(kKmLFull + wg), par, 110);
-                wait(bar(kKmSFull + wg), par, 111);
+        for (int piece = 0; w.left > 0; ++piece) {
+            uint64_t y0 = 0, y1 = 0;
+            const int key0 = w.jt * kKmTile + half * 128;
+            const int u_first = w.u0 + ((n0 ^ st) & 1);
+            int n = n0 + ((n0 ^ st) & 1);
+#pragma unroll 1
+            for (int u = u_first; u < w.u1; u += 2, n += 2) {
+                wait(bar(kKmSFull + wg), (n >> 1) & 1, 111);
                 tc_fence_after_sync();
-                const int key = w.jt * 128 + r, i0 = w.u * p.P;
-                // row c of the unit sees this key iff c / G + i0 + off >= key
-                const int hidden = i0 + off >= w.jt * 128 + 127 ? 0 : (key - off - i0) * p.G;
-                float a0 = 0.f, a1 = 0.f, a2 = 0.f, a3 = 0.f;
-#pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t s[32];
-                    tmem_ld32(tS + c * 32, s);
-                    tmem_wait_ld();
-                    if (hidden > c * 32) {
+                if (r == 0) mbar_arrive(bar(kKmQEmpty + q_slot));
+                q_slot += 2;
+                if (q_slot >= p.q_slots) q_slot -= p.q_slots;
+                // row c of the unit sees key r iff c / G + i0 + off >= key0 + r
+                const int i0 = u * p.P;
+                const bool masked = i0 + off < key0 + 127;
+                const int hidden = (key0 + r - off - i0) * p.G;
+                if (key0 < p.T_kv) {
+                    auto add_chunk = [&](uint32_t (&s)[16], int c) {
+                        if (masked) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (c * 32 + i < hidden) s[i] = 0xff800000u;
-                    }
-#pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        const float4 nl = s_lse[c * 8 + i / 4];
-                        float x0 = nl.x, x1 = nl.y, x2 = nl.z, x3 = nl.w;
-                        fma2_f32(__uint_as_float(s[i]), __uint_as_float(s[i + 1]), p.scale_log2, p.scale_log2, x0, x1);
-                        fma2_f32(__uint_as_float(s[i + 2]), __uint_as_float(s[i + 3]), p.scale_log2, p.scale_log2, x2, x3);
-                        add2_f32(fast_exp2(x0), fast_exp2(x1), a0, a1);
-                        add2_f32(fast_exp2(x2), fast_exp2(x3), a2, a3);
-                    }
-                }
-                acc += (a0 + a1) + (a2 + a3);
-                tc_fence_before_sync();
-                mbar_arrive(bar(kKmSEmpty + wg));
-            }
-            if (w.last_of_piece(p)) {
-                // the four warpgroups' sums meet in shared memory; the piece's owner adds them while the others go on.  (Behind piece - 1's
-                // barrier the owner of piece - 2 has read this buffer: it arrived there after that.)
-                if (piece >= 2) wait(bar(kKmDone + ((piece - 1) & 1)), ((piece - 1) >> 1) & 1, 112);
-                float* buf = s_acc + (piece & 1) * 512;
-                buf[wg * 128 + r] = acc;
-                mbar_arrive(bar(kKmDone + (piece & 1)));
-                const bool ends = w.last_of_tile(p);
-                if ((piece & 3) == wg) {
-                    wait(bar(kKmDone + (piece & 1)), (piece >> 1) & 1, 113);
-                    const float sum = (buf[r] + buf[128 + r]) + (buf[256 + r] + buf[384 + r]);
-                    const int key = w.jt * 128 + r;
-                    if (starts && ends) {
-                        if (key < p.T_kv) {
-                            const size_t at = size_t(w.bh) * p.T_cap + key;
-                            p.mass[at] = sum + (p.mass_in != nullptr && key < off ? p.mass_in[at] : 0.f);
+                            for (int i = 0; i < 16; ++i)
+                                if (c * 16 + i < hidden) s[i] = 0xff800000u;
                         }
-                    } else {
-                        const int slot = int(blockIdx.x) * 2 + (piece > 0);
-                        p.part[size_t(slot) * 128 + r] = sum;
-                        if (r == 0)
-                            reinterpret_cast<int2*>(p.part + size_t(gridDim.x) * 256)[slot] =
-                                make_int2(w.bh * p.tiles + w.jt, (starts ? kPieceStart : 0) | (ends ? kPieceEnd : 0));
+                        add_exp2_16<2>(s, p.scale_log2, p.least, y0, y1);
+                    };
+                    uint32_t sa[16], sb[16];
+                    tmem_ld16(tS, sa);
+#pragma unroll
+                    for (int c = 0; c < 8; c += 2) {
+                        tmem_wait_ld();
+                        tmem_ld16(tS + c * 16 + 16, sb);
+                        add_chunk(sa, c);
+                        tmem_wait_ld();
+                        if (c < 6) {
+                            tmem_ld16(tS + c * 16 + 32, sa);
+                        } else {
+                            tc_fence_before_sync();
+                            mbar_arrive(bar(kKmSEmpty + wg));
+                        }
+                        add_chunk(sb, c + 1);
                     }
+                } else {
+                    mbar_arrive(bar(kKmSEmpty + wg));
                 }
-                ++piece;
-                acc = 0.f;
-                starts = true;
+            }
+            n0 += w.u1 - w.u0;
+            // The warpgroups' sums meet in shared memory; a pair of them adds them up while the others go on.  (Behind piece - 1's barrier
+            // the pair that had piece - 2 has read this buffer: it arrived there after that.)
+            if (piece >= 2) wait(bar(kKmDone + ((piece - 1) & 1)), ((piece - 1) >> 1) & 1, 112);
+            float* buf = s_acc + (piece & 1) * 512;
+            buf[wg * 128 + r] = (__uint_as_float(uint32_t(y0)) + __uint_as_float(uint32_t(y0 >> 32))) +
+                                (__uint_as_float(uint32_t(y1)) + __uint_as_float(uint32_t(y1 >> 32)));
+            mbar_arrive(bar(kKmDone + (piece & 1)));
+            if ((piece & 1) == st) {
+                wait(bar(kKmDone + (piece & 1)), (piece >> 1) & 1, 113);
+                const float sum = buf[half * 128 + r] + buf[(half + 2) * 128 + r];
+                const int key = key0 + r;
+                if (w.starts && w.ends(p)) {
+                    if (key < p.T_kv) {
+                        const size_t at = size_t(w.bh) * p.T_cap + key;
+                        p.mass[at] = sum + (p.mass_in != nullptr && key < off ? p.mass_in[at] : 0.f);
+                    }
+                } else {
+                    const int slot = piece > 0;
+                    p.part[size_t(blockIdx.x * 2 + slot) * kKmTile + half * 128 + r] = sum;
+                    if (half == 0 && r == 0) dir[slot] = make_int2(w.bh * p.tiles + w.jt, (w.starts ? kPieceStart : 0) | (w.ends(p) ? kPieceEnd : 0));
+                }
             }
             w.next(p);
         }
-    } else if (warp == 16) {
+    } else {
+      setmaxnreg_dec<64>();
+      if (warp == 16) {
         // =========================== TMA producer ===========================
         if (lane == 0) {
             tma_prefetch_desc(&mapQ);
             tma_prefetch_desc(&mapK);
             const uint32_t unit_bytes = uint32_t(rows) * D * 2;
-            int n = 0, piece = 0;
-            bool fresh = true;
+            RingAt ka, qa;
+            int held = -1;                                               // (b, hk) that the slots' units are of
+            int fresh = 0;                                               // slots to fill with its units (p.stay)
+            int b = w.bh / p.Hk, hk = w.bh - b * p.Hk, bh = w.bh;
 #pragma unroll 1
-            for (; w.left > 0; ++n) {
-                const int b = w.bh / p.Hk, hk = w.bh - b * p.Hk;
-                if (fresh) {
-                    const int st = piece & 1;
-                    if (piece >= 2) wait(bar(kKmKEmpty + st), ((piece - 2) >> 1) & 1, 120);
-                    mbar_arrive_expect_tx(bar(kKmKFull + st), L::kTileBytes);
+            while (w.left > 0) {
+                if (bh != w.bh) {
+                    bh = w.bh;
+                    if ((hk += p.team) >= p.Hk) { hk -= p.Hk; ++b; }
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h, ka.next(p.k_slots)) {
+                    if (ka.round > 0) wait(bar(kKmKEmpty + ka.slot), (ka.round - 1) & 1, 120);
+                    mbar_arrive_expect_tx(bar(kKmKFull + ka.slot), L::kSlotBytes);
 #pragma unroll
                     for (int s = 0; s < NSUB; ++s)
-                        tma_load_4d(sbase + L::kK + st * L::kTileBytes + s * L::kSubBytes, &mapK, bar(kKmKFull + st), s * 64, hk, w.jt * 128, b);
-                    ++piece;
+                        tma_load_4d(sbase + ka.slot * L::kSlotBytes + s * L::kSubBytes, &mapK, bar(kKmKFull + ka.slot), s * 64, hk, w.jt * kKmTile + h * 128, b);
                 }
-                const int st = n & 3;
-                if (n >= 4) wait(bar(kKmSFull + st), ((n - 4) >> 2) & 1, 121);
-                mbar_arrive_expect_tx(bar(kKmQFull + st), unit_bytes);
+                if (held != bh) { held = bh; fresh = p.q_slots; }
+#pragma unroll 1
+                for (int u = w.u0; u < w.u1; ++u, qa.next(p.q_slots)) {
+                    if (qa.round > 0) wait(bar(kKmQEmpty + qa.slot), (qa.round - 1) & 1, 121);
+                    if (p.stay && fresh == 0) {
+                        mbar_arrive(bar(kKmQFull + qa.slot));
+                        continue;
+                    }
+                    --fresh;
+                    mbar_arrive_expect_tx(bar(kKmQFull + qa.slot), unit_bytes);
 #pragma unroll
-                for (int s = 0; s < NSUB; ++s)
-                    tma_load_4d(sbase + L::kQ + st * L::kTileBytes + s * L::kSubBytes, &mapQ, bar(kKmQFull + st), s * 64, hk * p.G, w.u * p.P, b);
-                fresh = w.last_of_tile(p);
+                    for (int s = 0; s < NSUB; ++s)
+                        tma_load_4d(sbase + (p.k_slots + qa.slot) * L::kSlotBytes + s * L::kSubBytes, &mapQ, bar(kKmQFull + qa.slot), s * 64, hk * p.G, u * p.P, b);
+                }
                 w.next(p);
             }
         }
-    } else if (warp == 17) {
-        // =========================== MMA issuer: S^T = K Q^T ===========================
+      } else if (warp != 18) {
+        // =========================== MMA issuers: S^T = K Q^T - LSE / scale of half h ===========================
+        // a warp for each half: one for both needs 890 to 1000 cycles a 128 x 128 tile, of which the tensor cores take 576 (d = 128)
+        const int h = warp == 17 ? 0 : 1;
         constexpr uint32_t idesc = make_idesc_bf16(128, 128, false, false);
-        const uint64_t dk0 = desc_kmajor_sw128(sbase + L::kK, 0), dq0 = desc_kmajor_sw128(sbase + L::kQ, 0);
-        int n = 0, piece = 0;
-        bool fresh = true;
+        const uint64_t dk0 = desc_kmajor_sw128(sbase, 0), dq0 = dk0 + uint64_t((p.k_slots * L::kSlotBytes) >> 4);
+        const uint64_t d_ones = make_smem_desc_noswz(sbase + L::kOnes, uint32_t(L::kZero - L::kOnes), 128u);
+        int n = 0;
+        RingAt ka, qa;
+        if (h == 1) ka.next(p.k_slots);
 #pragma unroll 1
-        for (; w.left > 0; ++n) {
-            const int st = n & 3, kst = piece & 1;
-            if (fresh) wait(bar(kKmKFull + kst), (piece >> 1) & 1, 130);
-            wait(bar(kKmQFull + st), (n >> 2) & 1, 131);
-            if (n >= 4) wait(bar(kKmSEmpty + st), ((n - 4) >> 2) & 1, 132);
-            tc_fence_after_sync();
-            const uint64_t dk = dk0 + uint64_t((kst * L::kTileBytes) >> 4), dq = dq0 + uint64_t((st * L::kTileBytes) >> 4);
+        while (w.left > 0) {
+            wait(bar(kKmKFull + ka.slot), ka.round & 1, 130);
+            const uint64_t dk = dk0 + uint64_t((ka.slot * L::kSlotBytes) >> 4);
+#pragma unroll 1
+            for (int u = w.u0; u < w.u1; ++u, ++n, qa.next(p.q_slots)) {
+                const int buf = (n & 1) * 2 + h;
+                if (n >= 2) wait.both(bar(kKmQFull + qa.slot), qa.round & 1, bar(kKmSEmpty + buf), ((n >> 1) & 1) ^ 1, 131, 132);
+                else wait(bar(kKmQFull + qa.slot), qa.round & 1, 133);
+                tc_fence_after_sync();
+                const uint64_t dq = dq0 + uint64_t((qa.slot * L::kSlotBytes) >> 4);
+                const int terms = L::kTerms + qa.slot * L::kTermBytes;
+                const uint32_t t = tmem + buf * 128;
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-                const uint64_t o = uint64_t(((kk >> 2) * L::kSubBytes + (kk & 3) * 32) >> 4);
-                umma_ss(tmem + st * 128, dk + o, dq + o, idesc, kk > 0);
+                for (int kk = 0; kk < D / 16; ++kk) {
+                    const uint64_t o = uint64_t(((kk >> 2) * L::kSubBytes + (kk & 3) * 32) >> 4);
+                    umma_ss(t, dk + o, dq + o, idesc, kk > 0);
+                }
+                umma_ss(t, d_ones, make_smem_desc_noswz(sbase + terms, uint32_t(L::kZero - terms), 128u), idesc, 1);
+                umma_commit(bar(kKmSFull + buf));
             }
-            umma_commit(bar(kKmSFull + st));
-            fresh = w.last_of_tile(p);
-            if (w.last_of_piece(p)) {
-                umma_commit(bar(kKmKEmpty + kst));
-                ++piece;
-            }
+            umma_commit(bar(kKmKEmpty + ka.slot));
+            ka.next(p.k_slots);
+            ka.next(p.k_slots);
             w.next(p);
         }
         if (*abort_flag != 0) {
             // A wait gave up somewhere: make sure no MMA of this thread is still in flight before TMEM is released.
-            umma_commit(bar(kKmDrain));
+            umma_commit(bar(kKmDrain + h));
             const uint64_t t0 = globaltimer_ns();
-            while (!mbar_try_wait(bar(kKmDrain), 0) && globaltimer_ns() - t0 < 20000000ull) {}
+            while (!mbar_try_wait(bar(kKmDrain + h), 0) && globaltimer_ns() - t0 < 20000000ull) {}
         }
-    } else if (warp == 18) {
-        // =========================== LSE of a unit's rows: -LSE log2(e), -inf where there is no row ===========================
-        float* s_lse = reinterpret_cast<float*>(smem + L::kLse);
-        int pos[4];
-        size_t at[4];
+      } else if (warp == 18) {
+        // =========================== LSE terms of a unit's rows ===========================
+        int pos[4], at[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int c = lane * 4 + i;
-            pos[i] = c < rows ? c / p.G : p.T_q;                     // T_q: no position of any unit
-            at[i] = size_t(c % p.G) * p.T_q + (c < rows ? c / p.G : 0);
+            const int c = lane + i * 32;
+            pos[i] = c < rows ? c / p.G : p.T_q;                         // T_q: no position of any unit
+            at[i] = (c < rows ? c % p.G : 0) * p.T_q + (c < rows ? c / p.G : 0);
         }
-        auto fetch = [&](const KeyMassWalk& k, float (&v)[4]) {
-            const int b = k.bh / p.Hk, hk = k.bh - b * p.Hk, i0 = k.u * p.P;
-            const float* src = p.LSE + (size_t(b) * p.H + hk * p.G) * p.T_q + i0;
+        // The values of the next two units are on their way while one is written.
+        int units = w.left, u = w.u0;
+        auto fetch = [&](float (&v)[4]) {
+            if (w.left <= 0) return;
+            const int i0 = u * p.P;
+            const float* src = p.LSE + size_t(w.bh) * p.G * p.T_q + i0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = pos[i] < p.T_q - i0 ? src[at[i]] : INFINITY;
+            for (int i = 0; i < 4; ++i) v[i] = pos[i] < p.T_q - i0 ? __ldg(src + at[i]) : INFINITY;
+            if (++u == w.u1) {
+                w.next(p);
+                u = w.u0;
+            }
         };
-        float v[4];
-        fetch(w, v);
+        float v[4], v1[4], v2[4];
+        fetch(v);
+        fetch(v1);
+        RingAt qa;
 #pragma unroll 1
-        for (int n = 0; w.left > 0; ++n) {
-            const int st = n & 3;
-            KeyMassWalk after = w;
-            after.next(p);
-            float ahead[4] = {0.f, 0.f, 0.f, 0.f};
-            if (after.left > 0) fetch(after, ahead);
-            if (n >= 4) wait(bar(kKmSEmpty + st), ((n - 4) >> 2) & 1, 140);
-            // a row without keys has the LSE -inf; its weights are 0
-            float4 o;
-            o.x = v[0] == -INFINITY ? -INFINITY : -v[0] * kLog2e;
-            o.y = v[1] == -INFINITY ? -INFINITY : -v[1] * kLog2e;
-            o.z = v[2] == -INFINITY ? -INFINITY : -v[2] * kLog2e;
-            o.w = v[3] == -INFINITY ? -INFINITY : -v[3] * kLog2e;
-            *reinterpret_cast<float4*>(s_lse + st * 128 + lane * 4) = o;
-            mbar_arrive(bar(kKmLFull + st));
-            w = after;
+        for (; units > 0; --units, qa.next(p.q_slots)) {
+            fetch(v2);
+            if (qa.round > 0) wait(bar(kKmQEmpty + qa.slot), (qa.round - 1) & 1, 140);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = ahead[i];
+            for (int i = 0; i < 4; ++i) {
+                uint4 t = make_uint4(0x0000ff80u, 0u, 0u, 0u);           // -inf: no row, or one without keys (LSE -inf)
+                if (fabsf(v[i]) != INFINITY) split3_bf16(-v[i] * p.inv_scale, t.x, t.y);
+                *reinterpret_cast<uint4*>(smem + L::kTerms + qa.slot * L::kTermBytes + (lane + i * 32) * 16) = t;
+                v[i] = v1[i];
+                v1[i] = v2[i];
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(kKmQFull + qa.slot));
         }
+      }
     }
 
     tc_fence_before_sync();
@@ -420,23 +488,23 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
     if (warp == 17) tmem_dealloc(tmem, 512);
 }
 
-// Adds the pieces of the key tiles that several runs share: CTA c takes the tile that starts in run c and does not end there.
-__global__ void __launch_bounds__(128)
+// Adds the pieces of the tiles that several runs share: CTA c takes the tile that starts in run c and does not end there.
+__global__ void __launch_bounds__(kKmTile)
 key_mass_join_kernel(const KeyMassParams p) {
     const int ctas = gridDim.x, c = blockIdx.x, r = threadIdx.x;
-    const int2* dir = reinterpret_cast<const int2*>(p.part + size_t(ctas) * 256);
-    grid_dependency_wait();
+    const int2* dir = reinterpret_cast<const int2*>(p.part + size_t(ctas) * 2 * kKmTile);
+    grid_dependency_wait();                           // (launched beside key_mass_kernel's last CTAs)
     // the piece at the end of run c: its second entry, or its first where the run is one piece
     int slot = 2 * c + 1;
     int2 d = dir[slot];
     if (d.y == kPieceNone) d = dir[--slot];
     if (d.y != kPieceStart) return;                   // ends in its run (or nothing is shared), or does not start in it
-    float sum = p.part[size_t(slot) * 128 + r];
-    for (int k = c + 1; k < ctas; ++k) {
-        sum += p.part[size_t(2 * k) * 128 + r];
+    float sum = p.part[size_t(slot) * kKmTile + r];
+    for (int k = c + p.team; k < ctas; k += p.team) {
+        sum += p.part[size_t(2 * k) * kKmTile + r];
         if (dir[2 * k].y & kPieceEnd) break;
     }
-    const int bh = d.x / p.tiles, key = (d.x - bh * p.tiles) * 128 + r;
+    const int bh = d.x / p.tiles, key = (d.x - bh * p.tiles) * kKmTile + r;
     if (key < p.T_kv) {
         const size_t at = size_t(bh) * p.T_cap + key;
         p.mass[at] = sum + (p.mass_in != nullptr && key < p.T_kv - p.T_q ? p.mass_in[at] : 0.f);

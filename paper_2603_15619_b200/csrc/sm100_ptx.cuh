@@ -585,6 +585,80 @@ __device__ __forceinline__ void add2_f32(float x0, float x1, float& y0, float& y
         "mov.b64 {%0, %1}, yy;\n"
         "}\n" : "+f"(y0), "+f"(y1) : "f"(x0), "f"(x1));
 }
+// Two floats in a register pair, for packed arithmetic that is written step by step.
+__device__ __forceinline__ uint64_t pair_f32(float lo, float hi) {
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
+    return v;
+}
+// y += sum of 2^(a s) over 16 scores: 8 - N pairs through the SFU, N on the FMA pipe, for kernels whose exponentials would fill the SFU (16
+// results a clock of an SM, the FMA pipe 128).  On the FMA pipe a s = n + f with the integer n nearest to it, 2^f by a polynomial of degree 5
+// on [-1/2, 1/2] (least largest relative error, by Remez exchange: 7.5e-8, in fp32 arithmetic 2.2e-7), times 2^n, whose bits are the low bits
+// of a s + 1.5 2^23 + 127.  `least` is -127 / a: from a s = -126.5 down nothing is added; NaN stays NaN.  For a > 0 and a s <= 127.
+// The steps of the two kinds alternate, so that neither pipe waits for the other's turn.
+template <int N>
+__device__ __forceinline__ void add_exp2_16(const uint32_t* s, float a, float least, uint64_t& y0, uint64_t& y1) {
+    const uint64_t aa = pair_f32(a, a), shift = pair_f32(12583039.f, 12583039.f);
+    const uint64_t c[6] = {pair_f32(1.0000000716547142f, 1.0000000716547142f), pair_f32(6.931469670650352e-1f, 6.931469670650352e-1f),
+                           pair_f32(2.402211972371072e-1f, 2.402211972371072e-1f), pair_f32(5.5507132718556444e-2f, 5.5507132718556444e-2f),
+                           pair_f32(9.675541343121328e-3f, 9.675541343121328e-3f), pair_f32(1.3276472631950876e-3f, 1.3276472631950876e-3f)};
+    constexpr int F = 8 - N;                                                 // pairs 0 .. F - 1 through the SFU
+    float e[2 * F];
+    uint64_t x[N], t[N], p[N];
+    auto fma2 = [](uint64_t& v, uint64_t a_, uint64_t b_, uint64_t c_) { asm volatile("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a_), "l"(b_), "l"(c_)); };
+    auto sfu = [&](int i) {
+        if (i >= F) return;
+        float lo, hi;
+        asm volatile("{\n.reg .b64 v;\nmov.b64 v, {%2, %3};\nmul.rn.f32x2 v, v, %4;\nmov.b64 {%0, %1}, v;\n}" : "=f"(lo), "=f"(hi)
+                     : "f"(__uint_as_float(s[2 * i])), "f"(__uint_as_float(s[2 * i + 1])), "l"(aa));
+        asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(e[2 * i]) : "f"(lo));
+        asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(e[2 * i + 1]) : "f"(hi));
+    };
+    sfu(0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float lo, hi;
+        asm volatile("max.NaN.f32 %0, %1, %2;" : "=f"(lo) : "f"(__uint_as_float(s[2 * (F + i)])), "f"(least));
+        asm volatile("max.NaN.f32 %0, %1, %2;" : "=f"(hi) : "f"(__uint_as_float(s[2 * (F + i) + 1])), "f"(least));
+        x[i] = pair_f32(lo, hi);
+    }
+    sfu(1);
+#pragma unroll
+    for (int i = 0; i < N; ++i) fma2(t[i], x[i], aa, shift);
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("sub.rn.f32x2 %0, %1, %2;" : "=l"(p[i]) : "l"(shift), "l"(t[i]));
+    sfu(2);
+#pragma unroll
+    for (int i = 0; i < N; ++i) fma2(x[i], x[i], aa, p[i]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) fma2(p[i], c[5], x[i], c[4]);
+    sfu(3);
+#pragma unroll
+    for (int i = 0; i < N; ++i) fma2(p[i], p[i], x[i], c[3]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) fma2(p[i], p[i], x[i], c[2]);
+    sfu(4);
+#pragma unroll
+    for (int i = 0; i < N; ++i) fma2(p[i], p[i], x[i], c[1]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) fma2(p[i], p[i], x[i], c[0]);
+    sfu(5);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        asm volatile("{\n.reg .b32 lo, hi;\nmov.b64 {lo, hi}, %0;\nshl.b32 lo, lo, 23;\nshl.b32 hi, hi, 23;\nmov.b64 %0, {lo, hi};\n}\n" : "+l"(t[i]));
+    sfu(6);
+    sfu(7);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        uint64_t& y = (i & 1) ? y1 : y0;
+        fma2(y, p[i], t[i], y);
+    }
+#pragma unroll
+    for (int i = 0; i < F; ++i) {
+        uint64_t& y = (i & 1) ? y0 : y1;
+        asm volatile("{\n.reg .b64 v;\nmov.b64 v, {%1, %2};\nadd.rn.f32x2 %0, %0, v;\n}" : "+l"(y) : "f"(e[2 * i]), "f"(e[2 * i + 1]));
+    }
+}
 // Four e4m3 bytes (lowest byte first) -> four floats.  Two hardware conversions to f16 pairs (exact: every e4m3 value is
 // an f16 value), then to f32.
 __device__ __forceinline__ void e4m3x4_to_f32(uint32_t w, float& f0, float& f1, float& f2, float& f3) {
