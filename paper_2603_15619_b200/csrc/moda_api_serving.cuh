@@ -108,6 +108,14 @@ int launch_shared(const void* q, const void* Kp, const void* Vp, const SharedMer
     return cuda_ok(cudaGetLastError()) ? MODA_OK : MODA_ERR_CUDA;
 }
 
+// CTAs that share the keys of a (sequence, head): their exchanges cost some 2 us, the keys of one CTA about 1 us per 1000.
+inline int evict_ranks(int T, long long rows) {
+    int ranks = 1;
+    while (ranks < 16 && T > 4096 * ranks && rows * ranks < 148) ranks *= 2;
+    while (ranks < 16 && evict_run(T, ranks) * kEvictThreads > kEvictKeys) ranks *= 2;
+    return ranks;
+}
+
 inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 size_t decode_mass_stride(int T_kv) { return (size_t(T_kv) + 7) / 8 * 8; }
@@ -227,16 +235,19 @@ int moda_kv_evict(const void* K, const void* V, const float* mass, const int* se
     int dev = 0;
     if (!cuda_ok(cudaGetDevice(&dev))) return MODA_ERR_CUDA;
     if (configured_dev != dev) {
-        if (!set_smem_limit(evict_select_kernel, evict_select_smem(kEvictKeys))) return MODA_ERR_CUDA;
+        if (!set_smem_limit(evict_select_kernel<true>, evict_select_smem(kEvictKeys / kEvictThreads)) ||
+            !cuda_ok(cudaFuncSetAttribute(evict_select_kernel<true>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) ||
+            !cuda_ok(cudaFuncSetAttribute(evict_select_kernel<false>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)))
+            return MODA_ERR_CUDA;
         configured_dev = dev;
     }
-    int ranks = 1;
-    while (ranks < 8 && T > 4096 * ranks) ranks *= 2;
-    const int share = ((T + ranks - 1) / ranks + kEvictThreads - 1) / kEvictThreads * kEvictThreads;
+    const int ranks = evict_ranks(T, B * H_kv);
+    const int run = evict_run(T, ranks);
+    const bool fits = run * kEvictThreads <= kEvictKeys;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(ranks), unsigned(H_kv), unsigned(B));
     cfg.blockDim = dim3(kEvictThreads, 1, 1);
-    cfg.dynamicSmemBytes = size_t(evict_select_smem(share));
+    cfg.dynamicSmemBytes = size_t(evict_select_smem(fits ? run : 0));
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -244,8 +255,9 @@ int moda_kv_evict(const void* K, const void* V, const float* mass, const int* se
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (!cuda_ok(cudaLaunchKernelEx(&cfg, evict_select_kernel, p))) return MODA_ERR_CUDA;
-    int rows = std::max(1, kEvictGatherRows * 8 * 8 / (H_kv * (d / 8)));
+    if (!cuda_ok(fits ? cudaLaunchKernelEx(&cfg, evict_select_kernel<true>, p) : cudaLaunchKernelEx(&cfg, evict_select_kernel<false>, p)))
+        return MODA_ERR_CUDA;
+    const int rows = std::max(1, kEvictGatherPieces / (H_kv * (d / 8)));
     const int longest = std::min(n_keep, T);
     cfg.gridDim = dim3(unsigned((longest + rows - 1) / rows), unsigned(B), 1);
     cfg.blockDim = dim3(kEvictGatherThreads, 1, 1);

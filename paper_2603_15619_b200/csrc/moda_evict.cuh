@@ -2,11 +2,11 @@
 // kept = min(n_keep, len) stay: the last min(n_recent, kept) ones, and of the older ones those of largest weight (equal weights: the lower
 // position; NaN counts as less than everything).  They keep their order.
 //
-//   evict_select_kernel  a cluster of 1 to 8 CTAs per (sequence, head): the weight of the last key kept is found digit by digit (radix
+//   evict_select_kernel  a cluster of 1 to 16 CTAs per (sequence, head): the weight of the last key kept is found digit by digit (radix
 //                        11 + 11 + 10 bits of the weight's order-preserving integer), by a histogram of the keys that agree with the digits
-//                        found so far; each CTA counts its share of the keys, held in its shared memory where they fit, and the
-//                        cluster's counts are added over distributed shared memory.  Then every warp counts what it keeps of its share and writes
-//                        positions and weights behind what is kept before it.
+//                        found so far, until all that are left in a bin stay.  Each CTA counts its share of the keys, held in its shared
+//                        memory where they fit, and the cluster's counts are added over distributed shared memory.  Then every thread, which
+//                        has a run of adjacent keys, counts what it keeps and writes positions and weights behind what is kept before it.
 //   evict_gather_kernel  copies the kept K and V rows, all heads of a few output positions per CTA: bound by HBM (each row read and
 //                        written once).
 #pragma once
@@ -45,17 +45,22 @@ __device__ __forceinline__ uint32_t evict_key(float w) {
 
 constexpr int kEvictThreads = 512;
 constexpr int kEvictWarps = kEvictThreads / 32;
-constexpr int kEvictBins = 2048;
-constexpr int kEvictKeys = 48 * 1024;             // keys of a CTA's share that its shared memory holds
+constexpr int kEvictBins = 2048, kEvictGroups = kEvictBins / 32;
+constexpr int kEvictKeys = 85 * kEvictThreads;    // keys of a CTA's share that its shared memory holds
 
 struct EvictShared {
-    uint32_t hist[kEvictBins];
-    uint32_t scan[kEvictWarps];
-    uint32_t found_bin, found_above;
+    uint32_t hist[3][kEvictBins];                 // of a pass each: nobody waits until another CTA has read the one before
+    uint32_t group[3][kEvictGroups];              // sums over 32 bins
+    uint32_t rank_group[kEvictWarps][kEvictGroups], rank_bin[kEvictWarps][32];   // what the cluster's CTAs have
     uint32_t warp_gt[kEvictWarps], warp_eq[kEvictWarps];
-    uint32_t cta_gt, cta_eq;
+    __align__(8) uint32_t cta_gt;
+    uint32_t cta_eq;
+    uint32_t pad[2];                              // the keys behind start on a 16-byte boundary
 };
-inline int evict_select_smem(int keys) { return int(sizeof(EvictShared)) + (keys < kEvictKeys ? keys : kEvictKeys) * 4; }
+static_assert(sizeof(EvictShared) % 16 == 0, "alignment of the keys");
+// Keys of a thread: an odd number, so that the threads' runs start in different banks.
+__host__ __device__ inline int evict_run(int keys, int ranks) { return ((keys + ranks - 1) / ranks + kEvictThreads - 1) / kEvictThreads | 1; }
+inline int evict_select_smem(int run) { return int(sizeof(EvictShared)) + (run * kEvictThreads < kEvictKeys ? run * kEvictThreads : kEvictKeys) * 4; }
 
 __device__ __forceinline__ uint4 ld_cluster_v4(uint32_t addr) {
     uint4 v;
@@ -68,12 +73,19 @@ __device__ __forceinline__ uint2 ld_cluster_v2(uint32_t addr) {
     return v;
 }
 
-// grid (cluster, Hk, B)
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cp_async_4(uint32_t smem_dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_dst), "l"(src) : "memory");
+}
+
+// grid (cluster, Hk, B).  FITS: a CTA's share of the keys is in its shared memory.
+template <bool FITS>
 __global__ void __launch_bounds__(kEvictThreads)
 evict_select_kernel(const EvictParams p) {
     extern __shared__ __align__(16) uint8_t evict_smem[];
     EvictShared& s = *reinterpret_cast<EvictShared*>(evict_smem);
-    uint32_t* held = reinterpret_cast<uint32_t*>(evict_smem + sizeof(EvictShared));
+    float* held = reinterpret_cast<float*>(evict_smem + sizeof(EvictShared));
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int ranks = gridDim.x, rank = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
     const int len = evict_len(p, b);
@@ -83,120 +95,162 @@ evict_select_kernel(const EvictParams p) {
     int* index = p.index + (size_t(b) * p.Hk + hk) * p.n_keep;
     float* mass_out = p.mass_out ? p.mass_out + (size_t(b) * p.Hk + hk) * p.T_out : nullptr;
 
-    // the shares of CTAs and, within them, of warps are runs of whole 32-key steps
-    const int share = ((old + ranks - 1) / ranks + 32 * kEvictWarps - 1) / (32 * kEvictWarps) * (32 * kEvictWarps);
+    const int run = evict_run(old, ranks), share = run * kEvictThreads;
     const int first = min(rank * share, old), n = min(share, old - first);
-    const bool fits = n <= kEvictKeys;
+    const bool some = want > 0 && want < old;
     grid_launch_dependents();
 
-    uint32_t above_thr = 0xffffffffu, ties = 0;                      // kept: key > above_thr, and the first `ties` keys equal to it
-    if (want == old) {
-        above_thr = 0u;
-        ties = uint32_t(old);                                        // everything: keys above 0, and all that equal 0
-    } else if (want > 0) {
-        if (fits)
-            for (int i = tid; i < n; i += kEvictThreads) held[i] = evict_key(mass[first + i]);
+    if (FITS && want > 0) {
+        const uint32_t dst = smem_u32(held);
+#pragma unroll 4
+        for (int i = tid; i < n; i += kEvictThreads) cp_async_4(dst + i * 4, mass + first + i);
+    }
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) *reinterpret_cast<uint4*>(&s.hist[pass][tid * 4]) = make_uint4(0u, 0u, 0u, 0u);
+    if (FITS) asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();
+    auto weight = [&](int i) -> float {
+        if constexpr (FITS) return held[i];
+        else return mass[first + i];
+    };
+
+    uint32_t thr = 0u, ties = uint32_t(old);                         // kept: key > thr, and the first `ties` keys equal to it
+    if (some) {
         uint32_t prefix = 0, left = uint32_t(want);                  // digits found; keys still to take among those that agree
+        uint32_t count = 0;
+        int shift = 32;
 #pragma unroll 1
         for (int pass = 0; pass < 3; ++pass) {
-            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
-            for (int i = tid; i < kEvictBins; i += kEvictThreads) s.hist[i] = 0;
-            __syncthreads();
-            for (int i = tid; i < n; i += kEvictThreads) {
-                const uint32_t k = fits ? held[i] : evict_key(mass[first + i]);
-                const bool agrees = pass == 0 || (pass == 1 ? (k >> 21) == prefix : (k >> 10) == prefix);
-                if (agrees) atomicAdd(&s.hist[(k >> shift) & uint32_t(bins - 1)], 1u);
+            const int bits = pass == 2 ? 10 : 11, agree = shift;
+            shift -= bits;
+            uint32_t* hist = s.hist[pass];
+            const uint32_t mask = (1u << bits) - 1u;
+            if (pass == 0) {
+#pragma unroll 4
+                for (int i = tid; i < n; i += kEvictThreads) atomicAdd(&hist[evict_key(weight(i)) >> 21], 1u);
+            } else {
+#pragma unroll 4
+                for (int i = tid; i < n; i += kEvictThreads) {
+                    const uint32_t k = evict_key(weight(i));
+                    if ((k >> agree) == prefix) atomicAdd(&hist[(k >> shift) & mask], 1u);
+                }
             }
-            // the cluster's counts of this thread's four bins
-            uint4 c;
+            __syncthreads();
+            {
+                const uint4 c = *reinterpret_cast<const uint4*>(&hist[tid * 4]);
+                uint32_t sum = (c.x + c.y) + (c.z + c.w);
+#pragma unroll
+                for (int off = 1; off < 8; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+                if ((tid & 7) == 0) s.group[pass][tid >> 3] = sum;
+            }
+            // The bin in two steps: its group of 32, by the groups' sums, then the bin.  Every warp finds it for itself; a warp per CTA of the
+            // cluster fetches that CTA's counts (64 and 32 words of the 2048: all of them from all took 3 us a pass).
+            uint2 g = make_uint2(0u, 0u);                            // of the groups 2 lane and 2 lane + 1, all CTAs
             if (ranks > 1) {
                 cluster_sync_all();
-                c = make_uint4(0u, 0u, 0u, 0u);
-                const uint32_t at = smem_u32(&s.hist[tid * 4]);
-#pragma unroll 4
+                if (warp < ranks)
+                    *reinterpret_cast<uint2*>(&s.rank_group[warp][2 * lane]) = ld_cluster_v2(cluster_map_shared(smem_u32(&s.group[pass][2 * lane]), uint32_t(warp)));
+                __syncthreads();
                 for (int r = 0; r < ranks; ++r) {
-                    const uint4 v = ld_cluster_v4(cluster_map_shared(at, uint32_t(r)));
-                    c.x += v.x; c.y += v.y; c.z += v.z; c.w += v.w;
+                    const uint2 v = *reinterpret_cast<const uint2*>(&s.rank_group[r][2 * lane]);
+                    g.x += v.x;
+                    g.y += v.y;
                 }
             } else {
                 __syncthreads();
-                c = *reinterpret_cast<const uint4*>(&s.hist[tid * 4]);
+                g = *reinterpret_cast<const uint2*>(&s.group[pass][2 * lane]);
             }
-            // keys in this thread's bins and those above (a scan from the top bin down)
-            const uint32_t mine = c.x + c.y + c.z + c.w;
-            uint32_t incl = mine;
+            auto above = [&](uint32_t mine) {                        // sum over the lanes above this one
+                uint32_t incl = mine;
 #pragma unroll
-            for (int off = 1; off < 32; off <<= 1) {
-                const uint32_t v = __shfl_down_sync(0xffffffffu, incl, off);
-                if (lane + off < 32) incl += v;
+                for (int off = 1; off < 32; off <<= 1) {
+                    const uint32_t v = __shfl_down_sync(0xffffffffu, incl, off);
+                    if (lane + off < 32) incl += v;
+                }
+                return incl - mine;
+            };
+            uint32_t over = above(g.x + g.y);                        // keys above this lane's two groups
+            int at = __ffs(__ballot_sync(0xffffffffu, over < left && over + g.x + g.y >= left)) - 1;   // one lane
+            const bool upper = over + g.y >= left;
+            const int group = 2 * at + __shfl_sync(0xffffffffu, int(upper), at);
+            left -= __shfl_sync(0xffffffffu, upper ? over : over + g.y, at);
+            uint32_t c = 0;                                          // of this lane's bin of the group, all CTAs
+            if (ranks > 1) {
+                if (warp < ranks) {
+                    uint32_t v;
+                    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(cluster_map_shared(smem_u32(&hist[group * 32 + lane]), uint32_t(warp))) : "memory");
+                    s.rank_bin[warp][lane] = v;
+                }
+                __syncthreads();
+                for (int r = 0; r < ranks; ++r) c += s.rank_bin[r][lane];
+            } else {
+                c = hist[group * 32 + lane];
             }
-            if (lane == 0) s.scan[warp] = incl;
-            __syncthreads();
-            uint32_t over = incl - mine;                             // keys above this thread's bins
-#pragma unroll
-            for (int w = 0; w < kEvictWarps; ++w)
-                if (w > warp) over += s.scan[w];
-            const uint32_t cc[4] = {c.x, c.y, c.z, c.w};
-#pragma unroll
-            for (int j = 3; j >= 0; --j) {
-                if (over < left && over + cc[j] >= left) { s.found_bin = uint32_t(tid * 4 + j); s.found_above = over; }
-                over += cc[j];
-            }
-            if (ranks > 1) cluster_sync_all();                       // the counts have been read: they may be cleared
-            else __syncthreads();
-            prefix = (prefix << (pass == 2 ? 10 : 11)) | s.found_bin;
-            left -= s.found_above;
+            over = above(c);
+            at = __ffs(__ballot_sync(0xffffffffu, over < left && over + c >= left)) - 1;
+            prefix = (prefix << bits) | uint32_t(group * 32 + at);
+            left -= __shfl_sync(0xffffffffu, over, at);
+            count = __shfl_sync(0xffffffffu, c, at);
+            if (count == left) break;                                // all that agree stay (the same in every CTA)
         }
-        above_thr = prefix;
-        ties = left;
+        if (shift > 0 || count == left) {
+            // key >= prefix << shift; where that is 0, every key, as `thr` and `ties` have it already
+            const uint32_t least = prefix << shift;
+            if (least != 0u) {
+                thr = least - 1u;
+                ties = 0u;
+            }
+        } else {
+            thr = prefix;
+            ties = left;
+        }
     }
 
-    // ---- positions and weights of the kept keys, in order ----
-    const int seg = share / kEvictWarps;                             // keys of a warp, a multiple of 32
-    const int w0 = min(warp * seg, n), w1 = min(w0 + seg, n);
-    auto key_of = [&](int i) { return fits && want > 0 && want < old ? held[i] : evict_key(mass[first + i]); };
+    // ---- positions and weights of the kept keys, in order: a thread has a run of adjacent ones ----
+    const int r0 = min(tid * run, n), r1 = min(r0 + run, n);
     uint32_t gt = 0, eq = 0;
-    if (want > 0) {
-        for (int i0 = w0; i0 < w1; i0 += 32) {
-            const int i = i0 + lane;
-            const uint32_t k = i < w1 ? key_of(i) : 0u;
-            gt += __popc(__ballot_sync(0xffffffffu, i < w1 && k > above_thr));
-            eq += __popc(__ballot_sync(0xffffffffu, i < w1 && k == above_thr));
+    if (some) {
+        for (int i = r0; i < r1; ++i) {
+            const uint32_t k = evict_key(weight(i));
+            gt += k > thr;
+            eq += k == thr;
         }
+    } else if (want > 0) {
+        gt = uint32_t(r1 - r0);                                      // every key
     }
-    if (lane == 0) { s.warp_gt[warp] = gt; s.warp_eq[warp] = eq; }
+    uint32_t gt_incl = gt, eq_incl = eq;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const uint32_t a = __shfl_up_sync(0xffffffffu, gt_incl, off), e = __shfl_up_sync(0xffffffffu, eq_incl, off);
+        if (lane >= off) { gt_incl += a; eq_incl += e; }
+    }
+    if (lane == 31) { s.warp_gt[warp] = gt_incl; s.warp_eq[warp] = eq_incl; }
     __syncthreads();
-    if (tid == 0) {
-        uint32_t a = 0, e = 0;
-        for (int w = 0; w < kEvictWarps; ++w) { a += s.warp_gt[w]; e += s.warp_eq[w]; }
-        s.cta_gt = a;
-        s.cta_eq = e;
+    const uint32_t w_gt = lane < kEvictWarps ? s.warp_gt[lane] : 0u, w_eq = lane < kEvictWarps ? s.warp_eq[lane] : 0u;
+    uint32_t gt_before = __reduce_add_sync(0xffffffffu, lane < warp ? w_gt : 0u) + gt_incl - gt;
+    uint32_t eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? w_eq : 0u) + eq_incl - eq;
+    if (ranks > 1) {
+        const uint32_t gt_all = __reduce_add_sync(0xffffffffu, w_gt), eq_all = __reduce_add_sync(0xffffffffu, w_eq);
+        if (tid == 0) { s.cta_gt = gt_all; s.cta_eq = eq_all; }
+        cluster_sync_all();
+        // a lane per CTA before this one
+        const uint2 v = lane < rank ? ld_cluster_v2(cluster_map_shared(smem_u32(&s.cta_gt), uint32_t(lane))) : make_uint2(0u, 0u);
+        gt_before += __reduce_add_sync(0xffffffffu, v.x);
+        eq_before += __reduce_add_sync(0xffffffffu, v.y);
+        cluster_arrive();                                            // no CTA leaves before all have read the others' counts
     }
-    if (ranks > 1) cluster_sync_all();
-    else __syncthreads();
-    uint32_t gt_before = 0, eq_before = 0;
-    for (int r = 0; r < rank; ++r) {
-        const uint2 v = ld_cluster_v2(cluster_map_shared(smem_u32(&s.cta_gt), uint32_t(r)));
-        gt_before += v.x;
-        eq_before += v.y;
-    }
-    for (int w = 0; w < warp; ++w) { gt_before += s.warp_gt[w]; eq_before += s.warp_eq[w]; }
     if (want > 0) {
-        const uint32_t below = (1u << lane) - 1u;
-        for (int i0 = w0; i0 < w1; i0 += 32) {
-            const int i = i0 + lane;
-            const uint32_t k = i < w1 ? key_of(i) : 0u;
-            const uint32_t bg = __ballot_sync(0xffffffffu, i < w1 && k > above_thr);
-            const uint32_t be = __ballot_sync(0xffffffffu, i < w1 && k == above_thr);
-            const uint32_t my_eq = eq_before + __popc(be & below);   // equal keys before this one
-            const bool is_gt = (bg >> lane) & 1u, is_eq = ((be >> lane) & 1u) && my_eq < ties;
-            if (is_gt || is_eq) {
-                const uint32_t at = gt_before + __popc(bg & below) + min(my_eq, ties);
+        uint32_t at = gt_before + min(eq_before, ties);
+        for (int i = r0; i < r1; ++i) {
+            const float w = weight(i);
+            const uint32_t k = evict_key(w);
+            const bool tie = some && k == thr;
+            if (!some || k > thr || (tie && eq_before < ties)) {
                 index[at] = first + i;
-                if (mass_out) mass_out[at] = mass[first + i];
+                if (mass_out) mass_out[at] = w;
+                ++at;
             }
-            gt_before += __popc(bg);
-            eq_before += __popc(be);
+            eq_before += tie;
         }
     }
     // the recent keys, and -1 behind the last one kept
@@ -205,11 +259,11 @@ evict_select_kernel(const EvictParams p) {
         if (i < recent && mass_out) mass_out[want + i] = mass[old + i];
     }
     if (rank == 0 && hk == 0 && tid == 0 && p.lens_out) p.lens_out[b] = kept;
-    if (ranks > 1) cluster_sync_all();                               // no CTA leaves while another reads its counts
+    if (ranks > 1) cluster_wait();
 }
 
 constexpr int kEvictGatherThreads = 256;
-constexpr int kEvictGatherRows = 32;              // (output position, head) pairs of a CTA, per 16 bytes of a row and 8 threads
+constexpr int kEvictGatherPieces = 1024;          // 16-byte pieces of K (and as many of V) of a CTA: 4 a thread, all on their way at once
 
 // grid (blocks of output positions, B): a block copies K and V of `rows` consecutive output positions, all heads.
 template <int D>
