@@ -724,6 +724,19 @@ int launch_decode_split(const DecodeParams& p, cudaStream_t stream) {
     const long long runs = !p.seq_lens && !p.cut.aligned ? (groups * units + shortest - 1) / shortest
                                                          : groups * ((units + shortest - 1) / shortest);
     const unsigned grid = unsigned((runs < p.teams ? runs : p.teams) * p.team);
+    if (p.beside) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(grid, 1, 1);
+        cfg.blockDim = dim3(kDecodeTmaThreads, 1, 1);
+        cfg.dynamicSmemBytes = L::kDynamic;
+        cfg.stream = stream;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        return cuda_ok(cudaLaunchKernelEx(&cfg, decode_split_tma_kernel<D, GF>, mK, mV, p)) ? MODA_OK : MODA_ERR_CUDA;
+    }
     decode_split_tma_kernel<D, GF><<<grid, kDecodeTmaThreads, L::kDynamic, stream>>>(mK, mV, p);
     return cuda_ok(cudaGetLastError()) ? MODA_OK : MODA_ERR_CUDA;
 }

@@ -46,10 +46,8 @@ int launch_key_mass(const void* Q, const void* K, int B, const KeyMassParams& p,
 }
 
 // ------------------------------------------------------------------------------------------------------ shared prefix
-constexpr int kSharedCtas = 148;
-
 // How the prefix of a call is cut, for `ctas` CTAs.
-SharedParams shared_plan(int B, int P, int H, int H_kv, int ctas) {
+SharedParams shared_plan(int B, int P, int H, int H_kv, int d, int ctas) {
     SharedParams p = {};
     p.B = B; p.P = P; p.H = H; p.Hk = H_kv; p.G = H / H_kv;
     if (P == 0) return p;
@@ -59,6 +57,7 @@ SharedParams shared_plan(int B, int P, int H, int H_kv, int ctas) {
     p.key_tiles = (P + 127) / 128;
     p.total = H_kv * p.pairs * p.key_tiles;
     p.run = (p.total + ctas - 1) / ctas;
+    shared_slots(d, p.row_tiles > 1, p.k_slots, p.v_slots);
     p.pieces = ((p.key_tiles + p.run - 2) / p.run + 1) * (p.row_tiles > 1 ? 1 : 2);
     return p;
 }
@@ -104,8 +103,18 @@ int launch_shared(const void* q, const void* Kp, const void* Vp, const SharedMer
         if (int rc = launch_shared_prefix<D>(q, Kp, Vp, p.pre, stream)) return rc;
     if (p.dec.T_kv > 0)
         if (int rc = launch_own_cache<D>(p.dec, stream)) return rc;
-    shared_merge_kernel<D><<<dim3(unsigned(p.dec.H), unsigned(p.dec.B)), kSharedMergeThreads, 0, stream>>>(p);
-    return cuda_ok(cudaGetLastError()) ? MODA_OK : MODA_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(p.dec.H), unsigned(p.dec.B), 1);
+    cfg.blockDim = dim3(kSharedMergeThreads, 1, 1);
+    // as for the merge of a decode step, within the 48 KiB that a kernel may have without asking
+    cfg.dynamicSmemBytes = std::min<size_t>(decode_merge_reserve((long long)p.dec.H * p.dec.B, p.dec.team * p.dec.teams), 42000);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = p.pre.P > 0 || p.dec.T_kv > 0 ? 1 : 0;
+    return cuda_ok(cudaLaunchKernelEx(&cfg, shared_merge_kernel<D>, p)) ? MODA_OK : MODA_ERR_CUDA;
 }
 
 // CTAs that share the keys of a (sequence, head): their exchanges cost some 2 us, the keys of one CTA about 1 us per 1000.
@@ -271,7 +280,7 @@ int moda_kv_evict(const void* K, const void* V, const float* mass, const int* se
 
 size_t moda_decode_shared_workspace_bytes(int B, int T_prefix, int H, int H_kv, int d) {
     if (B < 1 || T_prefix < 0 || H < 1 || check_groups(H, H_kv) || (d != 64 && d != 128)) return 0;
-    return decode_workspace_bytes(B, H, d) + shared_prefix_bytes(shared_plan(B, T_prefix, H, H_kv, kSharedCtas), d);
+    return decode_workspace_bytes(B, H, d) + shared_prefix_bytes(shared_plan(B, T_prefix, H, H_kv, d, kSharedCtas), d);
 }
 
 int moda_attn_decode_shared(const void* q, const void* K_prefix, const void* V_prefix, const void* K, const void* V, const int* seq_lens,
@@ -290,7 +299,7 @@ int moda_attn_decode_shared(const void* q, const void* K_prefix, const void* V_p
     if (!aligned4(seq_lens) || !aligned16(q) || !aligned16(O) || !aligned16(LSE) || (l > 0 && !aligned16(depth_kv_token)) ||
         (T_prefix > 0 && (!aligned16(K_prefix) || !aligned16(V_prefix))) || (max_seq_len > 0 && (!aligned16(K) || !aligned16(V))))
         return MODA_ERR_MISALIGNED;
-    const SharedParams most = shared_plan(B, T_prefix, H, H_kv, kSharedCtas);
+    const SharedParams most = shared_plan(B, T_prefix, H, H_kv, d, kSharedCtas);
     if ((long long)H_kv * most.pairs * most.key_tiles > 0x3fffffffLL) return MODA_ERR_BAD_SHAPE;
     if (!workspace || !aligned16(workspace) || workspace_bytes < moda_decode_shared_workspace_bytes(B, T_prefix, H, H_kv, d)) return MODA_ERR_WORKSPACE;
     if (int rc = check_device()) return rc;
@@ -300,7 +309,8 @@ int moda_attn_decode_shared(const void* q, const void* K_prefix, const void* V_p
     p.dec = decode_params(q, K, V, seq_lens, nullptr, depth_kv_token, B, std::max(max_seq_len, 1), T_cap, 0, 0, H, H_kv, d, l, scale, O, LSE,
                           workspace, sms);
     p.dec.T_kv = max_seq_len;
-    p.pre = shared_plan(B, T_prefix, H, H_kv, std::min(sms, kSharedCtas));
+    p.dec.beside = T_prefix > 0;
+    p.pre = shared_plan(B, T_prefix, H, H_kv, d, std::min(sms, kSharedCtas));
     uint8_t* at = static_cast<uint8_t*>(workspace) + decode_workspace_bytes(B, H, d);
     p.pre.o = reinterpret_cast<float*>(at);
     p.pre.ml = reinterpret_cast<float2*>(at + size_t(p.pre.pieces) * B * H * d * 4);

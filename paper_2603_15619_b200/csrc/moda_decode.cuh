@@ -63,6 +63,7 @@ struct DecodeParams {
     float scale_log2;             // scale * log2(e)
     float* scores;                // [B][Hk][G][score_stride]: scores of the cached keys, times log2(e) (kDecodeKeepScores only)
     size_t score_stride;
+    int beside;                   // the split kernel was launched beside another one, which it outlasts
 };
 
 // Added to the group size in the split kernel's second parameter: the form that keeps the scores, for moda_attn_decode_mass.
@@ -481,6 +482,8 @@ decode_split_tma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_c
             for (int spin = 0; spin < (1 << 20); ++spin)
                 if (mbar_try_wait(full_bar(i % L::kStages), (i / L::kStages) & 1)) break;
     }
+    // what waits for this kernel may then use what that one has written as well
+    if (p.beside) grid_dependency_wait();
 }
 
 // One CTA of four warps per (b, query head).  Lanes hold D / 32 adjacent features; a warp takes every

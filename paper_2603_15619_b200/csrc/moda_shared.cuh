@@ -10,12 +10,13 @@
 // shared_prefix_kernel: the 128-key tiles of all (kv head, pair of row tiles) groups, in this order, are cut into equal runs, one per
 // CTA; a CTA leaves a partial (m, l, o) per row for the part of each group that its run covers (a piece).  384 threads:
 //
-//   warps 0-3, 4-7   two streams, one thread per row: maximum, exponentials and sum of a score tile; P goes back over the scores
-//   warp 8 TMA producer      warps 9, 10 issue the products of streams 0, 1 (S = Q K^T, then O += P V); warp 9 owns TMEM
+//   warps 0-3, 4-7   two streams, one thread per row: a score tile goes into registers at once, so that its columns can take the next one; maximum,
+//                    exponentials and sum; P (bf16) to columns of its own
+//   warp 8 TMA producer (K tiles one ahead of V tiles)      warp 9 issues S = Q K^T of both streams, owns TMEM      warp 10 O += P V of both
 //
 // With a pair of row tiles the streams are its two tiles and both use every K, V tile.  With one row tile (few rows: bound by the bytes
 // of K and V) they take the key tiles in turn and each leaves a partial of its own.
-// TMEM columns of a stream: [0,128) scores, P in the first 64 of them, [128, 128 + D) O.
+// TMEM columns: d = 128: [0,128) scores, of the streams in turn, [128,256) P, [256,512) O; d = 64: [0,256) scores, [256,384) P, [384,512) O.
 #pragma once
 
 #include <cstdint>
@@ -30,6 +31,7 @@
 namespace moda {
 
 constexpr int kSpThreads = 384;
+constexpr int kSharedCtas = 148;       // most runs of a call: the workspace has room for their partials
 
 struct SharedParams {
     int B, P, H, Hk, G;
@@ -38,6 +40,7 @@ struct SharedParams {
     int key_tiles;                // 128-key tiles of the prefix
     int total, run;               // key tiles of all groups, of a CTA
     int pieces;                   // partials that a row has room for
+    int k_slots, v_slots;         // of shared memory, behind one or two row tiles
     float* o;                     // [pieces][B][H][d]
     float2* ml;                   // [pieces][B][H]: maximum (log2 domain), row sum
     float scale_log2;
@@ -50,15 +53,32 @@ template <int D>
 struct SharedSmem {
     static constexpr int kTileBytes = 128 * D * 2;
     static constexpr int kSubBytes = 128 * 128;
-    static constexpr int kQ = 0;                                   // two row tiles
-    static constexpr int kRing = 2 * kTileBytes;                   // K_0 V_0 K_1 V_1 ...
-    static constexpr int kStages = D == 128 ? 5 : 10;
-    static constexpr int kBars = kRing + kStages * kTileBytes;
-    static constexpr int kNumBars = 2 * kStages + 8;
+    static constexpr int kTiles = D == 128 ? 7 : 14;               // row tiles, K slots, V slots
+    static constexpr int kMaxSlots = 6;
+    static constexpr int kBars = kTiles * kTileBytes;
+    static constexpr int kNumBars = 4 * kMaxSlots + 12;
     static constexpr int kMisc = kBars + kNumBars * 8;             // tmem base, abort word
     static constexpr int kTotal = kMisc + 16;
     static constexpr int kDynamic = kTotal + 1024;
     static_assert(kDynamic <= 232448, "shared memory");
+};
+inline void shared_slots(int d, bool paired, int& k_slots, int& v_slots) {
+    k_slots = d == 64 ? 6 : paired ? 2 : 3;
+    v_slots = d == 64 ? 6 : 3;
+}
+
+enum SharedBar : int {
+    kSpKFull = 0,      // +slot (<= 6)
+    kSpKEmpty = 6,
+    kSpVFull = 12,
+    kSpVEmpty = 18,
+    kSpQFull = 24,
+    kSpSFull = 25,     // +stream
+    kSpXFree = 27,     // +stream (d = 64), one for both (d = 128): the scores are in registers
+    kSpPFull = 29,     // +stream
+    kSpODone = 31,     // +stream: P has been read, O holds everything up to this tile
+    kSpPieceDone = 33, // O has been read
+    kSpDrain = 34,     // +issuer
 };
 
 // A CTA's run, piece by piece.
@@ -81,8 +101,9 @@ __global__ void __launch_bounds__(kSpThreads, 1)
 shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK,
                      const __grid_constant__ CUtensorMap mapV, const SharedParams p) {
     using L = SharedSmem<D>;
-    constexpr int NSUB = D / 64, NST = L::kStages;
-    constexpr int kFull = 0, kEmpty = NST, kQFull = 2 * NST, kSFull = 2 * NST + 1, kPFull = 2 * NST + 3, kODone = 2 * NST + 5, kPieceDone = 2 * NST + 7;
+    constexpr int NSUB = D / 64;
+    constexpr int NX = D == 64 ? 2 : 1;                                // score buffers
+    constexpr uint32_t kColP = NX * 128, kColO = kColP + 128;
     if (g_moda_status != 0) return;   // an earlier kernel gave up a wait: do not pile up more timeouts
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -93,21 +114,26 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
     const PipeWait wait{abort_flag};
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const bool paired = p.row_tiles > 1;
-    const int rows = p.S * p.G;
+    const int rows = p.S * p.G, q_tiles = paired ? 2 : 1;
+    const uint32_t sK = sbase + q_tiles * L::kTileBytes, sV = sK + p.k_slots * L::kTileBytes;
 
     if (tid == 0) {
         *abort_flag = 0;
-        for (int s = 0; s < NST; ++s) {
-            mbar_init(bar(kFull + s), 1);
-            mbar_init(bar(kEmpty + s), paired ? 2 : 1);
+        for (int s = 0; s < L::kMaxSlots; ++s) {
+            mbar_init(bar(kSpKFull + s), 1);
+            mbar_init(bar(kSpKEmpty + s), 1);
+            mbar_init(bar(kSpVFull + s), 1);
+            mbar_init(bar(kSpVEmpty + s), 1);
         }
-        mbar_init(bar(kQFull), 1);
+        mbar_init(bar(kSpQFull), 1);
         for (int s = 0; s < 2; ++s) {
-            mbar_init(bar(kSFull + s), 1);
-            mbar_init(bar(kPFull + s), 128);
-            mbar_init(bar(kODone + s), 1);
+            mbar_init(bar(kSpSFull + s), 1);
+            mbar_init(bar(kSpXFree + s), 128);
+            mbar_init(bar(kSpPFull + s), 128);
+            mbar_init(bar(kSpODone + s), 1);
+            mbar_init(bar(kSpDrain + s), 1);
         }
-        mbar_init(bar(kPieceDone), 256);
+        mbar_init(bar(kSpPieceDone), 256);
         fence_mbar_init();
     }
     if (warp == 9) {
@@ -116,41 +142,46 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
     }
     // rows of the Q tiles that no box covers stay zero
     if (rows < 128) {
-        for (int e = tid; e < 2 * NSUB * (128 - rows) * 8; e += kSpThreads) {
+        for (int e = tid; e < q_tiles * NSUB * (128 - rows) * 8; e += kSpThreads) {
             const int piece = e & 7, r = rows + (e >> 3) % (128 - rows), sub = (e >> 3) / (128 - rows);
-            *reinterpret_cast<uint4*>(smem + L::kQ + sub * L::kSubBytes + r * 128 + piece * 16) = make_uint4(0u, 0u, 0u, 0u);
+            *reinterpret_cast<uint4*>(smem + sub * L::kSubBytes + r * 128 + piece * 16) = make_uint4(0u, 0u, 0u, 0u);
         }
         fence_proxy_async_smem();
     }
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
+    grid_launch_dependents();                                          // the split kernel of the sequences' own caches takes the SMs that this one leaves
     const uint32_t tmem = *tmem_slot;
     SharedWalk w;
     w.at = int(blockIdx.x) * p.run;
     w.end = min(w.at + p.run, p.total);
     w.set(p);
-    // Key tiles of a stream in a piece: all of them, or (one row tile) every second one.
-    const int step = paired ? 1 : 2;
 
     if (warp < 8) {
         // =========================== softmax of stream s: thread = row ===========================
+        setmaxnreg_inc<208>();
         const int s = warp >> 2, r = tid & 127;
-        const uint32_t tS = tmem + (uint32_t((warp & 3) * 32) << 16) + s * 256, tO = tS + 128;
-        int n = 0;                                                    // tiles of this stream so far
+        const uint32_t lane_addr = uint32_t((warp & 3) * 32) << 16;
+        const uint32_t tS = tmem + lane_addr + (NX == 2 ? s * 128 : 0), tP = tmem + lane_addr + kColP + s * 64, tO = tmem + lane_addr + kColO + s * D;
+        const uint32_t x_free = bar(kSpXFree + (NX == 2 ? s : 0));
+        int n = 0, tile0 = 0;                                          // tiles of this stream so far; key tiles of the CTA before the piece
 #pragma unroll 1
         while (w.at < w.end) {
             const int hk = w.group / p.pairs, pair = w.group - hk * p.pairs;
             float m_ref = -INFINITY, l_sum = 0.f;
             int in_piece = 0;
+            // one row tile: the CTA's key tiles in turn, whatever piece they belong to
 #pragma unroll 1
-            for (int j = w.j0 + (paired ? 0 : s); j < w.j1; j += step, ++n, ++in_piece) {
-                wait(bar(kSFull + s), n & 1, 150);
+            for (int j = w.j0 + (paired ? 0 : (tile0 ^ s) & 1); j < w.j1; j += paired ? 1 : 2, ++n, ++in_piece) {
+                wait(bar(kSpSFull + s), n & 1, 150);
                 tc_fence_after_sync();
                 uint32_t sv[4][32];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, sv[c]);
                 tmem_wait_ld();
+                tc_fence_before_sync();
+                mbar_arrive(x_free);
                 const int keys = p.P - j * 128;
                 if (keys < 128) {
 #pragma unroll
@@ -173,9 +204,9 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
                 const float m_new = fmaxf(m_ref, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2);
                 // The reference moves only when some row of the warp grew by more than 2^8 (the accesses to tensor memory are warp-wide).
                 const bool move = in_piece == 0 || __any_sync(0xffffffffu, m_new - m_ref > 8.f);
+                if (n > 0) wait(bar(kSpODone + s), (n - 1) & 1, 151);  // P of the tile before has been read, O is complete up to it
                 if (move) {
                     if (in_piece > 0) {
-                        wait(bar(kODone + s), (n - 1) & 1, 151);      // O holds everything up to the tile before
                         tc_fence_after_sync();
                         const float f = fast_exp2(m_ref - m_new);
                         l_sum *= f;
@@ -191,6 +222,8 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
                     }
                     m_ref = m_new;
                 }
+                const float neg_m = -m_ref;
+                tc_fence_after_sync();
                 float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
@@ -198,8 +231,8 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
 #pragma unroll
                     for (int i = 0; i < 16; i += 2) {
                         float a0, a1, b0, b1;
-                        fma2_scale(__uint_as_float(sv[c][2 * i]), __uint_as_float(sv[c][2 * i + 1]), p.scale_log2, -m_ref, a0, a1);
-                        fma2_scale(__uint_as_float(sv[c][2 * i + 2]), __uint_as_float(sv[c][2 * i + 3]), p.scale_log2, -m_ref, b0, b1);
+                        fma2_scale(__uint_as_float(sv[c][2 * i]), __uint_as_float(sv[c][2 * i + 1]), p.scale_log2, neg_m, a0, a1);
+                        fma2_scale(__uint_as_float(sv[c][2 * i + 2]), __uint_as_float(sv[c][2 * i + 3]), p.scale_log2, neg_m, b0, b1);
                         a0 = fast_exp2(a0);
                         a1 = fast_exp2(a1);
                         b0 = fast_exp2(b0);
@@ -209,13 +242,14 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
                         pk[i] = pack_bf16x2(a0, a1);
                         pk[i + 1] = pack_bf16x2(b0, b1);
                     }
-                    tmem_st16(tS + c * 16, pk);
+                    tmem_st16(tP + c * 16, pk);
                 }
                 l_sum += (s0 + s1) + (s2 + s3);
                 tmem_wait_st();
                 tc_fence_before_sync();
-                mbar_arrive(bar(kPFull + s));
+                mbar_arrive(bar(kSpPFull + s));
             }
+            tile0 += w.j1 - w.j0;
             // ---- the piece's partial of this row ----
             const int cta0 = shared_first_run(w.group, p.key_tiles, p.run);
             const int index = paired ? int(blockIdx.x) - cta0 : 2 * (int(blockIdx.x) - cta0) + s;
@@ -223,7 +257,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
             const bool there = r < rows && b < p.B;
             const size_t row = (size_t(index) * p.B + b) * p.H + hk * p.G + r % p.G;
             if (in_piece > 0) {
-                wait(bar(kODone + s), (n - 1) & 1, 152);
+                wait(bar(kSpODone + s), (n - 1) & 1, 152);
                 tc_fence_after_sync();
 #pragma unroll 1
                 for (int c = 0; c < D / 32; ++c) {
@@ -240,95 +274,118 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
             }
             if (there) p.ml[row] = make_float2(m_ref, l_sum);         // -inf, 0: a stream without a key tile in the piece
             tc_fence_before_sync();
-            mbar_arrive(bar(kPieceDone));
+            mbar_arrive(bar(kSpPieceDone));
             w.next(p);
         }
-    } else if (warp == 8) {
+    } else {
+      setmaxnreg_dec<88>();
+      if (warp == 8) {
         // =========================== TMA producer ===========================
         if (lane == 0) {
             tma_prefetch_desc(&mapQ);
             tma_prefetch_desc(&mapK);
             tma_prefetch_desc(&mapV);
-            int n = 0, piece = 0;
+            RingAt ka, va;
+            auto load = [&](const CUtensorMap& map, RingAt& at, uint32_t ring, int full, int empty, int slots, int hk, int j) {
+                if (at.round > 0) wait(bar(empty + at.slot), (at.round - 1) & 1, 161);
+                mbar_arrive_expect_tx(bar(full + at.slot), L::kTileBytes);
+#pragma unroll
+                for (int s = 0; s < NSUB; ++s)
+                    tma_load_4d(ring + at.slot * L::kTileBytes + s * L::kSubBytes, &map, bar(full + at.slot), s * 64, hk, j * 128, 0);
+                at.next(slots);
+            };
+            int piece = 0;
 #pragma unroll 1
             for (; w.at < w.end; ++piece) {
                 const int hk = w.group / p.pairs, pair = w.group - hk * p.pairs;
-                if (piece > 0) wait(bar(kPieceDone), (piece - 1) & 1, 160);   // every product of the piece before is complete
-                const int tiles = paired ? 2 : 1;
-                mbar_arrive_expect_tx(bar(kQFull), uint32_t(tiles * rows) * D * 2);
-                for (int t = 0; t < tiles; ++t)
+                load(mapK, ka, sK, kSpKFull, kSpKEmpty, p.k_slots, hk, w.j0);
+                if (piece > 0) wait(bar(kSpPieceDone), (piece - 1) & 1, 160);   // every product of the piece before is complete
+                mbar_arrive_expect_tx(bar(kSpQFull), uint32_t(q_tiles * rows) * D * 2);
+                for (int t = 0; t < q_tiles; ++t)
 #pragma unroll
                     for (int s = 0; s < NSUB; ++s)
-                        tma_load_4d(sbase + L::kQ + t * L::kTileBytes + s * L::kSubBytes, &mapQ, bar(kQFull), s * 64, hk * p.G, (2 * pair + t) * p.S, 0);
+                        tma_load_4d(sbase + t * L::kTileBytes + s * L::kSubBytes, &mapQ, bar(kSpQFull), s * 64, hk * p.G, (2 * pair + t) * p.S, 0);
 #pragma unroll 1
-                for (int j = w.j0; j < w.j1; ++j)
-#pragma unroll
-                    for (int kv = 0; kv < 2; ++kv, ++n) {
-                        const int st = n % NST;
-                        if (n >= NST) wait(bar(kEmpty + st), (n / NST - 1) & 1, 161);
-                        mbar_arrive_expect_tx(bar(kFull + st), L::kTileBytes);
-#pragma unroll
-                        for (int s = 0; s < NSUB; ++s)
-                            tma_load_4d(sbase + L::kRing + st * L::kTileBytes + s * L::kSubBytes, kv ? &mapV : &mapK, bar(kFull + st), s * 64, hk, j * 128, 0);
-                    }
+                for (int j = w.j0; j < w.j1; ++j) {
+                    if (j + 1 < w.j1) load(mapK, ka, sK, kSpKFull, kSpKEmpty, p.k_slots, hk, j + 1);
+                    load(mapV, va, sV, kSpVFull, kSpVEmpty, p.v_slots, hk, j);
+                }
                 w.next(p);
             }
         }
-    } else if (warp < 11) {
-        // =========================== products of stream s ===========================
-        const int s = warp - 9;
-        constexpr uint32_t idesc_s = make_idesc_bf16(128, 128, false, false), idesc_o = make_idesc_bf16(128, D, false, true);
-        const uint64_t dq0 = desc_kmajor_sw128(sbase + L::kQ + (paired ? s * L::kTileBytes : 0), 0);
-        const uint64_t dk0 = desc_kmajor_sw128(sbase + L::kRing, 0), dv0 = desc_mnmajor_sw128(sbase + L::kRing, 0, L::kSubBytes);
-        const uint32_t tS = tmem + s * 256, tO = tS + 128;
-        int n = 0, base = 0, piece = 0;                               // tiles of this stream; ring index of the piece's first K tile
+      } else if (warp == 9) {
+        // =========================== S = Q K^T of both streams ===========================
+        constexpr uint32_t idesc = make_idesc_bf16(128, 128, false, false);
+        const uint64_t dq0 = desc_kmajor_sw128(sbase, 0), dk0 = desc_kmajor_sw128(sK, 0);
+        RingAt ka;
+        int n = 0, piece = 0;                                          // products so far: stream n % 2
 #pragma unroll 1
         for (; w.at < w.end; ++piece) {
-            wait(bar(kQFull), piece & 1, 170);
-            bool first = true;
+            wait(bar(kSpQFull), piece & 1, 170);
 #pragma unroll 1
-            for (int j = w.j0; j < w.j1; ++j) {
-                const int ik = base + 2 * (j - w.j0), iv = ik + 1;
-                const int sk = ik % NST, sv = iv % NST;
-                wait(bar(kFull + sk), (ik / NST) & 1, 171);
-                if (!paired && ((j - w.j0) & 1) != s) {
-                    // the other stream's tile: its barriers are waited for all the same, since a wait tells only one phase from the next
-                    wait(bar(kFull + sv), (iv / NST) & 1, 175);
-                    continue;
-                }
-                if (n > 0) wait(bar(kODone + s), (n - 1) & 1, 174);   // P, in the columns of the scores, has been read
-                tc_fence_after_sync();
-                const uint64_t dk = dk0 + uint64_t((sk * L::kTileBytes) >> 4);
+            for (int j = w.j0; j < w.j1; ++j, ka.next(p.k_slots)) {
+                wait(bar(kSpKFull + ka.slot), ka.round & 1, 171);
+                const uint64_t dk = dk0 + uint64_t((ka.slot * L::kTileBytes) >> 4);
+#pragma unroll 1
+                for (int t = 0; t < q_tiles; ++t, ++n) {
+                    const int s = n & 1;
+                    // the buffer's last scores are in registers
+                    if (NX == 1) { if (n > 0) wait(bar(kSpXFree), (n - 1) & 1, 172); }
+                    else { if (n > 1) wait(bar(kSpXFree + s), ((n >> 1) - 1) & 1, 173); }
+                    tc_fence_after_sync();
+                    const uint64_t dq = dq0 + uint64_t((t * L::kTileBytes) >> 4);
+                    const uint32_t tS = tmem + (NX == 2 ? s * 128 : 0);
 #pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk) {
-                    const uint64_t o = uint64_t(((kk >> 2) * L::kSubBytes + (kk & 3) * 32) >> 4);
-                    umma_ss(tS, dq0 + o, dk + o, idesc_s, kk > 0);
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const uint64_t o = uint64_t(((kk >> 2) * L::kSubBytes + (kk & 3) * 32) >> 4);
+                        umma_ss(tS, dq + o, dk + o, idesc, kk > 0);
+                    }
+                    umma_commit(bar(kSpSFull + s));
                 }
-                umma_commit(bar(kSFull + s));
-                umma_commit(bar(kEmpty + sk));
-                wait(bar(kFull + sv), (iv / NST) & 1, 172);
-                wait(bar(kPFull + s), n & 1, 173);
-                tc_fence_after_sync();
-                const uint64_t dv = dv0 + uint64_t((sv * L::kTileBytes) >> 4);
-                umma_ts(tO, tS, dv, idesc_o, !first);
-#pragma unroll
-                for (int kk = 1; kk < 8; ++kk) umma_ts(tO, tS + kk * 8, dv + uint64_t(kk * 128), idesc_o, 1);
-                umma_commit(bar(kODone + s));
-                umma_commit(bar(kEmpty + sv));
-                first = false;
-                ++n;
+                umma_commit(bar(kSpKEmpty + ka.slot));
             }
-            base += 2 * (w.j1 - w.j0);
-            // O is read by the stream's warps before the next piece's first product writes it: they arrive on kPieceDone, which the
-            // next Q tiles wait for
             w.next(p);
         }
         if (*abort_flag != 0) {
             // A wait gave up somewhere: make sure no MMA of this warp is still in flight before TMEM is released.
-            umma_commit(bar(kODone + s));
+            umma_commit(bar(kSpDrain));
             const uint64_t t0 = globaltimer_ns();
-            while (globaltimer_ns() - t0 < 1000000ull) {}
+            while (!mbar_try_wait(bar(kSpDrain), 0) && globaltimer_ns() - t0 < 20000000ull) {}
         }
+      } else if (warp == 10) {
+        // =========================== O += P V of both streams ===========================
+        constexpr uint32_t idesc = make_idesc_bf16(128, D, false, true);
+        const uint64_t dv0 = desc_mnmajor_sw128(sV, 0, L::kSubBytes);
+        RingAt va;
+        int n = 0;
+#pragma unroll 1
+        while (w.at < w.end) {
+#pragma unroll 1
+            for (int j = w.j0; j < w.j1; ++j, va.next(p.v_slots)) {
+                wait(bar(kSpVFull + va.slot), va.round & 1, 174);
+                const uint64_t dv = dv0 + uint64_t((va.slot * L::kTileBytes) >> 4);
+#pragma unroll 1
+                for (int t = 0; t < q_tiles; ++t, ++n) {
+                    const int s = n & 1;
+                    wait(bar(kSpPFull + s), (n >> 1) & 1, 175);
+                    tc_fence_after_sync();
+                    const uint32_t tP = tmem + kColP + s * 64, tO = tmem + kColO + s * D;
+                    const bool first = paired ? j == w.j0 : j - w.j0 < 2;     // of the stream in the piece
+                    umma_ts(tO, tP, dv, idesc, !first);
+#pragma unroll
+                    for (int kk = 1; kk < 8; ++kk) umma_ts(tO, tP + kk * 8, dv + uint64_t(kk * 128), idesc, 1);
+                    umma_commit(bar(kSpODone + s));
+                }
+                umma_commit(bar(kSpVEmpty + va.slot));
+            }
+            w.next(p);
+        }
+        if (*abort_flag != 0) {
+            umma_commit(bar(kSpDrain + 1));
+            const uint64_t t0 = globaltimer_ns();
+            while (!mbar_try_wait(bar(kSpDrain + 1), 0) && globaltimer_ns() - t0 < 20000000ull) {}
+        }
+      }
     }
 
     tc_fence_before_sync();
@@ -338,7 +395,9 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
     if (warp == 9) tmem_dealloc(tmem, 512);
 }
 
-// One CTA per (b, query head): the prefix partials, the sequence's own pieces and the token's depth pairs.
+// One CTA per (b, query head): the prefix partials, the sequence's own pieces and the token's depth pairs.  It starts beside the
+// kernels before it (programmatic dependent launch) and has the depth pairs done when they end.  A chain of short dependent phases:
+// everything that a phase reads is requested at once.
 constexpr int kSharedMergeThreads = 128;
 
 struct SharedMergeParams {
@@ -349,8 +408,10 @@ struct SharedMergeParams {
 template <int D>
 __global__ void __launch_bounds__(kSharedMergeThreads)
 shared_merge_kernel(const SharedMergeParams p) {
-    constexpr int FPL = D / 32, NW = kSharedMergeThreads / 32;
-    __shared__ float s_w[2 * 160], s_own[kDecodeMaxSplits], s_d[256], s_red[NW];
+    constexpr int FPL = D / 32, NW = kSharedMergeThreads / 32, UN = 8;
+    constexpr int kMost = 2 * (kSharedCtas + 1) + kDecodeMaxSplits;  // partials of a row: streams of the prefix, own pieces
+    constexpr int PER = (kMost + kSharedMergeThreads - 1) / kSharedMergeThreads;
+    __shared__ float s_w[PER * kSharedMergeThreads], s_d[256], s_red[NW];
     __shared__ __align__(16) float s_acc[NW][D];
     const DecodeParams& q = p.dec;
     const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -366,21 +427,53 @@ shared_merge_kernel(const SharedMergeParams p) {
             x[0] = bf16_lo_to_f32(v); x[1] = bf16_hi_to_f32(v);
         }
     };
-    // ---- depth scores ----
-    float qv[FPL];
-    load_row(q.q + (size_t(b) * q.H + h) * D, qv);
+    // ---- depth pairs: their own softmax ----
+    float acc[FPL], m_d = -INFINITY, l_d = 0.f;
 #pragma unroll
-    for (int c = 0; c < FPL; ++c) qv[c] *= q.scale_log2;
-    const size_t slot_stride = size_t(q.B) * Hk_real * 2 * D;
-    const __nv_bfloat16* depth0 = q.depth + (size_t(b) * Hk_real + hk / q.kv_rep) * 2 * D;
-    for (int i = warp; i < q.l; i += NW) {
-        float kd[FPL], a = 0.f;
-        load_row(depth0 + size_t(i) * slot_stride, kd);
+    for (int c = 0; c < FPL; ++c) acc[c] = 0.f;
+    if (q.l > 0) {
+        float qv[FPL];
+        load_row(q.q + (size_t(b) * q.H + h) * D, qv);
 #pragma unroll
-        for (int c = 0; c < FPL; ++c) a = fmaf(qv[c], kd[c], a);
+        for (int c = 0; c < FPL; ++c) qv[c] *= q.scale_log2;
+        const size_t slot_stride = size_t(q.B) * Hk_real * 2 * D;
+        const __nv_bfloat16* depth0 = q.depth + (size_t(b) * Hk_real + hk / q.kv_rep) * 2 * D;
+        for (int i0 = warp; i0 < q.l; i0 += NW * UN) {
+            float kd[UN][FPL], a[UN];
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) a += __shfl_xor_sync(0xffffffffu, a, off);
-        if (lane == 0) s_d[i] = a;
+            for (int u = 0; u < UN; ++u) load_row(depth0 + size_t(min(i0 + u * NW, q.l - 1)) * slot_stride, kd[u]);
+#pragma unroll
+            for (int u = 0; u < UN; ++u) {
+                a[u] = 0.f;
+#pragma unroll
+                for (int c = 0; c < FPL; ++c) a[u] = fmaf(qv[c], kd[u][c], a[u]);
+            }
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+                for (int u = 0; u < UN; ++u) a[u] += __shfl_xor_sync(0xffffffffu, a[u], off);
+#pragma unroll
+            for (int u = 0; u < UN; ++u)
+                if (lane == 0 && i0 + u * NW < q.l) s_d[i0 + u * NW] = a[u];
+        }
+        __syncthreads();
+        for (int i = lane; i < q.l; i += 32) m_d = fmaxf(m_d, s_d[i]);
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) m_d = fmaxf(m_d, __shfl_xor_sync(0xffffffffu, m_d, off));
+        for (int i = lane; i < q.l; i += 32) l_d += fast_exp2(s_d[i] - m_d);
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) l_d += __shfl_xor_sync(0xffffffffu, l_d, off);
+        for (int i0 = warp; i0 < q.l; i0 += NW * UN) {
+            float vd[UN][FPL];
+#pragma unroll
+            for (int u = 0; u < UN; ++u) load_row(depth0 + size_t(min(i0 + u * NW, q.l - 1)) * slot_stride + D, vd[u]);
+#pragma unroll
+            for (int u = 0; u < UN; ++u) {
+                const float f = i0 + u * NW < q.l ? fast_exp2(s_d[i0 + u * NW] - m_d) : 0.f;
+#pragma unroll
+                for (int c = 0; c < FPL; ++c) acc[c] = fmaf(f, vd[u][c], acc[c]);
+            }
+        }
     }
     const int own_len = q.T_kv == 0 ? 0 : q.seq_lens ? min(max(q.seq_lens[b], 0), q.T_kv) : q.T_kv;
     int n_pre = 0;
@@ -390,80 +483,75 @@ shared_merge_kernel(const SharedMergeParams p) {
         const int c1 = int(((long long)(group + 1) * p.pre.key_tiles - 1) / p.pre.run);
         n_pre = (c1 - c0 + 1) * (p.pre.row_tiles > 1 ? 1 : 2);
     }
-    __syncthreads();
-    grid_dependency_wait();
-    int n_own = 0;
     const float* group = q.part + (size_t(b) * q.Hk + hk) * kDecodeMaxSplits * G * (D + 2);
     const float* part = group + g * (D + 2);
     const size_t split_stride = size_t(G) * (D + 2);
+    const size_t pre_stride = size_t(q.B) * q.H, pre_row = size_t(b) * q.H + h;
+    grid_dependency_wait();
+    // ---- from here on: what the kernels before have written ----
+    int n_own = 0;
     if (own_len > 0)
         n_own = q.seq_lens ? min(max(__float_as_int(__ldcg(group + (kDecodeMaxSplits - 1) * split_stride)), 1), q.max_pieces)
                            : decode_pieces_equal(q.cut, b * (q.Hk / q.team) + hk / q.team, q.T_kv, q.unit_log2);
-    const size_t pre_stride = size_t(q.B) * q.H, pre_row = size_t(b) * q.H + h;
-    // ---- maximum, weights, row sum ----
-    float mx = -INFINITY;
-    for (int i = tid; i < n_pre; i += kSharedMergeThreads) mx = fmaxf(mx, __ldcg(&p.pre.ml[i * pre_stride + pre_row].x));
-    for (int i = tid; i < n_own; i += kSharedMergeThreads) mx = fmaxf(mx, __ldcg(part + i * split_stride));
-    for (int i = tid; i < q.l; i += kSharedMergeThreads) mx = fmaxf(mx, s_d[i]);
+    const int n = n_pre + n_own;
+    float2 ml[PER];                                                  // maximum, row sum of the partials tid, tid + 128, ...
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int i = tid + k * kSharedMergeThreads;
+        ml[k] = make_float2(-INFINITY, 0.f);
+        if (i < n_pre) ml[k] = __ldcg(p.pre.ml + i * pre_stride + pre_row);
+        else if (i < n) ml[k] = __ldcg(reinterpret_cast<const float2*>(part + (i - n_pre) * split_stride));
+    }
+    float mx = m_d;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) mx = fmaxf(mx, ml[k].x);
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
     if (lane == 0) s_red[warp] = mx;
     __syncthreads();
     mx = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
-    __syncthreads();
     float lt = 0.f;
-    for (int i = tid; i < n_pre; i += kSharedMergeThreads) {
-        const float2 v = __ldcg(&p.pre.ml[i * pre_stride + pre_row]);
-        const float f = v.x == -INFINITY ? 0.f : fast_exp2(v.x - mx);
-        s_w[i] = f;
-        lt = fmaf(f, v.y, lt);
-    }
-    for (int i = tid; i < n_own; i += kSharedMergeThreads) {
-        const float m = __ldcg(part + i * split_stride);
-        const float f = m == -INFINITY ? 0.f : fast_exp2(m - mx);
-        s_own[i] = f;
-        lt = fmaf(f, __ldcg(part + i * split_stride + 1), lt);
-    }
-    for (int i = tid; i < q.l; i += kSharedMergeThreads) {
-        const float f = fast_exp2(s_d[i] - mx);
-        s_d[i] = f;
-        lt += f;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const float f = ml[k].x == -INFINITY ? 0.f : fast_exp2(ml[k].x - mx);
+        s_w[tid + k * kSharedMergeThreads] = f;
+        lt = fmaf(f, ml[k].y, lt);
     }
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) lt += __shfl_xor_sync(0xffffffffu, lt, off);
-    if (lane == 0) s_red[warp] = lt;
+    const float f_d = q.l > 0 ? fast_exp2(m_d - mx) : 0.f;
     __syncthreads();
-    lt = (s_red[0] + s_red[1]) + (s_red[2] + s_red[3]);
-    // ---- weighted sums: a warp takes every fourth partial and every fourth depth value ----
-    float acc[FPL];
+    if (lane == 0) s_red[warp] = lt;
+    // ---- weighted sum: a warp takes every fourth partial ----
 #pragma unroll
-    for (int c = 0; c < FPL; ++c) acc[c] = 0.f;
-#pragma unroll 4
-    for (int i = warp; i < n_pre; i += NW) {
-        const float f = s_w[i];
-        if (f == 0.f) continue;                                       // also a stream without keys, whose o is not written
-        const float* src = p.pre.o + (i * pre_stride + pre_row) * D + lane * FPL;
+    for (int c = 0; c < FPL; ++c) acc[c] *= f_d;
+#pragma unroll 1
+    for (int i0 = warp; i0 < n; i0 += NW * UN) {
+        float x[UN][FPL];
 #pragma unroll
-        for (int c = 0; c < FPL; ++c) acc[c] = fmaf(f, __ldcg(src + c), acc[c]);
-    }
-#pragma unroll 4
-    for (int i = warp; i < n_own; i += NW) {
-        const float f = s_own[i];
-        const float* src = part + i * split_stride + 2 + lane * FPL;
+        for (int u = 0; u < UN; ++u) {
+            const int i = min(i0 + u * NW, n - 1);
+            const float* src = i < n_pre ? p.pre.o + (i * pre_stride + pre_row) * D : part + (i - n_pre) * split_stride + 2;
 #pragma unroll
-        for (int c = 0; c < FPL; ++c) acc[c] = fmaf(f, __ldcg(src + c), acc[c]);
-    }
-#pragma unroll 4
-    for (int i = warp; i < q.l; i += NW) {
-        const float f = s_d[i];
-        float vd[FPL];
-        load_row(depth0 + size_t(i) * slot_stride + D, vd);
+            for (int c = 0; c < FPL; c += 2) {
+                const float2 v = __ldcg(reinterpret_cast<const float2*>(src + lane * FPL + c));
+                x[u][c] = v.x;
+                x[u][c + 1] = v.y;
+            }
+        }
 #pragma unroll
-        for (int c = 0; c < FPL; ++c) acc[c] = fmaf(f, vd[c], acc[c]);
+        for (int u = 0; u < UN; ++u) {
+            const float f = i0 + u * NW < n ? s_w[i0 + u * NW] : 0.f;
+            if (f != 0.f) {                                          // a stream without a key has written no o
+#pragma unroll
+                for (int c = 0; c < FPL; ++c) acc[c] = fmaf(f, x[u][c], acc[c]);
+            }
+        }
     }
 #pragma unroll
     for (int c = 0; c < FPL; ++c) s_acc[warp][lane * FPL + c] = acc[c];
     __syncthreads();
+    lt = (s_red[0] + s_red[1]) + (s_red[2] + s_red[3]) + f_d * l_d;
     // a row without any key: O = 0, LSE = -inf
     if (tid < D) {
         const float a = (s_acc[0][tid] + s_acc[1][tid]) + (s_acc[2][tid] + s_acc[3][tid]);
