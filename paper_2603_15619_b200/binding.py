@@ -169,7 +169,7 @@ _host = None
 
 class _NoHost:
     """Where the extension is not built for this Python and torch: every call takes the Python form."""
-    attn_fwd = attn_bwd = attention = decode = staticmethod(lambda *args: None)
+    attn_fwd = attn_bwd = attention = decode = key_mass = decode_mass = evict = decode_shared = staticmethod(lambda *args: None)
 
 
 def host():
@@ -801,6 +801,8 @@ def moda_attn_key_mass(Q, K, LSE, scale, T_kv=None, mass_in=None, mass=None, wor
     """Attention weight of the cached keys: mass [B,H_kv,T_cap] fp32, what the rows Q [B,T_q,H,d] at the end of the first T_kv (None: all)
     rows of K [B,T_cap,H_kv,d] gave to each of those keys, summed over the rows and the heads of a group, with the LSE [B,H,T_q] of their
     forward; added to ``mass_in`` (which may be ``mass``) for the positions before the T_q rows.  Positions past T_kv are not touched."""
+    if stream is None and (out := host().key_mass(Q, K, LSE, scale, T_kv, mass_in, mass, workspace)) is not None:
+        return out
     B, T_q, H, d = _bthd(Q, "Q")
     Bk, T_cap, Hk, dk = _bthd(K, "K")
     if (Bk, dk) != (B, d):
@@ -842,6 +844,8 @@ def moda_attn_decode_mass(q, K, V, depth_kv_token, max_seq_len, l, scale, seq_le
     """Decode step that also adds its weights to an accumulator per cached key: O [B,H,d], LSE [B,H] as from ``moda_attn_decode`` (or, with
     ``seq_lens``, ``moda_attn_decode_varlen``) and mass [B,H_kv,T_cap] fp32 = ``mass_in`` (0 for the token's own key, the last; None: 0 for all) + the
     probabilities of this step, summed over the heads of a group.  ``mass_in`` may be ``mass``; positions past a length are not touched."""
+    if stream is None and (out := host().decode_mass(q, K, V, seq_lens, depth_kv_token, max_seq_len, l, scale, mass_in, mass, O, LSE, workspace)) is not None:
+        return out
     B, H, d, T_cap, Hk = _decode_shapes(q, K, V, seq_lens, depth_kv_token, l)
     mass = _new((B, Hk, T_cap), torch.float32, q.device, stream) if mass is None else _mass(mass, "mass", (B, Hk, T_cap))
     if mass_in is not None:
@@ -863,6 +867,8 @@ def moda_kv_evict(K, V, mass, T, n_keep, n_recent=0, seq_lens=None, K_out=None, 
     last ``n_recent`` and those of largest ``mass`` [B,H_kv,T_cap] stay, ``n_keep`` in all, in their order.  Returns K_out, V_out [B,T_out,H_kv,d] (T_out =
     n_keep where they are allocated here), mass_out [B,H_kv,T_out], the old positions index int32 [B,H_kv,n_keep] (-1 behind the last one kept) and the
     new lengths lens_out int32 [B]."""
+    if stream is None and (out := host().evict(K, V, mass, T, n_keep, n_recent, seq_lens, K_out, V_out, mass_out, index, lens_out)) is not None:
+        return out
     B, T_cap, Hk, d = _bthd(K, "K")
     if _bthd(V, "V") != (B, T_cap, Hk, d):
         raise ValueError("V must be a bf16 tensor of K's shape")
@@ -893,6 +899,8 @@ def moda_attn_decode_shared(q, K_prefix, V_prefix, K, V, seq_lens, depth_kv_toke
     """Decode step of a batch that shares a prefix: q [B,H,d] attends, under one softmax, to K_prefix, V_prefix [T_prefix,H_kv,d] (read once for the
     batch), to the first seq_lens[b] (int32 [B], 0 .. max_seq_len; None: max_seq_len) rows of its own K, V [B,T_cap,H_kv,d] and to its
     depth pairs [l,B,H_kv,2,d].  K, V may be None where max_seq_len is 0.  Returns O [B,H,d] bf16 and LSE [B,H] fp32."""
+    if stream is None and (out := host().decode_shared(q, K_prefix, V_prefix, K, V, seq_lens, depth_kv_token, max_seq_len, l, scale, O, LSE, workspace)) is not None:
+        return out
     if K_prefix.dtype != torch.bfloat16 or K_prefix.dim() != 3 or V_prefix.dtype != torch.bfloat16 or V_prefix.shape != K_prefix.shape:
         raise ValueError("K_prefix and V_prefix must be bf16 [T_prefix, H_kv, d] tensors")
     P, Hk, dp = K_prefix.shape

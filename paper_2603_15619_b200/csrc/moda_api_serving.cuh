@@ -46,6 +46,17 @@ int launch_key_mass(const void* Q, const void* K, int B, const KeyMassParams& p,
 }
 
 // ------------------------------------------------------------------------------------------------------ shared prefix
+// CTAs that take adjacent heads at the same time, where the bytes of the prefix set the pace (one row tile): the largest divisor of the
+// heads up to 8.  us, a head alone / teams of 2 / 4 / 8: B = 37, 24 heads on 8, d = 64, 131072 keys 85 / 67 / 67 / 58, 10007 keys 20.0 / 20.1 /
+// 19.0 / 15.6; d = 128, 10007 keys 27.7 / 27.2 / 25.2 / 20.5.  With pairs of row tiles, bound by the products, they only leave SMs
+// without a team (B = 128, 32 heads on 8, 131072 keys, teams of 4: 225 -> 232).
+inline int shared_team(int H_kv, bool paired) {
+    if (paired) return 1;
+    int team = 8;
+    while (H_kv % team != 0) --team;
+    return team;
+}
+
 // How the prefix of a call is cut, for `ctas` CTAs.
 SharedParams shared_plan(int B, int P, int H, int H_kv, int d, int ctas) {
     SharedParams p = {};
@@ -55,8 +66,10 @@ SharedParams shared_plan(int B, int P, int H, int H_kv, int d, int ctas) {
     p.row_tiles = (B + p.S - 1) / p.S;
     p.pairs = (p.row_tiles + 1) / 2;
     p.key_tiles = (P + 127) / 128;
-    p.total = H_kv * p.pairs * p.key_tiles;
-    p.run = (p.total + ctas - 1) / ctas;
+    p.team = shared_team(H_kv, p.row_tiles > 1);
+    p.total = H_kv / p.team * p.pairs * p.key_tiles;
+    const int teams = ctas / p.team;
+    p.run = std::max((p.total + teams - 1) / teams, p.row_tiles > 1 ? 1 : 2);      // with one row tile: a key tile for each stream
     shared_slots(d, p.row_tiles > 1, p.k_slots, p.v_slots);
     p.pieces = ((p.key_tiles + p.run - 2) / p.run + 1) * (p.row_tiles > 1 ? 1 : 2);
     return p;
@@ -78,7 +91,7 @@ int launch_shared_prefix(const void* q, const void* Kp, const void* Vp, const Sh
         if (!set_smem_limit(shared_prefix_kernel<D>, L::kDynamic)) return MODA_ERR_CUDA;
         configured_dev = dev;
     }
-    shared_prefix_kernel<D><<<unsigned((p.total + p.run - 1) / p.run), kSpThreads, L::kDynamic, stream>>>(mQ, mK, mV, p);
+    shared_prefix_kernel<D><<<unsigned((p.total + p.run - 1) / p.run) * unsigned(p.team), kSpThreads, L::kDynamic, stream>>>(mQ, mK, mV, p);
     return cuda_ok(cudaGetLastError()) ? MODA_OK : MODA_ERR_CUDA;
 }
 
@@ -97,24 +110,39 @@ int launch_own_cache(const DecodeParams& p, cudaStream_t stream) {
     }
 }
 
+// Rows (sequence, query head) from which one warp merges a row, not four: they fill the SMs anyway, and a warp alone waits for nobody.  us of
+// the step, four -> one: 4096 rows of 10 partials 257 -> 249, of 3 27 -> 19; 888 rows of 38 partials 19 -> 28, 64 rows of 16 10.8 -> 13.4.
+constexpr long long kMergeWarpRows = 1776;
+
+// A short prefix (key tiles of a CTA, were it on all SMs) with own caches that are not large (elements of K): the prefix takes half of the SMs
+// and the own caches the others, at the same time; a CTA of either fills its SM.  Otherwise one behind the other, each on all
+// SMs.  us, one behind the other -> side by side, l = 24 (B, shared keys, longest own cache, heads, d): 37, 10007, 301, 24 on 8, 64: 26.9 -> 24.1; 16, 8192,
+// 512, 32 on 8, 128: 25.3 -> 22.2; 16, 30000, 512: 43.6 -> 41.4; 64, 4096, 128: 43.8 -> 34.1; 64, 16384, 128: 54.5 -> 49.6; 8, 20000, 2000, 16 on 4: 24.3 -> 20.9;
+// but 128, 4000, 200, 16 on 16, 64 (26 M elements): 56 -> 80.
+constexpr int kSharedShortRun = 16;
+constexpr long long kSharedShortOwn = 16ll << 20;
+
 template <int D>
 int launch_shared(const void* q, const void* Kp, const void* Vp, const SharedMergeParams& p, cudaStream_t stream) {
     if (p.pre.P > 0)
         if (int rc = launch_shared_prefix<D>(q, Kp, Vp, p.pre, stream)) return rc;
     if (p.dec.T_kv > 0)
         if (int rc = launch_own_cache<D>(p.dec, stream)) return rc;
+    const long long rows = (long long)p.dec.H * p.dec.B;
+    const bool many = rows > kMergeWarpRows;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(p.dec.H), unsigned(p.dec.B), 1);
+    cfg.gridDim = dim3(unsigned(many ? (rows + 3) / 4 : rows), 1, 1);
     cfg.blockDim = dim3(kSharedMergeThreads, 1, 1);
     // as for the merge of a decode step, within the 48 KiB that a kernel may have without asking
-    cfg.dynamicSmemBytes = std::min<size_t>(decode_merge_reserve((long long)p.dec.H * p.dec.B, p.dec.team * p.dec.teams), 42000);
+    cfg.dynamicSmemBytes = many ? 0 : std::min<size_t>(decode_merge_reserve(rows, p.dec.team * p.dec.teams), 42000);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = p.pre.P > 0 || p.dec.T_kv > 0 ? 1 : 0;
-    return cuda_ok(cudaLaunchKernelEx(&cfg, shared_merge_kernel<D>, p)) ? MODA_OK : MODA_ERR_CUDA;
+    return cuda_ok(many ? cudaLaunchKernelEx(&cfg, shared_merge_kernel<D, 1>, p) : cudaLaunchKernelEx(&cfg, shared_merge_kernel<D, 4>, p))
+               ? MODA_OK : MODA_ERR_CUDA;
 }
 
 // CTAs that share the keys of a (sequence, head): their exchanges cost some 2 us, the keys of one CTA about 1 us per 1000.
@@ -306,11 +334,16 @@ int moda_attn_decode_shared(const void* q, const void* K_prefix, const void* V_p
     int sms = 0;
     if (int rc = device_sm_count(&sms)) return rc;
     SharedMergeParams p = {};
+    p.pre = shared_plan(B, T_prefix, H, H_kv, d, std::min(sms, kSharedCtas));
+    int own_sms = sms;
+    if (T_prefix > 0 && max_seq_len > 0 && p.pre.run <= kSharedShortRun && (long long)B * max_seq_len * H_kv * d <= kSharedShortOwn) {
+        p.pre = shared_plan(B, T_prefix, H, H_kv, d, std::max(std::min(sms, kSharedCtas) / 2, p.pre.team));
+        own_sms = std::max(sms - (p.pre.total + p.pre.run - 1) / p.pre.run * p.pre.team, sms / 2);
+    }
     p.dec = decode_params(q, K, V, seq_lens, nullptr, depth_kv_token, B, std::max(max_seq_len, 1), T_cap, 0, 0, H, H_kv, d, l, scale, O, LSE,
-                          workspace, sms);
+                          workspace, own_sms);
     p.dec.T_kv = max_seq_len;
     p.dec.beside = T_prefix > 0;
-    p.pre = shared_plan(B, T_prefix, H, H_kv, d, std::min(sms, kSharedCtas));
     uint8_t* at = static_cast<uint8_t*>(workspace) + decode_workspace_bytes(B, H, d);
     p.pre.o = reinterpret_cast<float*>(at);
     p.pre.ml = reinterpret_cast<float2*>(at + size_t(p.pre.pieces) * B * H * d * 4);

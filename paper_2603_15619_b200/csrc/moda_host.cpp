@@ -9,7 +9,8 @@
 // Why: at the sizes of a decode step or of a small layer the device waits for the host.  Microseconds a call in a loop, through
 // Python and ctypes -> through here: decode of one sequence over 8192 keys 15.9 -> 12.3 (10 on the device); T = 256, 2 heads, l = 4:
 // forward 12.7 -> 8.5, backward 31.3 -> 20.5, moda_attention and its gradients 137 -> 86 (what is left is the engine's hand-over
-// to its device thread and back).
+// to its device thread and back).  Serving calls, host time alone: weights of the
+// keys 11 -> 6.2, decode step with weights 16 -> 9.3, eviction 17 -> 5.9, shared prefix 22 -> 8.9.
 #include <Python.h>
 #include <dlfcn.h>
 
@@ -36,7 +37,9 @@ using at::Tensor;
 #define MODA_HOST_CALLS(X)                                                                                              \
     X(moda_attn_fwd_gqa) X(moda_attn_fwd_append) X(moda_attn_bwd_gqa) X(moda_attn_bwd_gqa_stages) X(moda_attn_bwd_gqa_slot) \
     X(moda_bwd_workspace_bytes_gqa) X(moda_depth_cache_bytes) X(moda_attn_decode) X(moda_attn_decode_varlen)            \
-    X(moda_attn_decode_paged) X(moda_decode_workspace_bytes)
+    X(moda_attn_decode_paged) X(moda_decode_workspace_bytes)                                                            \
+    X(moda_attn_key_mass) X(moda_key_mass_workspace_bytes) X(moda_attn_decode_mass) X(moda_decode_mass_workspace_bytes) \
+    X(moda_kv_evict) X(moda_attn_decode_shared) X(moda_decode_shared_workspace_bytes)
 struct Library {
 #define X(name) decltype(&::name) name = nullptr;
     MODA_HOST_CALLS(X)
@@ -363,6 +366,142 @@ PyObject* decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- attention weight of cached keys, eviction, shared prefix ------------------------------------------------------------
+bool tensor_of(const Tensor* t, at::ScalarType type, std::initializer_list<int64_t> shape) { return t == nullptr || (t->scalar_type() == type && shape_is(*t, shape)); }
+bool lens_arg(PyObject* o, int B, const Tensor*& t) {
+    t = nullptr;
+    return o == Py_None || ((t = dense(o, at::kInt, 1)) != nullptr && t->size(0) == B);
+}
+Tensor scratch(const Tensor* given, size_t bytes, const Tensor& on) {
+    return given != nullptr ? *given : fresh({int64_t(std::max<size_t>(bytes, 16))}, at::kByte, on);
+}
+float* f32(const Tensor* t) { return static_cast<float*>(ptr(t)); }
+const int* i32(const Tensor* t) { return static_cast<const int*>(ptr(t)); }
+
+// key_mass(Q, K, LSE, scale, T_kv or None, mass_in, mass, workspace) -> mass
+PyObject* key_mass(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    float scale;
+    int T_kv;
+    if (n != 8 || !plain_thread() || !float_arg(a[3], scale)) return none();
+    const Tensor *Q = dense(a[0], at::kBFloat16, 4), *K = dense(a[1], at::kBFloat16, 4), *LSE = dense(a[2], at::kFloat, 3), *old, *mass, *ws;
+    if (Q == nullptr || K == nullptr || LSE == nullptr || !small(*Q) || !small(*K)) return none();
+    const int B = int(Q->size(0)), T_q = int(Q->size(1)), H = int(Q->size(2)), d = int(Q->size(3)), T_cap = int(K->size(1)), Hk = int(K->size(2));
+    if (K->size(0) != B || K->size(3) != d || !shape_is(*LSE, {B, H, T_q})) return none();
+    if (a[4] == Py_None) T_kv = T_cap;
+    else if (!int_arg(a[4], T_kv)) return none();
+    if (!optional_dense(a[5], old) || !optional_dense(a[6], mass) || !optional_dense(a[7], ws)) return none();
+    if (!tensor_of(old, at::kFloat, {B, Hk, T_cap}) || !tensor_of(mass, at::kFloat, {B, Hk, T_cap})) return none();
+    Tensor m = mass != nullptr ? *mass : Tensor();
+    {
+        NoGil nogil;
+        if (!m.defined()) m = fresh({B, Hk, T_cap}, at::kFloat, *Q);
+        const Tensor w = scratch(ws, ws != nullptr ? 0 : lib.moda_key_mass_workspace_bytes(B, T_q, T_kv, H, Hk, d), *Q);
+        const int rc = lib.moda_attn_key_mass(Q->data_ptr(), K->data_ptr(), f32(LSE), f32(old), B, T_q, T_kv, T_cap, H, Hk, d, scale, f32(&m), w.data_ptr(),
+                                              bytes_of(w), stream());
+        if (rc != 0) fail(rc, "moda_attn_key_mass");
+    }
+    return out(a[6], m);
+    END_HANDLE_TH_ERRORS
+}
+
+// What the two decode steps below have in common.
+struct Step { int B, H, d, T_cap, Hk, T, l; float scale; const Tensor *q, *K, *V, *lens, *depth; };
+bool step_args(PyObject* q, PyObject* K, PyObject* V, PyObject* lens, PyObject* depth, PyObject* T, PyObject* l, PyObject* scale, Step& s) {
+    if (!int_arg(T, s.T) || !int_arg(l, s.l) || s.l < 0 || !float_arg(scale, s.scale)) return false;
+    s.q = dense(q, at::kBFloat16, 3);
+    s.K = dense(K, at::kBFloat16, 4);
+    s.V = dense(V, at::kBFloat16, 4);
+    if (s.q == nullptr || s.K == nullptr || s.V == nullptr || !small(*s.q) || !small(*s.K) || s.V->sizes() != s.K->sizes()) return false;
+    s.B = int(s.q->size(0)), s.H = int(s.q->size(1)), s.d = int(s.q->size(2)), s.T_cap = int(s.K->size(1)), s.Hk = int(s.K->size(2));
+    if (s.K->size(0) != s.B || s.K->size(3) != s.d || !lens_arg(lens, s.B, s.lens)) return false;
+    s.depth = nullptr;
+    return s.l == 0 || ((s.depth = dense(depth, at::kBFloat16, 5)) != nullptr && shape_is(*s.depth, {s.l, s.B, s.Hk, 2, s.d}));
+}
+bool step_outputs(const Step& s, PyObject* o, PyObject* lse, PyObject* work, const Tensor*& O, const Tensor*& LSE, const Tensor*& ws) {
+    return optional_dense(o, O) && optional_dense(lse, LSE) && optional_dense(work, ws) && holds(O, at::kBFloat16, s.q->numel()) &&
+           holds(LSE, at::kFloat, int64_t(s.B) * s.H);
+}
+
+// decode_mass(q, K, V, seq_lens or None, depth, T, l, scale, mass_in, mass, O, LSE, workspace) -> (O, LSE, mass)
+PyObject* decode_mass(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Step s;
+    const Tensor *old, *mass, *O, *LSE, *ws;
+    if (n != 13 || !plain_thread() || !step_args(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], s) || !step_outputs(s, a[10], a[11], a[12], O, LSE, ws)) return none();
+    if (!optional_dense(a[8], old) || !optional_dense(a[9], mass)) return none();
+    if (!tensor_of(old, at::kFloat, {s.B, s.Hk, s.T_cap}) || !tensor_of(mass, at::kFloat, {s.B, s.Hk, s.T_cap})) return none();
+    Tensor o = O != nullptr ? *O : Tensor(), lse = LSE != nullptr ? *LSE : Tensor(), m = mass != nullptr ? *mass : Tensor();
+    {
+        NoGil nogil;
+        if (!o.defined()) o = like(*s.q);
+        if (!lse.defined()) lse = fresh({s.B, s.H}, at::kFloat, *s.q);
+        if (!m.defined()) m = fresh({s.B, s.Hk, s.T_cap}, at::kFloat, *s.q);
+        const Tensor w = scratch(ws, ws != nullptr ? 0 : lib.moda_decode_mass_workspace_bytes(s.B, s.T, s.H, s.Hk, s.d), *s.q);
+        const int rc = lib.moda_attn_decode_mass(s.q->data_ptr(), s.K->data_ptr(), s.V->data_ptr(), i32(s.lens), ptr(s.depth), f32(old), s.B, s.T, s.T_cap, s.H, s.Hk,
+                                                 s.d, s.l, s.scale, o.data_ptr(), f32(&lse), f32(&m), w.data_ptr(), bytes_of(w), stream());
+        if (rc != 0) fail(rc, "moda_attn_decode_mass");
+    }
+    return Py_BuildValue("NNN", out(a[10], o), out(a[11], lse), out(a[9], m));
+    END_HANDLE_TH_ERRORS
+}
+
+// evict(K, V, mass, T, n_keep, n_recent, seq_lens or None, K_out, V_out, mass_out, index, lens_out) -> (K_out, V_out, mass_out, index, lens_out)
+PyObject* evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int T, keep, recent;
+    if (n != 12 || !plain_thread() || !int_arg(a[3], T) || !int_arg(a[4], keep) || !int_arg(a[5], recent) || keep < 1) return none();
+    const Tensor *K = dense(a[0], at::kBFloat16, 4), *V = dense(a[1], at::kBFloat16, 4), *mass = dense(a[2], at::kFloat, 3), *lens, *g[5];
+    if (K == nullptr || V == nullptr || mass == nullptr || !small(*K) || V->sizes() != K->sizes()) return none();
+    const int B = int(K->size(0)), T_cap = int(K->size(1)), Hk = int(K->size(2)), d = int(K->size(3));
+    if (!shape_is(*mass, {B, Hk, T_cap}) || !lens_arg(a[6], B, lens)) return none();
+    for (int i = 0; i < 5; ++i)
+        if (!optional_dense(a[7 + i], g[i])) return none();
+    int64_t T_out = keep;
+    if (g[0] != nullptr && g[0]->dim() == 4) T_out = g[0]->size(1);
+    if (T_out > INT_MAX || !tensor_of(g[0], at::kBFloat16, {B, T_out, Hk, d}) || !tensor_of(g[1], at::kBFloat16, {B, T_out, Hk, d}) ||
+        !tensor_of(g[2], at::kFloat, {B, Hk, T_out}) || !tensor_of(g[3], at::kInt, {B, Hk, keep}) || !tensor_of(g[4], at::kInt, {B})) return none();
+    Tensor t[5];
+    for (int i = 0; i < 5; ++i)
+        if (g[i] != nullptr) t[i] = *g[i];
+    {
+        NoGil nogil;
+        for (int i = 0; i < 2; ++i)
+            if (!t[i].defined()) t[i] = fresh({B, T_out, Hk, d}, at::kBFloat16, *K);
+        if (!t[2].defined()) t[2] = fresh({B, Hk, T_out}, at::kFloat, *K);
+        if (!t[3].defined()) t[3] = fresh({B, Hk, keep}, at::kInt, *K);
+        if (!t[4].defined()) t[4] = fresh({B}, at::kInt, *K);
+        const int rc = lib.moda_kv_evict(K->data_ptr(), V->data_ptr(), f32(mass), i32(lens), B, T, T_cap, Hk, d, keep, recent, int(T_out), t[0].data_ptr(), t[1].data_ptr(),
+                                         f32(&t[2]), static_cast<int*>(t[3].data_ptr()), static_cast<int*>(t[4].data_ptr()), stream());
+        if (rc != 0) fail(rc, "moda_kv_evict");
+    }
+    return Py_BuildValue("NNNNN", out(a[7], t[0]), out(a[8], t[1]), out(a[9], t[2]), out(a[10], t[3]), out(a[11], t[4]));
+    END_HANDLE_TH_ERRORS
+}
+
+// decode_shared(q, K_prefix, V_prefix, K, V, seq_lens or None, depth, T, l, scale, O, LSE, workspace) -> (O, LSE)
+PyObject* decode_shared(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Step s;
+    const Tensor *O, *LSE, *ws;
+    if (n != 13 || !plain_thread() || !step_args(a[0], a[3], a[4], a[5], a[6], a[7], a[8], a[9], s) || !step_outputs(s, a[10], a[11], a[12], O, LSE, ws)) return none();
+    const Tensor *Kp = dense(a[1], at::kBFloat16, 3), *Vp = dense(a[2], at::kBFloat16, 3);
+    if (Kp == nullptr || Vp == nullptr || !small(*Kp) || Vp->sizes() != Kp->sizes() || Kp->size(1) != s.Hk || Kp->size(2) != s.d) return none();
+    const int P = int(Kp->size(0));
+    Tensor o = O != nullptr ? *O : Tensor(), lse = LSE != nullptr ? *LSE : Tensor();
+    {
+        NoGil nogil;
+        if (!o.defined()) o = like(*s.q);
+        if (!lse.defined()) lse = fresh({s.B, s.H}, at::kFloat, *s.q);
+        const Tensor w = scratch(ws, ws != nullptr ? 0 : lib.moda_decode_shared_workspace_bytes(s.B, P, s.H, s.Hk, s.d), *s.q);
+        const int rc = lib.moda_attn_decode_shared(s.q->data_ptr(), Kp->data_ptr(), Vp->data_ptr(), s.K->data_ptr(), s.V->data_ptr(), i32(s.lens), ptr(s.depth), s.B, P,
+                                                   s.T, s.T_cap, s.H, s.Hk, s.d, s.l, s.scale, o.data_ptr(), f32(&lse), w.data_ptr(), bytes_of(w), stream());
+        if (rc != 0) fail(rc, "moda_attn_decode_shared");
+    }
+    return Py_BuildValue("NN", out(a[10], o), out(a[11], lse));
+    END_HANDLE_TH_ERRORS
+}
+
 // ---- module -----------------------------------------------------------------------------------------------------------
 // bind(handle of libmoda_b200.so, check, DeviceContext): must come first
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -385,7 +524,9 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyMethodDef methods[] = {
     {"bind", FAST(bind), METH_FASTCALL, nullptr},         {"attn_fwd", FAST(attn_fwd), METH_FASTCALL, nullptr},
     {"attn_bwd", FAST(attn_bwd), METH_FASTCALL, nullptr}, {"attention", FAST(attention), METH_FASTCALL, nullptr},
-    {"decode", FAST(decode), METH_FASTCALL, nullptr},     {nullptr, nullptr, 0, nullptr},
+    {"decode", FAST(decode), METH_FASTCALL, nullptr},     {"key_mass", FAST(key_mass), METH_FASTCALL, nullptr},
+    {"decode_mass", FAST(decode_mass), METH_FASTCALL, nullptr}, {"evict", FAST(evict), METH_FASTCALL, nullptr},
+    {"decode_shared", FAST(decode_shared), METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

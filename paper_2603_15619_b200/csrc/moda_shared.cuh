@@ -7,8 +7,10 @@
 //   decode_split_tma_kernel  the sequences' own caches (moda_decode.cuh)
 //   shared_merge_kernel    joins the partials of both with the depth pairs.
 //
-// shared_prefix_kernel: the 128-key tiles of all (kv head, pair of row tiles) groups, in this order, are cut into equal runs, one per
-// CTA; a CTA leaves a partial (m, l, o) per row for the part of each group that its run covers (a piece).  384 threads:
+// shared_prefix_kernel: where few rows leave the pace to the bytes of K and V, teams of CTAs take adjacent kv heads, whose rows are adjacent
+// in memory, at the same time (a head alone is read in pieces of 2 d bytes: B = 37, 131072 keys, 8 heads, d = 64: 85 us, 58 us with teams of 8).
+// The 128-key tiles of all (heads of a team, pair of row tiles) groups, in this order, are cut into equal runs, one per team; a CTA leaves a
+// partial (m, l, o) per row for the part of each group that its run covers (a piece).  384 threads:
 //
 //   warps 0-3, 4-7   two streams, one thread per row: a score tile goes into registers at once, so that its columns can take the next one; maximum,
 //                    exponentials and sum; P (bf16) to columns of its own
@@ -38,7 +40,8 @@ struct SharedParams {
     int S;                        // sequences of a row tile: 128 / G
     int row_tiles, pairs;         // row tiles; groups of two of them (1: one stream per key tile in turn)
     int key_tiles;                // 128-key tiles of the prefix
-    int total, run;               // key tiles of all groups, of a CTA
+    int team;                     // CTAs of a team (divides Hk)
+    int total, run;               // key tiles of all groups, of a team
     int pieces;                   // partials that a row has room for
     int k_slots, v_slots;         // of shared memory, behind one or two row tiles
     float* o;                     // [pieces][B][H][d]
@@ -154,7 +157,8 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
     grid_launch_dependents();                                          // the split kernel of the sequences' own caches takes the SMs that this one leaves
     const uint32_t tmem = *tmem_slot;
     SharedWalk w;
-    w.at = int(blockIdx.x) * p.run;
+    const int my_team = int(blockIdx.x) / p.team, member = int(blockIdx.x) % p.team;
+    w.at = my_team * p.run;
     w.end = min(w.at + p.run, p.total);
     w.set(p);
 
@@ -168,7 +172,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
         int n = 0, tile0 = 0;                                          // tiles of this stream so far; key tiles of the CTA before the piece
 #pragma unroll 1
         while (w.at < w.end) {
-            const int hk = w.group / p.pairs, pair = w.group - hk * p.pairs;
+            const int heads = w.group / p.pairs, pair = w.group - heads * p.pairs, hk = heads * p.team + member;
             float m_ref = -INFINITY, l_sum = 0.f;
             int in_piece = 0;
             // one row tile: the CTA's key tiles in turn, whatever piece they belong to
@@ -252,7 +256,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
             tile0 += w.j1 - w.j0;
             // ---- the piece's partial of this row ----
             const int cta0 = shared_first_run(w.group, p.key_tiles, p.run);
-            const int index = paired ? int(blockIdx.x) - cta0 : 2 * (int(blockIdx.x) - cta0) + s;
+            const int index = paired ? my_team - cta0 : 2 * (my_team - cta0) + s;
             const int b = (paired ? 2 * pair + s : 0) * p.S + r / p.G;
             const bool there = r < rows && b < p.B;
             const size_t row = (size_t(index) * p.B + b) * p.H + hk * p.G + r % p.G;
@@ -297,7 +301,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
             int piece = 0;
 #pragma unroll 1
             for (; w.at < w.end; ++piece) {
-                const int hk = w.group / p.pairs, pair = w.group - hk * p.pairs;
+                const int heads = w.group / p.pairs, pair = w.group - heads * p.pairs, hk = heads * p.team + member;
                 load(mapK, ka, sK, kSpKFull, kSpKEmpty, p.k_slots, hk, w.j0);
                 if (piece > 0) wait(bar(kSpPieceDone), (piece - 1) & 1, 160);   // every product of the piece before is complete
                 mbar_arrive_expect_tx(bar(kSpQFull), uint32_t(q_tiles * rows) * D * 2);
@@ -395,7 +399,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
     if (warp == 9) tmem_dealloc(tmem, 512);
 }
 
-// One CTA per (b, query head): the prefix partials, the sequence's own pieces and the token's depth pairs.  It starts beside the
+// Per (b, query head): the prefix partials, the sequence's own pieces and the token's depth pairs, by WPR warps.  It starts beside the
 // kernels before it (programmatic dependent launch) and has the depth pairs done when they end.  A chain of short dependent phases:
 // everything that a phase reads is requested at once.
 constexpr int kSharedMergeThreads = 128;
@@ -405,27 +409,45 @@ struct SharedMergeParams {
     SharedParams pre;             // prefix (P == 0: none)
 };
 
-template <int D>
+template <int D, int WPR>
 __global__ void __launch_bounds__(kSharedMergeThreads)
 shared_merge_kernel(const SharedMergeParams p) {
-    constexpr int FPL = D / 32, NW = kSharedMergeThreads / 32, UN = 8;
+    constexpr int FPL = D / 32, ROWS = kSharedMergeThreads / 32 / WPR, UN = 8;
     constexpr int kMost = 2 * (kSharedCtas + 1) + kDecodeMaxSplits;  // partials of a row: streams of the prefix, own pieces
-    constexpr int PER = (kMost + kSharedMergeThreads - 1) / kSharedMergeThreads;
-    __shared__ float s_w[PER * kSharedMergeThreads], s_d[256], s_red[NW];
-    __shared__ __align__(16) float s_acc[NW][D];
+    __shared__ float s_w[ROWS][kMost], s_d[ROWS][256], s_red[2][4];
+    __shared__ __align__(16) float s_acc[WPR > 1 ? WPR : 1][D];
     const DecodeParams& q = p.dec;
-    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int warp = int(threadIdx.x >> 5) % WPR, lane = threadIdx.x & 31, tid = warp * 32 + lane;   // in the row
+    const int row_in = int(threadIdx.x >> 5) / WPR;
+    const int row = int(blockIdx.x) * ROWS + row_in;                 // b * H + h
+    const bool there = ROWS == 1 || row < q.B * q.H;
+    const int b = there ? row / q.H : 0, h = there ? row - b * q.H : 0;
     const int G = q.H / q.Hk, hk = h / G, g = h - hk * G;            // groups of at most 8 heads, as the split kernel has them
     const int Hk_real = q.Hk / q.kv_rep;
-
-    auto load_row = [&](const __nv_bfloat16* row, float (&x)[FPL]) {
+    float* w_of = s_w[row_in];
+    float* d_of = s_d[row_in];
+    auto sync = [] {
+        if constexpr (WPR > 1) __syncthreads();
+        else __syncwarp();
+    };
+    auto load_row = [&](const __nv_bfloat16* src, float (&x)[FPL]) {
         if constexpr (FPL == 4) {
-            const uint2 v = *reinterpret_cast<const uint2*>(row + lane * 4);
+            const uint2 v = *reinterpret_cast<const uint2*>(src + lane * 4);
             x[0] = bf16_lo_to_f32(v.x); x[1] = bf16_hi_to_f32(v.x); x[2] = bf16_lo_to_f32(v.y); x[3] = bf16_hi_to_f32(v.y);
         } else {
-            const uint32_t v = *reinterpret_cast<const uint32_t*>(row + lane * 2);
+            const uint32_t v = *reinterpret_cast<const uint32_t*>(src + lane * 2);
             x[0] = bf16_lo_to_f32(v); x[1] = bf16_hi_to_f32(v);
         }
+    };
+    auto warp_max = [](float v) {
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
+        return v;
+    };
+    auto warp_sum = [](float v) {
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+        return v;
     };
     // ---- depth pairs: their own softmax ----
     float acc[FPL], m_d = -INFINITY, l_d = 0.f;
@@ -433,15 +455,15 @@ shared_merge_kernel(const SharedMergeParams p) {
     for (int c = 0; c < FPL; ++c) acc[c] = 0.f;
     if (q.l > 0) {
         float qv[FPL];
-        load_row(q.q + (size_t(b) * q.H + h) * D, qv);
+        load_row(q.q + size_t(there ? row : 0) * D, qv);
 #pragma unroll
         for (int c = 0; c < FPL; ++c) qv[c] *= q.scale_log2;
         const size_t slot_stride = size_t(q.B) * Hk_real * 2 * D;
         const __nv_bfloat16* depth0 = q.depth + (size_t(b) * Hk_real + hk / q.kv_rep) * 2 * D;
-        for (int i0 = warp; i0 < q.l; i0 += NW * UN) {
+        for (int i0 = warp; i0 < q.l; i0 += WPR * UN) {
             float kd[UN][FPL], a[UN];
 #pragma unroll
-            for (int u = 0; u < UN; ++u) load_row(depth0 + size_t(min(i0 + u * NW, q.l - 1)) * slot_stride, kd[u]);
+            for (int u = 0; u < UN; ++u) load_row(depth0 + size_t(min(i0 + u * WPR, q.l - 1)) * slot_stride, kd[u]);
 #pragma unroll
             for (int u = 0; u < UN; ++u) {
                 a[u] = 0.f;
@@ -454,22 +476,20 @@ shared_merge_kernel(const SharedMergeParams p) {
                 for (int u = 0; u < UN; ++u) a[u] += __shfl_xor_sync(0xffffffffu, a[u], off);
 #pragma unroll
             for (int u = 0; u < UN; ++u)
-                if (lane == 0 && i0 + u * NW < q.l) s_d[i0 + u * NW] = a[u];
+                if (lane == 0 && i0 + u * WPR < q.l) d_of[i0 + u * WPR] = a[u];
         }
-        __syncthreads();
-        for (int i = lane; i < q.l; i += 32) m_d = fmaxf(m_d, s_d[i]);
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) m_d = fmaxf(m_d, __shfl_xor_sync(0xffffffffu, m_d, off));
-        for (int i = lane; i < q.l; i += 32) l_d += fast_exp2(s_d[i] - m_d);
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) l_d += __shfl_xor_sync(0xffffffffu, l_d, off);
-        for (int i0 = warp; i0 < q.l; i0 += NW * UN) {
+        sync();
+        for (int i = lane; i < q.l; i += 32) m_d = fmaxf(m_d, d_of[i]);
+        m_d = warp_max(m_d);
+        for (int i = lane; i < q.l; i += 32) l_d += fast_exp2(d_of[i] - m_d);
+        l_d = warp_sum(l_d);
+        for (int i0 = warp; i0 < q.l; i0 += WPR * UN) {
             float vd[UN][FPL];
 #pragma unroll
-            for (int u = 0; u < UN; ++u) load_row(depth0 + size_t(min(i0 + u * NW, q.l - 1)) * slot_stride + D, vd[u]);
+            for (int u = 0; u < UN; ++u) load_row(depth0 + size_t(min(i0 + u * WPR, q.l - 1)) * slot_stride + D, vd[u]);
 #pragma unroll
             for (int u = 0; u < UN; ++u) {
-                const float f = i0 + u * NW < q.l ? fast_exp2(s_d[i0 + u * NW] - m_d) : 0.f;
+                const float f = i0 + u * WPR < q.l ? fast_exp2(d_of[i0 + u * WPR] - m_d) : 0.f;
 #pragma unroll
                 for (int c = 0; c < FPL; ++c) acc[c] = fmaf(f, vd[u][c], acc[c]);
             }
@@ -478,7 +498,7 @@ shared_merge_kernel(const SharedMergeParams p) {
     const int own_len = q.T_kv == 0 ? 0 : q.seq_lens ? min(max(q.seq_lens[b], 0), q.T_kv) : q.T_kv;
     int n_pre = 0;
     if (p.pre.P > 0) {
-        const int group = (h / p.pre.G) * p.pre.pairs + (p.pre.row_tiles > 1 ? b / (2 * p.pre.S) : 0);
+        const int group = (h / p.pre.G / p.pre.team) * p.pre.pairs + (p.pre.row_tiles > 1 ? b / (2 * p.pre.S) : 0);
         const int c0 = shared_first_run(group, p.pre.key_tiles, p.pre.run);
         const int c1 = int(((long long)(group + 1) * p.pre.key_tiles - 1) / p.pre.run);
         n_pre = (c1 - c0 + 1) * (p.pre.row_tiles > 1 ? 1 : 2);
@@ -486,7 +506,7 @@ shared_merge_kernel(const SharedMergeParams p) {
     const float* group = q.part + (size_t(b) * q.Hk + hk) * kDecodeMaxSplits * G * (D + 2);
     const float* part = group + g * (D + 2);
     const size_t split_stride = size_t(G) * (D + 2);
-    const size_t pre_stride = size_t(q.B) * q.H, pre_row = size_t(b) * q.H + h;
+    const size_t pre_stride = size_t(q.B) * q.H, pre_row = size_t(there ? row : 0);
     grid_dependency_wait();
     // ---- from here on: what the kernels before have written ----
     int n_own = 0;
@@ -494,43 +514,46 @@ shared_merge_kernel(const SharedMergeParams p) {
         n_own = q.seq_lens ? min(max(__float_as_int(__ldcg(group + (kDecodeMaxSplits - 1) * split_stride)), 1), q.max_pieces)
                            : decode_pieces_equal(q.cut, b * (q.Hk / q.team) + hk / q.team, q.T_kv, q.unit_log2);
     const int n = n_pre + n_own;
-    float2 ml[PER];                                                  // maximum, row sum of the partials tid, tid + 128, ...
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        const int i = tid + k * kSharedMergeThreads;
-        ml[k] = make_float2(-INFINITY, 0.f);
-        if (i < n_pre) ml[k] = __ldcg(p.pre.ml + i * pre_stride + pre_row);
-        else if (i < n) ml[k] = __ldcg(reinterpret_cast<const float2*>(part + (i - n_pre) * split_stride));
+    auto fetch_ml = [&](int i) {                                     // maximum, row sum of a partial
+        if (i < n_pre) return __ldcg(p.pre.ml + i * pre_stride + pre_row);
+        if (i < n) return __ldcg(reinterpret_cast<const float2*>(part + (i - n_pre) * split_stride));
+        return make_float2(-INFINITY, 0.f);
+    };
+    // one partial a thread in registers, the others (very long prefixes, many runs) in shared memory
+    const float2 ml = fetch_ml(tid);
+    float mx = fmaxf(m_d, ml.x);
+    for (int i = tid + 32 * WPR; i < n; i += 32 * WPR) mx = fmaxf(mx, fetch_ml(i).x);
+    mx = warp_max(mx);
+    if constexpr (WPR > 1) {
+        if (lane == 0) s_red[0][warp] = mx;
+        __syncthreads();
+        mx = fmaxf(fmaxf(s_red[0][0], s_red[0][1]), fmaxf(s_red[0][2], s_red[0][3]));
     }
-    float mx = m_d;
-#pragma unroll
-    for (int k = 0; k < PER; ++k) mx = fmaxf(mx, ml[k].x);
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-    if (lane == 0) s_red[warp] = mx;
-    __syncthreads();
-    mx = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
-    float lt = 0.f;
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        const float f = ml[k].x == -INFINITY ? 0.f : fast_exp2(ml[k].x - mx);
-        s_w[tid + k * kSharedMergeThreads] = f;
-        lt = fmaf(f, ml[k].y, lt);
+    auto weight = [&](const float2& v) { return v.x == -INFINITY ? 0.f : fast_exp2(v.x - mx); };
+    float f = weight(ml), lt = f * ml.y;
+    if (tid < n) w_of[tid] = f;
+    for (int i = tid + 32 * WPR; i < n; i += 32 * WPR) {
+        const float2 v = fetch_ml(i);
+        w_of[i] = f = weight(v);
+        lt = fmaf(f, v.y, lt);
     }
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) lt += __shfl_xor_sync(0xffffffffu, lt, off);
+    lt = warp_sum(lt);
     const float f_d = q.l > 0 ? fast_exp2(m_d - mx) : 0.f;
-    __syncthreads();
-    if (lane == 0) s_red[warp] = lt;
-    // ---- weighted sum: a warp takes every fourth partial ----
+    if constexpr (WPR > 1) {
+        if (lane == 0) s_red[1][warp] = lt;
+    }
+    sync();
+    if constexpr (WPR > 1) lt = (s_red[1][0] + s_red[1][1]) + (s_red[1][2] + s_red[1][3]);
+    lt += f_d * l_d;
+    // ---- weighted sum: a warp takes every WPR-th partial ----
 #pragma unroll
     for (int c = 0; c < FPL; ++c) acc[c] *= f_d;
 #pragma unroll 1
-    for (int i0 = warp; i0 < n; i0 += NW * UN) {
+    for (int i0 = warp; i0 < n; i0 += WPR * UN) {
         float x[UN][FPL];
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
-            const int i = min(i0 + u * NW, n - 1);
+            const int i = min(i0 + u * WPR, n - 1);
             const float* src = i < n_pre ? p.pre.o + (i * pre_stride + pre_row) * D : part + (i - n_pre) * split_stride + 2;
 #pragma unroll
             for (int c = 0; c < FPL; c += 2) {
@@ -541,23 +564,31 @@ shared_merge_kernel(const SharedMergeParams p) {
         }
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
-            const float f = i0 + u * NW < n ? s_w[i0 + u * NW] : 0.f;
-            if (f != 0.f) {                                          // a stream without a key has written no o
+            const float wt = i0 + u * WPR < n ? w_of[i0 + u * WPR] : 0.f;
+            if (wt != 0.f) {                                         // a stream without a key has written no o
 #pragma unroll
-                for (int c = 0; c < FPL; ++c) acc[c] = fmaf(f, x[u][c], acc[c]);
+                for (int c = 0; c < FPL; ++c) acc[c] = fmaf(wt, x[u][c], acc[c]);
             }
         }
     }
-#pragma unroll
-    for (int c = 0; c < FPL; ++c) s_acc[warp][lane * FPL + c] = acc[c];
-    __syncthreads();
-    lt = (s_red[0] + s_red[1]) + (s_red[2] + s_red[3]) + f_d * l_d;
     // a row without any key: O = 0, LSE = -inf
-    if (tid < D) {
-        const float a = (s_acc[0][tid] + s_acc[1][tid]) + (s_acc[2][tid] + s_acc[3][tid]);
-        q.O[(size_t(b) * q.H + h) * D + tid] = __float2bfloat16(lt > 0.f || lt != lt ? a / lt : 0.f);
+    const float inv = lt > 0.f || lt != lt ? 1.f / lt : 0.f;
+    if constexpr (WPR > 1) {
+#pragma unroll
+        for (int c = 0; c < FPL; ++c) s_acc[warp][lane * FPL + c] = acc[c];
+        __syncthreads();
+        if (tid < D) {
+            const float a = (s_acc[0][tid] + s_acc[1][tid]) + (s_acc[2][tid] + s_acc[3][tid]);
+            q.O[size_t(row) * D + tid] = __float2bfloat16(inv == 0.f ? 0.f : a * inv);
+        }
+    } else if (there) {
+        if constexpr (FPL == 4)
+            *reinterpret_cast<uint2*>(q.O + size_t(row) * D + lane * 4) =
+                inv == 0.f ? make_uint2(0u, 0u) : make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
+        else
+            *reinterpret_cast<uint32_t*>(q.O + size_t(row) * D + lane * 2) = inv == 0.f ? 0u : pack_bf16x2(acc[0] * inv, acc[1] * inv);
     }
-    if (tid == 0) q.LSE[size_t(b) * q.H + h] = (mx + log2f(lt)) * kDecodeLn2;
+    if (tid == 0 && there) q.LSE[row] = (mx + log2f(lt)) * kDecodeLn2;
 }
 
 }  // namespace moda
