@@ -241,8 +241,16 @@ int moda_attn_decode_mass(const void* q, const void* K, const void* V, const int
     m.scores = p.scores; m.LSE = LSE; m.mass_in = mass_in; m.mass = mass; m.seq_lens = seq_lens;
     m.stride = p.score_stride; m.T_kv = T_kv; m.T_cap = T_cap; m.H = H; m.Hk = H_kv;
     const unsigned blocks = unsigned((T_kv + 4 * kDecodeMassThreads - 1) / (4 * kDecodeMassThreads));
-    decode_key_mass_kernel<<<dim3(blocks, unsigned(H_kv), unsigned(B)), kDecodeMassThreads, 0, st>>>(m);
-    return cuda_ok(cudaGetLastError()) ? MODA_OK : MODA_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks, unsigned(H_kv), unsigned(B));
+    cfg.blockDim = dim3(kDecodeMassThreads, 1, 1);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cuda_ok(cudaLaunchKernelEx(&cfg, decode_key_mass_kernel, m)) ? MODA_OK : MODA_ERR_CUDA;
 }
 
 int moda_kv_evict(const void* K, const void* V, const float* mass, const int* seq_lens,

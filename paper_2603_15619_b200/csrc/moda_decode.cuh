@@ -264,6 +264,8 @@ decode_split_tma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_c
         if (lane == 0) {
             tma_prefetch_desc(&mapK);
             tma_prefetch_desc(&mapV);
+            [[maybe_unused]] uint64_t policy = 0;
+            if constexpr (kScores) policy = l2_policy_evict_first();
             for (DecodeWalk k = walk_begin(); !k.done() && *abort_flag == 0; k.next(cut, heads, p.unit_log2, len_of)) {
                 const DecodePiece w = k.piece(cut, my_team, p.unit_log2, len_of);
                 const int n_stage = stages_of(w), kv_head = head_of(w.head_team) / p.kv_rep;
@@ -285,8 +287,14 @@ decode_split_tma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_c
                     const int c3 = table ? page : w.b;                     // page / batch index
 #pragma unroll
                     for (int h = 0; h < NH; ++h) {
-                        tma_load_4d(dst + h * kBoxBytes, &mapK, full_bar(st), 64 * h, kv_head, c2, c3);
-                        tma_load_4d(dst + (NH + h) * kBoxBytes, &mapV, full_bar(st), 64 * h, kv_head, c2, c3);
+                        if constexpr (kScores) {
+                            // read once: the scores, which are read again, stay in L2
+                            tma_load_4d_hint(dst + h * kBoxBytes, &mapK, full_bar(st), 64 * h, kv_head, c2, c3, policy);
+                            tma_load_4d_hint(dst + (NH + h) * kBoxBytes, &mapV, full_bar(st), 64 * h, kv_head, c2, c3, policy);
+                        } else {
+                            tma_load_4d(dst + h * kBoxBytes, &mapK, full_bar(st), 64 * h, kv_head, c2, c3);
+                            tma_load_4d(dst + (NH + h) * kBoxBytes, &mapV, full_bar(st), 64 * h, kv_head, c2, c3);
+                        }
                     }
                     n_issued = gi + 1;
                 }
@@ -521,6 +529,7 @@ decode_merge_kernel(const DecodeParams p) {
     const int Hk_real = p.Hk / p.kv_rep;                                            // p.Hk counts groups of at most 8 heads
     const __nv_bfloat16* depth0 = p.depth + (size_t(b) * Hk_real + hk / p.kv_rep) * 2 * D;   // slot 0: key row, value row at + D
 
+    grid_launch_dependents();                                                       // decode_key_mass_kernel may come up
     // ---- depth scores: warp `warp` takes slots warp, warp + 4, ..., UN at a time ----
     for (int i0 = warp; i0 < p.l; i0 += NW * UN) {
         float kd[UN][FPL];
