@@ -145,12 +145,37 @@ int launch_shared(const void* q, const void* Kp, const void* Vp, const SharedMer
                ? MODA_OK : MODA_ERR_CUDA;
 }
 
-// CTAs that share the keys of a (sequence, head): their exchanges cost some 2 us, the keys of one CTA about 1 us per 1000.
+// CTAs that share the keys of a (sequence, head): their exchanges cost some 2 us a pass, the keys of one CTA about 1 us per 2000.
 inline int evict_ranks(int T, long long rows) {
     int ranks = 1;
     while (ranks < 16 && T > 4096 * ranks && rows * ranks < 148) ranks *= 2;
-    while (ranks < 16 && evict_run(T, ranks) * kEvictThreads > kEvictKeys) ranks *= 2;
+    while (ranks < 16 && evict_run(T, ranks) > kEvictMostRun) ranks *= 2;
     return ranks;
+}
+
+template <int RUN>
+int launch_evict_select(const EvictParams& p, int ranks, int run, cudaStream_t stream) {
+    static thread_local int configured_dev = -1;
+    int dev = 0;
+    if (!cuda_ok(cudaGetDevice(&dev))) return MODA_ERR_CUDA;
+    if (configured_dev != dev) {
+        if (!set_smem_limit(evict_select_kernel<RUN>, evict_select_smem(RUN)) ||
+            !cuda_ok(cudaFuncSetAttribute(evict_select_kernel<RUN>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)))
+            return MODA_ERR_CUDA;
+        configured_dev = dev;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(ranks), unsigned(p.Hk), unsigned(p.B));
+    cfg.blockDim = dim3(kEvictThreads, 1, 1);
+    cfg.dynamicSmemBytes = size_t(evict_select_smem(RUN > 0 ? run : 0));
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = unsigned(ranks);
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cuda_ok(cudaLaunchKernelEx(&cfg, evict_select_kernel<RUN>, p)) ? MODA_OK : MODA_ERR_CUDA;
 }
 
 inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -276,32 +301,16 @@ int moda_kv_evict(const void* K, const void* V, const float* mass, const int* se
     p.lens_out = lens_out;
     p.B = B; p.T = T; p.T_cap = T_cap; p.T_out = T_out; p.Hk = H_kv; p.n_keep = n_keep; p.n_recent = n_recent;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    static thread_local int configured_dev = -1;
-    int dev = 0;
-    if (!cuda_ok(cudaGetDevice(&dev))) return MODA_ERR_CUDA;
-    if (configured_dev != dev) {
-        if (!set_smem_limit(evict_select_kernel<true>, evict_select_smem(kEvictKeys / kEvictThreads)) ||
-            !cuda_ok(cudaFuncSetAttribute(evict_select_kernel<true>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) ||
-            !cuda_ok(cudaFuncSetAttribute(evict_select_kernel<false>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)))
-            return MODA_ERR_CUDA;
-        configured_dev = dev;
-    }
-    const int ranks = evict_ranks(T, B * H_kv);
-    const int run = evict_run(T, ranks);
-    const bool fits = run * kEvictThreads <= kEvictKeys;
+    const int ranks = evict_ranks(T, (long long)B * H_kv), run = evict_run(T, ranks);
+    if (int rc = run <= 5 ? launch_evict_select<5>(p, ranks, run, st) : run <= 9 ? launch_evict_select<9>(p, ranks, run, st)
+               : run <= 17 ? launch_evict_select<17>(p, ranks, run, st) : run <= 33 ? launch_evict_select<33>(p, ranks, run, st)
+               : run <= kEvictMostRun ? launch_evict_select<kEvictMostRun>(p, ranks, run, st) : launch_evict_select<0>(p, ranks, run, st))
+        return rc;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(ranks), unsigned(H_kv), unsigned(B));
-    cfg.blockDim = dim3(kEvictThreads, 1, 1);
-    cfg.dynamicSmemBytes = size_t(evict_select_smem(fits ? run : 0));
-    cfg.stream = st;
     cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = unsigned(ranks);
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (!cuda_ok(fits ? cudaLaunchKernelEx(&cfg, evict_select_kernel<true>, p) : cudaLaunchKernelEx(&cfg, evict_select_kernel<false>, p)))
-        return MODA_ERR_CUDA;
     const int rows = std::max(1, kEvictGatherPieces / (H_kv * (d / 8)));
     const int longest = std::min(n_keep, T);
     cfg.gridDim = dim3(unsigned((longest + rows - 1) / rows), unsigned(B), 1);

@@ -3,7 +3,7 @@
 // position; NaN counts as less than everything).  They keep their order.
 //
 //   evict_select_kernel  a cluster of 1 to 16 CTAs per (sequence, head): the weight of the last key kept is found digit by digit (radix
-//                        11 + 11 + 10 bits of the weight's order-preserving integer), by a histogram of the keys that agree with the digits
+//                        12 + 12 + 8 bits of the weight's order-preserving integer), by a histogram of the keys that agree with the digits
 //                        found so far, until all that are left in a bin stay.  Each CTA counts its share of the keys, held in its shared
 //                        memory where they fit, and the cluster's counts are added over distributed shared memory.  Then every thread, which
 //                        has a run of adjacent keys, counts what it keeps and writes positions and weights behind what is kept before it.
@@ -45,11 +45,11 @@ __device__ __forceinline__ uint32_t evict_key(float w) {
 
 constexpr int kEvictThreads = 512;
 constexpr int kEvictWarps = kEvictThreads / 32;
-constexpr int kEvictBins = 2048, kEvictGroups = kEvictBins / 32;
-constexpr int kEvictKeys = 85 * kEvictThreads;    // keys of a CTA's share that its shared memory holds
+constexpr int kEvictBins = 4096, kEvictGroups = kEvictBins / 32;
+constexpr int kEvictMostRun = 65;                 // keys of a thread, of a share that shared memory holds
 
 struct EvictShared {
-    uint32_t hist[3][kEvictBins];                 // of a pass each: nobody waits until another CTA has read the one before
+    uint32_t hist[2][kEvictBins], hist3[256];     // of a pass each: nobody waits until another CTA has read the one before
     uint32_t group[3][kEvictGroups];              // sums over 32 bins
     uint32_t rank_group[kEvictWarps][kEvictGroups], rank_bin[kEvictWarps][32];   // what the cluster's CTAs have
     uint32_t warp_gt[kEvictWarps], warp_eq[kEvictWarps];
@@ -60,7 +60,7 @@ struct EvictShared {
 static_assert(sizeof(EvictShared) % 16 == 0, "alignment of the keys");
 // Keys of a thread: an odd number, so that the threads' runs start in different banks.
 __host__ __device__ inline int evict_run(int keys, int ranks) { return ((keys + ranks - 1) / ranks + kEvictThreads - 1) / kEvictThreads | 1; }
-inline int evict_select_smem(int run) { return int(sizeof(EvictShared)) + (run * kEvictThreads < kEvictKeys ? run * kEvictThreads : kEvictKeys) * 4; }
+inline int evict_select_smem(int run) { return int(sizeof(EvictShared)) + run * kEvictThreads * 4; }
 
 __device__ __forceinline__ uint4 ld_cluster_v4(uint32_t addr) {
     uint4 v;
@@ -79,10 +79,12 @@ __device__ __forceinline__ void cp_async_4(uint32_t smem_dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_dst), "l"(src) : "memory");
 }
 
-// grid (cluster, Hk, B).  FITS: a CTA's share of the keys is in its shared memory.
-template <bool FITS>
+// grid (cluster, Hk, B).  RUN: most keys of a thread; they are in shared memory and, up to 33, as integers in registers.  0: more than
+// shared memory holds, they are read again for every pass.
+template <int RUN>
 __global__ void __launch_bounds__(kEvictThreads)
 evict_select_kernel(const EvictParams p) {
+    constexpr bool kHeld = RUN > 0, kRegs = RUN > 0 && RUN <= 33;
     extern __shared__ __align__(16) uint8_t evict_smem[];
     EvictShared& s = *reinterpret_cast<EvictShared*>(evict_smem);
     float* held = reinterpret_cast<float*>(evict_smem + sizeof(EvictShared));
@@ -95,23 +97,44 @@ evict_select_kernel(const EvictParams p) {
     int* index = p.index + (size_t(b) * p.Hk + hk) * p.n_keep;
     float* mass_out = p.mass_out ? p.mass_out + (size_t(b) * p.Hk + hk) * p.T_out : nullptr;
 
+    // a thread has a run of adjacent keys
     const int run = evict_run(old, ranks), share = run * kEvictThreads;
     const int first = min(rank * share, old), n = min(share, old - first);
+    const int r0 = min(tid * run, n), mine = min(run, n - r0);
     const bool some = want > 0 && want < old;
     grid_launch_dependents();
 
-    if (FITS && want > 0) {
+    if (kHeld && want > 0) {
         const uint32_t dst = smem_u32(held);
 #pragma unroll 4
         for (int i = tid; i < n; i += kEvictThreads) cp_async_4(dst + i * 4, mass + first + i);
     }
 #pragma unroll
-    for (int pass = 0; pass < 3; ++pass) *reinterpret_cast<uint4*>(&s.hist[pass][tid * 4]) = make_uint4(0u, 0u, 0u, 0u);
-    if (FITS) asm volatile("cp.async.wait_all;" ::: "memory");
+    for (int i = 0; i < 2 * kEvictBins / 4; i += kEvictThreads) reinterpret_cast<uint4*>(s.hist[0])[i + tid] = make_uint4(0u, 0u, 0u, 0u);
+    if (tid < 64) reinterpret_cast<uint4*>(s.hist3)[tid] = make_uint4(0u, 0u, 0u, 0u);
+    if (kHeld) asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
-    auto weight = [&](int i) -> float {
-        if constexpr (FITS) return held[i];
-        else return mass[first + i];
+    auto weight = [&](int j) -> float {                              // of key j of this thread's run
+        if constexpr (kHeld) return held[r0 + j];
+        else return mass[first + r0 + j];
+    };
+    uint32_t keys[kRegs ? RUN : 1];
+    if constexpr (kRegs) {
+        if (some) {
+#pragma unroll
+            for (int j = 0; j < RUN; ++j) keys[j] = j < mine ? evict_key(weight(j)) : 0u;
+        }
+    }
+    // f(j, integer) for the keys of the run
+    auto each = [&](auto&& f) {
+        if constexpr (kRegs) {
+#pragma unroll
+            for (int j = 0; j < RUN; ++j)
+                if (j < mine) f(j, keys[j]);
+        } else {
+#pragma unroll 4
+            for (int j = 0; j < mine; ++j) f(j, evict_key(weight(j)));
+        }
     };
 
     uint32_t thr = 0u, ties = uint32_t(old);                         // kept: key > thr, and the first `ties` keys equal to it
@@ -121,59 +144,57 @@ evict_select_kernel(const EvictParams p) {
         int shift = 32;
 #pragma unroll 1
         for (int pass = 0; pass < 3; ++pass) {
-            const int bits = pass == 2 ? 10 : 11, agree = shift;
+            const int bits = pass == 2 ? 8 : 12, agree = shift;
             shift -= bits;
-            uint32_t* hist = s.hist[pass];
+            uint32_t* hist = pass == 2 ? s.hist3 : s.hist[pass];
             const uint32_t mask = (1u << bits) - 1u;
-            if (pass == 0) {
-#pragma unroll 4
-                for (int i = tid; i < n; i += kEvictThreads) atomicAdd(&hist[evict_key(weight(i)) >> 21], 1u);
-            } else {
-#pragma unroll 4
-                for (int i = tid; i < n; i += kEvictThreads) {
-                    const uint32_t k = evict_key(weight(i));
-                    if ((k >> agree) == prefix) atomicAdd(&hist[(k >> shift) & mask], 1u);
-                }
-            }
+            if (pass == 0) each([&](int, uint32_t k) { atomicAdd(&hist[k >> 20], 1u); });
+            else each([&](int, uint32_t k) { if ((k >> agree) == prefix) atomicAdd(&hist[(k >> shift) & mask], 1u); });
             __syncthreads();
             {
-                const uint4 c = *reinterpret_cast<const uint4*>(&hist[tid * 4]);
-                uint32_t sum = (c.x + c.y) + (c.z + c.w);
-#pragma unroll
-                for (int off = 1; off < 8; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-                if ((tid & 7) == 0) s.group[pass][tid >> 3] = sum;
+                uint32_t sum = 0;
+                if (pass < 2 || tid < 32) {                          // 8 bins a thread
+                    const uint4 c = *reinterpret_cast<const uint4*>(&hist[tid * 8]), e = *reinterpret_cast<const uint4*>(&hist[tid * 8 + 4]);
+                    sum = ((c.x + c.y) + (c.z + c.w)) + ((e.x + e.y) + (e.z + e.w));
+                }
+                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                if ((tid & 3) == 0) s.group[pass][tid >> 2] = sum;
             }
             // The bin in two steps: its group of 32, by the groups' sums, then the bin.  Every warp finds it for itself; a warp per CTA of the
-            // cluster fetches that CTA's counts (64 and 32 words of the 2048: all of them from all took 3 us a pass).
-            uint2 g = make_uint2(0u, 0u);                            // of the groups 2 lane and 2 lane + 1, all CTAs
+            // cluster fetches that CTA's counts (128 and 32 words: all 2048 of a smaller digit from all CTAs took 3 us a pass).
+            uint4 g = make_uint4(0u, 0u, 0u, 0u);                    // of the groups 4 lane .. 4 lane + 3, all CTAs
             if (ranks > 1) {
                 cluster_sync_all();
                 if (warp < ranks)
-                    *reinterpret_cast<uint2*>(&s.rank_group[warp][2 * lane]) = ld_cluster_v2(cluster_map_shared(smem_u32(&s.group[pass][2 * lane]), uint32_t(warp)));
+                    *reinterpret_cast<uint4*>(&s.rank_group[warp][4 * lane]) = ld_cluster_v4(cluster_map_shared(smem_u32(&s.group[pass][4 * lane]), uint32_t(warp)));
                 __syncthreads();
                 for (int r = 0; r < ranks; ++r) {
-                    const uint2 v = *reinterpret_cast<const uint2*>(&s.rank_group[r][2 * lane]);
-                    g.x += v.x;
-                    g.y += v.y;
+                    const uint4 v = *reinterpret_cast<const uint4*>(&s.rank_group[r][4 * lane]);
+                    g.x += v.x; g.y += v.y; g.z += v.z; g.w += v.w;
                 }
             } else {
                 __syncthreads();
-                g = *reinterpret_cast<const uint2*>(&s.group[pass][2 * lane]);
+                g = *reinterpret_cast<const uint4*>(&s.group[pass][4 * lane]);
             }
-            auto above = [&](uint32_t mine) {                        // sum over the lanes above this one
-                uint32_t incl = mine;
+            auto above = [&](uint32_t v) {                           // sum over the lanes above this one
+                uint32_t incl = v;
 #pragma unroll
                 for (int off = 1; off < 32; off <<= 1) {
-                    const uint32_t v = __shfl_down_sync(0xffffffffu, incl, off);
-                    if (lane + off < 32) incl += v;
+                    const uint32_t up = __shfl_down_sync(0xffffffffu, incl, off);
+                    if (lane + off < 32) incl += up;
                 }
-                return incl - mine;
+                return incl - v;
             };
-            uint32_t over = above(g.x + g.y);                        // keys above this lane's two groups
-            int at = __ffs(__ballot_sync(0xffffffffu, over < left && over + g.x + g.y >= left)) - 1;   // one lane
-            const bool upper = over + g.y >= left;
-            const int group = 2 * at + __shfl_sync(0xffffffffu, int(upper), at);
-            left -= __shfl_sync(0xffffffffu, upper ? over : over + g.y, at);
+            const uint32_t sum4 = (g.x + g.y) + (g.z + g.w);
+            uint32_t over = above(sum4);                             // keys above this lane's groups
+            int at = __ffs(__ballot_sync(0xffffffffu, over < left && over + sum4 >= left)) - 1;   // one lane
+            int group = 4 * lane + 3;
+            if (over + g.w < left) { over += g.w; --group;
+                if (over + g.z < left) { over += g.z; --group;
+                    if (over + g.y < left) { over += g.y; --group; } } }
+            group = __shfl_sync(0xffffffffu, group, at);
+            left -= __shfl_sync(0xffffffffu, over, at);
             uint32_t c = 0;                                          // of this lane's bin of the group, all CTAs
             if (ranks > 1) {
                 if (warp < ranks) {
@@ -206,17 +227,15 @@ evict_select_kernel(const EvictParams p) {
         }
     }
 
-    // ---- positions and weights of the kept keys, in order: a thread has a run of adjacent ones ----
-    const int r0 = min(tid * run, n), r1 = min(r0 + run, n);
+    // ---- positions and weights of the kept keys, in order ----
     uint32_t gt = 0, eq = 0;
     if (some) {
-        for (int i = r0; i < r1; ++i) {
-            const uint32_t k = evict_key(weight(i));
+        each([&](int, uint32_t k) {
             gt += k > thr;
             eq += k == thr;
-        }
+        });
     } else if (want > 0) {
-        gt = uint32_t(r1 - r0);                                      // every key
+        gt = uint32_t(mine);                                         // every key
     }
     uint32_t gt_incl = gt, eq_incl = eq;
 #pragma unroll
@@ -239,19 +258,20 @@ evict_select_kernel(const EvictParams p) {
         eq_before += __reduce_add_sync(0xffffffffu, v.y);
         cluster_arrive();                                            // no CTA leaves before all have read the others' counts
     }
-    if (want > 0) {
-        uint32_t at = gt_before + min(eq_before, ties);
-        for (int i = r0; i < r1; ++i) {
-            const float w = weight(i);
-            const uint32_t k = evict_key(w);
-            const bool tie = some && k == thr;
-            if (!some || k > thr || (tie && eq_before < ties)) {
-                index[at] = first + i;
-                if (mass_out) mass_out[at] = w;
-                ++at;
-            }
+    uint32_t at = gt_before + min(eq_before, ties);
+    auto keep = [&](int j) {
+        index[at] = first + r0 + j;
+        if (mass_out) mass_out[at] = weight(j);
+        ++at;
+    };
+    if (some) {
+        each([&](int j, uint32_t k) {
+            const bool tie = k == thr;
+            if (k > thr || (tie && eq_before < ties)) keep(j);
             eq_before += tie;
-        }
+        });
+    } else if (want > 0) {
+        for (int j = 0; j < mine; ++j) keep(j);
     }
     // the recent keys, and -1 behind the last one kept
     for (int i = rank * kEvictThreads + tid; i < p.n_keep - want; i += ranks * kEvictThreads) {
