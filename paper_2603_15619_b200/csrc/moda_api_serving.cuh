@@ -227,6 +227,7 @@ int moda_attn_key_mass(const void* Q, const void* K, const float* LSE, const flo
     p.inv_scale = 1.f / scale;
     p.least = -127.f / p.scale_log2;
     key_mass_slots(d, p.n_units, p.k_slots, p.q_slots);
+    p.by_tile = p.n_units <= 4 && p.k_slots == 4;                       // a slot of a half is that of even or of odd tiles
     p.stay = p.q_slots % p.n_units == 0 && all_see_all;
     const unsigned ctas = unsigned((p.total + run - 1) / run) * unsigned(p.team);
     cudaStream_t st = static_cast<cudaStream_t>(stream);

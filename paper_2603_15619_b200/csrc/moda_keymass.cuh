@@ -19,7 +19,14 @@
 //   atomics: the result is reproducible bit for bit).
 //
 //   20 warps: 0-15 four warpgroups (even units: tiles' first and second 128 keys, odd units: likewise), 16 TMA producer, 17 and 19 issue the
-//   products of the two halves (17 owns TMEM), 18 prepares the LSE terms.
+//   products of the two halves (17 owns TMEM), 18 prepares the LSE terms.  With few units a tile the warpgroups and issuers take even and
+//   odd tiles instead: their sums need not meet (64 rows over 8192 keys, B = 4, 32 heads on 8, two units: d = 128 32.7 -> 30.4 us, d = 64 29.7 -> 27.5; 300 rows over
+//   6000, B = 2, 16 heads, d = 64, three: 29.6 -> 27.7).
+//
+//   What bounds it: the exponentials, one per visible (row, key): 1024 cycles of the SFU a 128 x 128 tile against 576 of the tensor cores
+//   at d = 128, 320 at 64.  us, SFU time without the share of the FMA pipe / the kernel: 64 rows over 8192 as above 15 / 30.4 (8.5 of it the launch, its start
+//   and end); 1000 rows over 5003, B = 3, 16 heads, d = 64 52 / 66; 32768 rows and keys, 16 heads on 8, d = 128 1870 / 2140, and 2500 under a
+//   lasting load, when the power limit of 1000 W holds the SMs at 1.57 GHz.
 #pragma once
 
 #include <cstdint>
@@ -93,6 +100,7 @@ struct KeyMassParams {
     long long per_head, total;    // units of a (b, hk), of all groups of heads
     int run;                      // units of a team
     int k_slots, q_slots;         // of shared memory: halves of tiles, units
+    int by_tile;                  // the warpgroups take tiles in turn (few units a tile), not units
     int stay;                     // every tile sees every unit, and a unit comes round to its slot again with every tile: it stays there
     float scale_log2, inv_scale, least;   // least: -127 / scale_log2
 };
@@ -278,21 +286,23 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
         const int half = wg & 1, st = wg >> 1;                           // half of the tile; the units n % 2 == st are this warpgroup's
         const uint32_t tS = tmem + (uint32_t((warp & 3) * 32) << 16) + st * 256 + half * 128;
         float* s_acc = reinterpret_cast<float*>(smem + L::kAcc);
-        int n0 = 0;                                                      // units before the piece
-        int q_slot = st;                                                 // of this warpgroup's next unit
+        const int step = p.by_tile ? 1 : 2;
+        int n0 = 0, q0 = 0;                                              // units before the piece, slot of its first one
+        int cnt = 0;                                                     // units of this warpgroup so far
 #pragma unroll 1
         for (int piece = 0; w.left > 0; ++piece) {
             uint64_t y0 = 0, y1 = 0;
             const int key0 = w.jt * kKmTile + half * 128;
-            const int u_first = w.u0 + ((n0 ^ st) & 1);
-            int n = n0 + ((n0 ^ st) & 1);
+            const bool mine = !p.by_tile || (piece & 1) == st;
+            const int skip = p.by_tile ? 0 : (n0 ^ st) & 1;
+            int q_slot = q0 + skip;
 #pragma unroll 1
-            for (int u = u_first; u < w.u1; u += 2, n += 2) {
-                wait(bar(kKmSFull + wg), (n >> 1) & 1, 111);
+            for (int u = mine ? w.u0 + skip : w.u1; u < w.u1; u += step, ++cnt) {
+                wait(bar(kKmSFull + wg), cnt & 1, 111);
                 tc_fence_after_sync();
-                if (r == 0) mbar_arrive(bar(kKmQEmpty + q_slot));
-                q_slot += 2;
                 if (q_slot >= p.q_slots) q_slot -= p.q_slots;
+                if (r == 0) mbar_arrive(bar(kKmQEmpty + q_slot));
+                q_slot += step;
                 // row c of the unit sees key r iff c / G + i0 + off >= key0 + r
                 const int i0 = u * p.P;
                 const bool masked = i0 + off < key0 + 127;
@@ -327,16 +337,22 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                 }
             }
             n0 += w.u1 - w.u0;
-            // The warpgroups' sums meet in shared memory; a pair of them adds them up while the others go on.  (Behind piece - 1's barrier
-            // the pair that had piece - 2 has read this buffer: it arrived there after that.)
-            if (piece >= 2) wait(bar(kKmDone + ((piece - 1) & 1)), ((piece - 1) >> 1) & 1, 112);
-            float* buf = s_acc + (piece & 1) * 512;
-            buf[wg * 128 + r] = (__uint_as_float(uint32_t(y0)) + __uint_as_float(uint32_t(y0 >> 32))) +
-                                (__uint_as_float(uint32_t(y1)) + __uint_as_float(uint32_t(y1 >> 32)));
-            mbar_arrive(bar(kKmDone + (piece & 1)));
+            q0 = (q0 + w.u1 - w.u0) % p.q_slots;
+            float sum = (__uint_as_float(uint32_t(y0)) + __uint_as_float(uint32_t(y0 >> 32))) +
+                        (__uint_as_float(uint32_t(y1)) + __uint_as_float(uint32_t(y1 >> 32)));
+            if (!p.by_tile) {
+                // The warpgroups' sums meet in shared memory; a pair of them adds them up while the others go on.  (Behind piece - 1's
+                // barrier the pair that had piece - 2 has read this buffer: it arrived there after that.)
+                if (piece >= 2) wait(bar(kKmDone + ((piece - 1) & 1)), ((piece - 1) >> 1) & 1, 112);
+                float* buf = s_acc + (piece & 1) * 512;
+                buf[wg * 128 + r] = sum;
+                mbar_arrive(bar(kKmDone + (piece & 1)));
+                if ((piece & 1) == st) {
+                    wait(bar(kKmDone + (piece & 1)), (piece >> 1) & 1, 113);
+                    sum = buf[half * 128 + r] + buf[(half + 2) * 128 + r];
+                }
+            }
             if ((piece & 1) == st) {
-                wait(bar(kKmDone + (piece & 1)), (piece >> 1) & 1, 113);
-                const float sum = buf[half * 128 + r] + buf[(half + 2) * 128 + r];
                 const int key = key0 + r;
                 if (w.starts && w.ends(p)) {
                     if (key < p.T_kv) {
@@ -395,46 +411,58 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
             }
         }
       } else if (warp != 18) {
-        // =========================== MMA issuers: S^T = K Q^T - LSE / scale of half h ===========================
-        // a warp for each half: one for both needs 890 to 1000 cycles a 128 x 128 tile, of which the tensor cores take 576 (d = 128)
-        const int h = warp == 17 ? 0 : 1;
+        // =========================== MMA issuers: S^T = K Q^T - LSE / scale ===========================
+        // a warp for each half of the tiles, or for every second tile: one for all needs 890 to 1000 cycles a 128 x 128 product, of which the
+        // tensor cores take 576 (d = 128)
+        const int id = warp == 17 ? 0 : 1;
         constexpr uint32_t idesc = make_idesc_bf16(128, 128, false, false);
         const uint64_t dk0 = desc_kmajor_sw128(sbase, 0), dq0 = dk0 + uint64_t((p.k_slots * L::kSlotBytes) >> 4);
         const uint64_t d_ones = make_smem_desc_noswz(sbase + L::kOnes, uint32_t(L::kZero - L::kOnes), 128u);
-        int n = 0;
+        int n = 0, m = 0;                                                // units so far, of this warp's pieces
         RingAt ka, qa;
-        if (h == 1) ka.next(p.k_slots);
 #pragma unroll 1
-        while (w.left > 0) {
-            wait(bar(kKmKFull + ka.slot), ka.round & 1, 130);
-            const uint64_t dk = dk0 + uint64_t((ka.slot * L::kSlotBytes) >> 4);
+        for (int piece = 0; w.left > 0; ++piece) {
+            const bool mine = !p.by_tile || (piece & 1) == id;
+            RingAt kb = ka;
+            kb.next(p.k_slots);
+            if (mine && (p.by_tile || id == 0)) wait(bar(kKmKFull + ka.slot), ka.round & 1, 130);
+            if (mine && (p.by_tile || id == 1)) wait(bar(kKmKFull + kb.slot), kb.round & 1, 134);
 #pragma unroll 1
             for (int u = w.u0; u < w.u1; ++u, ++n, qa.next(p.q_slots)) {
-                const int buf = (n & 1) * 2 + h;
-                if (n >= 2) wait.both(bar(kKmQFull + qa.slot), qa.round & 1, bar(kKmSEmpty + buf), ((n >> 1) & 1) ^ 1, 131, 132);
-                else wait(bar(kKmQFull + qa.slot), qa.round & 1, 133);
-                tc_fence_after_sync();
+                wait(bar(kKmQFull + qa.slot), qa.round & 1, 131);        // also of the other warp's units: a wait tells only one phase from the next
+                if (!mine) continue;
                 const uint64_t dq = dq0 + uint64_t((qa.slot * L::kSlotBytes) >> 4);
                 const int terms = L::kTerms + qa.slot * L::kTermBytes;
-                const uint32_t t = tmem + buf * 128;
+                const uint64_t dt = make_smem_desc_noswz(sbase + terms, uint32_t(L::kZero - terms), 128u);
+                const int before = p.by_tile ? m : n >> 1;               // units that the score buffer has had
+#pragma unroll 1
+                for (int h = p.by_tile ? 0 : id; h < (p.by_tile ? 2 : id + 1); ++h) {
+                    const int buf = (p.by_tile ? id : n & 1) * 2 + h;
+                    if (before > 0) wait(bar(kKmSEmpty + buf), (before - 1) & 1, 132);
+                    tc_fence_after_sync();
+                    const uint64_t dk = dk0 + uint64_t(((h ? kb.slot : ka.slot) * L::kSlotBytes) >> 4);
+                    const uint32_t t = tmem + buf * 128;
 #pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk) {
-                    const uint64_t o = uint64_t(((kk >> 2) * L::kSubBytes + (kk & 3) * 32) >> 4);
-                    umma_ss(t, dk + o, dq + o, idesc, kk > 0);
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const uint64_t o = uint64_t(((kk >> 2) * L::kSubBytes + (kk & 3) * 32) >> 4);
+                        umma_ss(t, dk + o, dq + o, idesc, kk > 0);
+                    }
+                    umma_ss(t, d_ones, dt, idesc, 1);
+                    umma_commit(bar(kKmSFull + buf));
                 }
-                umma_ss(t, d_ones, make_smem_desc_noswz(sbase + terms, uint32_t(L::kZero - terms), 128u), idesc, 1);
-                umma_commit(bar(kKmSFull + buf));
+                ++m;
             }
-            umma_commit(bar(kKmKEmpty + ka.slot));
-            ka.next(p.k_slots);
-            ka.next(p.k_slots);
+            if (mine && (p.by_tile || id == 0)) umma_commit(bar(kKmKEmpty + ka.slot));
+            if (mine && (p.by_tile || id == 1)) umma_commit(bar(kKmKEmpty + kb.slot));
+            kb.next(p.k_slots);
+            ka = kb;
             w.next(p);
         }
         if (*abort_flag != 0) {
             // A wait gave up somewhere: make sure no MMA of this thread is still in flight before TMEM is released.
-            umma_commit(bar(kKmDrain + h));
+            umma_commit(bar(kKmDrain + id));
             const uint64_t t0 = globaltimer_ns();
-            while (!mbar_try_wait(bar(kKmDrain + h), 0) && globaltimer_ns() - t0 < 20000000ull) {}
+            while (!mbar_try_wait(bar(kKmDrain + id), 0) && globaltimer_ns() - t0 < 20000000ull) {}
         }
       } else if (warp == 18) {
         // =========================== LSE terms of a unit's rows ===========================
