@@ -46,14 +46,13 @@ int launch_key_mass(const void* Q, const void* K, int B, const KeyMassParams& p,
 }
 
 // ------------------------------------------------------------------------------------------------------ shared prefix
-// CTAs that take adjacent heads at the same time, where the bytes of the prefix set the pace (one row tile): the largest divisor of the
-// heads up to 8.  us, a head alone / teams of 2 / 4 / 8: B = 37, 24 heads on 8, d = 64, 131072 keys 85 / 67 / 67 / 58, 10007 keys 20.0 / 20.1 /
-// 19.0 / 15.6; d = 128, 10007 keys 27.7 / 27.2 / 25.2 / 20.5.  With pairs of row tiles, bound by the products, they only leave SMs
-// without a team (B = 128, 32 heads on 8, 131072 keys, teams of 4: 225 -> 232).
-inline int shared_team(int H_kv, bool paired) {
-    if (paired) return 1;
-    int team = 8;
-    while (H_kv % team != 0) --team;
+// CTAs that take the same key tiles at the same time (moda_shared.cuh): the largest divisor up to 8 of the heads with one row tile, up to 16 of
+// the pairs of row tiles with more.  us, one row tile, a head alone / teams of 2 / 4 / 8: B = 37, 24 heads on 8, d = 64, 131072 keys 85 / 67 / 67 /
+// 58, 10007 keys 20.0 / 20.1 / 19.0 / 15.6; d = 128, 10007 keys 27.7 / 27.2 / 25.2 / 20.5.
+inline int shared_team(int H_kv, int row_tiles, int pairs) {
+    const int of = row_tiles > 1 ? pairs : H_kv;
+    int team = row_tiles > 1 ? 16 : 8;
+    while (of % team != 0) --team;
     return team;
 }
 
@@ -66,8 +65,9 @@ SharedParams shared_plan(int B, int P, int H, int H_kv, int d, int ctas) {
     p.row_tiles = (B + p.S - 1) / p.S;
     p.pairs = (p.row_tiles + 1) / 2;
     p.key_tiles = (P + 127) / 128;
-    p.team = shared_team(H_kv, p.row_tiles > 1);
-    p.total = H_kv / p.team * p.pairs * p.key_tiles;
+    p.team = shared_team(H_kv, p.row_tiles, p.pairs);
+    p.total = shared_group(p, H_kv - 1, p.pairs - 1) + 1;
+    p.total *= p.key_tiles;
     const int teams = ctas / p.team;
     p.run = std::max((p.total + teams - 1) / teams, p.row_tiles > 1 ? 1 : 2);      // with one row tile: a key tile for each stream
     shared_slots(d, p.row_tiles > 1, p.k_slots, p.v_slots);

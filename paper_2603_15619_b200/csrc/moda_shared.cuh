@@ -7,10 +7,11 @@
 //   decode_split_tma_kernel  the sequences' own caches (moda_decode.cuh)
 //   shared_merge_kernel    joins the partials of both with the depth pairs.
 //
-// shared_prefix_kernel: where few rows leave the pace to the bytes of K and V, teams of CTAs take adjacent kv heads, whose rows are adjacent
-// in memory, at the same time (a head alone is read in pieces of 2 d bytes: B = 37, 131072 keys, 8 heads, d = 64: 85 us, 58 us with teams of 8).
-// The 128-key tiles of all (heads of a team, pair of row tiles) groups, in this order, are cut into equal runs, one per team; a CTA leaves a
-// partial (m, l, o) per row for the part of each group that its run covers (a piece).  384 threads:
+// shared_prefix_kernel: teams of CTAs take the same key tiles at the same time.  With one row tile, where the bytes of K and V set the pace, a
+// team has adjacent kv heads, whose rows are adjacent in memory (a head alone is read in pieces of 2 d bytes: B = 37, 131072 keys,
+// 8 heads, d = 64: 85 us, 58 us with teams of 8); with several it has the row tiles of a kv head, so that all but one find K and V in L2 (B = 128, 131072 keys, 32
+// heads on 8, alone -> in teams: d = 128 249 -> 218 us, d = 64 228 -> 174).  The 128-key tiles of all groups of a team's size (heads, or a head's pairs of row tiles), in this
+// order, are cut into equal runs, one per team; a CTA leaves a partial (m, l, o) per row for the part of each group that its run covers (a piece).  384 threads:
 //
 //   warps 0-3, 4-7   two streams, one thread per row: a score tile goes into registers at once, so that its columns can take the next one; maximum,
 //                    exponentials and sum; P (bf16) to columns of its own
@@ -40,7 +41,7 @@ struct SharedParams {
     int S;                        // sequences of a row tile: 128 / G
     int row_tiles, pairs;         // row tiles; groups of two of them (1: one stream per key tile in turn)
     int key_tiles;                // 128-key tiles of the prefix
-    int team;                     // CTAs of a team (divides Hk)
+    int team;                     // CTAs of a team: divides Hk (one row tile) or pairs
     int total, run;               // key tiles of all groups, of a team
     int pieces;                   // partials that a row has room for
     int k_slots, v_slots;         // of shared memory, behind one or two row tiles
@@ -49,6 +50,10 @@ struct SharedParams {
     float scale_log2;
 };
 
+// The group of a team's size that kv head `hk` and pair `pair` of row tiles belong to.
+__host__ __device__ inline int shared_group(const SharedParams& p, int hk, int pair) {
+    return p.row_tiles > 1 ? hk * (p.pairs / p.team) + pair / p.team : hk / p.team;
+}
 // Partials of a row: a piece per run that touches its group, two with one row tile (a stream each).
 inline __host__ __device__ int shared_first_run(int group, int key_tiles, int run) { return int((long long)group * key_tiles / run); }
 
@@ -158,6 +163,11 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
     const uint32_t tmem = *tmem_slot;
     SharedWalk w;
     const int my_team = int(blockIdx.x) / p.team, member = int(blockIdx.x) % p.team;
+    auto place = [&](int group) {                                      // kv head and pair of row tiles of this CTA
+        if (!paired) return make_int2(group * p.team + member, 0);
+        const int per_head = p.pairs / p.team, hk = group / per_head;
+        return make_int2(hk, (group - hk * per_head) * p.team + member);
+    };
     w.at = my_team * p.run;
     w.end = min(w.at + p.run, p.total);
     w.set(p);
@@ -172,7 +182,8 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
         int n = 0, tile0 = 0;                                          // tiles of this stream so far; key tiles of the CTA before the piece
 #pragma unroll 1
         while (w.at < w.end) {
-            const int heads = w.group / p.pairs, pair = w.group - heads * p.pairs, hk = heads * p.team + member;
+            const int2 at = place(w.group);
+            const int hk = at.x, pair = at.y;
             float m_ref = -INFINITY, l_sum = 0.f;
             int in_piece = 0;
             // one row tile: the CTA's key tiles in turn, whatever piece they belong to
@@ -301,7 +312,8 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
             int piece = 0;
 #pragma unroll 1
             for (; w.at < w.end; ++piece) {
-                const int heads = w.group / p.pairs, pair = w.group - heads * p.pairs, hk = heads * p.team + member;
+                const int2 at = place(w.group);
+                const int hk = at.x, pair = at.y;
                 load(mapK, ka, sK, kSpKFull, kSpKEmpty, p.k_slots, hk, w.j0);
                 if (piece > 0) wait(bar(kSpPieceDone), (piece - 1) & 1, 160);   // every product of the piece before is complete
                 mbar_arrive_expect_tx(bar(kSpQFull), uint32_t(q_tiles * rows) * D * 2);
@@ -498,7 +510,7 @@ shared_merge_kernel(const SharedMergeParams p) {
     const int own_len = q.T_kv == 0 ? 0 : q.seq_lens ? min(max(q.seq_lens[b], 0), q.T_kv) : q.T_kv;
     int n_pre = 0;
     if (p.pre.P > 0) {
-        const int group = (h / p.pre.G / p.pre.team) * p.pre.pairs + (p.pre.row_tiles > 1 ? b / (2 * p.pre.S) : 0);
+        const int group = shared_group(p.pre, h / p.pre.G, p.pre.row_tiles > 1 ? b / (2 * p.pre.S) : 0);
         const int c0 = shared_first_run(group, p.pre.key_tiles, p.pre.run);
         const int c1 = int(((long long)(group + 1) * p.pre.key_tiles - 1) / p.pre.run);
         n_pre = (c1 - c0 + 1) * (p.pre.row_tiles > 1 ? 1 : 2);
