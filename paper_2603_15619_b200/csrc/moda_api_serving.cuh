@@ -56,6 +56,8 @@ inline int shared_team(int H_kv, int row_tiles, int pairs) {
     return team;
 }
 
+constexpr long long kSharedMostTiles = 0x3fffffffll;
+
 // How the prefix of a call is cut, for `ctas` CTAs.
 SharedParams shared_plan(int B, int P, int H, int H_kv, int d, int ctas) {
     SharedParams p = {};
@@ -66,8 +68,8 @@ SharedParams shared_plan(int B, int P, int H, int H_kv, int d, int ctas) {
     p.pairs = (p.row_tiles + 1) / 2;
     p.key_tiles = (P + 127) / 128;
     p.team = shared_team(H_kv, p.row_tiles, p.pairs);
-    p.total = shared_group(p, H_kv - 1, p.pairs - 1) + 1;
-    p.total *= p.key_tiles;
+    const long long total = (long long)(shared_group(p, H_kv - 1, p.pairs - 1) + 1) * p.key_tiles;
+    p.total = int(std::min(total, kSharedMostTiles));
     const int teams = ctas / p.team;
     p.run = std::max((p.total + teams - 1) / teams, p.row_tiles > 1 ? 1 : 2);      // with one row tile: a key tile for each stream
     shared_slots(d, p.row_tiles > 1, p.k_slots, p.v_slots);
@@ -295,6 +297,10 @@ int moda_kv_evict(const void* K, const void* V, const float* mass, const int* se
         return b >= a + size_t(B) * T_cap * row || a >= b + size_t(B) * T_out * row;
     };
     if (!apart(K, K_out) || !apart(V, V_out) || !apart(K, V_out) || !apart(V, K_out)) return MODA_ERR_BAD_SHAPE;
+    if (mass_out) {
+        const auto a = reinterpret_cast<uintptr_t>(mass), b = reinterpret_cast<uintptr_t>(mass_out);
+        if (b < a + size_t(B) * H_kv * T_cap * 4 && a < b + size_t(B) * H_kv * T_out * 4) return MODA_ERR_BAD_SHAPE;
+    }
     if (int rc = check_device()) return rc;
     EvictParams p = {};
     p.K = static_cast<const __nv_bfloat16*>(K); p.V = static_cast<const __nv_bfloat16*>(V); p.mass = mass; p.seq_lens = seq_lens;
@@ -345,8 +351,7 @@ int moda_attn_decode_shared(const void* q, const void* K_prefix, const void* V_p
     if (!aligned4(seq_lens) || !aligned16(q) || !aligned16(O) || !aligned16(LSE) || (l > 0 && !aligned16(depth_kv_token)) ||
         (T_prefix > 0 && (!aligned16(K_prefix) || !aligned16(V_prefix))) || (max_seq_len > 0 && (!aligned16(K) || !aligned16(V))))
         return MODA_ERR_MISALIGNED;
-    const SharedParams most = shared_plan(B, T_prefix, H, H_kv, d, kSharedCtas);
-    if ((long long)H_kv * most.pairs * most.key_tiles > 0x3fffffffLL) return MODA_ERR_BAD_SHAPE;
+    if (shared_plan(B, T_prefix, H, H_kv, d, kSharedCtas).total >= kSharedMostTiles) return MODA_ERR_BAD_SHAPE;
     if (!workspace || !aligned16(workspace) || workspace_bytes < moda_decode_shared_workspace_bytes(B, T_prefix, H, H_kv, d)) return MODA_ERR_WORKSPACE;
     if (int rc = check_device()) return rc;
     int sms = 0;

@@ -425,11 +425,13 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
             const bool mine = !p.by_tile || (piece & 1) == id;
             RingAt kb = ka;
             kb.next(p.k_slots);
-            if (mine && (p.by_tile || id == 0)) wait(bar(kKmKFull + ka.slot), ka.round & 1, 130);
-            if (mine && (p.by_tile || id == 1)) wait(bar(kKmKFull + kb.slot), kb.round & 1, 134);
+            if (mine) {                                                  // both halves, also the other warp's: of three slots each is now one's, now the other's,
+                wait(bar(kKmKFull + ka.slot), ka.round & 1, 130);        // and a wait tells only one phase from the next
+                wait(bar(kKmKFull + kb.slot), kb.round & 1, 134);
+            }
 #pragma unroll 1
             for (int u = w.u0; u < w.u1; ++u, ++n, qa.next(p.q_slots)) {
-                wait(bar(kKmQFull + qa.slot), qa.round & 1, 131);        // also of the other warp's units: a wait tells only one phase from the next
+                wait(bar(kKmQFull + qa.slot), qa.round & 1, 131);        // likewise of every unit
                 if (!mine) continue;
                 const uint64_t dq = dq0 + uint64_t((qa.slot * L::kSlotBytes) >> 4);
                 const int terms = L::kTerms + qa.slot * L::kTermBytes;

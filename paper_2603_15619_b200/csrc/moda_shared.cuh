@@ -541,7 +541,8 @@ shared_merge_kernel(const SharedMergeParams p) {
         __syncthreads();
         mx = fmaxf(fmaxf(s_red[0][0], s_red[0][1]), fmaxf(s_red[0][2], s_red[0][3]));
     }
-    auto weight = [&](const float2& v) { return v.x == -INFINITY ? 0.f : fast_exp2(v.x - mx); };
+    // no key: 0; only NaN among the scores: NaN, as their sum is
+    auto weight = [&](const float2& v) { return v.x == -INFINITY ? v.y : fast_exp2(v.x - mx); };
     float f = weight(ml), lt = f * ml.y;
     if (tid < n) w_of[tid] = f;
     for (int i = tid + 32 * WPR; i < n; i += 32 * WPR) {

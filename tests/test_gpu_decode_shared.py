@@ -102,6 +102,44 @@ def test_scores_that_grow_along_the_prefix(where):
     check(x, [16] * B, 16, l, d ** -0.5)
 
 
+LARGE = [
+    # B, P, T, H, H_kv, d: one to many row tiles, teams of heads and of row tiles, side by side and one behind the other
+    (4, 30000, 100, 8, 8, 64), (40, 12000, 40, 28, 4, 128), (130, 5000, 30, 16, 4, 64), (96, 2500, 3, 40, 8, 128), (200, 1300, 20, 32, 2, 64), (64, 40000, 10, 16, 2, 128),
+    (33, 9000, 600, 12, 6, 128),
+]
+
+
+@pytest.mark.parametrize("B,P,T,H,Hk,d", LARGE)
+def test_large_batches_and_long_prefixes(B, P, T, H, Hk, d):
+    l, G = 2, H // Hk
+    x = inputs(B, P, T, H, Hk, d, l, seed=B)
+    lens = [(37 * b) % (T + 1) for b in range(B)]
+    O, LSE = call(x, lens, T, l, d ** -0.5)
+    at = torch.tensor(lens, device="cuda")
+    for k in range(Hk):
+        q = x["q"][:, k * G:(k + 1) * G].double()
+        s = torch.cat([torch.einsum("bgd,td->bgt", q, x["Kp"][:, k].double()), torch.einsum("bgd,btd->bgt", q, x["K"][:, :, k].double()),
+                       torch.einsum("bgd,lbd->bgl", q, x["depth"][:, :, k, 0].double())], -1) * d ** -0.5
+        gone = torch.zeros(s.shape[-1], dtype=torch.bool, device="cuda").repeat(B, 1)
+        gone[:, P:P + T] = torch.arange(T, device="cuda") >= at[:, None]
+        s.masked_fill_(gone[:, None], -torch.inf)
+        p = torch.softmax(s, -1)
+        o = (torch.einsum("bgt,td->bgd", p[..., :P], x["Vp"][:, k].double()) + torch.einsum("bgt,btd->bgd", p[..., P:P + T], x["V"][:, :, k].double()) +
+             torch.einsum("bgl,lbd->bgd", p[..., P + T:], x["depth"][:, :, k, 1].double()))
+        assert rel_l2(f64(O[:, k * G:(k + 1) * G]), f64(o)) <= TOL_O_REL_L2
+        assert np.abs(f64(LSE[:, k * G:(k + 1) * G]) - f64(torch.logsumexp(s, -1))).max() <= TOL_LSE_ABS
+
+
+def test_a_query_that_is_no_number_has_no_result():
+    for B, l in ((3, 0), (3, 2), (20, 0)):
+        x = inputs(B, 200, 10, 16, 2, 64, l, seed=3)
+        x["q"][1, 5] = float("nan")
+        O, LSE = call(x, [10] * B, 10, l, 0.125)
+        assert torch.isnan(O[1, 5]).all() and torch.isnan(LSE[1, 5])
+        O[1, 5], LSE[1, 5] = 0, 0
+        assert torch.isfinite(O.float()).all() and torch.isfinite(LSE).all()
+
+
 def test_repeatable_on_another_stream_and_guard_bands():
     B, P, T, H, Hk, d, l = 9, 1000, 40, 12, 4, 128, 3
     x = inputs(B, P, T, H, Hk, d, l, seed=9)

@@ -110,3 +110,26 @@ def test_outputs_of_the_callers_and_guard_bands():
     assert all(torch.equal(a, c) for a, c in zip(before, (K, V, mass)))      # the source is left as it was
     with pytest.raises(moda.ModaError, match=r"\[-3\]"):
         moda.moda_kv_evict(K, V, mass, T, n_keep, 5, K_out=K, V_out=torch.empty_like(K))
+    with pytest.raises(moda.ModaError, match=r"\[-3\]"):
+        moda.moda_kv_evict(K, V, mass, T, n_keep, 5, K_out=torch.empty_like(K), V_out=torch.empty_like(K), mass_out=mass)
+
+
+@pytest.mark.parametrize("T,n_keep,n_recent,ragged", [(300, 100, 10, True), (4000, 1000, 0, False), (8100, 2000, 33, True), (13000, 4000, 100, False), (17003, 900, 5, True)])
+def test_many_heads_at_once(T, n_keep, n_recent, ragged):
+    # one CTA a head, with few to many keys a thread; against a stable sort of all heads
+    B, Hk, d = 2, 80, 64
+    K, V, mass = inputs(B, T, Hk, d, seed=T)
+    mass = (mass * 8).round() / 8                                            # ties
+    lens = [T // 3, T] if ragged else [T, T]
+    seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    K_out, V_out, mass_out, index, lens_out = moda.moda_kv_evict(K, V, mass, T, n_keep, n_recent, seq_lens=seq)
+    for b, n in enumerate(lens):
+        kept = min(n_keep, n)
+        recent = min(n_recent, kept)
+        old = mass[b, :, :n - recent]
+        order = torch.sort(old, dim=-1, descending=True, stable=True).indices[:, :kept - recent]
+        want = torch.cat([torch.sort(order, dim=-1).values, torch.arange(n - recent, n, device="cuda").expand(Hk, -1)], -1)
+        assert torch.equal(index[b, :, :kept].long(), want) and bool((index[b, :, kept:] == -1).all()) and int(lens_out[b]) == kept
+        heads = torch.arange(Hk, device="cuda")[:, None].expand_as(want)
+        assert torch.equal(K_out[b, :kept].transpose(0, 1), K[b, want, heads]) and torch.equal(V_out[b, :kept].transpose(0, 1), V[b, want, heads])
+        assert torch.equal(mass_out[b, :, :kept], mass[b].gather(1, want))

@@ -62,6 +62,26 @@ def test_key_mass_of_a_long_prompt_adds_up():
     close(f64(mass)[:, :, -40:], orc.key_mass(*tail, d ** -0.5)[:, :, -40:])
 
 
+LARGE = [
+    # B, T_q, T_kv, H, H_kv, d: one to four units a tile and many of them, runs that share tiles and runs of whole tiles, several (b, head)
+    (4, 64, 3000, 16, 4, 128), (3, 33, 2500, 24, 8, 128), (2, 1, 7000, 8, 8, 64), (2, 300, 4001, 14, 7, 64), (2, 500, 2049, 5, 5, 64), (3, 257, 1500, 6, 2, 128),
+    (1, 1100, 3100, 32, 2, 64), (2, 1600, 1600, 6, 3, 128), (1, 3000, 3300, 5, 1, 128), (5, 129, 769, 4, 4, 128),
+]
+
+
+@pytest.mark.parametrize("B,T_q,T_kv,H,Hk,d", LARGE)
+def test_key_mass_of_many_tiles(B, T_q, T_kv, H, Hk, d):
+    Q, K, LSE = inputs(B, T_q, T_kv, H, Hk, d, 0, seed=T_q)
+    mass = moda.moda_attn_key_mass(Q, K, LSE, d ** -0.5)
+    assert moda.moda_last_status() == 0
+    want = torch.zeros((B, Hk, T_kv), device="cuda", dtype=torch.float64)
+    seen = torch.arange(T_kv, device="cuda") <= torch.arange(T_q, device="cuda")[:, None] + T_kv - T_q
+    for h in range(H):
+        s = torch.einsum("bid,bjd->bij", Q[:, :, h].double(), K[:, :, h // (H // Hk)].double()) * d ** -0.5
+        want[:, h // (H // Hk)] += torch.where(seen, (s - LSE[:, h, :, None].double()).exp(), 0.0).sum(1)
+    close(f64(mass), f64(want))
+
+
 def test_key_mass_accumulates_over_the_chunks_of_a_prompt():
     B, T, H, Hk, d = 2, 500, 6, 3, 64
     Q, K, LSE = inputs(B, T, T, H, Hk, d, 0, seed=3, T_cap=512)

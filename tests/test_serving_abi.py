@@ -52,8 +52,8 @@ def test_decode_mass_validation():
 def test_evict_validation():
     lib = binding.load()
 
-    def call(K=P, V=P, mass=P, lens=None, B=1, T=100, T_cap=128, Hk=2, d=64, keep=50, recent=10, T_out=64, K_out=FAR, V_out=FAR, index=FAR):
-        return lib.moda_kv_evict(K, V, mass, lens, B, T, T_cap, Hk, d, keep, recent, T_out, K_out, V_out, None, index, None, None)
+    def call(K=P, V=P, mass=P, lens=None, B=1, T=100, T_cap=128, Hk=2, d=64, keep=50, recent=10, T_out=64, K_out=FAR, V_out=FAR, index=FAR, mass_out=None):
+        return lib.moda_kv_evict(K, V, mass, lens, B, T, T_cap, Hk, d, keep, recent, T_out, K_out, V_out, mass_out, index, None, None)
 
     assert call(B=0) == -3 and call(T=0) == -3 and call(T=129) == -3 and call(keep=0) == -3 and call(keep=65) == -3
     assert call(recent=-1) == -3 and call(recent=51) == -3 and call(Hk=0) == -3 and call(d=80) == -4
@@ -64,6 +64,8 @@ def test_evict_validation():
     for out in (at, at + size - 16, at - 64 * 2 * 64 * 2 + 16):
         assert call(K=ctypes.c_void_p(at), K_out=ctypes.c_void_p(out)) == -3 and call(V=ctypes.c_void_p(at), K_out=ctypes.c_void_p(out)) == -3
         assert call(K=ctypes.c_void_p(at), V_out=ctypes.c_void_p(out)) == -3
+    for out in (at, at + 2 * 128 * 4 - 4, at - 2 * 64 * 4 + 4):
+        assert call(mass=ctypes.c_void_p(at), mass_out=ctypes.c_void_p(out)) == -3
 
 
 def test_decode_shared_validation():
