@@ -17,7 +17,7 @@ inline int key_mass_team(int H_kv, int n_units) {
     return team;
 }
 
-template <int D>
+template <int D, bool FEW>
 int launch_key_mass(const void* Q, const void* K, int B, const KeyMassParams& p, unsigned ctas, bool join, cudaStream_t stream) {
     using L = KeyMassSmem<D>;
     // query rows of a unit: P positions of the G heads, position after position
@@ -27,10 +27,10 @@ int launch_key_mass(const void* Q, const void* K, int B, const KeyMassParams& p,
     int dev = 0;
     if (!cuda_ok(cudaGetDevice(&dev))) return MODA_ERR_CUDA;
     if (configured_dev != dev) {
-        if (!set_smem_limit(key_mass_kernel<D>, L::kDynamic)) return MODA_ERR_CUDA;
+        if (!set_smem_limit(key_mass_kernel<D, FEW>, L::kDynamic)) return MODA_ERR_CUDA;
         configured_dev = dev;
     }
-    key_mass_kernel<D><<<ctas, kKmThreads, L::kDynamic, stream>>>(mQ, mK, p);
+    key_mass_kernel<D, FEW><<<ctas, kKmThreads, L::kDynamic, stream>>>(mQ, mK, p);
     if (!cuda_ok(cudaGetLastError())) return MODA_ERR_CUDA;
     if (!join) return MODA_OK;
     cudaLaunchConfig_t cfg = {};
@@ -229,11 +229,12 @@ int moda_attn_key_mass(const void* Q, const void* K, const float* LSE, const flo
     p.inv_scale = 1.f / scale;
     p.least = -127.f / p.scale_log2;
     key_mass_slots(d, p.n_units, p.k_slots, p.q_slots);
-    p.by_tile = p.n_units <= 4 && p.k_slots == 4;                       // a slot of a half is that of even or of odd tiles
+    const bool few = p.n_units <= 4 && p.k_slots == 4;                  // (a slot of a half is that of even or of odd tiles)
     p.stay = p.q_slots % p.n_units == 0 && all_see_all;
     const unsigned ctas = unsigned((p.total + run - 1) / run) * unsigned(p.team);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return d == 128 ? launch_key_mass<128>(Q, K, B, p, ctas, join, st) : launch_key_mass<64>(Q, K, B, p, ctas, join, st);
+    if (few) return d == 128 ? launch_key_mass<128, true>(Q, K, B, p, ctas, join, st) : launch_key_mass<64, true>(Q, K, B, p, ctas, join, st);
+    return d == 128 ? launch_key_mass<128, false>(Q, K, B, p, ctas, join, st) : launch_key_mass<64, false>(Q, K, B, p, ctas, join, st);
 }
 
 size_t moda_decode_mass_workspace_bytes(int B, int T_kv, int H, int H_kv, int d) {

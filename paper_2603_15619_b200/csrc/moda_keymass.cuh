@@ -100,7 +100,6 @@ struct KeyMassParams {
     long long per_head, total;    // units of a (b, hk), of all groups of heads
     int run;                      // units of a team
     int k_slots, q_slots;         // of shared memory: halves of tiles, units
-    int by_tile;                  // the warpgroups take tiles in turn (few units a tile), not units
     int stay;                     // every tile sees every unit, and a unit comes round to its slot again with every tile: it stays there
     float scale_log2, inv_scale, least;   // least: -127 / scale_log2
 };
@@ -166,6 +165,9 @@ __host__ __device__ __forceinline__ int key_mass_first_unit(int jt, int off, int
     return i > 0 ? i / P : 0;
 }
 
+// Columns of a unit's scores: its rows, at T_q's end fewer than of the others, in steps of 32.
+__device__ __forceinline__ int key_mass_filled(const KeyMassParams& p, int u) { return (min(p.P, p.T_q - u * p.P) * p.G + 31) & ~31; }
+
 // The pieces of a CTA's run.
 struct KeyMassWalk {
     int bh, jt, u0, u1;           // (b, kv head), tile, units of the piece
@@ -192,7 +194,8 @@ struct KeyMassWalk {
     }
 };
 
-template <int D>
+// FEW: few units a tile.  The warpgroups take tiles in turn, and of a unit only the rows that there are.
+template <int D, bool FEW>
 __global__ void __launch_bounds__(kKmThreads, 1)
 key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK, const KeyMassParams p) {
     using L = KeyMassSmem<D>;
@@ -286,15 +289,15 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
         const int half = wg & 1, st = wg >> 1;                           // half of the tile; the units n % 2 == st are this warpgroup's
         const uint32_t tS = tmem + (uint32_t((warp & 3) * 32) << 16) + st * 256 + half * 128;
         float* s_acc = reinterpret_cast<float*>(smem + L::kAcc);
-        const int step = p.by_tile ? 1 : 2;
+        const int step = FEW ? 1 : 2;
         int n0 = 0, q0 = 0;                                              // units before the piece, slot of its first one
         int cnt = 0;                                                     // units of this warpgroup so far
 #pragma unroll 1
         for (int piece = 0; w.left > 0; ++piece) {
             uint64_t y0 = 0, y1 = 0;
             const int key0 = w.jt * kKmTile + half * 128;
-            const bool mine = !p.by_tile || (piece & 1) == st;
-            const int skip = p.by_tile ? 0 : (n0 ^ st) & 1;
+            const bool mine = !FEW || (piece & 1) == st;
+            const int skip = FEW ? 0 : (n0 ^ st) & 1;
             int q_slot = q0 + skip;
 #pragma unroll 1
             for (int u = mine ? w.u0 + skip : w.u1; u < w.u1; u += step, ++cnt) {
@@ -316,20 +319,22 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                         }
                         add_exp2_16<2>(s, p.scale_log2, p.least, y0, y1);
                     };
+                    auto read = [&]() {                                  // the scores are in registers
+                        tc_fence_before_sync();
+                        mbar_arrive(bar(kKmSEmpty + wg));
+                    };
                     uint32_t sa[16], sb[16];
+                    const int filled = FEW ? key_mass_filled(p, u) : 128;  // the columns behind have not been computed
                     tmem_ld16(tS, sa);
 #pragma unroll
                     for (int c = 0; c < 8; c += 2) {
+                        if (FEW && c * 16 >= filled) break;
                         tmem_wait_ld();
                         tmem_ld16(tS + c * 16 + 16, sb);
                         add_chunk(sa, c);
                         tmem_wait_ld();
-                        if (c < 6) {
-                            tmem_ld16(tS + c * 16 + 32, sa);
-                        } else {
-                            tc_fence_before_sync();
-                            mbar_arrive(bar(kKmSEmpty + wg));
-                        }
+                        if (c < 6 && (!FEW || (c + 2) * 16 < filled)) tmem_ld16(tS + c * 16 + 32, sa);
+                        else read();
                         add_chunk(sb, c + 1);
                     }
                 } else {
@@ -340,7 +345,7 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
             q0 = (q0 + w.u1 - w.u0) % p.q_slots;
             float sum = (__uint_as_float(uint32_t(y0)) + __uint_as_float(uint32_t(y0 >> 32))) +
                         (__uint_as_float(uint32_t(y1)) + __uint_as_float(uint32_t(y1 >> 32)));
-            if (!p.by_tile) {
+            if (!FEW) {
                 // The warpgroups' sums meet in shared memory; a pair of them adds them up while the others go on.  (Behind piece - 1's
                 // barrier the pair that had piece - 2 has read this buffer: it arrived there after that.)
                 if (piece >= 2) wait(bar(kKmDone + ((piece - 1) & 1)), ((piece - 1) >> 1) & 1, 112);
@@ -415,14 +420,13 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
         // a warp for each half of the tiles, or for every second tile: one for all needs 890 to 1000 cycles a 128 x 128 product, of which the
         // tensor cores take 576 (d = 128)
         const int id = warp == 17 ? 0 : 1;
-        constexpr uint32_t idesc = make_idesc_bf16(128, 128, false, false);
         const uint64_t dk0 = desc_kmajor_sw128(sbase, 0), dq0 = dk0 + uint64_t((p.k_slots * L::kSlotBytes) >> 4);
         const uint64_t d_ones = make_smem_desc_noswz(sbase + L::kOnes, uint32_t(L::kZero - L::kOnes), 128u);
         int n = 0, m = 0;                                                // units so far, of this warp's pieces
         RingAt ka, qa;
 #pragma unroll 1
         for (int piece = 0; w.left > 0; ++piece) {
-            const bool mine = !p.by_tile || (piece & 1) == id;
+            const bool mine = !FEW || (piece & 1) == id;
             RingAt kb = ka;
             kb.next(p.k_slots);
             if (mine) {                                                  // both halves, also the other warp's: of three slots each is now one's, now the other's,
@@ -436,10 +440,11 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                 const uint64_t dq = dq0 + uint64_t((qa.slot * L::kSlotBytes) >> 4);
                 const int terms = L::kTerms + qa.slot * L::kTermBytes;
                 const uint64_t dt = make_smem_desc_noswz(sbase + terms, uint32_t(L::kZero - terms), 128u);
-                const int before = p.by_tile ? m : n >> 1;               // units that the score buffer has had
+                const int before = FEW ? m : n >> 1;               // units that the score buffer has had
+                const uint32_t idesc = make_idesc_bf16(128, FEW ? key_mass_filled(p, u) : 128, false, false);
 #pragma unroll 1
-                for (int h = p.by_tile ? 0 : id; h < (p.by_tile ? 2 : id + 1); ++h) {
-                    const int buf = (p.by_tile ? id : n & 1) * 2 + h;
+                for (int h = FEW ? 0 : id; h < (FEW ? 2 : id + 1); ++h) {
+                    const int buf = (FEW ? id : n & 1) * 2 + h;
                     if (before > 0) wait(bar(kKmSEmpty + buf), (before - 1) & 1, 132);
                     tc_fence_after_sync();
                     const uint64_t dk = dk0 + uint64_t(((h ? kb.slot : ka.slot) * L::kSlotBytes) >> 4);
@@ -454,8 +459,8 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                 }
                 ++m;
             }
-            if (mine && (p.by_tile || id == 0)) umma_commit(bar(kKmKEmpty + ka.slot));
-            if (mine && (p.by_tile || id == 1)) umma_commit(bar(kKmKEmpty + kb.slot));
+            if (mine && (FEW || id == 0)) umma_commit(bar(kKmKEmpty + ka.slot));
+            if (mine && (FEW || id == 1)) umma_commit(bar(kKmKEmpty + kb.slot));
             kb.next(p.k_slots);
             ka = kb;
             w.next(p);
