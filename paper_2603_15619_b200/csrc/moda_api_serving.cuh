@@ -147,10 +147,11 @@ int launch_shared(const void* q, const void* Kp, const void* Vp, const SharedMer
                ? MODA_OK : MODA_ERR_CUDA;
 }
 
-// CTAs that share the keys of a (sequence, head): their exchanges cost some 2 us a pass, the keys of one CTA about 1 us per 2000.
+// CTAs that share the keys of a (sequence, head): their exchanges cost some 2 us a pass, the keys of one CTA about 1 us per 2000.  us, at most 4 / 8 / 16: 131001
+// keys to 16001, 8 heads 42.6 / 31.0 / 31.1, to 100 23.8 / 15.9 / 18.0; 32768 keys 12.2 / 10.6 / 10.6.  16 where 8 cannot hold them.
 inline int evict_ranks(int T, long long rows) {
     int ranks = 1;
-    while (ranks < 16 && T > 4096 * ranks && rows * ranks < 148) ranks *= 2;
+    while (ranks < 8 && T > 4096 * ranks && rows * ranks < 148) ranks *= 2;
     while (ranks < 16 && evict_run(T, ranks) > kEvictMostRun) ranks *= 2;
     return ranks;
 }

@@ -8,7 +8,10 @@
 //                        memory where they fit, and the cluster's counts are added over distributed shared memory.  Then every thread, which
 //                        has a run of adjacent keys, counts what it keeps and writes positions and weights behind what is kept before it.
 //   evict_gather_kernel  copies the kept K and V rows, all heads of a few output positions per CTA: bound by HBM (each row read and
-//                        written once).
+//                        written once; 32 sequences, 1024 rows of 8 heads kept, d = 128: 268 MB in 38 us).
+//
+// The selection is a chain of short phases, bound by their latencies (per CTA of 8192 keys some 8 us: 2.3 the weights' way here, 2 each of the two or three
+// passes, 2.5 counting and writing).  us, both kernels: 32 x 8192 keys to 1024, 8 heads 53; 131001 keys to 16001, 8 heads, d = 64 31; 2176 to 2048 8.6.
 #pragma once
 
 #include <cstdint>
@@ -106,8 +109,12 @@ evict_select_kernel(const EvictParams p) {
 
     if (kHeld && want > 0) {
         const uint32_t dst = smem_u32(held);
+        const int quads = (reinterpret_cast<uintptr_t>(mass + first) & 15u) == 0 ? n / 4 : 0;   // rows of any length and start
 #pragma unroll 4
-        for (int i = tid; i < n; i += kEvictThreads) cp_async_4(dst + i * 4, mass + first + i);
+        for (int i = tid; i < quads; i += kEvictThreads)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + i * 16), "l"(mass + first + i * 4) : "memory");
+#pragma unroll 4
+        for (int i = quads * 4 + tid; i < n; i += kEvictThreads) cp_async_4(dst + i * 4, mass + first + i);
     }
 #pragma unroll
     for (int i = 0; i < 2 * kEvictBins / 4; i += kEvictThreads) reinterpret_cast<uint4*>(s.hist[0])[i + tid] = make_uint4(0u, 0u, 0u, 0u);
@@ -169,6 +176,7 @@ evict_select_kernel(const EvictParams p) {
                 if (warp < ranks)
                     *reinterpret_cast<uint4*>(&s.rank_group[warp][4 * lane]) = ld_cluster_v4(cluster_map_shared(smem_u32(&s.group[pass][4 * lane]), uint32_t(warp)));
                 __syncthreads();
+#pragma unroll 8
                 for (int r = 0; r < ranks; ++r) {
                     const uint4 v = *reinterpret_cast<const uint4*>(&s.rank_group[r][4 * lane]);
                     g.x += v.x; g.y += v.y; g.z += v.z; g.w += v.w;
@@ -203,6 +211,7 @@ evict_select_kernel(const EvictParams p) {
                     s.rank_bin[warp][lane] = v;
                 }
                 __syncthreads();
+#pragma unroll 8
                 for (int r = 0; r < ranks; ++r) c += s.rank_bin[r][lane];
             } else {
                 c = hist[group * 32 + lane];
