@@ -112,14 +112,21 @@ int launch_own_cache(const DecodeParams& p, cudaStream_t stream) {
     }
 }
 
-// Rows (sequence, query head) from which one warp merges a row, not four: they fill the SMs anyway, and a warp alone waits for nobody.  us of
-// the step, four -> one: 4096 rows of 10 partials 257 -> 249, of 3 27 -> 19; 888 rows of 38 partials 19 -> 28, 64 rows of 16 10.8 -> 13.4.
-constexpr long long kMergeWarpRows = 1776;
+// Warps that merge a row (sequence, query head): four while the SMs hold all rows so, one when they would take turns, as a warp alone waits for
+// nobody.  us of the step without own caches, l = 24, four / two / one: 128 rows of d = 128 10.5 / 10.7 / 11.7, 256 (long prefix) 24.9 / 26.8 / 33.5, 512
+// 13.9 / 12.6 / 13.2, 2048 27.7 / 24.9 / 27.5, 2400 27.9 / 24.5 / 22.0, 3200 32.8 / 27.1 / 26.0, 4096 64 / 57 / 47.
+constexpr long long kMergeFourWarps = 400, kMergeTwoWarps = 2200;
+
+// Own caches (longest x heads of a group, longest) that the merge reads itself: every head of a group reads their keys again, but no
+// kernel runs for them, whose pieces of a few keys cost some 2 us each, one behind the other.  us, split kernel / here (B, shared keys, heads on kv
+// heads, d, l; longest own cache): 128, 16384, 32 on 8, 128, 24: 32 keys 73.7 / 55.8, 96 73.3 / 71.1, 128 73.7 / 78.7; 64, 1000, 64 on 8, 64, 16: 32 24.9 / 20.1,
+// 64 24.9 / 23.2, 96 25.2 / 26.5; 128, 2000, 40 on 40, 128, 12: 32 114 / 54, 128 122 / 93, 256 137 / 140.
+constexpr int kMergeOwnWork = 384, kMergeOwnLen = 192;
 
 // A short prefix (key tiles of a CTA, were it on all SMs) with own caches that are not large (elements of K): the prefix takes half of the SMs
 // and the own caches the others, at the same time; a CTA of either fills its SM.  Otherwise one behind the other, each on all
-// SMs.  us, one behind the other -> side by side, l = 24 (B, shared keys, longest own cache, heads, d): 37, 10007, 301, 24 on 8, 64: 26.9 -> 24.1; 16, 8192,
-// 512, 32 on 8, 128: 25.3 -> 22.2; 16, 30000, 512: 43.6 -> 41.4; 64, 4096, 128: 43.8 -> 34.1; 64, 16384, 128: 54.5 -> 49.6; 8, 20000, 2000, 16 on 4: 24.3 -> 20.9;
+// SMs.  us, one behind the other -> side by side, l = 24 (B, shared keys, longest own cache, heads, d): 37, 10007, 301, 24 on 8, 64: 28.4 -> 23.1; 16, 8192,
+// 512, 32 on 8, 128: 29.9 -> 24.2; 16, 30000, 512: 43.9 -> 41.0; 64, 4096, 128: 42.7 -> 35.8; 64, 16384, 128: 54.2 -> 52.0; 8, 20000, 2000, 16 on 4: 26.1 -> 22.0;
 // but 128, 4000, 200, 16 on 16, 64 (26 M elements): 56 -> 80.
 constexpr int kSharedShortRun = 16;
 constexpr long long kSharedShortOwn = 16ll << 20;
@@ -128,23 +135,26 @@ template <int D>
 int launch_shared(const void* q, const void* Kp, const void* Vp, const SharedMergeParams& p, cudaStream_t stream) {
     if (p.pre.P > 0)
         if (int rc = launch_shared_prefix<D>(q, Kp, Vp, p.pre, stream)) return rc;
-    if (p.dec.T_kv > 0)
+    if (p.dec.T_kv > 0 && !p.own_here)
         if (int rc = launch_own_cache<D>(p.dec, stream)) return rc;
     const long long rows = (long long)p.dec.H * p.dec.B;
-    const bool many = rows > kMergeWarpRows;
+    const int warps = rows <= kMergeFourWarps ? 4 : rows <= kMergeTwoWarps ? 2 : 1;
+    const long long ctas = (rows * warps * 32 + kSharedMergeThreads - 1) / kSharedMergeThreads;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(many ? (rows + 3) / 4 : rows), 1, 1);
+    cfg.gridDim = dim3(unsigned(ctas), 1, 1);
     cfg.blockDim = dim3(kSharedMergeThreads, 1, 1);
     // as for the merge of a decode step, within the 48 KiB that a kernel may have without asking
-    cfg.dynamicSmemBytes = many ? 0 : std::min<size_t>(decode_merge_reserve(rows, p.dec.team * p.dec.teams), 42000);
+    cfg.dynamicSmemBytes = warps == 1 ? 0 : std::min<size_t>(decode_merge_reserve(ctas, p.dec.team * p.dec.teams), 36000);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = p.pre.P > 0 || p.dec.T_kv > 0 ? 1 : 0;
-    return cuda_ok(many ? cudaLaunchKernelEx(&cfg, shared_merge_kernel<D, 1>, p) : cudaLaunchKernelEx(&cfg, shared_merge_kernel<D, 4>, p))
-               ? MODA_OK : MODA_ERR_CUDA;
+    cfg.numAttrs = p.pre.P > 0 || (p.dec.T_kv > 0 && !p.own_here) ? 1 : 0;
+    const cudaError_t rc = warps == 4   ? cudaLaunchKernelEx(&cfg, shared_merge_kernel<D, 4>, p)
+                           : warps == 2 ? cudaLaunchKernelEx(&cfg, shared_merge_kernel<D, 2>, p)
+                                        : cudaLaunchKernelEx(&cfg, shared_merge_kernel<D, 1>, p);
+    return cuda_ok(rc) ? MODA_OK : MODA_ERR_CUDA;
 }
 
 // CTAs that share the keys of a (sequence, head): their exchanges cost some 2 us a pass, the keys of one CTA about 1 us per 2000.  us, at most 4 / 8 / 16: 131001
@@ -360,8 +370,9 @@ int moda_attn_decode_shared(const void* q, const void* K_prefix, const void* V_p
     if (int rc = device_sm_count(&sms)) return rc;
     SharedMergeParams p = {};
     p.pre = shared_plan(B, T_prefix, H, H_kv, d, std::min(sms, kSharedCtas));
+    p.own_here = max_seq_len <= kMergeOwnLen && max_seq_len * std::min(H / H_kv, 8) <= kMergeOwnWork;
     int own_sms = sms;
-    if (T_prefix > 0 && max_seq_len > 0 && p.pre.run <= kSharedShortRun && (long long)B * max_seq_len * H_kv * d <= kSharedShortOwn) {
+    if (T_prefix > 0 && !p.own_here && max_seq_len > 0 && p.pre.run <= kSharedShortRun && (long long)B * max_seq_len * H_kv * d <= kSharedShortOwn) {
         p.pre = shared_plan(B, T_prefix, H, H_kv, d, std::max(std::min(sms, kSharedCtas) / 2, p.pre.team));
         own_sms = std::max(sms - (p.pre.total + p.pre.run - 1) / p.pre.run * p.pre.team, sms / 2);
     }

@@ -5,7 +5,7 @@
 //                          tcgen05 tiles (128 rows = S = 128 / G sequences with the G heads of the group), so a key is read once per 256 rows
 //                          instead of once per sequence, and the products run at the tensor cores' rate.
 //   decode_split_tma_kernel  the sequences' own caches (moda_decode.cuh)
-//   shared_merge_kernel    joins the partials of both with the depth pairs.
+//   shared_merge_kernel    joins the partials of both with the depth pairs; short own caches it reads itself.
 //
 // shared_prefix_kernel: teams of CTAs take the same key tiles at the same time.  With one row tile, where the bytes of K and V set the pace, a
 // team has adjacent kv heads, whose rows are adjacent in memory (a head alone is read in pieces of 2 d bytes: B = 37, 131072 keys,
@@ -411,45 +411,39 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
     if (warp == 9) tmem_dealloc(tmem, 512);
 }
 
-// Per (b, query head): the prefix partials, the sequence's own pieces and the token's depth pairs, by WPR warps.  It starts beside the
-// kernels before it (programmatic dependent launch) and has the depth pairs done when they end.  A chain of short dependent phases:
-// everything that a phase reads is requested at once.
+// Per (b, query head): the prefix partials, the sequence's own pieces (or, of a short cache, its keys) and the token's depth pairs, by WPR
+// warps.  It starts beside the kernels before it (programmatic dependent launch) and has the keys and depth pairs done when they end.
+// Bound by latency and by the rows that an SM holds: few dependent loads, and few registers where there are many rows (l = 24, d = 128, one warp a row: with
+// 4 loads of 16 bytes in flight 80 registers, with 2 64; 4096 rows 52.8 -> 47.1 us, 14240 rows of d = 64 35.5 -> 33.3).
 constexpr int kSharedMergeThreads = 128;
 
 struct SharedMergeParams {
     DecodeParams dec;             // own caches and depth pairs (T_kv == 0: none of the former)
     SharedParams pre;             // prefix (P == 0: none)
+    int own_here;                 // the own caches are short: no split kernel has run, this one reads them
 };
 
 template <int D, int WPR>
 __global__ void __launch_bounds__(kSharedMergeThreads)
 shared_merge_kernel(const SharedMergeParams p) {
-    constexpr int FPL = D / 32, ROWS = kSharedMergeThreads / 32 / WPR, UN = 8;
+    constexpr int LPR = D / 8, KPL = 32 / LPR;                       // lanes of a key (16 bytes each), keys of a warp's load
+    constexpr int ROWS = kSharedMergeThreads / 32 / WPR, UN = WPR > 1 ? 4 : 2;
     constexpr int kMost = 2 * (kSharedCtas + 1) + kDecodeMaxSplits;  // partials of a row: streams of the prefix, own pieces
-    __shared__ float s_w[ROWS][kMost], s_d[ROWS][256], s_red[2][4];
-    __shared__ __align__(16) float s_acc[WPR > 1 ? WPR : 1][D];
+    __shared__ float s_w[ROWS][kMost], s_red[2][ROWS][WPR];
+    __shared__ __align__(16) float s_acc[ROWS][WPR][D];
     const DecodeParams& q = p.dec;
     const int warp = int(threadIdx.x >> 5) % WPR, lane = threadIdx.x & 31, tid = warp * 32 + lane;   // in the row
+    const int sub = lane / LPR, col = lane % LPR * 8;                // key of a load, first of the lane's 8 elements
     const int row_in = int(threadIdx.x >> 5) / WPR;
     const int row = int(blockIdx.x) * ROWS + row_in;                 // b * H + h
     const bool there = ROWS == 1 || row < q.B * q.H;
     const int b = there ? row / q.H : 0, h = there ? row - b * q.H : 0;
     const int G = q.H / q.Hk, hk = h / G, g = h - hk * G;            // groups of at most 8 heads, as the split kernel has them
-    const int Hk_real = q.Hk / q.kv_rep;
+    const int Hk_real = q.Hk / q.kv_rep, hk_real = hk / q.kv_rep;
     float* w_of = s_w[row_in];
-    float* d_of = s_d[row_in];
     auto sync = [] {
         if constexpr (WPR > 1) __syncthreads();
         else __syncwarp();
-    };
-    auto load_row = [&](const __nv_bfloat16* src, float (&x)[FPL]) {
-        if constexpr (FPL == 4) {
-            const uint2 v = *reinterpret_cast<const uint2*>(src + lane * 4);
-            x[0] = bf16_lo_to_f32(v.x); x[1] = bf16_hi_to_f32(v.x); x[2] = bf16_lo_to_f32(v.y); x[3] = bf16_hi_to_f32(v.y);
-        } else {
-            const uint32_t v = *reinterpret_cast<const uint32_t*>(src + lane * 2);
-            x[0] = bf16_lo_to_f32(v); x[1] = bf16_hi_to_f32(v);
-        }
     };
     auto warp_max = [](float v) {
 #pragma unroll
@@ -461,53 +455,70 @@ shared_merge_kernel(const SharedMergeParams p) {
         for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
         return v;
     };
-    // ---- depth pairs: their own softmax ----
-    float acc[FPL], m_d = -INFINITY, l_d = 0.f;
+    auto unpack = [](const uint4& v, float (&x)[8]) {
+        x[0] = bf16_lo_to_f32(v.x); x[1] = bf16_hi_to_f32(v.x); x[2] = bf16_lo_to_f32(v.y); x[3] = bf16_hi_to_f32(v.y);
+        x[4] = bf16_lo_to_f32(v.z); x[5] = bf16_hi_to_f32(v.z); x[6] = bf16_lo_to_f32(v.w); x[7] = bf16_hi_to_f32(v.w);
+    };
+    // ---- a short own cache and the depth pairs, one pass: LPR lanes keep the running maximum, sum and o of every WPR KPL-th key ----
+    const int own_len = q.T_kv == 0 ? 0 : q.seq_lens ? min(max(q.seq_lens[b], 0), q.T_kv) : q.T_kv;
+    const int n_here = p.own_here ? own_len : 0, n_near = n_here + q.l;
+    float acc[8], m_d = -INFINITY, l_d = 0.f;
 #pragma unroll
-    for (int c = 0; c < FPL; ++c) acc[c] = 0.f;
-    if (q.l > 0) {
-        float qv[FPL];
-        load_row(q.q + size_t(there ? row : 0) * D, qv);
+    for (int c = 0; c < 8; ++c) acc[c] = 0.f;
+    if (n_near > 0) {
+        float qv[8];
+        unpack(*reinterpret_cast<const uint4*>(q.q + size_t(there ? row : 0) * D + col), qv);
 #pragma unroll
-        for (int c = 0; c < FPL; ++c) qv[c] *= q.scale_log2;
-        const size_t slot_stride = size_t(q.B) * Hk_real * 2 * D;
-        const __nv_bfloat16* depth0 = q.depth + (size_t(b) * Hk_real + hk / q.kv_rep) * 2 * D;
-        for (int i0 = warp; i0 < q.l; i0 += WPR * UN) {
-            float kd[UN][FPL], a[UN];
-#pragma unroll
-            for (int u = 0; u < UN; ++u) load_row(depth0 + size_t(min(i0 + u * WPR, q.l - 1)) * slot_stride, kd[u]);
+        for (int c = 0; c < 8; ++c) qv[c] *= q.scale_log2;
+        const size_t own0 = (size_t(b) * q.T_cap * Hk_real + hk_real) * D + col, own_stride = size_t(Hk_real) * D;
+        const size_t depth0 = (size_t(b) * Hk_real + hk_real) * 2 * D + col, slot_stride = size_t(q.B) * Hk_real * 2 * D;
+#pragma unroll 1
+        for (int i0 = warp * KPL; i0 < n_near; i0 += WPR * KPL * UN) {
+            uint4 k[UN], v[UN];
 #pragma unroll
             for (int u = 0; u < UN; ++u) {
+                const int i = min(i0 + u * WPR * KPL + sub, n_near - 1);
+                const bool own = i < n_here;
+                const size_t at = own ? own0 + i * own_stride : depth0 + (i - n_here) * slot_stride;
+                k[u] = *reinterpret_cast<const uint4*>((own ? q.K : q.depth) + at);
+                v[u] = *reinterpret_cast<const uint4*>((own ? q.V : q.depth + D) + at);
+            }
+            float a[UN];
+#pragma unroll
+            for (int u = 0; u < UN; ++u) {
+                float x[8];
+                unpack(k[u], x);
                 a[u] = 0.f;
 #pragma unroll
-                for (int c = 0; c < FPL; ++c) a[u] = fmaf(qv[c], kd[u][c], a[u]);
+                for (int c = 0; c < 8; ++c) a[u] = fmaf(qv[c], x[c], a[u]);
             }
 #pragma unroll
-            for (int off = 16; off > 0; off >>= 1)
+            for (int off = LPR / 2; off > 0; off >>= 1)
 #pragma unroll
                 for (int u = 0; u < UN; ++u) a[u] += __shfl_xor_sync(0xffffffffu, a[u], off);
-#pragma unroll
-            for (int u = 0; u < UN; ++u)
-                if (lane == 0 && i0 + u * WPR < q.l) d_of[i0 + u * WPR] = a[u];
-        }
-        sync();
-        for (int i = lane; i < q.l; i += 32) m_d = fmaxf(m_d, d_of[i]);
-        m_d = warp_max(m_d);
-        for (int i = lane; i < q.l; i += 32) l_d += fast_exp2(d_of[i] - m_d);
-        l_d = warp_sum(l_d);
-        for (int i0 = warp; i0 < q.l; i0 += WPR * UN) {
-            float vd[UN][FPL];
-#pragma unroll
-            for (int u = 0; u < UN; ++u) load_row(depth0 + size_t(min(i0 + u * WPR, q.l - 1)) * slot_stride + D, vd[u]);
+            float m = m_d;
 #pragma unroll
             for (int u = 0; u < UN; ++u) {
-                const float f = i0 + u * WPR < q.l ? fast_exp2(d_of[i0 + u * WPR] - m_d) : 0.f;
+                if (i0 + u * WPR * KPL + sub >= n_near) a[u] = -INFINITY;
+                m = fmaxf(m, a[u]);
+            }
+            const float m_safe = m == -INFINITY ? 0.f : m, old = fast_exp2(m_d - m_safe);
+            m_d = m;
+            l_d *= old;
 #pragma unroll
-                for (int c = 0; c < FPL; ++c) acc[c] = fmaf(f, vd[u][c], acc[c]);
+            for (int c = 0; c < 8; ++c) acc[c] *= old;
+#pragma unroll
+            for (int u = 0; u < UN; ++u) {
+                const bool in = i0 + u * WPR * KPL + sub < n_near;
+                const float f = fast_exp2(a[u] - m_safe);
+                float x[8];
+                unpack(in ? v[u] : make_uint4(0, 0, 0, 0), x);
+                l_d += f;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) acc[c] = fmaf(f, x[c], acc[c]);
             }
         }
     }
-    const int own_len = q.T_kv == 0 ? 0 : q.seq_lens ? min(max(q.seq_lens[b], 0), q.T_kv) : q.T_kv;
     int n_pre = 0;
     if (p.pre.P > 0) {
         const int group = shared_group(p.pre, h / p.pre.G, p.pre.row_tiles > 1 ? b / (2 * p.pre.S) : 0);
@@ -522,7 +533,7 @@ shared_merge_kernel(const SharedMergeParams p) {
     grid_dependency_wait();
     // ---- from here on: what the kernels before have written ----
     int n_own = 0;
-    if (own_len > 0)
+    if (own_len > n_here)
         n_own = q.seq_lens ? min(max(__float_as_int(__ldcg(group + (kDecodeMaxSplits - 1) * split_stride)), 1), q.max_pieces)
                            : decode_pieces_equal(q.cut, b * (q.Hk / q.team) + hk / q.team, q.T_kv, q.unit_log2);
     const int n = n_pre + n_own;
@@ -537,9 +548,10 @@ shared_merge_kernel(const SharedMergeParams p) {
     for (int i = tid + 32 * WPR; i < n; i += 32 * WPR) mx = fmaxf(mx, fetch_ml(i).x);
     mx = warp_max(mx);
     if constexpr (WPR > 1) {
-        if (lane == 0) s_red[0][warp] = mx;
+        if (lane == 0) s_red[0][row_in][warp] = mx;
         __syncthreads();
-        mx = fmaxf(fmaxf(s_red[0][0], s_red[0][1]), fmaxf(s_red[0][2], s_red[0][3]));
+#pragma unroll
+        for (int w = 0; w < WPR; ++w) mx = fmaxf(mx, s_red[0][row_in][w]);
     }
     // no key: 0; only NaN among the scores: NaN, as their sum is
     auto weight = [&](const float2& v) { return v.x == -INFINITY ? v.y : fast_exp2(v.x - mx); };
@@ -550,56 +562,86 @@ shared_merge_kernel(const SharedMergeParams p) {
         w_of[i] = f = weight(v);
         lt = fmaf(f, v.y, lt);
     }
-    lt = warp_sum(lt);
-    const float f_d = q.l > 0 ? fast_exp2(m_d - mx) : 0.f;
+    const float f_d = weight(make_float2(m_d, l_d));
+    lt = warp_sum(col == 0 ? fmaf(f_d, l_d, lt) : lt);
     if constexpr (WPR > 1) {
-        if (lane == 0) s_red[1][warp] = lt;
+        if (lane == 0) s_red[1][row_in][warp] = lt;
     }
     sync();
-    if constexpr (WPR > 1) lt = (s_red[1][0] + s_red[1][1]) + (s_red[1][2] + s_red[1][3]);
-    lt += f_d * l_d;
-    // ---- weighted sum: a warp takes every WPR-th partial ----
+    if constexpr (WPR > 1) {
+        lt = s_red[1][row_in][0];
 #pragma unroll
-    for (int c = 0; c < FPL; ++c) acc[c] *= f_d;
+        for (int w = 1; w < WPR; ++w) lt += s_red[1][row_in][w];
+    }
+    // ---- weighted sum: LPR lanes take every WPR KPL-th partial, in pairs of columns so that a load takes whole sectors ----
+    float2 o[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o[c] = make_float2(0.f, 0.f);
 #pragma unroll 1
-    for (int i0 = warp; i0 < n; i0 += WPR * UN) {
-        float x[UN][FPL];
+    for (int i0 = warp * KPL; i0 < n; i0 += WPR * KPL * UN) {
+        float2 x[UN][4];
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
-            const int i = min(i0 + u * WPR, n - 1);
-            const float* src = i < n_pre ? p.pre.o + (i * pre_stride + pre_row) * D : part + (i - n_pre) * split_stride + 2;
+            const int i = min(i0 + u * WPR * KPL + sub, n - 1);
+            const float* src = (i < n_pre ? p.pre.o + (i * pre_stride + pre_row) * D : part + (i - n_pre) * split_stride + 2) + col / 4;
 #pragma unroll
-            for (int c = 0; c < FPL; c += 2) {
-                const float2 v = __ldcg(reinterpret_cast<const float2*>(src + lane * FPL + c));
-                x[u][c] = v.x;
-                x[u][c + 1] = v.y;
-            }
+            for (int c = 0; c < 4; ++c) x[u][c] = __ldcg(reinterpret_cast<const float2*>(src) + c * LPR);
         }
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
-            const float wt = i0 + u * WPR < n ? w_of[i0 + u * WPR] : 0.f;
+            const int i = i0 + u * WPR * KPL + sub;
+            const float wt = i < n ? w_of[i] : 0.f;
             if (wt != 0.f) {                                         // a stream without a key has written no o
 #pragma unroll
-                for (int c = 0; c < FPL; ++c) acc[c] = fmaf(wt, x[u][c], acc[c]);
+                for (int c = 0; c < 4; ++c) o[c] = make_float2(fmaf(wt, x[u][c].x, o[c].x), fmaf(wt, x[u][c].y, o[c].y));
             }
         }
+    }
+#pragma unroll
+    for (int off = LPR; off < 32; off <<= 1)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            o[c].x += __shfl_xor_sync(0xffffffffu, o[c].x, off);
+            o[c].y += __shfl_xor_sync(0xffffffffu, o[c].y, off);
+        }
+    float* sum_of = s_acc[row_in][warp];
+    if (n_near > 0) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) acc[c] *= f_d;
+#pragma unroll
+        for (int off = LPR; off < 32; off <<= 1)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) acc[c] += __shfl_xor_sync(0xffffffffu, acc[c], off);
+        if (sub == 0) {
+#pragma unroll
+            for (int c = 0; c < 8; c += 4) *reinterpret_cast<float4*>(sum_of + col + c) = make_float4(acc[c], acc[c + 1], acc[c + 2], acc[c + 3]);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const float2 near = reinterpret_cast<const float2*>(sum_of + col / 4)[c * LPR];
+            o[c] = make_float2(o[c].x + near.x, o[c].y + near.y);
+        }
+        __syncwarp();
     }
     // a row without any key: O = 0, LSE = -inf
     const float inv = lt > 0.f || lt != lt ? 1.f / lt : 0.f;
     if constexpr (WPR > 1) {
+        if (sub == 0) {
 #pragma unroll
-        for (int c = 0; c < FPL; ++c) s_acc[warp][lane * FPL + c] = acc[c];
-        __syncthreads();
-        if (tid < D) {
-            const float a = (s_acc[0][tid] + s_acc[1][tid]) + (s_acc[2][tid] + s_acc[3][tid]);
-            q.O[size_t(row) * D + tid] = __float2bfloat16(inv == 0.f ? 0.f : a * inv);
+            for (int c = 0; c < 4; ++c) reinterpret_cast<float2*>(sum_of + col / 4)[c * LPR] = o[c];
         }
-    } else if (there) {
-        if constexpr (FPL == 4)
-            *reinterpret_cast<uint2*>(q.O + size_t(row) * D + lane * 4) =
-                inv == 0.f ? make_uint2(0u, 0u) : make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
-        else
-            *reinterpret_cast<uint32_t*>(q.O + size_t(row) * D + lane * 2) = inv == 0.f ? 0u : pack_bf16x2(acc[0] * inv, acc[1] * inv);
+        __syncthreads();
+        for (int c = tid; there && c < D; c += 32 * WPR) {
+            float a = s_acc[row_in][0][c];
+#pragma unroll
+            for (int w = 1; w < WPR; ++w) a += s_acc[row_in][w][c];
+            q.O[size_t(row) * D + c] = __float2bfloat16(inv == 0.f ? 0.f : a * inv);
+        }
+    } else if (there && sub == 0) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            reinterpret_cast<uint32_t*>(q.O + size_t(row) * D + col / 4)[c * LPR] = inv == 0.f ? 0u : pack_bf16x2(o[c].x * inv, o[c].y * inv);
     }
     if (tid == 0 && there) q.LSE[row] = (mx + log2f(lt)) * kDecodeLn2;
 }

@@ -109,25 +109,60 @@ LARGE = [
 ]
 
 
-@pytest.mark.parametrize("B,P,T,H,Hk,d", LARGE)
-def test_large_batches_and_long_prefixes(B, P, T, H, Hk, d):
-    l, G = 2, H // Hk
-    x = inputs(B, P, T, H, Hk, d, l, seed=B)
-    lens = [(37 * b) % (T + 1) for b in range(B)]
+def check_on_device(x, lens, T, l):
+    B, H, d = x["q"].shape
+    P, Hk = x["Kp"].shape[:2]
+    G = H // Hk
     O, LSE = call(x, lens, T, l, d ** -0.5)
-    at = torch.tensor(lens, device="cuda")
+    at = torch.tensor([T] * B if lens is None else lens, device="cuda")
     for k in range(Hk):
         q = x["q"][:, k * G:(k + 1) * G].double()
-        s = torch.cat([torch.einsum("bgd,td->bgt", q, x["Kp"][:, k].double()), torch.einsum("bgd,btd->bgt", q, x["K"][:, :, k].double()),
+        s = torch.cat([torch.einsum("bgd,td->bgt", q, x["Kp"][:, k].double()), torch.einsum("bgd,btd->bgt", q, x["K"][:, :T, k].double()),
                        torch.einsum("bgd,lbd->bgl", q, x["depth"][:, :, k, 0].double())], -1) * d ** -0.5
         gone = torch.zeros(s.shape[-1], dtype=torch.bool, device="cuda").repeat(B, 1)
         gone[:, P:P + T] = torch.arange(T, device="cuda") >= at[:, None]
         s.masked_fill_(gone[:, None], -torch.inf)
         p = torch.softmax(s, -1)
-        o = (torch.einsum("bgt,td->bgd", p[..., :P], x["Vp"][:, k].double()) + torch.einsum("bgt,btd->bgd", p[..., P:P + T], x["V"][:, :, k].double()) +
+        o = (torch.einsum("bgt,td->bgd", p[..., :P], x["Vp"][:, k].double()) + torch.einsum("bgt,btd->bgd", p[..., P:P + T], x["V"][:, :T, k].double()) +
              torch.einsum("bgl,lbd->bgd", p[..., P + T:], x["depth"][:, :, k, 1].double()))
         assert rel_l2(f64(O[:, k * G:(k + 1) * G]), f64(o)) <= TOL_O_REL_L2
         assert np.abs(f64(LSE[:, k * G:(k + 1) * G]) - f64(torch.logsumexp(s, -1))).max() <= TOL_LSE_ABS
+
+
+@pytest.mark.parametrize("B,P,T,H,Hk,d", LARGE)
+def test_large_batches_and_long_prefixes(B, P, T, H, Hk, d):
+    x = inputs(B, P, T, H, Hk, d, 2, seed=B)
+    check_on_device(x, [(37 * b) % (T + 1) for b in range(B)], T, 2)
+
+
+NEAR = [
+    # B, P, T, H, H_kv, d, l: four, two and one warp a row, with the last CTA full and not; the longest own caches that are read beside the depth pairs
+    # and one key more; many depth pairs; no depth pairs; no prefix
+    (3, 500, 192, 2, 1, 64, 256), (3, 500, 193, 2, 1, 64, 256), (25, 800, 48, 16, 2, 128, 1), (51, 800, 48, 8, 1, 64, 33), (50, 800, 49, 16, 2, 128, 7),
+    (69, 300, 128, 32, 32, 64, 17), (70, 300, 192, 32, 16, 128, 0), (111, 300, 193, 20, 20, 128, 15), (183, 129, 96, 13, 13, 64, 256), (95, 0, 24, 32, 2, 128, 16),
+    (95, 0, 25, 32, 1, 64, 9), (200, 64, 1, 12, 4, 128, 0),
+]
+
+
+@pytest.mark.parametrize("B,P,T,H,Hk,d,l", NEAR)
+def test_short_own_caches_and_depth_pairs(B, P, T, H, Hk, d, l):
+    x = inputs(B, P, T + 3, H, Hk, d, l, seed=T)
+    for n in "KV":
+        x[n][:, T:] = float("nan")                                           # not read beyond the longest cache
+    check_on_device(x, [(31 * b + T) % (T + 1) for b in range(B)], T, l)
+    check_on_device(x, None, T, l)
+
+
+def test_numbers_behind_a_short_cache_are_not_used():
+    B, P, T, H, Hk, d, l = 90, 200, 40, 32, 8, 64, 5
+    x = inputs(B, P, T, H, Hk, d, l, seed=2)
+    lens = [b % (T + 1) for b in range(B)]
+    a = call(x, lens, T, l, 0.125)
+    for b, n in enumerate(lens):
+        x["K"][b, n:] = float("inf")
+        x["V"][b, n:] = float("nan")
+    c = call(x, lens, T, l, 0.125)
+    assert torch.equal(a[0], c[0]) and torch.equal(a[1], c[1])
 
 
 def test_a_query_that_is_no_number_has_no_result():
