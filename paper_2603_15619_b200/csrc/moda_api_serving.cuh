@@ -157,30 +157,33 @@ int launch_shared(const void* q, const void* Kp, const void* Vp, const SharedMer
     return cuda_ok(rc) ? MODA_OK : MODA_ERR_CUDA;
 }
 
-// CTAs that share the keys of a (sequence, head): their exchanges cost some 2 us a pass, the keys of one CTA about 1 us per 2000.  us, at most 4 / 8 / 16: 131001
-// keys to 16001, 8 heads 42.6 / 31.0 / 31.1, to 100 23.8 / 15.9 / 18.0; 32768 keys 12.2 / 10.6 / 10.6.  16 where 8 cannot hold them.
+// CTAs that share the keys of a (sequence, head): their exchanges cost some 2 us a pass, the keys of one CTA about 1 us per 2000.  While the SMs have room for all:
+// us, at most 4 / 8 / 16: 131001 keys to 16001, 8 heads 42.6 / 31.0 / 31.1, to 100 23.8 / 15.9 / 18.0; 32768 keys 12.2 / 10.6 / 10.6; 1 / 2 / 4: 7 x 36950
+// keys, 8 heads 22.5 / 22.3 / 30.3, 8 x 16384 18.5 / 16.5 / 18.2, 15 x 19512 21.5 / 30.8 / 31.6.  Then up to 4 so that two CTAs fit an SM (19 x 12000 25 -> 21, 27 x
+// 96889, 4 heads 101 -> 96; with up to 8 93, but 2 x 131072 25.5 -> 28.8), and 16 where fewer cannot hold the keys.
 inline int evict_ranks(int T, long long rows) {
     int ranks = 1;
-    while (ranks < 8 && T > 4096 * ranks && rows * ranks < 148) ranks *= 2;
-    while (ranks < 16 && evict_run(T, ranks) > kEvictMostRun) ranks *= 2;
+    while (ranks < 8 && T > 4096 * ranks && rows * ranks * 2 <= 148) ranks *= 2;
+    while (ranks < 4 && evict_run(T, ranks, 512) > 33) ranks *= 2;
+    while (ranks < kEvictMostRanks && evict_run(T, ranks, kEvictMostThreads) > kEvictMostRun) ranks *= 2;
     return ranks;
 }
 
-template <int RUN>
-int launch_evict_select(const EvictParams& p, int ranks, int run, cudaStream_t stream) {
+template <int RUN, int NT, int CTAS>
+int launch_evict_select(const EvictParams& p, int ranks, cudaStream_t stream) {
     static thread_local int configured_dev = -1;
     int dev = 0;
     if (!cuda_ok(cudaGetDevice(&dev))) return MODA_ERR_CUDA;
     if (configured_dev != dev) {
-        if (!set_smem_limit(evict_select_kernel<RUN>, evict_select_smem(RUN)) ||
-            !cuda_ok(cudaFuncSetAttribute(evict_select_kernel<RUN>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)))
+        if (!set_smem_limit(evict_select_kernel<RUN, NT, CTAS>, evict_select_smem(RUN, NT)) ||
+            !cuda_ok(cudaFuncSetAttribute(evict_select_kernel<RUN, NT, CTAS>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)))
             return MODA_ERR_CUDA;
         configured_dev = dev;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(ranks), unsigned(p.Hk), unsigned(p.B));
-    cfg.blockDim = dim3(kEvictThreads, 1, 1);
-    cfg.dynamicSmemBytes = size_t(evict_select_smem(RUN > 0 ? run : 0));
+    cfg.blockDim = dim3(NT, 1, 1);
+    cfg.dynamicSmemBytes = size_t(evict_select_smem(RUN > 0 ? evict_run(p.T, ranks, NT) : 0, NT));
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -188,7 +191,7 @@ int launch_evict_select(const EvictParams& p, int ranks, int run, cudaStream_t s
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cuda_ok(cudaLaunchKernelEx(&cfg, evict_select_kernel<RUN>, p)) ? MODA_OK : MODA_ERR_CUDA;
+    return cuda_ok(cudaLaunchKernelEx(&cfg, evict_select_kernel<RUN, NT, CTAS>, p)) ? MODA_OK : MODA_ERR_CUDA;
 }
 
 inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -320,10 +323,13 @@ int moda_kv_evict(const void* K, const void* V, const float* mass, const int* se
     p.lens_out = lens_out;
     p.B = B; p.T = T; p.T_cap = T_cap; p.T_out = T_out; p.Hk = H_kv; p.n_keep = n_keep; p.n_recent = n_recent;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const int ranks = evict_ranks(T, (long long)B * H_kv), run = evict_run(T, ranks);
-    if (int rc = run <= 5 ? launch_evict_select<5>(p, ranks, run, st) : run <= 9 ? launch_evict_select<9>(p, ranks, run, st)
-               : run <= 17 ? launch_evict_select<17>(p, ranks, run, st) : run <= 33 ? launch_evict_select<33>(p, ranks, run, st)
-               : run <= kEvictMostRun ? launch_evict_select<kEvictMostRun>(p, ranks, run, st) : launch_evict_select<0>(p, ranks, run, st))
+    const int ranks = evict_ranks(T, (long long)B * H_kv), run = evict_run(T, ranks, 512);
+    const bool alone = (long long)B * H_kv * ranks <= 148;           // an SM has one CTA anyway
+    if (int rc = run <= 5 ? launch_evict_select<5, 512, 2>(p, ranks, st) : run <= 9 ? launch_evict_select<9, 512, 2>(p, ranks, st)
+               : run <= 17 ? launch_evict_select<17, 512, 2>(p, ranks, st)
+               : run <= 33 ? (alone ? launch_evict_select<33, 512, 1>(p, ranks, st) : launch_evict_select<33, 512, 2>(p, ranks, st))
+               : evict_run(T, ranks, kEvictMostThreads) <= kEvictMostRun ? launch_evict_select<kEvictMostRun, kEvictMostThreads, 1>(p, ranks, st)
+               : launch_evict_select<0, 512, 1>(p, ranks, st))
         return rc;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];

@@ -46,15 +46,13 @@ __device__ __forceinline__ uint32_t evict_key(float w) {
     return u ^ ((u & 0x80000000u) ? 0xffffffffu : 0x80000000u);
 }
 
-constexpr int kEvictThreads = 512;
-constexpr int kEvictWarps = kEvictThreads / 32;
-constexpr int kEvictBins = 4096, kEvictGroups = kEvictBins / 32;
-constexpr int kEvictMostRun = 65;                 // keys of a thread, of a share that shared memory holds
+constexpr int kEvictBins = 4096, kEvictGroups = kEvictBins / 32, kEvictMostRanks = 16;
+constexpr int kEvictMostRun = 33, kEvictMostThreads = 1024, kEvictWarps = kEvictMostThreads / 32;   // the largest share that shared memory holds
 
 struct EvictShared {
     uint32_t hist[2][kEvictBins], hist3[256];     // of a pass each: nobody waits until another CTA has read the one before
     uint32_t group[3][kEvictGroups];              // sums over 32 bins
-    uint32_t rank_group[kEvictWarps][kEvictGroups], rank_bin[kEvictWarps][32];   // what the cluster's CTAs have
+    uint32_t rank_group[kEvictMostRanks][kEvictGroups], rank_bin[kEvictMostRanks][32];   // what the cluster's CTAs have
     uint32_t warp_gt[kEvictWarps], warp_eq[kEvictWarps];
     __align__(8) uint32_t cta_gt;
     uint32_t cta_eq;
@@ -62,8 +60,8 @@ struct EvictShared {
 };
 static_assert(sizeof(EvictShared) % 16 == 0, "alignment of the keys");
 // Keys of a thread: an odd number, so that the threads' runs start in different banks.
-__host__ __device__ inline int evict_run(int keys, int ranks) { return ((keys + ranks - 1) / ranks + kEvictThreads - 1) / kEvictThreads | 1; }
-inline int evict_select_smem(int run) { return int(sizeof(EvictShared)) + run * kEvictThreads * 4; }
+__host__ __device__ inline int evict_run(int keys, int ranks, int threads) { return ((keys + ranks - 1) / ranks + threads - 1) / threads | 1; }
+inline int evict_select_smem(int run, int threads) { return int(sizeof(EvictShared)) + run * threads * 4; }
 
 __device__ __forceinline__ uint4 ld_cluster_v4(uint32_t addr) {
     uint4 v;
@@ -82,12 +80,14 @@ __device__ __forceinline__ void cp_async_4(uint32_t smem_dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_dst), "l"(src) : "memory");
 }
 
-// grid (cluster, Hk, B).  RUN: most keys of a thread; they are in shared memory and, up to 33, as integers in registers.  0: more than
-// shared memory holds, they are read again for every pass.
-template <int RUN>
-__global__ void __launch_bounds__(kEvictThreads)
+// grid (cluster, Hk, B).  RUN: most keys of a thread; they are in shared memory and, where the registers hold them, there as integers.  0: more
+// than shared memory holds, they are read again for every pass.  CTAS: that share an SM, so that one computes while the other waits.  With up to 33 keys a
+// thread two of them leave no registers for the keys: 64 x 16384 keys, 8 heads, one with / two without 60 / 53 us, but where there are no more
+// CTAs than SMs 30.7 / 34.1 (131001 keys to 16001, 8 heads).  More keys: 1024 threads (27 x 96889 keys, 4 heads, 512 / 1024 101 / 97 us).
+template <int RUN, int NT, int CTAS>
+__global__ void __launch_bounds__(NT, CTAS)
 evict_select_kernel(const EvictParams p) {
-    constexpr bool kHeld = RUN > 0, kRegs = RUN > 0 && RUN <= 33;
+    constexpr bool kHeld = RUN > 0, kRegs = RUN > 0 && RUN <= (CTAS == 1 && NT == 512 ? 33 : 17);
     extern __shared__ __align__(16) uint8_t evict_smem[];
     EvictShared& s = *reinterpret_cast<EvictShared*>(evict_smem);
     float* held = reinterpret_cast<float*>(evict_smem + sizeof(EvictShared));
@@ -101,7 +101,7 @@ evict_select_kernel(const EvictParams p) {
     float* mass_out = p.mass_out ? p.mass_out + (size_t(b) * p.Hk + hk) * p.T_out : nullptr;
 
     // a thread has a run of adjacent keys
-    const int run = evict_run(old, ranks), share = run * kEvictThreads;
+    const int run = evict_run(old, ranks, NT), share = run * NT;
     const int first = min(rank * share, old), n = min(share, old - first);
     const int r0 = min(tid * run, n), mine = min(run, n - r0);
     const bool some = want > 0 && want < old;
@@ -111,13 +111,13 @@ evict_select_kernel(const EvictParams p) {
         const uint32_t dst = smem_u32(held);
         const int quads = (reinterpret_cast<uintptr_t>(mass + first) & 15u) == 0 ? n / 4 : 0;   // rows of any length and start
 #pragma unroll 4
-        for (int i = tid; i < quads; i += kEvictThreads)
+        for (int i = tid; i < quads; i += NT)
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + i * 16), "l"(mass + first + i * 4) : "memory");
 #pragma unroll 4
-        for (int i = quads * 4 + tid; i < n; i += kEvictThreads) cp_async_4(dst + i * 4, mass + first + i);
+        for (int i = quads * 4 + tid; i < n; i += NT) cp_async_4(dst + i * 4, mass + first + i);
     }
 #pragma unroll
-    for (int i = 0; i < 2 * kEvictBins / 4; i += kEvictThreads) reinterpret_cast<uint4*>(s.hist[0])[i + tid] = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = 0; i < 2 * kEvictBins / 4; i += NT) reinterpret_cast<uint4*>(s.hist[0])[i + tid] = make_uint4(0u, 0u, 0u, 0u);
     if (tid < 64) reinterpret_cast<uint4*>(s.hist3)[tid] = make_uint4(0u, 0u, 0u, 0u);
     if (kHeld) asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
@@ -160,13 +160,13 @@ evict_select_kernel(const EvictParams p) {
             __syncthreads();
             {
                 uint32_t sum = 0;
-                if (pass < 2 || tid < 32) {                          // 8 bins a thread
+                if (tid < (pass < 2 ? kEvictBins / 8 : 32)) {                          // 8 bins a thread
                     const uint4 c = *reinterpret_cast<const uint4*>(&hist[tid * 8]), e = *reinterpret_cast<const uint4*>(&hist[tid * 8 + 4]);
                     sum = ((c.x + c.y) + (c.z + c.w)) + ((e.x + e.y) + (e.z + e.w));
                 }
                 sum += __shfl_xor_sync(0xffffffffu, sum, 1);
                 sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                if ((tid & 3) == 0) s.group[pass][tid >> 2] = sum;
+                if ((tid & 3) == 0 && tid < kEvictBins / 8) s.group[pass][tid >> 2] = sum;
             }
             // The bin in two steps: its group of 32, by the groups' sums, then the bin.  Every warp finds it for itself; a warp per CTA of the
             // cluster fetches that CTA's counts (128 and 32 words: all 2048 of a smaller digit from all CTAs took 3 us a pass).
@@ -254,7 +254,7 @@ evict_select_kernel(const EvictParams p) {
     }
     if (lane == 31) { s.warp_gt[warp] = gt_incl; s.warp_eq[warp] = eq_incl; }
     __syncthreads();
-    const uint32_t w_gt = lane < kEvictWarps ? s.warp_gt[lane] : 0u, w_eq = lane < kEvictWarps ? s.warp_eq[lane] : 0u;
+    const uint32_t w_gt = lane < NT / 32 ? s.warp_gt[lane] : 0u, w_eq = lane < NT / 32 ? s.warp_eq[lane] : 0u;
     uint32_t gt_before = __reduce_add_sync(0xffffffffu, lane < warp ? w_gt : 0u) + gt_incl - gt;
     uint32_t eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? w_eq : 0u) + eq_incl - eq;
     if (ranks > 1) {
@@ -283,7 +283,7 @@ evict_select_kernel(const EvictParams p) {
         for (int j = 0; j < mine; ++j) keep(j);
     }
     // the recent keys, and -1 behind the last one kept
-    for (int i = rank * kEvictThreads + tid; i < p.n_keep - want; i += ranks * kEvictThreads) {
+    for (int i = rank * NT + tid; i < p.n_keep - want; i += ranks * NT) {
         index[want + i] = i < recent ? old + i : -1;
         if (i < recent && mass_out) mass_out[want + i] = mass[old + i];
     }
