@@ -523,7 +523,8 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
     if (warp == 17) tmem_dealloc(tmem, 512);
 }
 
-// Adds the pieces of the tiles that several runs share: CTA c takes the tile that starts in run c and does not end there.
+// Adds the pieces of the tiles that several runs share: CTA c takes the tile that starts in run c and does not end there.  First how many there are, 32 runs
+// at a look, then the sums, 16 on their way at once and added in order (one after the other: 1409 rows, 8 heads on 1, d = 64, 25 pieces a tile: 19.4 -> 12.7 us).
 __global__ void __launch_bounds__(kKmTile)
 key_mass_join_kernel(const KeyMassParams p) {
     const int ctas = gridDim.x, c = blockIdx.x, r = threadIdx.x;
@@ -535,9 +536,21 @@ key_mass_join_kernel(const KeyMassParams p) {
     if (d.y == kPieceNone) d = dir[--slot];
     if (d.y != kPieceStart) return;                   // ends in its run (or nothing is shared), or does not start in it
     float sum = p.part[size_t(slot) * kKmTile + r];
-    for (int k = c + p.team; k < ctas; k += p.team) {
-        sum += p.part[size_t(2 * k) * kKmTile + r];
-        if (dir[2 * k].y & kPieceEnd) break;
+    int more = 0;
+    for (bool found = false; !found;) {
+        const int k = c + (more + (r & 31) + 1) * p.team;
+        const unsigned there = __ballot_sync(0xffffffffu, k < ctas), last = __ballot_sync(0xffffffffu, k < ctas && (dir[2 * k].y & kPieceEnd));
+        found = last != 0u || there != 0xffffffffu;
+        more += last != 0u ? __ffs(last) : __popc(there);
+    }
+    constexpr int UN = 16;
+    for (int i0 = 1; i0 <= more; i0 += UN) {
+        float x[UN];
+#pragma unroll
+        for (int u = 0; u < UN; ++u) x[u] = p.part[size_t(2 * (c + min(i0 + u, more) * p.team)) * kKmTile + r];
+#pragma unroll
+        for (int u = 0; u < UN; ++u)
+            if (i0 + u <= more) sum += x[u];
     }
     const int bh = d.x / p.tiles, key = (d.x - bh * p.tiles) * kKmTile + r;
     if (key < p.T_kv) {

@@ -138,8 +138,8 @@ def test_many_heads_at_once(T, n_keep, n_recent, ragged):
 @pytest.mark.parametrize("B,T,Hk,n_keep,n_recent", [
     (20, 12000, 8, 700, 50),        # more CTAs than SMs, two of them on one
     (5, 16001, 1, 300, 0),          # keys of a thread in registers, a CTA for each SM
-    (10, 99001, 8, 100, 7),         # clusters of 4 with 1024 threads
-    (3, 280000, 27, 64, 64),        # clusters of 16
+    (19, 99001, 1, 100, 7),         # clusters of 4 with 1024 threads
+    (1, 280000, 2, 64, 64),         # clusters of 16
 ])
 def test_many_long_rows(B, T, Hk, n_keep, n_recent):
     K, V, mass = inputs(B, T, Hk, 64, seed=T)
