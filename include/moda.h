@@ -556,7 +556,7 @@ int moda_depth_slot_mass(const void* Q, const void* depth_kv, const float* LSE,
  *     K, V     : bf16 [B][T_cap][H_kv][d]       mass : fp32 [B][H_kv][T_cap]; neither is changed
  *     K_out, V_out : bf16 [B][T_out][H_kv][d], T_out >= n_keep; rows [0, kept) written; must not overlap K, V (MODA_ERR_BAD_SHAPE)
  *     mass_out : fp32 [B][H_kv][T_out], rows [0, kept) written, must not overlap mass, or NULL       index : int32 [B][H_kv][n_keep], old positions of the kept rows, -1 behind them
- *     lens_out : int32 [B], kept, or NULL
+ *     lens_out : int32 [B], kept, or NULL; may be seq_lens itself, must not overlap it in another way (MODA_ERR_BAD_SHAPE)
  *   1 <= n_keep, 0 <= n_recent <= n_keep.  The positions of a head differ from another's: positional information has to be in the keys.  Two launches.
  *
  * moda_attn_decode_shared decode step of B sequences over a prefix that all share, each sequence's own cache, and the token's depth pairs, under

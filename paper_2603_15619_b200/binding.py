@@ -866,7 +866,7 @@ def moda_kv_evict(K, V, mass, T, n_keep, n_recent=0, seq_lens=None, K_out=None, 
     """Cuts a cache to its most used keys: of the T (or, with ``seq_lens`` int32 [B], fewer) rows of K, V [B,T_cap,H_kv,d], per (sequence, key/value head) the
     last ``n_recent`` and those of largest ``mass`` [B,H_kv,T_cap] stay, ``n_keep`` in all, in their order.  Returns K_out, V_out [B,T_out,H_kv,d] (T_out =
     n_keep where they are allocated here), mass_out [B,H_kv,T_out], the old positions index int32 [B,H_kv,n_keep] (-1 behind the last one kept) and the
-    new lengths lens_out int32 [B]."""
+    new lengths lens_out int32 [B], which may be ``seq_lens`` itself."""
     if stream is None and (out := host().evict(K, V, mass, T, n_keep, n_recent, seq_lens, K_out, V_out, mass_out, index, lens_out)) is not None:
         return out
     B, T_cap, Hk, d = _bthd(K, "K")

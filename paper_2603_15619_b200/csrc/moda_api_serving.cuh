@@ -316,6 +316,10 @@ int moda_kv_evict(const void* K, const void* V, const float* mass, const int* se
         const auto a = reinterpret_cast<uintptr_t>(mass), b = reinterpret_cast<uintptr_t>(mass_out);
         if (b < a + size_t(B) * H_kv * T_cap * 4 && a < b + size_t(B) * H_kv * T_out * 4) return MODA_ERR_BAD_SHAPE;
     }
+    if (seq_lens && lens_out && lens_out != seq_lens) {              // in place, but not over another sequence's length
+        const auto a = reinterpret_cast<uintptr_t>(seq_lens), b = reinterpret_cast<uintptr_t>(lens_out);
+        if (b < a + size_t(B) * 4 && a < b + size_t(B) * 4) return MODA_ERR_BAD_SHAPE;
+    }
     if (int rc = check_device()) return rc;
     EvictParams p = {};
     p.K = static_cast<const __nv_bfloat16*>(K); p.V = static_cast<const __nv_bfloat16*>(V); p.mass = mass; p.seq_lens = seq_lens;

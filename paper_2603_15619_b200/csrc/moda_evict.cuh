@@ -8,7 +8,8 @@
 //                        memory where they fit, and the cluster's counts are added over distributed shared memory.  Then every thread, which
 //                        has a run of adjacent keys, counts what it keeps and writes positions and weights behind what is kept before it.
 //   evict_gather_kernel  copies the kept K and V rows, all heads of a few output positions per CTA: bound by HBM (each row read and
-//                        written once; 32 sequences, 1024 rows of 8 heads kept, d = 128: 268 MB in 38 us).
+//                        written once; 32 sequences, 1024 rows of 8 heads kept, d = 128: 268 MB in 38 us).  It writes the new lengths too: they may
+//                        take the place of the old ones, which the selection of any head, whenever its CTAs get their turn, has to read.
 //
 // The selection is a chain of short phases, bound by their latencies (per CTA of 8192 keys some 8 us: 2.3 the weights' way here, 2 each of the two or three
 // passes, 2.5 counting and writing).  us, both kernels: 32 x 8192 keys to 1024, 8 heads 53; 131001 keys to 16001, 8 heads, d = 64 31; 2176 to 2048 8.6.
@@ -31,7 +32,7 @@ struct EvictParams {
     __nv_bfloat16* V_out;
     float* mass_out;              // [B][Hk][T_out], may be null
     int* index;                   // [B][Hk][n_keep]
-    int* lens_out;                // [B], may be null
+    int* lens_out;                // [B], may be null, may be seq_lens
     int B, T, T_cap, T_out, Hk, n_keep, n_recent;
 };
 
@@ -287,7 +288,6 @@ evict_select_kernel(const EvictParams p) {
         index[want + i] = i < recent ? old + i : -1;
         if (i < recent && mass_out) mass_out[want + i] = mass[old + i];
     }
-    if (rank == 0 && hk == 0 && tid == 0 && p.lens_out) p.lens_out[b] = kept;
     if (ranks > 1) cluster_wait();
 }
 
@@ -301,8 +301,9 @@ evict_gather_kernel(const EvictParams p, int rows) {
     constexpr int CH = D / 8;                                        // 16-byte pieces of a row
     extern __shared__ int s_index[];                                 // [rows][Hk]
     const int b = blockIdx.y, n0 = int(blockIdx.x) * rows;
-    const int kept = min(p.n_keep, evict_len(p, b));
+    const int kept = min(p.n_keep, evict_len(p, b));                 // the same of the old length and of the new one
     grid_dependency_wait();
+    if (blockIdx.x == 0 && threadIdx.x == 0 && p.lens_out) p.lens_out[b] = kept;   // every head's selection has ended
     const int here = min(rows, kept - n0);
     if (here <= 0) return;
     for (int e = threadIdx.x; e < here * p.Hk; e += kEvictGatherThreads) {
