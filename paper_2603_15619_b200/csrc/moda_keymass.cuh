@@ -200,6 +200,9 @@ __global__ void __launch_bounds__(kKmThreads, 1)
 key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK, const KeyMassParams p) {
     using L = KeyMassSmem<D>;
     constexpr int NSUB = D / 64;
+    // first of all, whatever happens then: the join takes places in `mass` from here, and the workspace holds anything
+    int2* dir = reinterpret_cast<int2*>(p.part + size_t(gridDim.x) * 2 * kKmTile) + blockIdx.x * 2;
+    if (threadIdx.x < 2) dir[threadIdx.x] = make_int2(0, kPieceNone);
     if (g_moda_status != 0) return;   // an earlier kernel gave up a wait: do not pile up more timeouts
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -212,9 +215,7 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int off = p.T_kv - p.T_q;
     const int rows = p.P * p.G;                       // query rows of a unit, at most 128
-    int2* dir = reinterpret_cast<int2*>(p.part + size_t(gridDim.x) * 2 * kKmTile) + blockIdx.x * 2;
 
-    if (tid < 2) dir[tid] = make_int2(0, kPieceNone);
     if (tid == 0) {
         *abort_flag = 0;
         for (int s = 0; s < 4; ++s) {
@@ -529,7 +530,8 @@ __global__ void __launch_bounds__(kKmTile)
 key_mass_join_kernel(const KeyMassParams p) {
     const int ctas = gridDim.x, c = blockIdx.x, r = threadIdx.x;
     const int2* dir = reinterpret_cast<const int2*>(p.part + size_t(ctas) * 2 * kKmTile);
-    grid_dependency_wait();                           // (launched beside key_mass_kernel's last CTAs)
+    grid_dependency_wait();
+    if (g_moda_status != 0) return;                   // a wait was given up before or in key_mass_kernel: there are no sums
     // the piece at the end of run c: its second entry, or its first where the run is one piece
     int slot = 2 * c + 1;
     int2 d = dir[slot];
