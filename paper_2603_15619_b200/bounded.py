@@ -67,6 +67,7 @@ class BoundedCache:
         at = self.lens.long()
         self.K[self._rows, at] = k
         self.V[self._rows, at] = v
+        self.mass[self._rows, :, at] = 0                       # the buffer holds what an earlier key had there
         self.lens += 1
         self.longest += 1
 
