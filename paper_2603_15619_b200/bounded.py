@@ -32,6 +32,7 @@ class BoundedCache:
         self.lens = torch.zeros((B,), device=device, dtype=torch.int32)
         self.longest = 0                                       # no length is above this (known without asking the device)
         self._rows = torch.arange(B, device=device)
+        self._attended = False                                 # the newest key has taken part in a step
 
     @property
     def K(self):
@@ -59,6 +60,7 @@ class BoundedCache:
             raise ValueError("K must be [B, T, H_kv, d] of this cache")
         mass = binding.moda_attn_key_mass(Q, K, LSE, scale)
         self._cut_into(K, V, mass, K.shape[1], None)
+        self._attended = True
 
     def append(self, k, v):
         """The next token's key and value rows [B,H_kv,d]; cuts the cache first if it is full."""
@@ -70,13 +72,21 @@ class BoundedCache:
         self.mass[self._rows, :, at] = 0                       # the buffer holds what an earlier key had there
         self.lens += 1
         self.longest += 1
+        self._attended = False
 
     def attend(self, q, depth_kv_token, l, scale, O=None, LSE=None, workspace=None):
-        """The step of the token appended last: O [B,H,d], LSE [B,H]; its weights are added to the accumulated ones."""
+        """The step of the token appended last, or of another query over the same keys: O [B,H,d], LSE [B,H]; its weights are added to the
+        accumulated ones."""
         if self.longest < 1:
             raise ValueError("append the token's key and value first")
+        # the call starts the newest key from 0, which is right for a token's first step alone
+        newest = (self._rows, slice(None), self.lens.long() - 1) if self._attended else None
+        had = self.mass[newest] if self._attended else None
         O, LSE, _ = binding.moda_attn_decode_mass(q, self.K, self.V, depth_kv_token, self.longest, l, scale, seq_lens=self.lens, mass_in=self.mass, mass=self.mass,
                                                   O=O, LSE=LSE, workspace=workspace)
+        if self._attended:
+            self.mass[newest] += had
+        self._attended = True
         return O, LSE
 
 
