@@ -69,4 +69,36 @@ inline unsigned bwd_row_ctas(int d, long long bh, int T, int l, unsigned units, 
 // T = 300 (16) 27.2 / 26.4; G = 8: T = 100 (16) 21.3 / 20.9, T = 256 (24) 38.1 / 36.1.
 inline bool bwd_alternates(int d, int T, int G) { return d == 64 && G * ((T + 127) / 128 + 1) > 7; }
 
+// The selection of an eviction (moda_evict.cuh) and the form of its kernel.
+constexpr int kEvictMostRanks = 16, kEvictMostThreads = 1024;
+constexpr int kEvictMostRun = 33;                          // keys of a thread, of 1024: the largest share that shared memory holds
+// Keys of a thread: an odd number, so that the threads' runs start in different banks.
+#if defined(__CUDACC__)
+__host__ __device__
+#endif
+inline int evict_run(int keys, int ranks, int threads) { return ((keys + ranks - 1) / ranks + threads - 1) / threads | 1; }
+
+struct EvictForm {
+    int ranks;                    // CTAs of a cluster, which share the keys of a (sequence, head)
+    int most, threads, ctas;      // keys of a thread at most (0: they are read again for every pass), threads of a CTA, CTAs of an SM
+};
+// Ranks: their exchanges cost some 2 us a pass, the keys of one CTA about 1 us per 2000.  While the SMs have room for all:
+// us, at most 4 / 8 / 16: 131001 keys to 16001, 8 heads 42.6 / 31.0 / 31.1, to 100 23.8 / 15.9 / 18.0; 32768 keys 12.2 / 10.6 / 10.6; 1 / 2 / 4: 7 x 36950
+// keys, 8 heads 22.5 / 22.3 / 30.3, 8 x 16384 18.5 / 16.5 / 18.2, 15 x 19512 21.5 / 30.8 / 31.6.  Then up to 4 so that two CTAs fit an SM (19 x 12000 25 -> 21, 27 x
+// 96889, 4 heads 101 -> 96; with up to 8 93, but 2 x 131072 25.5 -> 28.8), and 16 where fewer cannot hold the keys.
+// CTAs of an SM: one computes while the other waits.  With up to 33 keys a
+// thread two of them leave no registers for the keys: 64 x 16384 keys, 8 heads, one with / two without 60 / 53 us, but where there are no more
+// CTAs than SMs 30.7 / 34.1 (131001 keys to 16001, 8 heads).  More keys: 1024 threads (27 x 96889 keys, 4 heads, 512 / 1024 101 / 97 us).
+inline EvictForm evict_form(int T, long long rows, int sms) {
+    int ranks = 1;
+    while (ranks < 8 && T > 4096 * ranks && rows * ranks * 2 <= sms) ranks *= 2;
+    while (ranks < 4 && evict_run(T, ranks, 512) > 33) ranks *= 2;
+    while (ranks < kEvictMostRanks && evict_run(T, ranks, kEvictMostThreads) > kEvictMostRun) ranks *= 2;
+    const int run = evict_run(T, ranks, 512);
+    if (run <= 17) return {ranks, run <= 5 ? 5 : run <= 9 ? 9 : 17, 512, 2};
+    if (run <= 33) return {ranks, 33, 512, rows * ranks <= sms ? 1 : 2};
+    if (evict_run(T, ranks, kEvictMostThreads) <= kEvictMostRun) return {ranks, kEvictMostRun, kEvictMostThreads, 1};
+    return {ranks, 0, 512, 1};
+}
+
 }  // namespace moda

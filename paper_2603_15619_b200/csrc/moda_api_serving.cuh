@@ -157,18 +157,6 @@ int launch_shared(const void* q, const void* Kp, const void* Vp, const SharedMer
     return cuda_ok(rc) ? MODA_OK : MODA_ERR_CUDA;
 }
 
-// CTAs that share the keys of a (sequence, head): their exchanges cost some 2 us a pass, the keys of one CTA about 1 us per 2000.  While the SMs have room for all:
-// us, at most 4 / 8 / 16: 131001 keys to 16001, 8 heads 42.6 / 31.0 / 31.1, to 100 23.8 / 15.9 / 18.0; 32768 keys 12.2 / 10.6 / 10.6; 1 / 2 / 4: 7 x 36950
-// keys, 8 heads 22.5 / 22.3 / 30.3, 8 x 16384 18.5 / 16.5 / 18.2, 15 x 19512 21.5 / 30.8 / 31.6.  Then up to 4 so that two CTAs fit an SM (19 x 12000 25 -> 21, 27 x
-// 96889, 4 heads 101 -> 96; with up to 8 93, but 2 x 131072 25.5 -> 28.8), and 16 where fewer cannot hold the keys.
-inline int evict_ranks(int T, long long rows) {
-    int ranks = 1;
-    while (ranks < 8 && T > 4096 * ranks && rows * ranks * 2 <= 148) ranks *= 2;
-    while (ranks < 4 && evict_run(T, ranks, 512) > 33) ranks *= 2;
-    while (ranks < kEvictMostRanks && evict_run(T, ranks, kEvictMostThreads) > kEvictMostRun) ranks *= 2;
-    return ranks;
-}
-
 template <int RUN, int NT, int CTAS>
 int launch_evict_select(const EvictParams& p, int ranks, cudaStream_t stream) {
     static thread_local int configured_dev = -1;
@@ -327,13 +315,16 @@ int moda_kv_evict(const void* K, const void* V, const float* mass, const int* se
     p.lens_out = lens_out;
     p.B = B; p.T = T; p.T_cap = T_cap; p.T_out = T_out; p.Hk = H_kv; p.n_keep = n_keep; p.n_recent = n_recent;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const int ranks = evict_ranks(T, (long long)B * H_kv), run = evict_run(T, ranks, 512);
-    const bool alone = (long long)B * H_kv * ranks <= 148;           // an SM has one CTA anyway
-    if (int rc = run <= 5 ? launch_evict_select<5, 512, 2>(p, ranks, st) : run <= 9 ? launch_evict_select<9, 512, 2>(p, ranks, st)
-               : run <= 17 ? launch_evict_select<17, 512, 2>(p, ranks, st)
-               : run <= 33 ? (alone ? launch_evict_select<33, 512, 1>(p, ranks, st) : launch_evict_select<33, 512, 2>(p, ranks, st))
-               : evict_run(T, ranks, kEvictMostThreads) <= kEvictMostRun ? launch_evict_select<kEvictMostRun, kEvictMostThreads, 1>(p, ranks, st)
-               : launch_evict_select<0, 512, 1>(p, ranks, st))
+    int sms = 0;
+    if (int rc = device_sm_count(&sms)) return rc;
+    const EvictForm f = evict_form(T, (long long)B * H_kv, sms);
+    if (int rc = f.most == 5    ? launch_evict_select<5, 512, 2>(p, f.ranks, st)
+                 : f.most == 9  ? launch_evict_select<9, 512, 2>(p, f.ranks, st)
+                 : f.most == 17 ? launch_evict_select<17, 512, 2>(p, f.ranks, st)
+                 : f.most == 0  ? launch_evict_select<0, 512, 1>(p, f.ranks, st)
+                 : f.threads > 512 ? launch_evict_select<kEvictMostRun, kEvictMostThreads, 1>(p, f.ranks, st)
+                 : f.ctas == 2  ? launch_evict_select<33, 512, 2>(p, f.ranks, st)
+                                : launch_evict_select<33, 512, 1>(p, f.ranks, st))
         return rc;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];

@@ -19,6 +19,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include "launch_rules.h"
 #include "sm100_ptx.cuh"
 
 namespace moda {
@@ -47,8 +48,7 @@ __device__ __forceinline__ uint32_t evict_key(float w) {
     return u ^ ((u & 0x80000000u) ? 0xffffffffu : 0x80000000u);
 }
 
-constexpr int kEvictBins = 4096, kEvictGroups = kEvictBins / 32, kEvictMostRanks = 16;
-constexpr int kEvictMostRun = 33, kEvictMostThreads = 1024, kEvictWarps = kEvictMostThreads / 32;   // the largest share that shared memory holds
+constexpr int kEvictBins = 4096, kEvictGroups = kEvictBins / 32, kEvictWarps = kEvictMostThreads / 32;
 
 struct EvictShared {
     uint32_t hist[2][kEvictBins], hist3[256];     // of a pass each: nobody waits until another CTA has read the one before
@@ -60,8 +60,6 @@ struct EvictShared {
     uint32_t pad[2];                              // the keys behind start on a 16-byte boundary
 };
 static_assert(sizeof(EvictShared) % 16 == 0, "alignment of the keys");
-// Keys of a thread: an odd number, so that the threads' runs start in different banks.
-__host__ __device__ inline int evict_run(int keys, int ranks, int threads) { return ((keys + ranks - 1) / ranks + threads - 1) / threads | 1; }
 inline int evict_select_smem(int run, int threads) { return int(sizeof(EvictShared)) + run * threads * 4; }
 
 __device__ __forceinline__ uint4 ld_cluster_v4(uint32_t addr) {
@@ -81,10 +79,8 @@ __device__ __forceinline__ void cp_async_4(uint32_t smem_dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_dst), "l"(src) : "memory");
 }
 
-// grid (cluster, Hk, B).  RUN: most keys of a thread; they are in shared memory and, where the registers hold them, there as integers.  0: more
-// than shared memory holds, they are read again for every pass.  CTAS: that share an SM, so that one computes while the other waits.  With up to 33 keys a
-// thread two of them leave no registers for the keys: 64 x 16384 keys, 8 heads, one with / two without 60 / 53 us, but where there are no more
-// CTAs than SMs 30.7 / 34.1 (131001 keys to 16001, 8 heads).  More keys: 1024 threads (27 x 96889 keys, 4 heads, 512 / 1024 101 / 97 us).
+// grid (cluster, Hk, B).  RUN: most keys of a thread (evict_form); they are in shared memory and, where the registers hold them, there as integers.  0: more
+// than shared memory holds, they are read again for every pass.  CTAS: that share an SM.
 template <int RUN, int NT, int CTAS>
 __global__ void __launch_bounds__(NT, CTAS)
 evict_select_kernel(const EvictParams p) {
