@@ -154,9 +154,6 @@ struct RingAt {
 struct PipeWait {
     volatile int* abort_flag;
     __device__ __forceinline__ void operator()(uint32_t bar, uint32_t parity, int site) const { mbar_wait(bar, parity, abort_flag, site); }
-    __device__ __forceinline__ void both(uint32_t bar_a, uint32_t parity_a, uint32_t bar_b, uint32_t parity_b, int site_a, int site_b) const {
-        mbar_wait2(bar_a, parity_a, bar_b, parity_b, abort_flag, site_a, site_b);
-    }
 };
 
 // First unit that sees tile `jt`: the one of the first position i with i + off >= 256 jt.
@@ -530,7 +527,7 @@ __global__ void __launch_bounds__(kKmTile)
 key_mass_join_kernel(const KeyMassParams p) {
     const int ctas = gridDim.x, c = blockIdx.x, r = threadIdx.x;
     const int2* dir = reinterpret_cast<const int2*>(p.part + size_t(ctas) * 2 * kKmTile);
-    grid_dependency_wait();
+    grid_dependency_wait();                           // launched when key_mass_kernel's last CTA has gone, which lets nothing start earlier
     if (g_moda_status != 0) return;                   // a wait was given up before or in key_mass_kernel: there are no sums
     // the piece at the end of run c: its second entry, or its first where the run is one piece
     int slot = 2 * c + 1;
