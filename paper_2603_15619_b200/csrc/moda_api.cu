@@ -755,7 +755,7 @@ int launch_decode_g(const DecodeParams& p, cudaStream_t stream) {
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (!cuda_ok(cudaLaunchKernelEx(&cfg, decode_merge_kernel<D>, p))) return MODA_ERR_CUDA;
+    if (!cuda_ok(cudaLaunchKernelEx(&cfg, decode_merge_kernel<D, (GF >= kDecodeKeepScores)>, p))) return MODA_ERR_CUDA;
     return MODA_OK;
 }
 template <int D, int MORE = 0>

@@ -499,7 +499,10 @@ decode_split_tma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_c
 // of short dependent phases, so its time is load latency, not bandwidth).
 constexpr int kDecodeMergeThreads = 128;
 
-template <int D>
+// THEN: another kernel comes behind this one and may come up beside it.  (A form of its own: the instruction costs the d = 64 form 7 registers and with them a
+// quarter of the CTAs of an SM.  us, plain step without / with it: 96 x 1500 keys, 24 heads on 8, d = 64, l = 32 61.2 / 62.1, with lengths 61.4 / 62.8; one
+// sequence, 2048 keys, 16 heads on 8, d = 128, l = 24 8.47 / 8.53, with lengths 9.02 / 9.15.)
+template <int D, bool THEN>
 __global__ void __launch_bounds__(kDecodeMergeThreads)
 decode_merge_kernel(const DecodeParams p) {
     constexpr int FPL = D / 32, NW = kDecodeMergeThreads / 32, UN = 4;
@@ -529,7 +532,7 @@ decode_merge_kernel(const DecodeParams p) {
     const int Hk_real = p.Hk / p.kv_rep;                                            // p.Hk counts groups of at most 8 heads
     const __nv_bfloat16* depth0 = p.depth + (size_t(b) * Hk_real + hk / p.kv_rep) * 2 * D;   // slot 0: key row, value row at + D
 
-    grid_launch_dependents();                                                       // decode_key_mass_kernel may come up
+    if constexpr (THEN) grid_launch_dependents();                                   // decode_key_mass_kernel
     // ---- depth scores: warp `warp` takes slots warp, warp + 4, ..., UN at a time ----
     for (int i0 = warp; i0 < p.l; i0 += NW * UN) {
         float kd[UN][FPL];
