@@ -537,7 +537,7 @@ int moda_depth_slot_mass(const void* Q, const void* depth_kv, const float* LSE,
  *     mass[b, hk, j] = old + sum_{h in group hk} sum_{i : i + T_kv - T_q >= j} exp( scale <Q[b,i,h,:], K[b,j,hk,:]> - LSE[b,h,i] )
  *
  *     Q        : bf16 [B][T_q][H][d]        K : bf16 [B][T_cap][H_kv][d], rows [0, T_kv) read
- *     LSE      : fp32 [B][H][T_q], of the forward of these rows; a row whose LSE is -inf (it saw no key) has no weight
+ *     LSE      : fp32 [B][H][T_q], of the forward of these rows; a row whose LSE is -inf (it saw no key) has no weight, whatever its Q holds
  *     mass_in  : NULL, or the weights before the call, of which the positions before the T_q new ones (j < T_kv - T_q) are read: `old`; may be `mass`
  *     mass     : positions [0, T_kv) written
  *     workspace: moda_key_mass_workspace_bytes

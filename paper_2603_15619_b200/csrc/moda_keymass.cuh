@@ -19,7 +19,8 @@
 //   atomics: the result is reproducible bit for bit).
 //
 //   20 warps: 0-15 four warpgroups (even units: tiles' first and second 128 keys, odd units: likewise), 16 TMA producer, 17 and 19 issue the
-//   products of the two halves (17 owns TMEM), 18 prepares the LSE terms.  With few units a tile the warpgroups and issuers take even and
+//   products of the two halves (17 owns TMEM), 18 prepares the LSE terms and clears the queries of rows that saw no key (LSE -inf;
+//   a test of every unit by the weights' warps instead: 67.9 -> 69.7 us in the second case below, this way 68.1).  With few units a tile the warpgroups and issuers take even and
 //   odd tiles instead: their sums need not meet (64 rows over 8192 keys, B = 4, 32 heads on 8, two units: d = 128 32.7 -> 30.4 us, d = 64 29.7 -> 27.5; 300 rows over
 //   6000, B = 2, 16 heads, d = 64, three: 29.6 -> 27.7).
 //
@@ -134,8 +135,9 @@ inline void key_mass_slots(int d, int n_units, int& k_slots, int& q_slots) {
 enum KeyMassBar : int {
     kKmKFull = 0,      // +slot of a tile's half (<= 4)
     kKmKEmpty = 4,     // +slot: every product with it is complete
-    kKmQFull = 8,      // +slot of a unit (<= 6): its rows and their LSE terms
+    kKmQFull = 8,      // +slot of a unit (<= 6): its LSE terms, and rows that saw no key are zero
     kKmQEmpty = 14,    // +slot: the products of both halves with it are complete
+    kKmQHere = 20,     // +slot: its rows are there
     kKmSFull = 26,     // +(n % 2) * 2 + half: the scores are there
     kKmSEmpty = 30,    // +(n % 2) * 2 + half: the scores have been read
     kKmDone = 34,      // +(piece % 2): the warpgroups' sums of a piece are in shared memory
@@ -154,6 +156,9 @@ struct RingAt {
 struct PipeWait {
     volatile int* abort_flag;
     __device__ __forceinline__ void operator()(uint32_t bar, uint32_t parity, int site) const { mbar_wait(bar, parity, abort_flag, site); }
+    __device__ __forceinline__ void both(uint32_t bar_a, uint32_t parity_a, uint32_t bar_b, uint32_t parity_b, int site_a, int site_b) const {
+        mbar_wait2(bar_a, parity_a, bar_b, parity_b, abort_flag, site_a, site_b);
+    }
 };
 
 // First unit that sees tile `jt`: the one of the first position i with i + off >= 256 jt.
@@ -222,7 +227,8 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
             mbar_init(bar(kKmSEmpty + s), 128);
         }
         for (int s = 0; s < L::kMaxUnits; ++s) {
-            mbar_init(bar(kKmQFull + s), 2);
+            mbar_init(bar(kKmQFull + s), 1);
+            mbar_init(bar(kKmQHere + s), 1);
             mbar_init(bar(kKmQEmpty + s), 2);
         }
         for (int s = 0; s < 2; ++s) mbar_init(bar(kKmDone + s), 512);
@@ -401,14 +407,14 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                 for (int u = w.u0; u < w.u1; ++u, qa.next(p.q_slots)) {
                     if (qa.round > 0) wait(bar(kKmQEmpty + qa.slot), (qa.round - 1) & 1, 121);
                     if (p.stay && fresh == 0) {
-                        mbar_arrive(bar(kKmQFull + qa.slot));
+                        mbar_arrive(bar(kKmQHere + qa.slot));
                         continue;
                     }
                     --fresh;
-                    mbar_arrive_expect_tx(bar(kKmQFull + qa.slot), unit_bytes);
+                    mbar_arrive_expect_tx(bar(kKmQHere + qa.slot), unit_bytes);
 #pragma unroll
                     for (int s = 0; s < NSUB; ++s)
-                        tma_load_4d(sbase + (p.k_slots + qa.slot) * L::kSlotBytes + s * L::kSubBytes, &mapQ, bar(kKmQFull + qa.slot), s * 64, hk * p.G, u * p.P, b);
+                        tma_load_4d(sbase + (p.k_slots + qa.slot) * L::kSlotBytes + s * L::kSubBytes, &mapQ, bar(kKmQHere + qa.slot), s * 64, hk * p.G, u * p.P, b);
                 }
                 w.next(p);
             }
@@ -433,7 +439,7 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
             }
 #pragma unroll 1
             for (int u = w.u0; u < w.u1; ++u, ++n, qa.next(p.q_slots)) {
-                wait(bar(kKmQFull + qa.slot), qa.round & 1, 131);        // likewise of every unit
+                wait.both(bar(kKmQFull + qa.slot), qa.round & 1, bar(kKmQHere + qa.slot), qa.round & 1, 131, 135);   // likewise of every unit
                 if (!mine) continue;
                 const uint64_t dq = dq0 + uint64_t((qa.slot * L::kSlotBytes) >> 4);
                 const int terms = L::kTerms + qa.slot * L::kTermBytes;
@@ -470,7 +476,7 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
             while (!mbar_try_wait(bar(kKmDrain + id), 0) && globaltimer_ns() - t0 < 20000000ull) {}
         }
       } else if (warp == 18) {
-        // =========================== LSE terms of a unit's rows ===========================
+        // =========================== LSE terms of a unit's rows; rows that saw no key ===========================
         int pos[4], at[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -504,6 +510,19 @@ key_mass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                 uint4 t = make_uint4(0x0000ff80u, 0u, 0u, 0u);           // -inf: no row, or one without keys (LSE -inf)
                 if (fabsf(v[i]) != INFINITY) split3_bf16(-v[i] * p.inv_scale, t.x, t.y);
                 *reinterpret_cast<uint4*>(smem + L::kTerms + qa.slot * L::kTermBytes + (lane + i * 32) * 16) = t;
+            }
+            if (__any_sync(0xffffffffu, v[0] == -INFINITY || v[1] == -INFINITY || v[2] == -INFINITY || v[3] == -INFINITY)) {
+                // -inf takes up any number, but not NaN: the query of a row that saw no key may hold anything
+                wait(bar(kKmQHere + qa.slot), qa.round & 1, 141);
+#pragma unroll 1
+                for (int e = 0; e < 4 * NSUB * 8; ++e) {
+                    const int i = e / (NSUB * 8), r = lane + i * 32, sub = e / 8 % NSUB;
+                    if ((i == 0 ? v[0] : i == 1 ? v[1] : i == 2 ? v[2] : v[3]) == -INFINITY)
+                        *reinterpret_cast<uint4*>(smem + (p.k_slots + qa.slot) * L::kSlotBytes + sub * L::kSubBytes + r * 128 + (e & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
                 v[i] = v1[i];
                 v1[i] = v2[i];
             }
