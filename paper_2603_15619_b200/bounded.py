@@ -44,11 +44,12 @@ class BoundedCache:
 
     @property
     def mass(self):
-        """Accumulated weights [B, H_kv, capacity]; those of a sequence's first ``lens`` keys have a meaning."""
+        """Accumulated weights [B, H_kv, capacity] of a sequence's first ``lens`` keys; 0 behind them."""
         return self._sets[0][2]
 
     def _cut_into(self, K, V, mass, longest, lens):
         Ko, Vo, mo = self._sets[1]
+        mo.zero_()                                             # behind the keys that stay it holds weights of an earlier cut: a new key has none
         binding.moda_kv_evict(K, V, mass, longest, self.keep, self.recent, seq_lens=lens, K_out=Ko, V_out=Vo, mass_out=mo, index=self.index, lens_out=self.lens)
         self._sets.reverse()
         self.longest = min(longest, self.keep)
@@ -69,7 +70,6 @@ class BoundedCache:
         at = self.lens.long()
         self.K[self._rows, at] = k
         self.V[self._rows, at] = v
-        self.mass[self._rows, :, at] = 0                       # the buffer holds what an earlier key had there
         self.lens += 1
         self.longest += 1
         self._attended = False
