@@ -24,10 +24,11 @@
 //   odd tiles instead: their sums need not meet (64 rows over 8192 keys, B = 4, 32 heads on 8, two units: d = 128 32.7 -> 30.4 us, d = 64 29.7 -> 27.5; 300 rows over
 //   6000, B = 2, 16 heads, d = 64, three: 29.6 -> 27.7).
 //
-//   What bounds it: the exponentials, one per visible (row, key): 1024 cycles of the SFU a 128 x 128 tile against 576 of the tensor cores
-//   at d = 128, 320 at 64.  us, SFU time without the share of the FMA pipe / the kernel: 64 rows over 8192 as above 15 / 30.4 (8.5 of it the launch, its start
-//   and end); 1000 rows over 5003, B = 3, 16 heads, d = 64 52 / 66; 32768 rows and keys, 16 heads on 8, d = 128 1870 / 2140, and 2500 under a
-//   lasting load, when the power limit of 1000 W holds the SMs at 1.57 GHz.
+//   What bounds it: the exponentials, one per visible (row, key), of which a quarter goes to the FMA pipe: 768 cycles of the SFU a 128 x 128 tile
+//   against 576 of the tensor cores at d = 128, 320 at 64.  us, SFU time of its three quarters / the kernel: 64 rows over 8192 as above 11 / 31 (8.5 of it the
+//   launch, its start and end); 1000 rows over 5003, B = 3, 16 heads, d = 64 38 / 68; 32768 rows and keys, 16 heads on 8, d = 128 1430 / 2140, and 1750 / 2500
+//   under a lasting load, when the power limit of 1000 W holds the SMs at 1.57 GHz.  The kernels stand at 1.4 to 1.8 of that bound (the first case, with its
+//   start and end, at 2.8): scores come from tensor memory 16 columns a wait, and the form for many units a tile spills 28 bytes (48 loaded).
 #pragma once
 
 #include <cstdint>
