@@ -589,6 +589,57 @@ int moda_attn_decode_shared(const void* q, const void* K_prefix, const void* V_p
                             int B, int T_prefix, int max_seq_len, int T_cap, int H, int H_kv, int d, int l, float scale,
                             void* O, float* LSE, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * ---- Serving: a paged sequence cache in 8 bits ----
+ *
+ * A decode step reads the whole sequence cache of its layer.  These calls keep that cache in e4m3 with one fp32 scale per row (the depth
+ * cache's format: scale = max|x| / 448, 1 for a row of zeros, code = e4m3(x / scale)), in pages, write it, read it back, and attend to all of it or to the blocks that a token
+ * selects.  A block is 64 positions; a page has page_size of them, a multiple of 64.  For every (page, block of the page, key/value head), contiguous:
+ *
+ *     pages    { key codes [64][d], value codes [d][64], key scales fp32 [64], value scales fp32 [64] }          moda_kv_page_e4m3_bytes a page
+ *     bounds   { largest int8 [d], smallest int8 [d], scale fp32, 12 bytes of nothing }                           moda_kv_page_bounds_bytes a page
+ *
+ *     block_table : device int32 [B][max_blocks_per_seq] as for moda_attn_decode_paged (a "block" there is a page).  An entry outside [0, num_pages) is no page:
+ *                   nothing is written there, its rows read as zeros, its keys have no weight.
+ *
+ * moda_kv_write_e4m3      row i of K, V (bf16 [B][T][H_kv][d]), i < n_new[b] (device int32 [B], 0 .. T; NULL: T), becomes position start[b] + i (device int32 [B]; NULL: 0)
+ *                         of sequence b.  Positions behind the table's end are dropped.  Of the blocks that it touches, other positions' codes and scales stay as they are.
+ *                         bounds (may be NULL): those of every touched block are set anew, over its positions before start[b] + n_new[b]: per feature the largest and the
+ *                         smallest dequantised key, over scale = max / 127, rounded up and down (a block with a value that is not finite: codes 0, scale inf).
+ *                         A page that is written belongs to one sequence.  One launch.
+ * moda_kv_read_e4m3       row i of K_out, V_out (bf16 [B][T][H_kv][d]) = bf16(scale * code) of position start[b] + i, for positions before seq_lens[b]; other
+ *                         rows stay as they are.  (For moda_attn_fwd_prefill over a cached prefix.)  One launch.
+ * moda_kv_select_blocks   the blocks that a token attends to.  Of the n = ceil(seq_lens[b] / 64) blocks of (b, hk), kept = min(n_blocks, n) are: the last min(n_recent, kept),
+ *                         and of the others those of the highest rating (equal ratings: the lower block).  With q8 = rint(q (127 / max|q|)), one maximum over the heads of a group,
+ *
+ *                             rating = scale * max_{h in group} sum_f max(q8[h, f] smallest[f], q8[h, f] largest[f])
+ *
+ *                         (what a key within the bounds could score at most; the sums are of whole numbers).  index : int32 [B][H_kv][n_blocks], ascending, -1 behind them.
+ *                         A block without a page is rated last, one whose bounds have scale inf first.  max_seq_len <= 64 * 32768.  One launch.
+ * moda_attn_decode_e4m3   the decode step: O, LSE, depth_kv_token, groups and scale as for moda_attn_decode_paged, with seq_lens[b] in 0 .. max_seq_len.  index (int32
+ *                         [B][H_kv][n_blocks]) NULL: all blocks; else the blocks of the first min(n_blocks, ceil(seq_lens[b] / 64)) entries of a row, an entry that is no block
+ *                         of the sequence being passed over (one that comes twice counts twice).  A token without any key has O = 0 and LSE = -inf.
+ *                         workspace : moda_decode_e4m3_workspace_bytes.  B <= 16384.  Two launches.
+ *
+ * The products take the codes as they are (exact in f16), q times a power of two, and weights rounded to f16; scales, maxima, sums and the accumulators are fp32.
+ * Sums in an order that depends on the lengths of all sequences and the device's SM count: the same call gives the same bits.
+ * Ownership, asynchrony and error codes as for the other calls.
+ */
+size_t moda_kv_page_e4m3_bytes(int page_size, int H_kv, int d);
+size_t moda_kv_page_bounds_bytes(int page_size, int H_kv, int d);
+int moda_kv_write_e4m3(void* pages, void* bounds, const void* K, const void* V, const int* block_table, const int* start, const int* n_new,
+                       int B, int T, int page_size, int num_pages, int max_blocks_per_seq, int H_kv, int d, void* stream);
+int moda_kv_read_e4m3(const void* pages, const int* block_table, const int* seq_lens, const int* start,
+                      int B, int T, int page_size, int num_pages, int max_blocks_per_seq, int H_kv, int d, void* K_out, void* V_out, void* stream);
+int moda_kv_select_blocks(const void* q, const void* bounds, const int* block_table, const int* seq_lens,
+                          int B, int max_seq_len, int page_size, int num_pages, int max_blocks_per_seq, int H, int H_kv, int d,
+                          int n_blocks, int n_recent, int* index, void* stream);
+size_t moda_decode_e4m3_workspace_bytes(int B, int H, int H_kv, int d);
+int moda_attn_decode_e4m3(const void* q, const void* pages, const int* block_table, const int* seq_lens, const int* index, int n_blocks,
+                          const void* depth_kv_token,
+                          int B, int max_seq_len, int page_size, int num_pages, int max_blocks_per_seq, int H, int H_kv, int d, int l, float scale,
+                          void* O, float* LSE, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

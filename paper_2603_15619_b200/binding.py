@@ -41,6 +41,9 @@ SYMBOLS = (
     "moda_decode_mass_workspace_bytes", "moda_attn_decode_mass",
     "moda_kv_evict",
     "moda_decode_shared_workspace_bytes", "moda_attn_decode_shared",
+    "moda_kv_page_e4m3_bytes", "moda_kv_page_bounds_bytes",
+    "moda_kv_write_e4m3", "moda_kv_read_e4m3", "moda_kv_select_blocks",
+    "moda_decode_e4m3_workspace_bytes", "moda_attn_decode_e4m3",
 )
 MODA_STATIC_SCRATCH_ROWS = 1 << 20
 MODA_BWD_STAGE_ROWTERMS, MODA_BWD_STAGE_DQ, MODA_BWD_STAGE_DKDV, MODA_BWD_ALL_STAGES = 1, 2, 4, 7
@@ -160,6 +163,18 @@ def load() -> ctypes.CDLL:
     lib.moda_decode_shared_workspace_bytes.argtypes = [ci] * 5
     lib.moda_attn_decode_shared.restype = ci
     lib.moda_attn_decode_shared.argtypes = [vp] * 7 + [ci] * 8 + [cf] + [vp] * 3 + [sz, vp]
+    lib.moda_kv_page_e4m3_bytes.restype = lib.moda_kv_page_bounds_bytes.restype = sz
+    lib.moda_kv_page_e4m3_bytes.argtypes = lib.moda_kv_page_bounds_bytes.argtypes = [ci] * 3
+    lib.moda_kv_write_e4m3.restype = ci
+    lib.moda_kv_write_e4m3.argtypes = [vp] * 7 + [ci] * 7 + [vp]
+    lib.moda_kv_read_e4m3.restype = ci
+    lib.moda_kv_read_e4m3.argtypes = [vp] * 4 + [ci] * 7 + [vp] * 3
+    lib.moda_kv_select_blocks.restype = ci
+    lib.moda_kv_select_blocks.argtypes = [vp] * 4 + [ci] * 10 + [vp] * 2
+    lib.moda_decode_e4m3_workspace_bytes.restype = sz
+    lib.moda_decode_e4m3_workspace_bytes.argtypes = [ci] * 4
+    lib.moda_attn_decode_e4m3.restype = ci
+    lib.moda_attn_decode_e4m3.argtypes = [vp] * 5 + [ci, vp] + [ci] * 9 + [cf] + [vp] * 3 + [sz, vp]
     _lib = lib
     return lib
 
@@ -170,6 +185,7 @@ _host = None
 class _NoHost:
     """Where the extension is not built for this Python and torch: every call takes the Python form."""
     attn_fwd = attn_bwd = attention = decode = key_mass = decode_mass = evict = decode_shared = staticmethod(lambda *args: None)
+    kv_write = kv_read = kv_select = decode_e4m3 = staticmethod(lambda *args: None)
 
 
 def host():
@@ -922,4 +938,133 @@ def moda_attn_decode_shared(q, K_prefix, V_prefix, K, V, seq_lens, depth_kv_toke
                                           _token(depth_kv_token, l, B, Hk, d), B, P, int(max_seq_len), T_cap, H, Hk, d, int(l), float(scale),
                                           _ptr(O), _ptr(LSE), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
            "moda_attn_decode_shared")
+    return O, LSE
+
+
+# ---- the paged sequence cache in 8 bits ----
+def moda_kv_page_e4m3_bytes(page_size, H_kv, d) -> int:
+    return int(load().moda_kv_page_e4m3_bytes(page_size, H_kv, d))
+
+
+def moda_kv_page_bounds_bytes(page_size, H_kv, d) -> int:
+    return int(load().moda_kv_page_bounds_bytes(page_size, H_kv, d))
+
+
+def alloc_kv_pages_e4m3(num_pages, page_size, H_kv, d, device="cuda", stream=None) -> torch.Tensor:
+    """Caller-side helper: pages [num_pages, page_size / 64, H_kv, 128 d + 512] uint8 (uninitialised)."""
+    if num_pages < 1 or moda_kv_page_e4m3_bytes(page_size, H_kv, d) == 0:
+        raise ValueError("bad shape of pages")
+    return _new((num_pages, page_size // 64, H_kv, 128 * d + 512), torch.uint8, device, stream)
+
+
+def alloc_kv_bounds(num_pages, page_size, H_kv, d, device="cuda", stream=None) -> torch.Tensor:
+    """Caller-side helper: the pages' bounds [num_pages, page_size / 64, H_kv, 2 d + 16] uint8 (uninitialised)."""
+    if num_pages < 1 or moda_kv_page_bounds_bytes(page_size, H_kv, d) == 0:
+        raise ValueError("bad shape of pages")
+    return _new((num_pages, page_size // 64, H_kv, 2 * d + 16), torch.uint8, device, stream)
+
+
+def _paged(pages, block_table, bounds=False):
+    """page_size, num_pages, H_kv, d of pages (or of their bounds); B and pages of a sequence of the table."""
+    fixed, per = (16, 2) if bounds else (512, 128)
+    name = "bounds" if bounds else "pages"
+    if pages.dtype != torch.uint8 or pages.dim() != 4 or (pages.shape[3] - fixed) % per != 0:
+        raise ValueError(f"{name} must be a uint8 [num_pages, page_size / 64, H_kv, {per} d + {fixed}] tensor")
+    if block_table.dtype != torch.int32 or block_table.dim() != 2:
+        raise ValueError("block_table must be an int32 [B, max_blocks] tensor")
+    num_pages, sub, Hk, n = pages.shape
+    return 64 * sub, num_pages, Hk, (n - fixed) // per, *block_table.shape
+
+
+def _bounds_for(bounds, pages, d):
+    if bounds is not None and (bounds.dtype != torch.uint8 or tuple(bounds.shape) != (*pages.shape[:3], 2 * d + 16)):
+        raise ValueError("bounds must be a uint8 [num_pages, page_size / 64, H_kv, 2 d + 16] tensor matching pages")
+    return _ptr(bounds)
+
+
+def moda_kv_write_e4m3(pages, K, V, block_table, start=None, n_new=None, bounds=None, stream=None):
+    """Quantises rows K, V [B,T,H_kv,d] into the pages of their sequences: row i < n_new[b] (int32 [B]; None: T) is position start[b] + i (int32 [B]; None: 0).
+    ``bounds``: those of every touched block are set anew, over its positions before start[b] + n_new[b]."""
+    if stream is None and host().kv_write(pages, K, V, block_table, start, n_new, bounds) is not None:
+        return
+    page_size, num_pages, Hk, d, B, most = _paged(pages, block_table)
+    Bk, T, Hn, dk = _bthd(K, "K")
+    if (Bk, Hn, dk) != (B, Hk, d) or _bthd(V, "V") != (B, T, Hk, d):
+        raise ValueError("K and V must be bf16 [B, T, H_kv, d] tensors matching the pages and the table")
+    for t, name in ((start, "start"), (n_new, "n_new")):
+        if t is not None:
+            _int32(t, name, (B,))
+    _check(load().moda_kv_write_e4m3(_ptr(pages), _bounds_for(bounds, pages, d), _ptr(K), _ptr(V), _ptr(block_table), _ptr(start), _ptr(n_new),
+                                     B, T, page_size, num_pages, most, Hk, d, _stream(stream)), "moda_kv_write_e4m3")
+
+
+def moda_kv_read_e4m3(pages, block_table, seq_lens, T, start=None, K_out=None, V_out=None, stream=None):
+    """Rows of the pages as bf16 again: K_out, V_out [B,T,H_kv,d], row i = position start[b] + i (int32 [B]; None: 0) where that is below seq_lens[b]
+    (int32 [B]); other rows stay as they are (zeros where the outputs are allocated here)."""
+    if stream is None and (out := host().kv_read(pages, block_table, seq_lens, T, start, K_out, V_out)) is not None:
+        return out
+    page_size, num_pages, Hk, d, B, most = _paged(pages, block_table)
+    T = int(T)
+    _int32(seq_lens, "seq_lens", (B,))
+    if start is not None:
+        _int32(start, "start", (B,))
+    shape = (B, max(T, 1), Hk, d)                                           # what the C call refuses is allocated all the same
+    outs = []
+    for t, name in ((K_out, "K_out"), (V_out, "V_out")):
+        if t is None:
+            t = _new(shape, torch.bfloat16, pages.device, stream)
+            with torch.cuda.stream(stream):
+                t.zero_()
+        elif _bthd(t, name) != shape:
+            raise ValueError("K_out and V_out must be bf16 [B, T, H_kv, d] tensors matching the pages and the table")
+        outs.append(t)
+    _check(load().moda_kv_read_e4m3(_ptr(pages), _ptr(block_table), _ptr(seq_lens), _ptr(start), B, T, page_size, num_pages, most, Hk, d,
+                                    _ptr(outs[0]), _ptr(outs[1]), _stream(stream)), "moda_kv_read_e4m3")
+    return tuple(outs)
+
+
+def moda_kv_select_blocks(q, bounds, block_table, seq_lens, max_seq_len, n_blocks, n_recent=1, index=None, stream=None):
+    """The blocks of 64 positions that a token's queries q [B,H,d] attend to: per (sequence, key/value head) the last ``n_recent`` and those that the bounds of their
+    keys rate highest, ``n_blocks`` in all: index int32 [B,H_kv,n_blocks], ascending, -1 behind the last one."""
+    if stream is None and (out := host().kv_select(q, bounds, block_table, seq_lens, max_seq_len, n_blocks, n_recent, index)) is not None:
+        return out
+    page_size, num_pages, Hk, d, B, most = _paged(bounds, block_table, bounds=True)
+    if q.dtype != torch.bfloat16 or q.dim() != 3 or (q.shape[0], q.shape[2]) != (B, d):
+        raise ValueError("q must be a bf16 [B, H, d] tensor matching the bounds and the table")
+    _int32(seq_lens, "seq_lens", (B,))
+    n_blocks = int(n_blocks)
+    shape = (B, Hk, max(n_blocks, 1))
+    index = _new(shape, torch.int32, q.device, stream) if index is None else _int32(index, "index", shape)
+    _check(load().moda_kv_select_blocks(_ptr(q), _ptr(bounds), _ptr(block_table), _ptr(seq_lens), B, int(max_seq_len), page_size, num_pages, most,
+                                        q.shape[1], Hk, d, n_blocks, int(n_recent), _ptr(index), _stream(stream)), "moda_kv_select_blocks")
+    return index
+
+
+def moda_decode_e4m3_workspace_bytes(B, H, H_kv, d) -> int:
+    return int(load().moda_decode_e4m3_workspace_bytes(B, H, H_kv, d))
+
+
+def moda_attn_decode_e4m3(q, pages, block_table, seq_lens, depth_kv_token, max_seq_len, l, scale, index=None, O=None, LSE=None, workspace=None,
+                          stream=None):
+    """Decode step over pages in 8 bits: q [B,H,d] attends, under one softmax, to the first seq_lens[b] (int32 [B], 0 .. max_seq_len) positions of its sequence, or
+    with ``index`` int32 [B,H_kv,n] to those in the blocks that it names, and to its depth pairs [l,B,H_kv,2,d].  Returns O [B,H,d] bf16 and LSE [B,H] fp32."""
+    if stream is None and (out := host().decode_e4m3(q, pages, block_table, seq_lens, depth_kv_token, max_seq_len, l, scale, index, O, LSE, workspace)) is not None:
+        return out
+    page_size, num_pages, Hk, d, B, most = _paged(pages, block_table)
+    if q.dtype != torch.bfloat16 or q.dim() != 3 or (q.shape[0], q.shape[2]) != (B, d):
+        raise ValueError("q must be a bf16 [B, H, d] tensor matching the pages and the table")
+    H = q.shape[1]
+    _int32(seq_lens, "seq_lens", (B,))
+    if index is not None and (index.dtype != torch.int32 or index.dim() != 3 or tuple(index.shape[:2]) != (B, Hk)):
+        raise ValueError("index must be an int32 [B, H_kv, n] tensor")
+    if l > 0 and depth_kv_token is None:
+        raise ValueError("depth_kv_token must be a bf16 [l, B, H_kv, 2, d] tensor")
+    O = _new_like(q, stream) if O is None else _given(O, B * H * d, torch.bfloat16)
+    LSE = _new((B, H), torch.float32, q.device, stream) if LSE is None else _given(LSE, B * H, torch.float32)
+    if workspace is None:
+        workspace = _new((max(moda_decode_e4m3_workspace_bytes(B, H, Hk, d), 16),), torch.uint8, q.device, stream)
+    _check(load().moda_attn_decode_e4m3(_ptr(q), _ptr(pages), _ptr(block_table), _ptr(seq_lens), _ptr(index), 0 if index is None else index.shape[2],
+                                        _token(depth_kv_token, l, B, Hk, d), B, int(max_seq_len), page_size, num_pages, most, H, Hk, d, int(l),
+                                        float(scale), _ptr(O), _ptr(LSE), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                        _stream(stream)), "moda_attn_decode_e4m3")
     return O, LSE

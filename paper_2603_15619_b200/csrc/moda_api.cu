@@ -16,6 +16,8 @@
 #include "moda_fwd_wide.cuh"
 #include "moda_fwd_wide128.cuh"
 #include "moda_evict.cuh"
+#include "moda_pages.cuh"
+#include "moda_decode_pages.cuh"
 #include "moda_keymass.cuh"
 #include "moda_mass.cuh"
 #include "moda_kvproj.cuh"
@@ -1412,3 +1414,4 @@ extern "C" int moda_attn_bwd_static_scratch(const void* Q, const void* K, const 
 }
 
 #include "moda_api_serving.cuh"
+#include "moda_api_pages.cuh"

@@ -39,7 +39,8 @@ using at::Tensor;
     X(moda_bwd_workspace_bytes_gqa) X(moda_depth_cache_bytes) X(moda_attn_decode) X(moda_attn_decode_varlen)            \
     X(moda_attn_decode_paged) X(moda_decode_workspace_bytes)                                                            \
     X(moda_attn_key_mass) X(moda_key_mass_workspace_bytes) X(moda_attn_decode_mass) X(moda_decode_mass_workspace_bytes) \
-    X(moda_kv_evict) X(moda_attn_decode_shared) X(moda_decode_shared_workspace_bytes)
+    X(moda_kv_evict) X(moda_attn_decode_shared) X(moda_decode_shared_workspace_bytes)                                   \
+    X(moda_kv_write_e4m3) X(moda_kv_read_e4m3) X(moda_kv_select_blocks) X(moda_attn_decode_e4m3) X(moda_decode_e4m3_workspace_bytes)
 struct Library {
 #define X(name) decltype(&::name) name = nullptr;
     MODA_HOST_CALLS(X)
@@ -502,6 +503,110 @@ PyObject* decode_shared(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- the paged sequence cache in 8 bits ---------------------------------------------------------------------------------
+// Pages, or their bounds (`per` d + `fixed` bytes a block), with the block table of a batch.
+struct Paged { int page, pages, Hk, d, B, most; const Tensor *data, *table; };
+bool paged_args(PyObject* data, PyObject* table, int per, int fixed, Paged& s) {
+    s.data = dense(data, at::kByte, 4);
+    s.table = dense(table, at::kInt, 2);
+    if (s.data == nullptr || s.table == nullptr || !small(*s.data) || !small(*s.table) || s.data->size(1) > INT_MAX / 64) return false;
+    const int64_t n = s.data->size(3) - fixed;
+    if (n <= 0 || n % per != 0) return false;
+    s.pages = int(s.data->size(0)), s.page = 64 * int(s.data->size(1)), s.Hk = int(s.data->size(2)), s.d = int(n / per);
+    s.B = int(s.table->size(0)), s.most = int(s.table->size(1));
+    return true;
+}
+
+// kv_write(pages, K, V, table, start or None, n_new or None, bounds or None) -> True
+PyObject* kv_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Paged s;
+    const Tensor *K = nullptr, *V = nullptr, *start, *count, *bounds = nullptr;
+    if (n != 7 || !plain_thread() || !paged_args(a[0], a[3], 128, 512, s)) return none();
+    if ((K = dense(a[1], at::kBFloat16, 4)) == nullptr || (V = dense(a[2], at::kBFloat16, 4)) == nullptr || !small(*K) || V->sizes() != K->sizes() ||
+        K->size(0) != s.B || K->size(2) != s.Hk || K->size(3) != s.d || !lens_arg(a[4], s.B, start) || !lens_arg(a[5], s.B, count)) return none();
+    if (a[6] != Py_None && ((bounds = dense(a[6], at::kByte, 4)) == nullptr || !shape_is(*bounds, {s.pages, s.page / 64, s.Hk, 2 * s.d + 16}))) return none();
+    {
+        NoGil nogil;
+        const int rc = lib.moda_kv_write_e4m3(s.data->data_ptr(), ptr(bounds), K->data_ptr(), V->data_ptr(), i32(s.table), i32(start), i32(count), s.B, int(K->size(1)),
+                                              s.page, s.pages, s.most, s.Hk, s.d, stream());
+        if (rc != 0) fail(rc, "moda_kv_write_e4m3");
+    }
+    Py_RETURN_TRUE;
+    END_HANDLE_TH_ERRORS
+}
+
+// kv_read(pages, table, seq_lens, T, start or None, K_out, V_out) -> (K_out, V_out), both given
+PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Paged s;
+    int T;
+    const Tensor *lens, *start, *g[2];
+    if (n != 7 || !plain_thread() || !paged_args(a[0], a[1], 128, 512, s) || a[2] == Py_None || !lens_arg(a[2], s.B, lens) || !int_arg(a[3], T) ||
+        !lens_arg(a[4], s.B, start)) return none();
+    for (int i = 0; i < 2; ++i)
+        if ((g[i] = dense(a[5 + i], at::kBFloat16, 4)) == nullptr || !shape_is(*g[i], {s.B, T, s.Hk, s.d})) return none();
+    {
+        NoGil nogil;
+        const int rc = lib.moda_kv_read_e4m3(s.data->data_ptr(), i32(s.table), i32(lens), i32(start), s.B, T, s.page, s.pages, s.most, s.Hk, s.d, g[0]->data_ptr(),
+                                             g[1]->data_ptr(), stream());
+        if (rc != 0) fail(rc, "moda_kv_read_e4m3");
+    }
+    return Py_BuildValue("OO", a[5], a[6]);
+    END_HANDLE_TH_ERRORS
+}
+
+// kv_select(q, bounds, table, seq_lens, max_seq_len, n_blocks, n_recent, index) -> index
+PyObject* kv_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Paged s;
+    int T, keep, recent;
+    const Tensor *lens, *index, *q;
+    if (n != 8 || !plain_thread() || !paged_args(a[1], a[2], 2, 16, s) || a[3] == Py_None || !lens_arg(a[3], s.B, lens) || !int_arg(a[4], T) ||
+        !int_arg(a[5], keep) || !int_arg(a[6], recent) || keep < 1) return none();
+    if ((q = dense(a[0], at::kBFloat16, 3)) == nullptr || !small(*q) || q->size(0) != s.B || q->size(2) != s.d || !optional_dense(a[7], index) ||
+        !tensor_of(index, at::kInt, {s.B, s.Hk, keep})) return none();
+    Tensor t = index != nullptr ? *index : Tensor();
+    {
+        NoGil nogil;
+        if (!t.defined()) t = fresh({s.B, s.Hk, keep}, at::kInt, *q);
+        const int rc = lib.moda_kv_select_blocks(q->data_ptr(), s.data->data_ptr(), i32(s.table), i32(lens), s.B, T, s.page, s.pages, s.most, int(q->size(1)), s.Hk, s.d,
+                                                 keep, recent, static_cast<int*>(t.data_ptr()), stream());
+        if (rc != 0) fail(rc, "moda_kv_select_blocks");
+    }
+    return out(a[7], t);
+    END_HANDLE_TH_ERRORS
+}
+
+// decode_e4m3(q, pages, table, seq_lens, depth, max_seq_len, l, scale, index or None, O, LSE, workspace) -> (O, LSE)
+PyObject* decode_e4m3(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Paged s;
+    int T, l;
+    float scale;
+    const Tensor *q, *lens, *depth = nullptr, *index = nullptr, *O, *LSE, *ws;
+    if (n != 12 || !plain_thread() || !paged_args(a[1], a[2], 128, 512, s) || a[3] == Py_None || !lens_arg(a[3], s.B, lens) || !int_arg(a[5], T) ||
+        !int_arg(a[6], l) || l < 0 || !float_arg(a[7], scale)) return none();
+    if ((q = dense(a[0], at::kBFloat16, 3)) == nullptr || !small(*q) || q->size(0) != s.B || q->size(2) != s.d) return none();
+    if (l > 0 && ((depth = dense(a[4], at::kBFloat16, 5)) == nullptr || !shape_is(*depth, {l, s.B, s.Hk, 2, s.d}))) return none();
+    if (a[8] != Py_None && ((index = dense(a[8], at::kInt, 3)) == nullptr || !small(*index) || index->size(0) != s.B || index->size(1) != s.Hk)) return none();
+    const int H = int(q->size(1));
+    if (!optional_dense(a[9], O) || !optional_dense(a[10], LSE) || !optional_dense(a[11], ws) || !holds(O, at::kBFloat16, q->numel()) ||
+        !holds(LSE, at::kFloat, int64_t(s.B) * H)) return none();
+    Tensor o = O != nullptr ? *O : Tensor(), lse = LSE != nullptr ? *LSE : Tensor();
+    {
+        NoGil nogil;
+        if (!o.defined()) o = like(*q);
+        if (!lse.defined()) lse = fresh({s.B, H}, at::kFloat, *q);
+        const Tensor w = scratch(ws, ws != nullptr ? 0 : lib.moda_decode_e4m3_workspace_bytes(s.B, H, s.Hk, s.d), *q);
+        const int rc = lib.moda_attn_decode_e4m3(q->data_ptr(), s.data->data_ptr(), i32(s.table), i32(lens), i32(index), index != nullptr ? int(index->size(2)) : 0, ptr(depth),
+                                                 s.B, T, s.page, s.pages, s.most, H, s.Hk, s.d, l, scale, o.data_ptr(), f32(&lse), w.data_ptr(), bytes_of(w), stream());
+        if (rc != 0) fail(rc, "moda_attn_decode_e4m3");
+    }
+    return Py_BuildValue("NN", out(a[9], o), out(a[10], lse));
+    END_HANDLE_TH_ERRORS
+}
+
 // ---- module -----------------------------------------------------------------------------------------------------------
 // bind(handle of libmoda_b200.so, check, DeviceContext): must come first
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -526,7 +631,9 @@ PyMethodDef methods[] = {
     {"attn_bwd", FAST(attn_bwd), METH_FASTCALL, nullptr}, {"attention", FAST(attention), METH_FASTCALL, nullptr},
     {"decode", FAST(decode), METH_FASTCALL, nullptr},     {"key_mass", FAST(key_mass), METH_FASTCALL, nullptr},
     {"decode_mass", FAST(decode_mass), METH_FASTCALL, nullptr}, {"evict", FAST(evict), METH_FASTCALL, nullptr},
-    {"decode_shared", FAST(decode_shared), METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr},
+    {"decode_shared", FAST(decode_shared), METH_FASTCALL, nullptr}, {"kv_write", FAST(kv_write), METH_FASTCALL, nullptr},
+    {"kv_read", FAST(kv_read), METH_FASTCALL, nullptr},   {"kv_select", FAST(kv_select), METH_FASTCALL, nullptr},
+    {"decode_e4m3", FAST(decode_e4m3), METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

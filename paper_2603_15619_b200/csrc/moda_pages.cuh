@@ -1,0 +1,550 @@
+// The paged sequence cache in 8 bits: its layout, the kernels that write and read it, and the selection of the blocks that a token attends to.
+//
+// A block is 64 positions; a page has page_size / 64 of them.  Of every (block, key/value head):
+//
+//   pages   [page][block of the page][Hk] { key codes [64][d], value codes [d][64], key scales [64] fp32, value scales [64] fp32 }
+//   bounds  [page][block of the page][Hk] { largest [d] int8, smallest [d] int8, scale fp32, 12 bytes that nothing reads }
+//
+// Codes are e4m3 by the depth cache's rule (moda_cache.cuh): scale = max|x| / 448 of a row, 1 for a row of zeros, code = e4m3(x / scale).  Keys lie row by
+// row and values feature by feature, so that a lane of the decode step (moda_decode_pages.cuh) has its operands of a matrix product in 16 adjacent bytes
+// of either and nothing is turned on the way.  The bounds of a block are those of its first keys, up to the sequence's end at the last write: largest and
+// smallest dequantised value of each feature, over scale = max / 127, rounded outwards.  A block with a key that is not finite has codes 0 and scale inf.
+#pragma once
+
+#include <cstdint>
+#include <cuda_runtime.h>
+
+#include "launch_rules.h"
+#include "moda_cache.cuh"
+#include "moda_evict.cuh"
+#include "sm100_ptx.cuh"
+
+namespace moda {
+
+constexpr int kPageBlock = 64;
+__host__ __device__ constexpr size_t page_block_bytes(int d) { return size_t(2 * kPageBlock) * d + 8 * kPageBlock; }
+__host__ __device__ constexpr size_t page_bounds_bytes(int d) { return 2 * size_t(d) + 16; }
+
+// What all calls over the pages have in common.
+struct PagesParams {
+    const int* table;             // [B][max_blocks]: page of every page_size positions of a sequence
+    int B, Hk, sub, num_pages, max_blocks;   // sub: blocks of a page
+    // Number of block `blk` of a sequence, over all pages; -1 where the table has no page for it.
+    __device__ __forceinline__ int tile(int b, int blk) const {
+        const int at = blk / sub;
+        const int page = at < max_blocks ? table[size_t(b) * max_blocks + at] : -1;
+        return unsigned(page) < unsigned(num_pages) ? page * sub + (blk - at * sub) : -1;
+    }
+};
+
+// Codes of 4 bytes as two pairs of f16 (exact).
+__device__ __forceinline__ void e4m3x4_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    asm("{\n"
+        ".reg .b16 a, b;\n"
+        "mov.b32 {a, b}, %2;\n"
+        "cvt.rn.f16x2.e4m3x2 %0, a;\n"
+        "cvt.rn.f16x2.e4m3x2 %1, b;\n"
+        "}\n"
+        : "=r"(lo), "=r"(hi) : "r"(w));
+}
+__device__ __forceinline__ float2 f16x2_to_f32(uint32_t h) {
+    float2 f;
+    asm("{\n"
+        ".reg .b16 a, b;\n"
+        "mov.b32 {a, b}, %2;\n"
+        "cvt.f32.f16 %0, a;\n"
+        "cvt.f32.f16 %1, b;\n"
+        "}\n"
+        : "=f"(f.x), "=f"(f.y) : "r"(h));
+    return f;
+}
+// Four words of four bytes, turned: byte j of a word i becomes byte i of word j.
+__device__ __forceinline__ void turn4x4(uint32_t& a, uint32_t& b, uint32_t& c, uint32_t& d) {
+    const uint32_t ab0 = __byte_perm(a, b, 0x5140), ab1 = __byte_perm(a, b, 0x7362), cd0 = __byte_perm(c, d, 0x5140), cd1 = __byte_perm(c, d, 0x7362);
+    a = __byte_perm(ab0, cd0, 0x5410);
+    b = __byte_perm(ab0, cd0, 0x7632);
+    c = __byte_perm(ab1, cd1, 0x5410);
+    d = __byte_perm(ab1, cd1, 0x7632);
+}
+
+// 16 features of a row that `lanes` adjacent lanes hold: their codes and the row's scale.
+template <int LANES>
+__device__ __forceinline__ uint4 quantise_row16(const uint4& lo, const uint4& hi, float& scale) {
+    const uint32_t w8[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    float x[16], am = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        x[2 * k] = __uint_as_float(w8[k] << 16);
+        x[2 * k + 1] = __uint_as_float(w8[k] & 0xffff0000u);
+        am = fmaxf(am, fmaxf(fabsf(x[2 * k]), fabsf(x[2 * k + 1])));
+    }
+#pragma unroll
+    for (int off = 1; off < LANES; off <<= 1) am = fmaxf(am, __shfl_xor_sync(0xffffffffu, am, off));
+    scale = am > 0.f ? __fdiv_rn(am, 448.f) : 1.f;
+    const RowDivider dv = make_row_divider(scale);
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        uint16_t a, b;
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(a) : "f"(div_rn(x[4 * k + 1], dv)), "f"(div_rn(x[4 * k], dv)));
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(b) : "f"(div_rn(x[4 * k + 3], dv)), "f"(div_rn(x[4 * k + 2], dv)));
+        w[k] = uint32_t(a) | (uint32_t(b) << 16);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+struct PagesRowsParams : PagesParams {
+    uint8_t* pages;
+    uint8_t* bounds;              // may be null (and is for a read)
+    const uint4* K;               // [B][T][Hk][d] bf16: rows that are written, or read into
+    const uint4* V;
+    const int* start;             // [B] position of a sequence's row 0, or null: 0
+    const int* count;             // write: [B] rows that a sequence brings (0 .. T), or null: T.  read: [B] lengths of the sequences
+    int T;
+};
+
+// Rows of block `blk` (blockIdx.x blocks behind the first one touched) that a call has to do with: [r0, r1), row r at position 64 blk + r, which is
+// row `base` + r of the tensor.  False: none.
+struct PagesRows { int blk, r0, r1, base; };
+template <bool READ>
+__device__ __forceinline__ bool pages_rows(const PagesRowsParams& p, int b, PagesRows& w) {
+    const long long cap = (long long)p.max_blocks * p.sub * kPageBlock;
+    const long long start = min((long long)(p.start ? max(p.start[b], 0) : 0), cap);
+    long long end = start + p.T;
+    if (READ) end = min(end, (long long)max(p.count[b], 0));
+    else if (p.count) end = start + min(max(p.count[b], 0), p.T);
+    end = min(end, cap);
+    const long long blk = start / kPageBlock + blockIdx.x, p0 = blk * kPageBlock;
+    w.blk = int(blk);
+    w.r0 = int(max(start - p0, 0ll));
+    w.r1 = int(min(end - p0, (long long)kPageBlock));
+    w.base = int(p0 - start);
+    return w.r0 < w.r1;
+}
+
+constexpr int kPagesThreads = 256;
+
+// grid (blocks that T rows can touch, Hk, B): a CTA quantises the rows of one block of one head, and where `bounds` is given reads what the block's earlier
+// keys left and writes the bounds anew.  It is the only one that writes the block (a page belongs to one sequence).
+template <int D>
+__global__ void __launch_bounds__(kPagesThreads)
+pages_write_kernel(const PagesRowsParams p) {
+    constexpr int CH = D / 8, LPR = D / 16, RPP = kPagesThreads / LPR, PASSES = kPageBlock / RPP;   // lanes of a row, rows at a time
+    constexpr int KW = D / 4 + 4;                                    // words of a row of codes in shared memory, padded by 16 bytes
+    constexpr int SETS = kPagesThreads / (D / 4);                    // threads that share four features of the bounds
+    __shared__ __align__(16) uint32_t s_k[kPageBlock][KW], s_v[kPageBlock][KW];
+    __shared__ float s_scale[kPageBlock], s_hi[SETS][D], s_lo[SETS][D], s_most[kPagesThreads / 32];
+    __shared__ int s_bad;
+    const int b = blockIdx.z, hk = blockIdx.y, tid = threadIdx.x;
+    PagesRows w;
+    if (!pages_rows<false>(p, b, w)) return;
+    const int tile = p.tile(b, w.blk);
+    if (tile < 0) return;
+    uint8_t* rec = p.pages + (size_t(tile) * p.Hk + hk) * page_block_bytes(D);
+    float* scales = reinterpret_cast<float*>(rec + 2 * kPageBlock * D);
+    const int c = tid % LPR, row0 = tid / LPR;                       // 16 features; first row
+    if (tid == 0) s_bad = 0;
+    // the block's earlier keys
+    if (p.bounds) {
+        for (int e = tid; e < w.r0 * LPR; e += kPagesThreads)
+            *reinterpret_cast<uint4*>(&s_k[e / LPR][4 * (e % LPR)]) = *reinterpret_cast<const uint4*>(rec + size_t(e) * 16);
+        if (tid < w.r0) s_scale[tid] = scales[tid];
+    }
+    uint4 in[PASSES][2][2];
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+        const int row = row0 + i * RPP;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+            in[i][kv][0] = in[i][kv][1] = make_uint4(0u, 0u, 0u, 0u);
+            if (row >= w.r0 && row < w.r1) {
+                const uint4* src = (kv ? p.V : p.K) + ((size_t(b) * p.T + (w.base + row)) * p.Hk + hk) * CH + 2 * c;
+                in[i][kv][0] = src[0];
+                in[i][kv][1] = src[1];
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+        const int row = row0 + i * RPP;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+            float scale;
+            const uint4 codes = quantise_row16<LPR>(in[i][kv][0], in[i][kv][1], scale);
+            if (row >= w.r0 && row < w.r1) {
+                *reinterpret_cast<uint4*>(kv ? &s_v[row][4 * c] : &s_k[row][4 * c]) = codes;
+                if (kv == 0) *reinterpret_cast<uint4*>(rec + size_t(row) * D + 16 * c) = codes;
+                if (c == 0) {
+                    scales[kv * kPageBlock + row] = scale;
+                    if (kv == 0) s_scale[row] = scale;
+                }
+            }
+        }
+    }
+    __syncthreads();
+    // values feature by feature: a thread turns 4 features of 16 positions
+    for (int e = tid; e < D; e += kPagesThreads) {
+        const int k0 = 16 * (e & 3), f = e >> 2;                     // first position; features 4 f .. 4 f + 3
+        if (k0 + 16 <= w.r0 || k0 >= w.r1) continue;
+        uint32_t t[4][4];                                            // [feature][positions 4 i ..]
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) t[j][i] = s_v[k0 + 4 * i + j][f];
+            turn4x4(t[0][i], t[1][i], t[2][i], t[3][i]);
+        }
+        uint8_t* to = rec + kPageBlock * D + size_t(4 * f) * kPageBlock + k0;
+        if (k0 >= w.r0 && k0 + 16 <= w.r1) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4*>(to + j * kPageBlock) = make_uint4(t[j][0], t[j][1], t[j][2], t[j][3]);
+        } else {                                                     // beside positions that stay as they are
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                if (k0 + k >= w.r0 && k0 + k < w.r1) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) to[j * kPageBlock + k] = uint8_t(t[j][k >> 2] >> (8 * (k & 3)));
+                }
+        }
+    }
+    if (!p.bounds) return;
+    const int f = tid % (D / 4), set = tid / (D / 4);
+    float hi[4], lo[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { hi[j] = -INFINITY; lo[j] = INFINITY; }
+    bool bad = false;
+    for (int row = set; row < w.r1; row += SETS) {
+        uint32_t a, e;
+        e4m3x4_to_f16(s_k[row][f], a, e);
+        const float2 x = f16x2_to_f32(a), y = f16x2_to_f32(e);
+        const float v[4] = {x.x * s_scale[row], x.y * s_scale[row], y.x * s_scale[row], y.y * s_scale[row]};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            bad |= !(fabsf(v[j]) < INFINITY);
+            hi[j] = fmaxf(hi[j], v[j]);
+            lo[j] = fminf(lo[j], v[j]);
+        }
+    }
+    if (bad) s_bad = 1;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { s_hi[set][4 * f + j] = hi[j]; s_lo[set][4 * f + j] = lo[j]; }
+    __syncthreads();
+    float h = -INFINITY, l = INFINITY, most = 0.f;
+    if (tid < D) {
+#pragma unroll
+        for (int s = 0; s < SETS; ++s) { h = fmaxf(h, s_hi[s][tid]); l = fminf(l, s_lo[s][tid]); }
+        most = fmaxf(fabsf(h), fabsf(l));
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
+    if (tid % 32 == 0) s_most[tid / 32] = most;
+    __syncthreads();
+    if (tid < D) {
+        most = s_most[0];
+#pragma unroll
+        for (int i = 1; i < D / 32; ++i) most = fmaxf(most, s_most[i]);
+        const float scale = s_bad ? INFINITY : __fdiv_rn(most, 127.f);
+        uint8_t* to = p.bounds + (size_t(tile) * p.Hk + hk) * page_bounds_bytes(D);
+        const bool flat = s_bad || !(scale > 0.f);
+        to[tid] = uint8_t(flat ? 0 : int(fminf(ceilf(__fdiv_rn(h, scale)), 127.f)));
+        to[D + tid] = uint8_t(flat ? 0 : int(fmaxf(floorf(__fdiv_rn(l, scale)), -127.f)));
+        if (tid == 0) *reinterpret_cast<float*>(to + 2 * D) = scale;
+    }
+}
+
+// grid (blocks that T rows can touch, Hk, B): rows of one block of one head, as bf16(scale * code).
+template <int D>
+__global__ void __launch_bounds__(kPagesThreads)
+pages_read_kernel(const PagesRowsParams p) {
+    constexpr int CH = D / 8, LPR = D / 16, RPP = kPagesThreads / LPR, PASSES = kPageBlock / RPP;
+    constexpr int KW = D / 4 + 4;
+    __shared__ __align__(16) uint32_t s_v[kPageBlock][KW];
+    const int b = blockIdx.z, hk = blockIdx.y, tid = threadIdx.x;
+    PagesRows w;
+    if (!pages_rows<true>(p, b, w)) return;
+    const int tile = p.tile(b, w.blk);
+    const uint8_t* rec = p.pages + (size_t(max(tile, 0)) * p.Hk + hk) * page_block_bytes(D);
+    const float* scales = reinterpret_cast<const float*>(rec + 2 * kPageBlock * D);
+    const int c = tid % LPR, row0 = tid / LPR;
+    uint4 codes[PASSES];
+    float scale[PASSES][2];
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+        const int row = row0 + i * RPP;
+        codes[i] = make_uint4(0u, 0u, 0u, 0u);
+        scale[i][0] = scale[i][1] = 0.f;
+        if (tile >= 0 && row >= w.r0 && row < w.r1) {
+            codes[i] = *reinterpret_cast<const uint4*>(rec + size_t(row) * D + 16 * c);
+            scale[i][0] = scales[row];
+            scale[i][1] = scales[kPageBlock + row];
+        }
+    }
+    for (int e = tid; e < D; e += kPagesThreads) {
+        const int k0 = 16 * (e & 3), f = e >> 2;
+        uint32_t t[4][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint4 x = make_uint4(0u, 0u, 0u, 0u);
+            if (tile >= 0) x = *reinterpret_cast<const uint4*>(rec + kPageBlock * D + size_t(4 * f + j) * kPageBlock + k0);
+            t[j][0] = x.x; t[j][1] = x.y; t[j][2] = x.z; t[j][3] = x.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            turn4x4(t[0][i], t[1][i], t[2][i], t[3][i]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s_v[k0 + 4 * i + j][f] = t[j][i];
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+        const int row = row0 + i * RPP;
+        if (row < w.r0 || row >= w.r1) continue;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+            const uint4 x = kv ? *reinterpret_cast<const uint4*>(&s_v[row][4 * c]) : codes[i];
+            const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+            uint32_t out[8];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                uint32_t a, e;
+                e4m3x4_to_f16(in[k], a, e);
+                const float2 u = f16x2_to_f32(a), v = f16x2_to_f32(e);
+                out[2 * k] = pack_bf16x2(u.x * scale[i][kv], u.y * scale[i][kv]);
+                out[2 * k + 1] = pack_bf16x2(v.x * scale[i][kv], v.y * scale[i][kv]);
+            }
+            uint4* to = const_cast<uint4*>(kv ? p.V : p.K) + ((size_t(b) * p.T + (w.base + row)) * p.Hk + hk) * CH + 2 * c;
+            to[0] = make_uint4(out[0], out[1], out[2], out[3]);
+            to[1] = make_uint4(out[4], out[5], out[6], out[7]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Selection.  Of the n = ceil(len / 64) blocks of (sequence, key/value head) the kept = min(n_keep, n) stay: the last min(n_recent, kept), and of the
+// others those of the highest rating (equal ratings: the lower block).  With q8 = rint(q * (127 / max|q|)), one maximum for the heads of a group,
+//
+//     rating = scale * max over the heads of  sum_f max(q8_f smallest_f, q8_f largest_f)
+//
+// which is what a key within the block's bounds could score at most.  The sums are of whole numbers (dp4a), so that a rating has one value whatever the order, and
+// ties are ties.
+//
+// A cluster of `ranks` CTAs per (sequence, head), each rating a share of the blocks; all ratings go to the first one's shared memory, which finds the
+// lowest that stays digit by digit (8 bits, from the highest bit in which any two differ) and writes the blocks in their order.
+// ---------------------------------------------------------------------------------------------------------------------
+struct PagesSelectParams : PagesParams {
+    const __nv_bfloat16* q;       // [B][Hk * G][d]
+    const uint8_t* bounds;
+    const int* lens;              // [B]
+    int* index;                   // [B][Hk][n_keep]
+    int G, max_len, n_keep, n_recent;
+};
+
+constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
+constexpr int kSelectSets = 4;                                       // blocks that a group of lanes has on its way
+constexpr int kSelectMostGroup = 32;
+
+__host__ __device__ inline int pages_blocks(int len) { return len / kPageBlock + (len % kPageBlock != 0); }
+inline int select_smem(int G, int d, int blocks) { return 2 * G * d + 4 * blocks; }
+
+__device__ __forceinline__ void st_cluster_u32(uint32_t addr, uint32_t v) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
+template <int D>
+__global__ void __launch_bounds__(kSelectThreads)
+pages_select_kernel(const PagesSelectParams p) {
+    constexpr int LPB = D / 16, GPW = 32 / LPB;                      // lanes of a block (16 features each), blocks of a warp at a time
+    extern __shared__ __align__(16) uint8_t select_smem_raw[];
+    uint32_t* s_qp = reinterpret_cast<uint32_t*>(select_smem_raw);   // [G][D / 4] positive parts of the queries
+    uint32_t* s_qn = s_qp + p.G * (D / 4);                           // negative parts
+    uint32_t* s_key = s_qn + p.G * (D / 4);                          // [blocks], of the first CTA
+    __shared__ uint32_t s_hist[4][256], s_gt[kSelectWarps], s_eq[kSelectWarps], s_min, s_max;
+    __shared__ float s_most[kSelectWarps];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int ranks = gridDim.x, rank = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
+    const int len = min(max(p.lens[b], 0), p.max_len), n = pages_blocks(len);
+    const int kept = min(p.n_keep, n), recent = min(p.n_recent, kept);
+    const int old = n - recent, want = kept - recent;
+    int* index = p.index + (size_t(b) * p.Hk + hk) * p.n_keep;
+    grid_launch_dependents();
+    const bool some = want > 0 && want < old;
+
+    if (some) {
+        // ---- the queries in 8 bits ----
+        const __nv_bfloat16* q = p.q + (size_t(b) * p.Hk + hk) * p.G * D;
+        float most = 0.f;
+        for (int e = tid; e < p.G * (D / 4); e += kSelectThreads) {
+            const uint2 v = reinterpret_cast<const uint2*>(q)[e];
+            most = fmaxf(most, fmaxf(fmaxf(fabsf(bf16_lo_to_f32(v.x)), fabsf(bf16_hi_to_f32(v.x))), fmaxf(fabsf(bf16_lo_to_f32(v.y)), fabsf(bf16_hi_to_f32(v.y)))));
+        }
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
+        if (lane == 0) s_most[warp] = most;
+        for (int i = tid; i < 4 * 256; i += kSelectThreads) s_hist[0][i] = 0u;
+        if (tid == 0) { s_min = 0xffffffffu; s_max = 0u; }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kSelectWarps; ++i) most = fmaxf(most, s_most[i]);
+        const float inv = most > 0.f ? __fdiv_rn(127.f, most) : 0.f;
+        for (int e = tid; e < p.G * (D / 4); e += kSelectThreads) {
+            const uint2 v = reinterpret_cast<const uint2*>(q)[e];
+            const float x[4] = {bf16_lo_to_f32(v.x), bf16_hi_to_f32(v.x), bf16_lo_to_f32(v.y), bf16_hi_to_f32(v.y)};
+            uint32_t pos = 0u, neg = 0u;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int i = min(max(__float2int_rn(x[j] * inv), -127), 127);
+                pos |= uint32_t(max(i, 0)) << (8 * j);
+                neg |= (uint32_t(min(i, 0)) & 0xffu) << (8 * j);
+            }
+            s_qp[e] = pos;
+            s_qn[e] = neg;
+        }
+        __syncthreads();
+        // ---- ratings ----
+        if (ranks > 1) cluster_sync_all();                           // the first CTA has started
+        const uint32_t keys = ranks > 1 ? cluster_map_shared(smem_u32(s_key), 0u) : smem_u32(s_key);
+        const int grp = lane / LPB, sub = lane % LPB;
+        constexpr int STEP = GPW * kSelectSets;                      // blocks of a warp's iteration
+        const int mine = (LPB == 8 ? (sub >> 1) : sub);              // which set this lane ends up with
+        for (int i0 = (rank * kSelectWarps + warp) * STEP; i0 < old; i0 += ranks * kSelectWarps * STEP) {
+            const uint8_t* rec[kSelectSets];
+            uint4 hi[kSelectSets], lo[kSelectSets];
+#pragma unroll
+            for (int s = 0; s < kSelectSets; ++s) {
+                const int blk = i0 + s * GPW + grp;
+                const int tile = blk < old ? p.tile(b, blk) : -1;
+                rec[s] = tile >= 0 ? p.bounds + (size_t(tile) * p.Hk + hk) * page_bounds_bytes(D) : nullptr;
+            }
+#pragma unroll
+            for (int s = 0; s < kSelectSets; ++s) {
+                hi[s] = lo[s] = make_uint4(0u, 0u, 0u, 0u);
+                if (rec[s]) {
+                    hi[s] = *reinterpret_cast<const uint4*>(rec[s] + 16 * sub);
+                    lo[s] = *reinterpret_cast<const uint4*>(rec[s] + D + 16 * sub);
+                }
+            }
+            const uint8_t* own = rec[0];
+#pragma unroll
+            for (int s = 1; s < kSelectSets; ++s) own = mine == s ? rec[s] : own;
+            const float scale = own ? *reinterpret_cast<const float*>(own + 2 * D) : 0.f;
+            int best = INT_MIN;
+            for (int h = 0; h < p.G; ++h) {
+                const uint4 qp = *reinterpret_cast<const uint4*>(s_qp + h * (D / 4) + 4 * sub), qn = *reinterpret_cast<const uint4*>(s_qn + h * (D / 4) + 4 * sub);
+                int a[kSelectSets];
+#pragma unroll
+                for (int s = 0; s < kSelectSets; ++s) {
+                    int v = __dp4a(int(qp.x), int(hi[s].x), 0);
+                    v = __dp4a(int(qp.y), int(hi[s].y), v);
+                    v = __dp4a(int(qp.z), int(hi[s].z), v);
+                    v = __dp4a(int(qp.w), int(hi[s].w), v);
+                    v = __dp4a(int(qn.x), int(lo[s].x), v);
+                    v = __dp4a(int(qn.y), int(lo[s].y), v);
+                    v = __dp4a(int(qn.z), int(lo[s].z), v);
+                    a[s] = __dp4a(int(qn.w), int(lo[s].w), v);
+                }
+                // sums over the lanes of a block; each lane keeps one of the four sets
+                constexpr int O2 = LPB / 2, O1 = LPB / 4;
+                const bool up2 = sub & O2, up1 = sub & O1;
+                const int g0 = __shfl_xor_sync(0xffffffffu, up2 ? a[0] : a[2], O2), g1 = __shfl_xor_sync(0xffffffffu, up2 ? a[1] : a[3], O2);
+                const int c0 = (up2 ? a[2] : a[0]) + g0, c1 = (up2 ? a[3] : a[1]) + g1;
+                int v = (up1 ? c1 : c0) + __shfl_xor_sync(0xffffffffu, up1 ? c0 : c1, O1);
+                if (LPB == 8) v += __shfl_xor_sync(0xffffffffu, v, 1);
+                best = max(best, v);
+            }
+            const int blk = i0 + mine * GPW + grp;
+            if ((LPB == 4 || (sub & 1) == 0) && blk < old) {
+                // a block without a page is the last to be taken, one with keys that are not finite the first
+                const float r = own ? (scale < INFINITY ? float(best) * scale : INFINITY) : -INFINITY;
+                st_cluster_u32(keys + 4u * uint32_t(blk), evict_key(r));
+            }
+        }
+        if (ranks > 1) {
+            cluster_sync_all();
+            if (rank != 0) return;
+        } else {
+            __syncthreads();
+        }
+    }
+    if (rank != 0) return;
+
+    // ---- the lowest key that stays: keys > thr do, and the first `ties` that equal it ----
+    const int run = ((old + kSelectThreads - 1) / kSelectThreads) | 1;   // keys of a thread: adjacent ones, an odd number for the banks
+    const int r0 = min(tid * run, old), r1 = min(r0 + run, old);
+    uint32_t thr = 0u, ties = 0u;
+    if (some) {
+        uint32_t mn = 0xffffffffu, mx = 0u;
+        for (int i = r0; i < r1; ++i) { const uint32_t k = s_key[i]; mn = min(mn, k); mx = max(mx, k); }
+        mn = __reduce_min_sync(0xffffffffu, mn);
+        mx = __reduce_max_sync(0xffffffffu, mx);
+        if (lane == 0) { atomicMin(&s_min, mn); atomicMax(&s_max, mx); }
+        __syncthreads();
+        mn = s_min; mx = s_max;
+        int shift = mn == mx ? 0 : 32 - __clz(mn ^ mx);              // bits below `shift` are still to be found
+        uint32_t left = uint32_t(want);
+        thr = shift < 32 ? mx >> shift << shift : 0u;
+        for (int pass = 0; shift > 0; ++pass) {
+            const int bits = min(shift, 8), agree = shift;
+            shift -= bits;
+            uint32_t* hist = s_hist[pass];
+            for (int i = r0; i < r1; ++i) {
+                const uint32_t k = s_key[i];
+                if (agree == 32 || ((k ^ thr) >> agree) == 0u) atomicAdd(&hist[(k >> shift) & ((1u << bits) - 1u)], 1u);
+            }
+            __syncthreads();
+            // every warp for itself: 8 bins a lane
+            const uint4 x = *reinterpret_cast<const uint4*>(&hist[8 * lane]), y = *reinterpret_cast<const uint4*>(&hist[8 * lane + 4]);
+            const uint32_t c[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+            uint32_t sum = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum += c[j];
+            uint32_t incl = sum;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+                const uint32_t up = __shfl_down_sync(0xffffffffu, incl, off);
+                if (lane + off < 32) incl += up;
+            }
+            uint32_t over = incl - sum;                              // keys in bins above this lane's
+            const int at = __ffs(__ballot_sync(0xffffffffu, over < left && incl >= left)) - 1;
+            uint32_t bin = 8u * lane;
+#pragma unroll
+            for (int j = 7; j > 0; --j) {
+                if (over + c[j] >= left) { bin += uint32_t(j); break; }
+                over += c[j];
+            }
+            thr |= __shfl_sync(0xffffffffu, bin, at) << shift;
+            left -= __shfl_sync(0xffffffffu, over, at);
+        }
+        ties = left;
+    }
+    // ---- the blocks in their order ----
+    uint32_t gt = 0, eq = 0;
+    if (some) {
+        for (int i = r0; i < r1; ++i) { const uint32_t k = s_key[i]; gt += k > thr; eq += k == thr; }
+    } else if (want > 0) {
+        gt = uint32_t(r1 - r0);
+    }
+    uint32_t gt_incl = gt, eq_incl = eq;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, gt_incl, off), y = __shfl_up_sync(0xffffffffu, eq_incl, off);
+        if (lane >= off) { gt_incl += x; eq_incl += y; }
+    }
+    if (lane == 31) { s_gt[warp] = gt_incl; s_eq[warp] = eq_incl; }
+    __syncthreads();
+    uint32_t gt_before = __reduce_add_sync(0xffffffffu, lane < warp ? s_gt[lane] : 0u) + gt_incl - gt;
+    uint32_t eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? s_eq[lane] : 0u) + eq_incl - eq;
+    uint32_t at = gt_before + min(eq_before, ties);
+    if (some) {
+        for (int i = r0; i < r1; ++i) {
+            const uint32_t k = s_key[i];
+            const bool tie = k == thr;
+            if (k > thr || (tie && eq_before < ties)) index[at++] = i;
+            eq_before += tie;
+        }
+    } else if (want > 0) {
+        for (int i = r0; i < r1; ++i) index[at++] = i;
+    }
+    for (int i = tid; i < p.n_keep - want; i += kSelectThreads) index[want + i] = i < recent ? old + i : -1;
+}
+
+}  // namespace moda

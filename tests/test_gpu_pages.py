@@ -1,0 +1,260 @@
+"""The paged sequence cache in 8 bits on the GPU: written, read back, blocks selected, decode steps over all of it and over the selected blocks."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2603_15619_b200 as moda
+
+import pages_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+WRITES = [  # B, T, Hk, d, page, starts, n_new
+    (1, 1, 1, 64, 64, [0], [1]),
+    (3, 1, 2, 128, 64, [63, 64, 200], [1, 1, 1]),
+    (2, 130, 3, 64, 128, [5, 61], [130, 77]),
+    (2, 130, 3, 128, 64, [0, 64], [130, 128]),
+    (4, 100, 1, 128, 256, [17, 0, 300, 48], [0, 100, 1, 16]),
+    (1, 515, 5, 64, 64, [31], [515]),
+]
+
+
+@pytest.mark.parametrize("B,T,Hk,d,page,start,n_new", WRITES)
+def test_write_gives_the_bytes_of_the_definition(B, T, Hk, d, page, start, n_new):
+    rng = np.random.default_rng(T)
+    lens = [s for s in start]
+    most = max(s + n for s, n in zip(start, n_new))
+    pages, bounds, table, _ = ref.make(B, most, Hk, d, page, [max(s + n, 1) for s, n in zip(start, n_new)], seed=T + d)
+    K, V = (ref.bf16(rng.standard_normal((B, T, Hk, d)) * np.exp(rng.standard_normal((B, T, Hk, 1)) * 3)) for _ in range(2))
+    K[0, 0, 0] = 0.0                                            # a row of zeros
+    V[-1, -1, -1, 1:] = 0.0
+    want = ref.write(pages, bounds, K, V, table, start, n_new, page)
+    dev = [torch.from_numpy(x.copy()).cuda() for x in (pages, bounds, table)]
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    moda.moda_kv_write_e4m3(dev[0], ref.put(K), ref.put(V), dev[2], start=i32(start), n_new=i32(n_new), bounds=dev[1])
+    assert moda.moda_last_status() == 0
+    assert np.array_equal(dev[0].cpu().numpy(), want[0])
+    got, w = dev[1].cpu().numpy(), want[1]
+    assert np.array_equal(got[..., :2 * d + 4], w[..., :2 * d + 4])
+    # without bounds: the same pages
+    again = torch.from_numpy(pages.copy()).cuda()
+    moda.moda_kv_write_e4m3(again, ref.put(K), ref.put(V), dev[2], start=i32(start), n_new=i32(n_new))
+    assert torch.equal(again, dev[0])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_that_are_not_finite(d):
+    pages, bounds, table, dev = ref.make(1, 100, 2, d, 64, [100], seed=3)
+    K, V = (ref.bf16(np.random.default_rng(i).standard_normal((1, 3, 2, d))) for i in range(2))
+    K[0, 1, 0, 5], K[0, 2, 1, 7], V[0, 0, 0, 3] = np.nan, np.inf, -np.inf
+    moda.moda_kv_write_e4m3(dev[0], ref.put(K), ref.put(V), dev[2], start=torch.tensor([100], dtype=torch.int32, device="cuda"), bounds=dev[1])
+    b = dev[1].cpu().numpy().reshape(-1, 2, 2 * d + 16)[table[0, 1]]
+    for h in range(2):
+        assert not b[h, :2 * d].any() and np.isinf(b[h, 2 * d:2 * d + 4].copy().view(np.float32)[0])
+    K2, _ = moda.moda_kv_read_e4m3(dev[0], dev[2], torch.tensor([103], dtype=torch.int32, device="cuda"), 103)
+    K2 = K2.float().cpu().numpy()
+    assert np.isnan(K2[0, 101, 0, 5]) and np.isfinite(np.delete(K2[0, 101, 0], 5)).all() and np.isnan(K2[0, 102, 1]).all() and np.isfinite(K2[0, 100]).all()
+
+
+@pytest.mark.parametrize("B,T,Hk,d,page,lens,start", [(1, 1, 1, 64, 64, [1], None), (3, 200, 2, 128, 128, [0, 200, 77], None), (2, 70, 3, 64, 64, [150, 90], [90, 33]),
+                                                      (2, 129, 1, 128, 256, [300, 60], [255, 0])])
+def test_read_gives_the_rounded_products(B, T, Hk, d, page, lens, start):
+    pages, _, table, dev = ref.make(B, max(lens), Hk, d, page, lens, seed=T)
+    i32 = lambda x: None if x is None else torch.tensor(x, dtype=torch.int32, device="cuda")
+    K, V = (torch.full((B, T, Hk, d), 7.0, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    out = moda.moda_kv_read_e4m3(dev[0], dev[2], i32(lens), T, start=i32(start), K_out=K, V_out=V)
+    assert out[0] is K and out[1] is V and moda.moda_last_status() == 0
+    for b in range(B):
+        s = start[b] if start else 0
+        n = min(max(lens[b] - s, 0), T)
+        for k in range(Hk):
+            for got, want in zip((K, V), ref.gather(pages, table, b, k, lens[b], page, d)):
+                assert np.array_equal(got[b, :n, k].float().cpu().numpy(), ref.bf16(want[s:s + n].astype(np.float32)))
+        assert (K[b, n:] == 7).all() and (V[b, n:] == 7).all()
+    # the outputs that are made here: zeros behind
+    K2, V2 = moda.moda_kv_read_e4m3(dev[0], dev[2], i32(lens), T, start=i32(start))
+    assert torch.equal(K2, torch.where(K == 7, 0, K)) or (K == 7).float().mean() > 0
+
+
+SELECTS = [  # B, lens, H, Hk, d, page, keep, recent
+    (1, [64 * 40], 2, 2, 128, 64, 8, 1), (3, [0, 64 * 33 + 5, 64 * 9], 12, 3, 64, 128, 9, 2), (2, [64 * 300, 64 * 290 + 1], 8, 1, 128, 64, 40, 0),
+    (1, [64 * 700 + 3], 32, 1, 64, 64, 100, 4), (2, [1, 64 * 70], 16, 1, 128, 256, 70, 70), (1, [64 * 1100], 5, 1, 64, 64, 1, 0),
+]
+
+
+def _bounds(num, sub, Hk, d, seed, few):
+    """Bounds with many equal ratings (`few`) or of all kinds."""
+    rng = np.random.default_rng(seed)
+    out = np.zeros((num, sub, Hk, 2 * d + 16), np.uint8)
+    top = 3 if few else 127
+    out[..., :d] = rng.integers(-top, top + 1, out[..., :d].shape).astype(np.int8).view(np.uint8)
+    out[..., d:2 * d] = np.minimum(out[..., :d].view(np.int8), rng.integers(-top, top + 1, out[..., :d].shape).astype(np.int8)).view(np.uint8)
+    s = np.ones(out.shape[:3], np.float32) if few else np.exp(rng.standard_normal(out.shape[:3]) * (20 if seed % 2 else 0.1)).astype(np.float32)
+    if few:
+        out[..., :d] *= rng.integers(0, 2, (*out.shape[:3], 1), dtype=np.uint8)      # blocks with nothing in them
+        out[..., d:2 * d] *= (out[..., :d].max(-1, keepdims=True) > 0).astype(np.uint8)
+    out[..., 2 * d:2 * d + 4] = s[..., None].view(np.uint8)
+    return out
+
+
+@pytest.mark.parametrize("few", [False, True])
+@pytest.mark.parametrize("B,lens,H,Hk,d,page,keep,recent", SELECTS)
+def test_selection_is_the_definition(B, lens, H, Hk, d, page, keep, recent, few):
+    rng = np.random.default_rng(keep)
+    sub = page // 64
+    most = -(-max(lens) // page)
+    table = rng.permutation(B * most + 1).astype(np.int32)[:B * most].reshape(B, most)
+    bounds = _bounds(B * most + 1, sub, Hk, d, keep, few)
+    q = ref.bf16(rng.integers(-1, 2, (B, H, d)) if few else rng.standard_normal((B, H, d)))
+    want = ref.select(q, bounds, table, lens, page, keep, recent)
+    index = moda.moda_kv_select_blocks(ref.put(q), torch.from_numpy(bounds).cuda(), torch.from_numpy(table).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"),
+                                       max(lens), keep, recent)
+    assert moda.moda_last_status() == 0
+    assert np.array_equal(index.cpu().numpy(), want)
+
+
+def test_selection_of_blocks_without_a_page_or_with_values_that_are_not_finite():
+    d, n = 64, 50
+    bounds = _bounds(n, 1, 1, d, 1, False)
+    table = np.arange(n, dtype=np.int32)[None].copy()
+    table[0, [3, 8]] = [-1, n]
+    bounds[[20, 33], 0, 0, :2 * d] = 0
+    bounds[[20, 33], 0, 0, 2 * d:2 * d + 4] = np.array([np.inf], np.float32).view(np.uint8)
+    q = ref.bf16(np.random.default_rng(0).standard_normal((1, 4, d)))
+    for keep in (2, 10, n - 1):
+        got = moda.moda_kv_select_blocks(ref.put(q), torch.from_numpy(bounds).cuda(), torch.from_numpy(table).cuda(),
+                                         torch.tensor([64 * n], dtype=torch.int32, device="cuda"), 64 * n, keep, 0).cpu().numpy()
+        assert np.array_equal(got, ref.select(q, bounds, table, [64 * n], 64, keep, 0))
+        assert {20, 33} <= set(got[0, 0])
+    # queries that are zero or NaN: all ratings are equal, the lower blocks stay
+    for v in (0.0, float("nan")):
+        got = moda.moda_kv_select_blocks(ref.put(q * 0 + v), torch.from_numpy(bounds[:20]).cuda(), torch.arange(10, 20, dtype=torch.int32, device="cuda")[None].contiguous(),
+                                         torch.tensor([640], dtype=torch.int32, device="cuda"), 640, 4, 1).cpu().numpy()
+        assert got.tolist() == [[[0, 1, 2, 9]]]
+
+
+DECODES = [  # B, lens, H, Hk, d, page, l
+    (1, [1], 1, 1, 64, 64, 0), (1, [64], 2, 2, 128, 64, 3), (2, [63, 65], 6, 2, 64, 128, 0), (3, [0, 200, 1], 8, 1, 128, 64, 5), (4, [0, 0, 300, 0], 21, 3, 64, 256, 0),
+    (2, [1000, 513], 4, 4, 128, 64, 33), (1, [3001], 5, 1, 64, 64, 2), (2, [700, 129], 16, 1, 128, 128, 4), (1, [400], 64, 2, 64, 64, 1), (3, [0, 0, 0], 4, 2, 64, 64, 2),
+]
+
+
+def _decode(B, lens, H, Hk, d, page, l, index=None, seed=0, scale=None, sharp=1.0, **kw):
+    T = max(max(lens), 1)
+    pages, _, table, dev = ref.make(B, T, Hk, d, page, lens, seed=seed + d + B)
+    rng = np.random.default_rng(seed + 5)
+    q = ref.bf16(rng.standard_normal((B, H, d)) * sharp)
+    depth = ref.bf16(rng.standard_normal((l, B, Hk, 2, d)))
+    scale = d ** -0.5 if scale is None else scale
+    idx = None if index is None else torch.from_numpy(index).cuda()
+    O, LSE = moda.moda_attn_decode_e4m3(ref.put(q), dev[0], dev[2], torch.tensor(lens, dtype=torch.int32, device="cuda"), ref.put(depth) if l else None, T, l, scale,
+                                        index=idx, **kw)
+    assert moda.moda_last_status() == 0
+    return O, LSE, ref.decode(q, pages, table, lens, depth, scale, page, index)
+
+
+def _check(O, LSE, want):
+    o, lse, o_tol, lse_tol = want
+    O, LSE = O.double().cpu().numpy(), LSE.double().cpu().numpy()
+    empty = np.isneginf(lse)
+    assert np.array_equal(np.isneginf(LSE), empty) and (O[empty] == 0).all()
+    assert (np.abs(O - o) <= o_tol).all(), float((np.abs(O - o) / np.maximum(o_tol, 1e-30)).max())
+    assert (np.abs(LSE - lse)[~empty] <= lse_tol[~empty]).all(), float((np.abs(LSE - lse)[~empty] / lse_tol[~empty]).max())
+
+
+@pytest.mark.parametrize("sharp", [1.0, 30.0])
+@pytest.mark.parametrize("B,lens,H,Hk,d,page,l", DECODES)
+def test_decode_against_64_bits(B, lens, H, Hk, d, page, l, sharp):
+    _check(*_decode(B, lens, H, Hk, d, page, l, sharp=sharp))
+
+
+@pytest.mark.parametrize("H,Hk,d", [(8, 2, 128), (3, 1, 64), (32, 1, 64)])
+def test_decode_over_named_blocks(H, Hk, d):
+    rng = np.random.default_rng(H)
+    lens = [64 * 30 + 7, 0, 64 * 3, 50]
+    index = np.full((4, Hk, 9), -1, np.int32)
+    for k in range(Hk):
+        index[0, k] = np.sort(rng.permutation(31)[:9])
+        index[2, k, :3] = [0, 2, 1]
+        index[3, k, 0] = 0
+    index[0, 0, 4] = 31                                         # no block of the sequence: passed over
+    index[2, 0, 1] = -5
+    _check(*_decode(4, lens, H, Hk, d, 64, 2, index=index))
+    _check(*_decode(4, lens, H, Hk, d, 128, 0, index=index))
+
+
+def test_blocks_without_a_page_have_no_weight():
+    B, lens, H, Hk, d = 1, [64 * 6], 4, 2, 128
+    pages, _, table, dev = ref.make(B, lens[0], Hk, d, 128, lens, seed=9)
+    table[0, 1] = pages.shape[0]
+    q = ref.bf16(np.random.default_rng(1).standard_normal((B, H, d)))
+    t = torch.from_numpy(table).cuda()
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    _check(*moda.moda_attn_decode_e4m3(ref.put(q), dev[0], t, n, None, lens[0], 0, 0.1), ref.decode(q, pages, table, lens, None, 0.1, 128))
+    K, V = moda.moda_kv_read_e4m3(dev[0], t, n, lens[0])
+    assert (K[0, 128:256] == 0).all() and (V[0, 128:256] == 0).all() and (K[0, :128] != 0).any()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("power", [-60, 60])
+def test_values_of_very_different_sizes(d, power):
+    # value rows around 2^power and far from each other: their scales go into the weights, which must neither overflow nor vanish
+    B, n, H, Hk = 1, 300, 4, 2
+    rng = np.random.default_rng(d)
+    K = ref.bf16(rng.standard_normal((B, n, Hk, d)))
+    V = ref.bf16(rng.standard_normal((B, n, Hk, d)) * 2.0 ** (power + rng.integers(-20, 21, (B, n, Hk, 1))))
+    pages, bounds, table, dev = ref.make(B, n, Hk, d, 64, [n], seed=1)
+    pages, _ = ref.write(pages, None, K, V, table, [0], [n], 64)
+    q = ref.bf16(rng.standard_normal((B, H, d)) * 2.0 ** 40)
+    scale = 2.0 ** -40 * d ** -0.5
+    got = moda.moda_attn_decode_e4m3(ref.put(q), torch.from_numpy(pages).cuda(), dev[2], torch.tensor([n], dtype=torch.int32, device="cuda"), None, n, 0, scale)
+    _check(*got, ref.decode(q, pages, table, [n], None, scale, 64))
+
+
+def test_many_sequences():
+    # more than a thread per sequence, and empty ones among them
+    lens = [(37 * i) % 130 for i in range(700)]
+    _check(*_decode(700, lens, 2, 1, 64, 64, 1))
+
+
+def test_nan_stays_where_it_is():
+    B, lens, H, Hk, d = 2, [100, 100], 4, 2, 64
+    pages, _, table, dev = ref.make(B, 100, Hk, d, 64, lens, seed=2)
+    q = ref.bf16(np.random.default_rng(1).standard_normal((B, H, d)))
+    q[0, 1, 3] = np.nan
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    O, LSE = moda.moda_attn_decode_e4m3(ref.put(q), dev[0], dev[2], n, None, 100, 0, 0.1)
+    bad = torch.isnan(O).all(-1).cpu().numpy()
+    assert bad.tolist() == [[False, True, False, False], [False] * 4] and torch.isfinite(O[1]).all() and torch.isnan(LSE[0, 1])
+
+
+def test_same_bits_again_on_another_stream_and_captured():
+    B, lens, H, Hk, d, l = 3, [700, 64, 333], 8, 2, 128, 3
+    pages, bounds, table, dev = ref.make(B, 700, Hk, d, 64, lens, seed=4)
+    rng = np.random.default_rng(2)
+    q, depth = ref.put(ref.bf16(rng.standard_normal((B, H, d)))), ref.put(ref.bf16(rng.standard_normal((l, B, Hk, 2, d))))
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    work = torch.empty(moda.moda_decode_e4m3_workspace_bytes(B, H, Hk, d), dtype=torch.uint8, device="cuda")
+
+    def step(**kw):
+        index = moda.moda_kv_select_blocks(q, dev[1], dev[2], n, 700, 5, 1, **kw)
+        return (index, *moda.moda_attn_decode_e4m3(q, dev[0], dev[2], n, depth, 700, l, 0.1, index=index, **kw))
+
+    first = step()
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(other):
+        second = step()
+    third = step(stream=other)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        index = moda.moda_kv_select_blocks(q, dev[1], dev[2], n, 700, 5, 1)
+        fourth = (index, *moda.moda_attn_decode_e4m3(q, dev[0], dev[2], n, depth, 700, l, 0.1, index=index, workspace=work))
+    for t in fourth:
+        t.zero_()
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    for got in (second, third, fourth):
+        assert all(torch.equal(x, y) for x, y in zip(first, got))
