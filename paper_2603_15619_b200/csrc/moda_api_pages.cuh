@@ -22,14 +22,13 @@ int pages_rows_grid(int B, int T, int H_kv, dim3* grid) {
     return MODA_OK;
 }
 
-constexpr int kPagesMostCtas = 148;               // times the CTAs of an SM: partial results of that many fit the workspace
+constexpr int kPagesMostCtas = 148;               // partial results of that many fit the workspace
 
-inline size_t pages_part_bytes(int B, int H, int G) {
-    return (size_t(kPagesMostCtas) * kPagesDecodeCtas(64) * kPagesDecodeWarps * G + size_t(B) * H) * 4;
+inline size_t pages_part_bytes(int B, int H, int G, int d) {
+    return (size_t(kPagesMostCtas) * kPagesDecodeWarps(d) * G + size_t(B) * H) * (d + 2) * 4;
 }
 size_t pages_workspace_bytes(int B, int H, int H_kv, int d) {
-    const int G = std::min(H / H_kv, 8);
-    return (pages_part_bytes(B, H, G) * (d + 2) + size_t(B + 1) * 4 + 15) / 16 * 16;
+    return (pages_part_bytes(B, H, std::min(H / H_kv, 8), d) + size_t(B + 1) * 4 + 15) / 16 * 16;
 }
 
 template <typename P>
@@ -71,17 +70,16 @@ int launch_select(const PagesSelectParams& p, int ranks, cudaStream_t stream) {
 
 template <int D>
 int launch_decode_pages(const PagesDecodeParams& p, cudaStream_t stream) {
-    const size_t smem = size_t(p.B + 1) * 4;
-    if (smem > 40000) {
-        static thread_local int configured_dev = -1;
-        int dev = 0;
-        if (!cuda_ok(cudaGetDevice(&dev))) return MODA_ERR_CUDA;
-        if (configured_dev != dev) {
-            if (!set_smem_limit(pages_split_kernel<D>, (kPagesMostBatch + 1) * 4)) return MODA_ERR_CUDA;
-            configured_dev = dev;
-        }
+    static thread_local int configured_dev = -1;
+    int dev = 0;
+    if (!cuda_ok(cudaGetDevice(&dev))) return MODA_ERR_CUDA;
+    if (configured_dev != dev) {
+        if (!set_smem_limit(pages_split_kernel<D>, kPagesSplitSmem(D, kPagesMostBatch))) return MODA_ERR_CUDA;
+        configured_dev = dev;
     }
-    if (int rc = launch_pages(pages_split_kernel<D>, dim3(unsigned(p.warps / kPagesDecodeWarps)), kPagesDecodeThreads, smem, p.index != nullptr, p, stream)) return rc;
+    if (int rc = launch_pages(pages_split_kernel<D>, dim3(unsigned(p.warps / kPagesDecodeWarps(D))), kPagesDecodeWarps(D) * 32, size_t(kPagesSplitSmem(D, p.B)),
+                              p.index != nullptr, p, stream))
+        return rc;
     return launch_pages(pages_merge_kernel<D>, dim3(unsigned(p.H), unsigned(p.B)), kPagesMergeThreads, 0, true, p, stream);
 }
 
@@ -182,8 +180,8 @@ int moda_attn_decode_e4m3(const void* q, const void* pages, const int* block_tab
     p.depth = static_cast<const __nv_bfloat16*>(depth_kv_token); p.O = static_cast<__nv_bfloat16*>(O); p.LSE = LSE;
     p.G = H / p.Hk; p.H = H; p.l = l; p.max_len = max_seq_len; p.n_index = n_blocks;
     p.part = static_cast<float*>(workspace);
-    p.before = reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + pages_part_bytes(B, H, p.G) * (d + 2));
-    p.warps = std::min(sms, kPagesMostCtas) * kPagesDecodeCtas(d) * kPagesDecodeWarps;
+    p.before = reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + pages_part_bytes(B, H, p.G, d));
+    p.warps = std::min(sms, kPagesMostCtas) * kPagesDecodeWarps(d);
     p.scale_log2 = scale * kDecodeLog2e;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return d == 128 ? launch_decode_pages<128>(p, st) : launch_decode_pages<64>(p, st);

@@ -3,8 +3,8 @@
 //
 //   pages_split_kernel    a block of a (sequence, key/value head) is a unit; the units of all, in this order, are cut into equal runs, one per warp of the
 //                         device, and every warp works through its own: nothing waits for another warp.  A lane's share of a block's keys is the operand of its
-//                         matrix products as it lies in memory, and so is its share of the values, so both go from global memory to registers,
-//                         one block ahead of the one in work; shared memory holds the 128 scales of the block alone.
+//                         matrix products as it lies in memory, and so is its share of the values: nothing is turned on the way.  A warp has a ring of
+//                         its own for three pieces (a block's keys, or its values) in shared memory, two on their way while one is worked on: 128 KiB an SM.
 //   pages_merge_kernel    a CTA per (sequence, query head): the depth pairs, then the partial results of the group's warps.
 //
 // One block, lane = (g, t) = (lane / 4, lane % 4), products m16n8k16 of f16 with fp32 sums:
@@ -23,6 +23,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include "moda_depth_gqa.cuh"
 #include "moda_pages.cuh"
 #include "sm100_ptx.cuh"
 
@@ -49,10 +50,13 @@ struct PagesDecodeParams : PagesParams {
     }
 };
 
-constexpr int kPagesDecodeThreads = 256, kPagesDecodeWarps = kPagesDecodeThreads / 32;
-constexpr int kPagesMostBatch = 16384;                               // sequences of a call: their blocks are counted in shared memory
+constexpr int kPagesMostBatch = 4096;                                // sequences of a call: their blocks are counted in shared memory
 constexpr int kPagesMergeThreads = 128;
-constexpr int kPagesDecodeCtas(int d) { return d == 64 ? 2 : 1; }    // of an SM: the registers' measure
+constexpr int kPagesDecodeWarps(int d) { return d == 64 ? 16 : 8; }  // of a CTA, one an SM
+constexpr int kPagesPieces = 3;                                      // key or value halves of blocks that a warp has in shared memory or on the way
+constexpr int kPagesWarpBytes(int d) { return kPagesPieces * kPageBlock * d + 2 * 8 * kPageBlock; }
+constexpr int kPagesSplitSmem(int d, int B) { return kPagesDecodeWarps(d) * kPagesWarpBytes(d) + (B + 1) * 4; }
+static_assert(kPagesSplitSmem(128, kPagesMostBatch) <= 226 * 1024 && kPagesSplitSmem(64, kPagesMostBatch) <= 226 * 1024, "shared memory");
 
 __device__ __forceinline__ void mma_f16_16x8x16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -64,12 +68,6 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-__device__ __forceinline__ uint4 ld_once(const uint8_t* at) {        // read once: not kept in L1
-    uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(at));
-    return v;
-}
-
 // Where a warp is in the order of all units.
 struct PagesWalk {
     int b, r, j, n;               // sequence, group of it, unit of that group, units of a group of this sequence
@@ -97,18 +95,20 @@ struct PagesWalk {
 };
 
 template <int D>
-__global__ void __launch_bounds__(kPagesDecodeThreads, kPagesDecodeCtas(D))
+__global__ void __launch_bounds__(kPagesDecodeWarps(D) * 32, 1)
 pages_split_kernel(const PagesDecodeParams p) {
+    constexpr int NW = kPagesDecodeWarps(D), NT = NW * 32;
     constexpr int KP = D / 64, FB = D / 16;                          // 64-feature parts of a key row; 16-feature rows of the value product
-    extern __shared__ int s_before[];                                // [B + 1]
-    __shared__ __align__(16) float s_scale[kPagesDecodeWarps][2 * kPageBlock];
-    __shared__ int s_sum[kPagesDecodeWarps];
+    constexpr int PIECE = kPageBlock * D, CH = D / 16;               // bytes of a block's key or value codes; 16-byte pieces of a key row
+    extern __shared__ __align__(16) uint8_t split_smem[];
+    int* s_before = reinterpret_cast<int*>(split_smem + NW * kPagesWarpBytes(D));   // [B + 1]
+    __shared__ int s_sum[NW];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int g = lane >> 2, t = lane & 3;
     if (p.index) grid_dependency_wait();                             // launched beside what comes before it in the stream
     // ---- blocks of the sequences before each ----
     {
-        const int per = (p.B + kPagesDecodeThreads - 1) / kPagesDecodeThreads;
+        const int per = (p.B + NT - 1) / NT;
         const int b0 = min(tid * per, p.B), b1 = min(b0 + per, p.B);
         int sum = 0;
         for (int b = b0; b < b1; ++b) sum += p.units(b);
@@ -129,63 +129,80 @@ pages_split_kernel(const PagesDecodeParams p) {
         if (b0 < b1 && b1 == p.B) s_before[p.B] = at;
         __syncthreads();
         if (blockIdx.x == 0)
-            for (int b = tid; b <= p.B; b += kPagesDecodeThreads) p.before[b] = s_before[b];
+            for (int b = tid; b <= p.B; b += NT) p.before[b] = s_before[b];
     }
     const long long total = (long long)s_before[p.B] * p.Hk, runs = min(total, (long long)p.warps);
     const int w = warp * gridDim.x + blockIdx.x;                     // neighbours in the order are on different SMs
     if (w >= runs) return;
-    long long u = total * w / runs;
-    const long long end = total * (w + 1) / runs;
+    const int first = int(total * w / runs), n_unit = int(total * (w + 1) / runs) - first;
 
-    PagesWalk at;
-    at.begin(s_before, p.B, p.Hk, u);
-    // block and its place of a unit
-    auto block_of = [&](const PagesWalk& k) {
-        return p.index ? p.index[(size_t(k.b) * (p.Hk / p.kv_rep) + k.r / p.kv_rep) * p.n_index + k.j] : k.j;
+    // ---- the ring: pieces (keys of a unit, then its values) in order, the next two on their way while one is worked on ----
+    const uint8_t* ring = split_smem + warp * kPagesWarpBytes(D);
+    const uint32_t ring_u32 = smem_u32(ring);
+    float* scales = reinterpret_cast<float*>(split_smem + warp * kPagesWarpBytes(D) + kPagesPieces * PIECE);   // [2][128], of even and odd units
+    PagesWalk ahead;                                                 // the unit whose pieces are requested next
+    ahead.begin(s_before, p.B, p.Hk, first);
+    PagesWalk at = ahead;                                            // the one in work
+    int left = n_unit;                                               // units not yet looked up
+    // Block of a unit, and where it lies (null: nowhere).
+    struct Place { const uint8_t* rec; int rows; };
+    auto block_of = [&]() -> int {
+        return p.index ? p.index[(size_t(ahead.b) * (p.Hk / p.kv_rep) + ahead.r / p.kv_rep) * p.n_index + ahead.j] : ahead.j;
     };
-    auto rows_of = [&](const PagesWalk& k, int blk) { return min(max(p.len(k.b) - blk * kPageBlock, 0), kPageBlock); };
-    auto place_of = [&](const PagesWalk& k, int blk) -> const uint8_t* {
-        const int tile = blk >= 0 && blk < pages_blocks(p.len(k.b)) ? p.tile(k.b, blk) : -1;
-        return tile >= 0 ? p.pages + (size_t(tile) * (p.Hk / p.kv_rep) + k.r / p.kv_rep) * page_block_bytes(D) : nullptr;
+    auto look_up = [&](int blk) -> Place {
+        const int len = p.len(ahead.b);
+        const int tile = blk >= 0 && blk < pages_blocks(len) ? p.tile(ahead.b, blk) : -1;
+        Place x;
+        x.rec = tile >= 0 ? p.pages + (size_t(tile) * (p.Hk / p.kv_rep) + ahead.r / p.kv_rep) * page_block_bytes(D) : nullptr;
+        x.rows = tile >= 0 ? min(len - blk * kPageBlock, kPageBlock) : 0;
+        if (--left > 0) ahead.next(s_before, p.Hk);
+        return x;
     };
-    uint4 kr[8][KP], vr[FB][2];
-    float2 sk, sv;
-    auto load_k = [&](const uint8_t* rec) {
+    // 16-byte piece c of key row r lies at c ^ 4 (r % 2) where a row has 8, so that two adjacent rows of four lanes each are in different banks.
+    auto request_k = [&](const uint8_t* rec, int piece, int unit) {
         if (rec) {
+            const uint32_t dst = ring_u32 + (piece % kPagesPieces) * PIECE;
 #pragma unroll
-            for (int n = 0; n < 8; ++n)
-#pragma unroll
-                for (int i = 0; i < KP; ++i) kr[n][i] = ld_once(rec + (16 * (g >> 1) + 2 * n + (g & 1)) * D + 64 * i + 16 * t);
-            sk = *reinterpret_cast<const float2*>(rec + 2 * kPageBlock * D + 8 * lane);
-            sv = *reinterpret_cast<const float2*>(rec + 2 * kPageBlock * D + 4 * kPageBlock + 8 * lane);
+            for (int i = 0; i < PIECE / 512; ++i) {
+                const int e = i * 32 + lane, r = e / CH, c = e % CH;
+                cp_async_16(dst + r * D + 16 * (D == 128 ? c ^ ((r & 1) << 2) : c), rec + e * 16);
+            }
+            cp_async_16(smem_u32(scales) + (unit & 1) * 512 + lane * 16, rec + 2 * PIECE + lane * 16);
         }
+        cp_async_commit();
     };
-    auto load_v = [&](const uint8_t* rec) {
+    auto request_v = [&](const uint8_t* rec, int piece) {
         if (rec) {
+            const uint32_t dst = ring_u32 + (piece % kPagesPieces) * PIECE;
 #pragma unroll
-            for (int f = 0; f < FB; ++f)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) vr[f][i] = ld_once(rec + kPageBlock * D + (16 * f + 8 * i + g) * kPageBlock + 16 * t);
+            for (int i = 0; i < PIECE / 512; ++i) cp_async_16(dst + (i * 32 + lane) * 16, rec + PIECE + (i * 32 + lane) * 16);
         }
+        cp_async_commit();
     };
+    Place here = look_up(block_of()), next = {nullptr, 0};
+    request_k(here.rec, 0, 0);
+    request_v(here.rec, 1);
+    if (n_unit > 1) next = look_up(block_of());
+    request_k(next.rec, 2, 1);
+
     uint32_t qf[KP][8];                                              // this lane's features of head g, f16
     float q_scale;                                                   // their power of two, times scale log2(e)
     auto load_q = [&]() {
-        float x[KP][16], most = 0.f;
+        uint4 v[KP][2];
+        float most = 0.f;
 #pragma unroll
         for (int i = 0; i < KP; ++i) {
-            uint4 v[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
+            v[i][0] = v[i][1] = make_uint4(0u, 0u, 0u, 0u);
             if (g < p.G) {
                 const uint4* src = reinterpret_cast<const uint4*>(p.q + (size_t(at.b) * p.H + at.r * p.G + g) * D + 64 * i + 16 * t);
-                v[0] = src[0];
-                v[1] = src[1];
+                v[i][0] = src[0];
+                v[i][1] = src[1];
             }
-            const uint32_t words[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                x[i][2 * k] = bf16_lo_to_f32(words[k]);
-                x[i][2 * k + 1] = bf16_hi_to_f32(words[k]);
-                most = fmaxf(most, fmaxf(fabsf(x[i][2 * k]), fabsf(x[i][2 * k + 1])));
+            for (int k = 0; k < 2; ++k) {
+                const uint32_t words[4] = {v[i][k].x, v[i][k].y, v[i][k].z, v[i][k].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) most = fmaxf(most, fmaxf(fabsf(bf16_lo_to_f32(words[j])), fabsf(bf16_hi_to_f32(words[j]))));
             }
         }
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
@@ -196,41 +213,40 @@ pages_split_kernel(const PagesDecodeParams p) {
 #pragma unroll
         for (int i = 0; i < KP; ++i)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) qf[i][k] = pack_f16x2(x[i][2 * k] * up, x[i][2 * k + 1] * up);
+            for (int k = 0; k < 2; ++k) {
+                const uint32_t words[4] = {v[i][k].x, v[i][k].y, v[i][k].z, v[i][k].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) qf[i][4 * k + j] = pack_f16x2(bf16_lo_to_f32(words[j]) * up, bf16_hi_to_f32(words[j]) * up);
+            }
     };
+    load_q();
 
     float m = -INFINITY, mw = -INFINITY, sum = 0.f;                  // of head g: maxima of the scores and of the weights' exponents, row sum (this lane's keys)
     float o[FB][4];                                                  // features 16 f + g (c0 c1) and + 8 (c2 c3) of heads 2 t, 2 t + 1
 #pragma unroll
     for (int f = 0; f < FB; ++f) { o[f][0] = 0.f; o[f][1] = 0.f; o[f][2] = 0.f; o[f][3] = 0.f; }
-    int blk = block_of(at);
-    const uint8_t* rec = place_of(at, blk);
-    load_k(rec);
-    load_v(rec);
-    load_q();
 #pragma unroll 1
-    while (true) {
-        const int rows = rec ? rows_of(at, blk) : 0;                 // keys of this block
-        const bool more = u + 1 < end;
-        PagesWalk next = at;
-        const bool leaves = more && next.next(s_before, p.Hk);
-        const int next_blk = more ? block_of(next) : 0;
-        const uint8_t* next_rec = more ? place_of(next, next_blk) : nullptr;
-        if (!more) grid_launch_dependents();                         // all loads are on their way: the merge may come up
+    for (int u = 0; u < n_unit; ++u) {
+        const int rows = here.rows;
+        const int ahead_blk = left > 0 ? block_of() : 0;             // of unit u + 2
+        if (u + 1 == n_unit) grid_launch_dependents();               // all loads are on their way: the merge may come up
+        cp_async_wait<2>();
+        __syncwarp();
+        const uint8_t* sk = ring + (2 * u % kPagesPieces) * PIECE;
+        const uint8_t* sv = ring + ((2 * u + 1) % kPagesPieces) * PIECE;
+        float* own = scales + (u & 1) * 128;
+        uint32_t pw[8];                                              // weights of keys 16 t + 2 n, + 1
         if (rows > 0) {
-            __syncwarp();
-            *reinterpret_cast<float2*>(&s_scale[warp][2 * lane]) = sk;
-            *reinterpret_cast<float2*>(&s_scale[warp][kPageBlock + 2 * lane]) = make_float2(__log2f(sv.x), __log2f(sv.y));
-            __syncwarp();
-        }
-        float s[8][2];
-        if (rows > 0) {
+            const float2 v = *reinterpret_cast<const float2*>(own + kPageBlock + 2 * lane);
+            *reinterpret_cast<float2*>(own + kPageBlock + 2 * lane) = make_float2(__log2f(v.x), __log2f(v.y));
+            float s[8][2];
 #pragma unroll
             for (int n = 0; n < 8; ++n) {
                 float c[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int i = 0; i < KP; ++i) {
-                    const uint32_t word[4] = {kr[n][i].x, kr[n][i].y, kr[n][i].z, kr[n][i].w};
+                    const uint4 x = *reinterpret_cast<const uint4*>(sk + (16 * (g >> 1) + 2 * n + (g & 1)) * D + 16 * (D == 128 ? (4 * i + t) ^ ((g & 1) << 2) : t));
+                    const uint32_t word[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         uint32_t b0, b1;
@@ -241,73 +257,81 @@ pages_split_kernel(const PagesDecodeParams p) {
                 s[n][0] = c[0];
                 s[n][1] = c[1];
             }
-        }
-        load_k(next_rec);
-        if (rows > 0) {
-            uint32_t pw[8];                                          // weights of keys 16 t + 2 n, + 1
-            {
-                float x[8][2];                                       // log2 of the values' scales, then the weights' exponents
+            __syncwarp();                                            // everyone has read the keys; the logarithms are there
+            request_v(next.rec, 2 * u + 3);
+            float x[8][2];                                           // log2 of the values' scales, then the weights' exponents
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float4 a = *reinterpret_cast<const float4*>(&s_scale[warp][16 * t + 4 * i]);
-                    const float4 c = *reinterpret_cast<const float4*>(&s_scale[warp][kPageBlock + 16 * t + 4 * i]);
-                    s[2 * i][0] *= a.x * q_scale; s[2 * i][1] *= a.y * q_scale;
-                    s[2 * i + 1][0] *= a.z * q_scale; s[2 * i + 1][1] *= a.w * q_scale;
-                    x[2 * i][0] = c.x; x[2 * i][1] = c.y; x[2 * i + 1][0] = c.z; x[2 * i + 1][1] = c.w;
-                }
-                if (rows < kPageBlock) {                             // what lies past the last key may hold anything
-#pragma unroll
-                    for (int n = 0; n < 8; ++n)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i)
-                            if (16 * t + 2 * n + i >= rows) { s[n][i] = -INFINITY; x[n][i] = 0.f; }
-#pragma unroll
-                    for (int f = 0; f < FB; ++f)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            uint32_t* word = &vr[f][i].x;
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                const int here = min(max(rows - 16 * t - 4 * k, 0), 4);
-                                word[k] &= here == 4 ? 0xffffffffu : (1u << (8 * here)) - 1u;
-                            }
-                        }
-                }
-                float mx = -INFINITY, mxw = -INFINITY;
+            for (int i = 0; i < 4; ++i) {
+                const float4 a = *reinterpret_cast<const float4*>(own + 16 * t + 4 * i);
+                const float4 c = *reinterpret_cast<const float4*>(own + kPageBlock + 16 * t + 4 * i);
+                s[2 * i][0] *= a.x * q_scale; s[2 * i][1] *= a.y * q_scale;
+                s[2 * i + 1][0] *= a.z * q_scale; s[2 * i + 1][1] *= a.w * q_scale;
+                x[2 * i][0] = c.x; x[2 * i][1] = c.y; x[2 * i + 1][0] = c.z; x[2 * i + 1][1] = c.w;
+            }
+            if (rows < kPageBlock) {                                 // what lies past the last key may hold anything
 #pragma unroll
                 for (int n = 0; n < 8; ++n)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        x[n][i] += s[n][i];
-                        mx = fmaxf(mx, s[n][i]);
-                        mxw = fmaxf(mxw, x[n][i]);
+                    for (int i = 0; i < 2; ++i)
+                        if (16 * t + 2 * n + i >= rows) { s[n][i] = -INFINITY; x[n][i] = 0.f; }
+            }
+            float mx = -INFINITY, mxw = -INFINITY;
+#pragma unroll
+            for (int n = 0; n < 8; ++n)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    x[n][i] += s[n][i];
+                    mx = fmaxf(mx, s[n][i]);
+                    mxw = fmaxf(mxw, x[n][i]);
+                }
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+            mxw = fmaxf(mxw, __shfl_xor_sync(0xffffffffu, mxw, 1));
+            mx = fmaxf(m, fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2)));
+            mxw = fmaxf(mw, fmaxf(mxw, __shfl_xor_sync(0xffffffffu, mxw, 2)));
+            const float base = mx == -INFINITY ? 0.f : mx, alpha = fast_exp2(m - base);
+            const float base_w = mxw == -INFINITY ? 0.f : mxw - 14.f, alpha_w = fast_exp2(mw - mxw);
+            float part = 0.f;
+#pragma unroll
+            for (int n = 0; n < 8; ++n) {
+                part += fast_exp2(s[n][0] - base) + fast_exp2(s[n][1] - base);
+                pw[n] = pack_f16x2(fast_exp2(x[n][0] - base_w), fast_exp2(x[n][1] - base_w));
+            }
+            sum = sum * alpha + part;
+            const bool moved = mw != mxw && mw != -INFINITY;
+            m = mx;
+            mw = mxw;
+            if (__any_sync(0xffffffffu, moved)) {
+                const float f = moved ? alpha_w : 1.f;
+                const float a0 = __shfl_sync(0xffffffffu, f, 8 * t), a1 = __shfl_sync(0xffffffffu, f, 8 * t + 4);
+#pragma unroll
+                for (int i = 0; i < FB; ++i) { o[i][0] *= a0; o[i][1] *= a1; o[i][2] *= a0; o[i][3] *= a1; }
+            }
+        } else {
+            request_v(next.rec, 2 * u + 3);
+        }
+        const bool leaves = u + 1 < n_unit && at.j + 1 == at.n;
+        const Place then = left > 0 ? look_up(ahead_blk) : Place{nullptr, 0};
+        cp_async_wait<2>();
+        __syncwarp();
+        if (rows > 0) {
+            if (rows < kPageBlock) {                                 // value codes past the last key: zero, their weights are 0
+                for (int e = lane; e < D * 4; e += 32) {
+                    uint4* c = reinterpret_cast<uint4*>(const_cast<uint8_t*>(sv)) + e;
+                    uint32_t word[4] = {c->x, c->y, c->z, c->w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int some = min(max(rows - 16 * (e & 3) - 4 * k, 0), 4);
+                        word[k] = some == 4 ? word[k] : word[k] & ((1u << (8 * some)) - 1u);
                     }
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-                mxw = fmaxf(mxw, __shfl_xor_sync(0xffffffffu, mxw, 1));
-                mx = fmaxf(m, fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2)));
-                mxw = fmaxf(mw, fmaxf(mxw, __shfl_xor_sync(0xffffffffu, mxw, 2)));
-                const float base = mx == -INFINITY ? 0.f : mx, alpha = fast_exp2(m - base);
-                const float base_w = mxw == -INFINITY ? 0.f : mxw - 14.f, alpha_w = fast_exp2(mw - mxw);
-                float part = 0.f;
-#pragma unroll
-                for (int n = 0; n < 8; ++n) {
-                    part += fast_exp2(s[n][0] - base) + fast_exp2(s[n][1] - base);
-                    pw[n] = pack_f16x2(fast_exp2(x[n][0] - base_w), fast_exp2(x[n][1] - base_w));
+                    *c = make_uint4(word[0], word[1], word[2], word[3]);
                 }
-                sum = sum * alpha + part;
-                const bool moved = mw != mxw && mw != -INFINITY;
-                m = mx;
-                mw = mxw;
-                if (__any_sync(0xffffffffu, moved)) {
-                    const float f = moved ? alpha_w : 1.f;
-                    const float a0 = __shfl_sync(0xffffffffu, f, 8 * t), a1 = __shfl_sync(0xffffffffu, f, 8 * t + 4);
-#pragma unroll
-                    for (int i = 0; i < FB; ++i) { o[i][0] *= a0; o[i][1] *= a1; o[i][2] *= a0; o[i][3] *= a1; }
-                }
+                __syncwarp();
             }
 #pragma unroll
             for (int f = 0; f < FB; ++f) {
-                const uint32_t x[4] = {vr[f][0].x, vr[f][0].y, vr[f][0].z, vr[f][0].w}, y[4] = {vr[f][1].x, vr[f][1].y, vr[f][1].z, vr[f][1].w};
+                const uint4 v0 = *reinterpret_cast<const uint4*>(sv + (16 * f + g) * kPageBlock + 16 * t);
+                const uint4 v1 = *reinterpret_cast<const uint4*>(sv + (16 * f + 8 + g) * kPageBlock + 16 * t);
+                const uint32_t x[4] = {v0.x, v0.y, v0.z, v0.w}, y[4] = {v1.x, v1.y, v1.z, v1.w};
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     uint32_t a0, a1, a2, a3;
@@ -317,8 +341,11 @@ pages_split_kernel(const PagesDecodeParams p) {
                 }
             }
         }
-        load_v(next_rec);
-        if (!more || leaves) {
+        __syncwarp();                                                // everyone has read the values (and the scales)
+        request_k(then.rec, 2 * u + 4, u);
+        here = next;
+        next = then;
+        if (leaves || u + 1 == n_unit) {
             // ---- the group's partial result of this warp ----
             sum += __shfl_xor_sync(0xffffffffu, sum, 1);
             sum += __shfl_xor_sync(0xffffffffu, sum, 2);
@@ -342,12 +369,10 @@ pages_split_kernel(const PagesDecodeParams p) {
             m = mw = -INFINITY;
             sum = 0.f;
         }
-        if (!more) break;
-        ++u;
-        at = next;
-        blk = next_blk;
-        rec = next_rec;
-        if (leaves) load_q();
+        if (u + 1 < n_unit) {
+            at.next(s_before, p.Hk);
+            if (leaves) load_q();
+        }
     }
 }
 
