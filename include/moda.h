@@ -619,7 +619,7 @@ int moda_attn_decode_shared(const void* q, const void* K_prefix, const void* V_p
  * moda_attn_decode_e4m3   the decode step: O, LSE, depth_kv_token, groups and scale as for moda_attn_decode_paged, with seq_lens[b] in 0 .. max_seq_len.  index (int32
  *                         [B][H_kv][n_blocks]) NULL: all blocks; else the blocks of the first min(n_blocks, ceil(seq_lens[b] / 64)) entries of a row, an entry that is no block
  *                         of the sequence being passed over (one that comes twice counts twice).  A token without any key has O = 0 and LSE = -inf.
- *                         workspace : moda_decode_e4m3_workspace_bytes.  B <= 4096.  Two launches.
+ *                         workspace : moda_decode_e4m3_workspace_bytes.  B <= 2048.  Two launches.
  *
  * The products take the codes as they are (exact in f16), q times a power of two, and weights rounded to f16; scales, maxima, sums and the accumulators are fp32.
  * Sums in an order that depends on the lengths of all sequences and the device's SM count: the same call gives the same bits.

@@ -22,10 +22,11 @@ int pages_rows_grid(int B, int T, int H_kv, dim3* grid) {
     return MODA_OK;
 }
 
+constexpr long long kPagesWideMerge = 592;
 constexpr int kPagesMostCtas = 148;               // partial results of that many fit the workspace
 
 inline size_t pages_part_bytes(int B, int H, int G, int d) {
-    return (size_t(kPagesMostCtas) * kPagesDecodeWarps(d) * G + size_t(B) * H) * (d + 2) * 4;
+    return (size_t(kPagesMostCtas) * kPagesWarps * G + size_t(2) * B * H) * (d + 2) * 4;
 }
 size_t pages_workspace_bytes(int B, int H, int H_kv, int d) {
     return (pages_part_bytes(B, H, std::min(H / H_kv, 8), d) + size_t(B + 1) * 4 + 15) / 16 * 16;
@@ -74,13 +75,15 @@ int launch_decode_pages(const PagesDecodeParams& p, cudaStream_t stream) {
     int dev = 0;
     if (!cuda_ok(cudaGetDevice(&dev))) return MODA_ERR_CUDA;
     if (configured_dev != dev) {
-        if (!set_smem_limit(pages_split_kernel<D>, kPagesSplitSmem(D, kPagesMostBatch))) return MODA_ERR_CUDA;
+        if (!set_smem_limit(pages_split_kernel<D>, kPagesSplitSmem(kPagesMostBatch))) return MODA_ERR_CUDA;
         configured_dev = dev;
     }
-    if (int rc = launch_pages(pages_split_kernel<D>, dim3(unsigned(p.warps / kPagesDecodeWarps(D))), kPagesDecodeWarps(D) * 32, size_t(kPagesSplitSmem(D, p.B)),
-                              p.index != nullptr, p, stream))
+    if (int rc = launch_pages(pages_split_kernel<D>, dim3(unsigned(p.warps / kPagesWarps)), kPagesSplitThreads, size_t(kPagesSplitSmem(p.B)), p.index != nullptr, p, stream))
         return rc;
-    return launch_pages(pages_merge_kernel<D>, dim3(unsigned(p.H), unsigned(p.B)), kPagesMergeThreads, 0, true, p, stream);
+    const long long rows = (long long)p.B * p.H;
+    const bool wide = rows <= kPagesWideMerge;
+    const long long per = kPagesMergeThreads / 32 / (wide ? 4 : 1);
+    return launch_pages(wide ? pages_merge_kernel<D, 4> : pages_merge_kernel<D, 1>, dim3(unsigned((rows + per - 1) / per)), kPagesMergeThreads, 0, true, p, stream);
 }
 
 }  // namespace
@@ -181,7 +184,7 @@ int moda_attn_decode_e4m3(const void* q, const void* pages, const int* block_tab
     p.G = H / p.Hk; p.H = H; p.l = l; p.max_len = max_seq_len; p.n_index = n_blocks;
     p.part = static_cast<float*>(workspace);
     p.before = reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + pages_part_bytes(B, H, p.G, d));
-    p.warps = std::min(sms, kPagesMostCtas) * kPagesDecodeWarps(d);
+    p.warps = std::min(sms, kPagesMostCtas) * kPagesWarps;
     p.scale_log2 = scale * kDecodeLog2e;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return d == 128 ? launch_decode_pages<128>(p, st) : launch_decode_pages<64>(p, st);

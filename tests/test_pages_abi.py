@@ -29,7 +29,7 @@ def test_sizes():
         with pytest.raises(ValueError):
             moda.alloc_kv_bounds(1, *bad)
     assert moda.moda_decode_e4m3_workspace_bytes(2, 8, 2, 64) > 0
-    for bad in ((0, 8, 2, 64), (4097, 8, 2, 64), (2, 9, 2, 64), (2, 9, 1, 64), (2, 8, 2, 80)):
+    for bad in ((0, 8, 2, 64), (2049, 8, 2, 64), (2, 9, 2, 64), (2, 9, 1, 64), (2, 8, 2, 80)):
         assert moda.moda_decode_e4m3_workspace_bytes(*bad) == 0
 
 
@@ -78,7 +78,7 @@ def test_decode_validation():
         return binding.load().moda_attn_decode_e4m3(q, pages, table, lens, index, n, depth, B, T, page, pages_n, most, H, Hk, d, l, F(scale), O, LSE, work,
                                                     ctypes.c_size_t(wb), None)
 
-    for bad in (dict(B=0), dict(B=4097), dict(T=-1), dict(T=257), dict(page=65), dict(pages_n=0), dict(index=P), dict(index=P, n=1 << 30), dict(H=0)):
+    for bad in (dict(B=0), dict(B=2049), dict(T=-1), dict(T=257), dict(page=65), dict(pages_n=0), dict(index=P), dict(index=P, n=1 << 30), dict(H=0)):
         assert call(**bad) == -3, bad
     assert call(d=32) == -4 and call(H=5) == -12 and call(H=18) == -12 and call(l=-1) == -5 and call(l=257) == -5
     assert call(scale=0.0) == -13 and call(scale=float("nan")) == -13
