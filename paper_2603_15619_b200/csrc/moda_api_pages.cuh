@@ -25,8 +25,9 @@ int pages_rows_grid(int B, int T, int H_kv, dim3* grid) {
 constexpr long long kPagesWideMerge = 592;
 constexpr int kPagesMostCtas = 148;               // partial results of that many fit the workspace
 
+inline int pages_split_warps(int d) { return d == 64 ? PagesSplit<64>::kWarps : PagesSplit<128>::kWarps; }
 inline size_t pages_part_bytes(int B, int H, int G, int d) {
-    return (size_t(kPagesMostCtas) * kPagesWarps * G + size_t(2) * B * H) * (d + 2) * 4;
+    return (size_t(kPagesMostCtas) * pages_split_warps(d) * G + size_t(2) * B * H) * (d + 2) * 4;
 }
 size_t pages_workspace_bytes(int B, int H, int H_kv, int d) {
     return (pages_part_bytes(B, H, std::min(H / H_kv, 8), d) + size_t(B + 1) * 4 + 15) / 16 * 16;
@@ -75,10 +76,10 @@ int launch_decode_pages(const PagesDecodeParams& p, cudaStream_t stream) {
     int dev = 0;
     if (!cuda_ok(cudaGetDevice(&dev))) return MODA_ERR_CUDA;
     if (configured_dev != dev) {
-        if (!set_smem_limit(pages_split_kernel<D>, kPagesSplitSmem(kPagesMostBatch))) return MODA_ERR_CUDA;
+        if (!set_smem_limit(pages_split_kernel<D>, PagesSplit<D>::smem(kPagesMostBatch))) return MODA_ERR_CUDA;
         configured_dev = dev;
     }
-    if (int rc = launch_pages(pages_split_kernel<D>, dim3(unsigned(p.warps / kPagesWarps)), kPagesSplitThreads, size_t(kPagesSplitSmem(p.B)), p.index != nullptr, p, stream))
+    if (int rc = launch_pages(pages_split_kernel<D>, dim3(unsigned(p.warps / PagesSplit<D>::kWarps)), PagesSplit<D>::kThreads, size_t(PagesSplit<D>::smem(p.B)), p.index != nullptr, p, stream))
         return rc;
     const long long rows = (long long)p.B * p.H;
     const bool wide = rows <= kPagesWideMerge;
@@ -184,7 +185,7 @@ int moda_attn_decode_e4m3(const void* q, const void* pages, const int* block_tab
     p.G = H / p.Hk; p.H = H; p.l = l; p.max_len = max_seq_len; p.n_index = n_blocks;
     p.part = static_cast<float*>(workspace);
     p.before = reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + pages_part_bytes(B, H, p.G, d));
-    p.warps = std::min(sms, kPagesMostCtas) * kPagesWarps;
+    p.warps = std::min(sms, kPagesMostCtas) * pages_split_warps(d);
     p.scale_log2 = scale * kDecodeLog2e;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return d == 128 ? launch_decode_pages<128>(p, st) : launch_decode_pages<64>(p, st);

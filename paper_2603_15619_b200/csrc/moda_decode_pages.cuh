@@ -20,6 +20,7 @@
 #pragma once
 
 #include <cstdint>
+#include <type_traits>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -51,14 +52,17 @@ struct PagesDecodeParams : PagesParams {
 };
 
 constexpr int kPagesMostBatch = 2048;                                // sequences of a call: their blocks are counted in shared memory
-constexpr int kPagesWarps = 11, kPagesDepthWarps = 1;                // of a CTA, one an SM
-constexpr int kPagesSplitThreads = (kPagesWarps + kPagesDepthWarps) * 32;
-constexpr int kPagesPiece = 64 * kPageBlock;                         // bytes: 64 features of a block's keys, or of its values
-constexpr int kPagesPieces = 4;                                      // that a warp has in shared memory or on the way
-constexpr int kPagesScaleSets = 3;                                   // blocks whose scales it has there
-constexpr int kPagesWarpBytes = kPagesPieces * kPagesPiece + kPagesScaleSets * 8 * kPageBlock;
-constexpr int kPagesSplitSmem(int B) { return kPagesWarps * kPagesWarpBytes + (B + 1) * 4; }
-static_assert(kPagesSplitSmem(kPagesMostBatch) + 4096 <= 232448, "shared memory");
+template <int D>
+struct PagesSplit {
+    static constexpr int kWarps = D == 64 ? 9 : 8, kDepthWarps = D == 64 ? 3 : 4;   // of a CTA, one an SM
+    static constexpr int kThreads = (kWarps + kDepthWarps) * 32;
+    static constexpr int kPiece = kPageBlock * D;                    // bytes: a block's key codes, or its value codes
+    static constexpr int kPieces = D == 64 ? 4 : 3;                  // that a warp has in shared memory or on the way
+    static constexpr int kScaleSets = D == 64 ? 3 : 2;               // blocks whose scales it has there
+    static constexpr int kWarpBytes = kPieces * kPiece + kScaleSets * 8 * kPageBlock;
+    static constexpr int smem(int B) { return kWarps * kWarpBytes + (B + 1) * 4; }
+    static_assert(smem(kPagesMostBatch) + 4096 <= 232448, "shared memory");
+};
 constexpr int kPagesMergeThreads = 128;
 
 __device__ __forceinline__ void mma_f16_16x8x16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -71,6 +75,13 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
+// An 8 x 8 matrix of 16-bit numbers, two adjacent ones of a row a lane, turned.
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
 // Where a warp is in the order of all units.
 struct PagesWalk {
     int b, r, j, n;               // sequence, group of it, unit of that group, units of a group of this sequence
@@ -117,27 +128,37 @@ __device__ __forceinline__ void pages_depth(const PagesDecodeParams& p, int b, i
     for (int h = 0; h < 8; ++h)
 #pragma unroll
         for (int c = 0; c < FPL; ++c) acc[h][c] = 0.f;
+    constexpr int BATCH = 64 / FPL;                                  // value rows that are on their way together
+    using Row = typename std::conditional<FPL == 4, uint2, uint32_t>::type;
 #pragma unroll 1
     for (int i0 = 0; i0 < p.l; i0 += SLOTS) {
         const int n_slot = min(p.l - i0, SLOTS);
+        uint4 k[4][D / 32];                                          // rows past the last slot are that one's again
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            const uint4* row = reinterpret_cast<const uint4*>(depth0 + size_t(i0 + min(8 * n + g, n_slot - 1)) * stride);
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) k[n][i] = row[4 * i + t];
+        }
+        Row v[BATCH];
+        auto load_v = [&](int j0) {
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) v[j] = *reinterpret_cast<const Row*>(depth0 + size_t(i0 + min(j0 + j, n_slot - 1)) * stride + D + lane * FPL);
+        };
+        if (FPL == 2) load_v(0);                                     // (both at once are more than the registers hold at d = 128)
         float s[4][2];
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
             float c[4] = {0.f, 0.f, 0.f, 0.f};
-            if (8 * n < n_slot) {
-                const uint4* row = reinterpret_cast<const uint4*>(depth0 + size_t(i0 + min(8 * n + g, n_slot - 1)) * stride);
-                uint4 k[D / 32];
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i) k[i] = row[4 * i + t];
-#pragma unroll
-                for (int i = 0; i < D / 32; ++i) {
-                    mma_bf16_16x8x16(c, q[i].x, 0u, q[i].y, 0u, k[i].x, k[i].y);
-                    mma_bf16_16x8x16(c, q[i].z, 0u, q[i].w, 0u, k[i].z, k[i].w);
-                }
+            for (int i = 0; i < D / 32; ++i) {
+                mma_bf16_16x8x16(c, q[i].x, 0u, q[i].y, 0u, k[n][i].x, k[n][i].y);
+                mma_bf16_16x8x16(c, q[i].z, 0u, q[i].w, 0u, k[n][i].z, k[n][i].w);
             }
             s[n][0] = 8 * n + 2 * t < n_slot ? c[0] * p.scale_log2 : -INFINITY;
             s[n][1] = 8 * n + 2 * t + 1 < n_slot ? c[1] * p.scale_log2 : -INFINITY;
         }
+        if (FPL == 4) load_v(0);
         float top = m;
 #pragma unroll
         for (int n = 0; n < 4; ++n) top = fmaxf(top, fmaxf(s[n][0], s[n][1]));
@@ -162,23 +183,26 @@ __device__ __forceinline__ void pages_depth(const PagesDecodeParams& p, int b, i
 #pragma unroll
             for (int c = 0; c < FPL; ++c) acc[h][c] *= f;
         }
-#pragma unroll 8
-        for (int i = 0; i < n_slot; ++i) {
-            const __nv_bfloat16* row = depth0 + size_t(i0 + i) * stride + D + lane * FPL;
-            float v[FPL];
-            if constexpr (FPL == 4) {
-                const uint2 x = *reinterpret_cast<const uint2*>(row);
-                v[0] = bf16_lo_to_f32(x.x); v[1] = bf16_hi_to_f32(x.x); v[2] = bf16_lo_to_f32(x.y); v[3] = bf16_hi_to_f32(x.y);
-            } else {
-                const uint32_t x = *reinterpret_cast<const uint32_t*>(row);
-                v[0] = bf16_lo_to_f32(x); v[1] = bf16_hi_to_f32(x);
+#pragma unroll
+        for (int j0 = 0; j0 < SLOTS; j0 += BATCH) {
+            if (j0 >= n_slot) break;
+            if (j0 > 0) load_v(j0);
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) {
+                if (j0 + j >= n_slot) break;
+                float x[FPL];
+                if constexpr (FPL == 4) {
+                    x[0] = bf16_lo_to_f32(v[j].x); x[1] = bf16_hi_to_f32(v[j].x); x[2] = bf16_lo_to_f32(v[j].y); x[3] = bf16_hi_to_f32(v[j].y);
+                } else {
+                    x[0] = bf16_lo_to_f32(v[j]); x[1] = bf16_hi_to_f32(v[j]);
+                }
+                const float4 w0 = *reinterpret_cast<const float4*>(&s_w[j0 + j][0]), w1 = *reinterpret_cast<const float4*>(&s_w[j0 + j][4]);
+                const float w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+#pragma unroll
+                for (int h = 0; h < 8; ++h)
+#pragma unroll
+                    for (int c = 0; c < FPL; ++c) acc[h][c] = fmaf(w[h], x[c], acc[h][c]);
             }
-            const float4 w0 = *reinterpret_cast<const float4*>(&s_w[i][0]), w1 = *reinterpret_cast<const float4*>(&s_w[i][4]);
-            const float w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
-#pragma unroll
-            for (int h = 0; h < 8; ++h)
-#pragma unroll
-                for (int c = 0; c < FPL; ++c) acc[h][c] = fmaf(w[h], v[c], acc[h][c]);
         }
     }
     sum += __shfl_xor_sync(0xffffffffu, sum, 1);
@@ -193,22 +217,23 @@ __device__ __forceinline__ void pages_depth(const PagesDecodeParams& p, int b, i
 }
 
 template <int D>
-__global__ void __launch_bounds__(kPagesSplitThreads, 1)
+__global__ void __launch_bounds__(PagesSplit<D>::kThreads, 1)
 pages_split_kernel(const PagesDecodeParams p) {
-    constexpr int NW = kPagesWarps;
-    constexpr int KP = D / 64, FB = D / 16;                          // 64-feature parts of keys and values; 16-feature rows of the value product
-    constexpr int AHEAD = kPagesPieces / (2 * KP);                   // units that the ring is ahead
+    using L = PagesSplit<D>;
+    constexpr int NW = L::kWarps, NP = L::kPieces, PIECE = L::kPiece;
+    constexpr int KP = D / 64, FB = D / 16, CH = D / 16;             // 64-feature parts of a key; 16-feature rows of the value product; 16-byte pieces of a key
+    constexpr int AHEAD = (1 + NP) / 2;                              // units that the ring is ahead, at most
     extern __shared__ __align__(16) uint8_t split_smem[];
-    int* s_before = reinterpret_cast<int*>(split_smem + NW * kPagesWarpBytes);      // [B + 1]
+    int* s_before = reinterpret_cast<int*>(split_smem + NW * L::kWarpBytes);      // [B + 1]
     __shared__ int s_sum[NW];
-    __shared__ __align__(16) float s_w[kPagesDepthWarps][32][8];
+    __shared__ __align__(16) float s_w[L::kDepthWarps][32][8];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int g = lane >> 2, t = lane & 3;
     if (p.index) grid_dependency_wait();                             // launched beside what comes before it in the stream
     if (warp >= NW) {
-        // ---- two warps for the depth pairs ----
+        // ---- warps for the depth pairs ----
         const int groups = p.l > 0 ? p.B * p.Hk : 0;
-        for (int i = (warp - NW) * gridDim.x + blockIdx.x; i < groups; i += kPagesDepthWarps * gridDim.x)
+        for (int i = (warp - NW) * gridDim.x + blockIdx.x; i < groups; i += L::kDepthWarps * gridDim.x)
             pages_depth<D>(p, i / p.Hk, i % p.Hk, s_w[warp - NW], p.part + (size_t(p.warps) + size_t(p.B) * p.Hk + i) * p.G * (D + 2), lane);
         return;
     }
@@ -242,10 +267,10 @@ pages_split_kernel(const PagesDecodeParams p) {
     if (w >= runs) return;
     const int first = int(total * w / runs), n_unit = int(total * (w + 1) / runs) - first;
 
-    // ---- the ring: pieces (64 features of a unit's keys, then of its values) in order, three on their way while one is worked on ----
-    uint8_t* ring = split_smem + warp * kPagesWarpBytes;
+    // ---- the ring: pieces (a unit's keys, then its values) in order, the next ones on their way while one is worked on ----
+    uint8_t* ring = split_smem + warp * L::kWarpBytes;
     const uint32_t ring_u32 = smem_u32(ring);
-    float* scales = reinterpret_cast<float*>(ring + kPagesPieces * kPagesPiece);    // [kPagesScaleSets][128], of consecutive units
+    float* scales = reinterpret_cast<float*>(ring + NP * PIECE);     // [kScaleSets][128], of consecutive units
     PagesWalk ahead;                                                 // the unit that is looked up next
     ahead.begin(s_before, p.B, p.Hk, first);
     PagesWalk at = ahead;                                            // the one in work
@@ -263,19 +288,20 @@ pages_split_kernel(const PagesDecodeParams p) {
         if (--left > 0) ahead.next(s_before, p.Hk);
         return x;
     };
-    // Piece `i` of a unit (0 .. KP - 1: keys, then values) into its slot of the ring.
-    auto request = [&](const uint8_t* rec, int unit, int i) {
+    // The keys (i = 0) or the values of a unit into a slot of the ring.  16-byte piece c of key row r lies at c ^ 4 (r % 2) where a row has 8, so that two
+    // adjacent rows of four lanes each are in different banks.
+    auto request = [&](const uint8_t* rec, int unit, int i, int slot) {
         if (rec) {
-            const uint32_t dst = ring_u32 + (unit % AHEAD * 2 * KP + i) * kPagesPiece + lane * 16;
-            if (i < KP) {
-                const uint8_t* src = rec + (lane >> 2) * D + 64 * i + 16 * (lane & 3);
+            const uint32_t dst = ring_u32 + slot * PIECE;
+            if (i == 0) {
+                const int r = lane / CH, c = lane % CH;
+                const uint32_t to = dst + r * D + 16 * (D == 128 ? c ^ ((r & 1) << 2) : c);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) cp_async_16(dst + k * 512, src + k * 8 * D);
-                if (i == 0) cp_async_16(smem_u32(scales) + unit % kPagesScaleSets * 512 + lane * 16, rec + 2 * kPageBlock * D + lane * 16);
+                for (int k = 0; k < PIECE / 512; ++k) cp_async_16(to + k * 512, rec + k * 512 + lane * 16);
+                cp_async_16(smem_u32(scales) + unit % L::kScaleSets * 512 + lane * 16, rec + 2 * PIECE + lane * 16);
             } else {
-                const uint8_t* src = rec + kPageBlock * D + (i - KP) * kPagesPiece + lane * 16;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) cp_async_16(dst + k * 512, src + k * 512);
+                for (int k = 0; k < PIECE / 512; ++k) cp_async_16(dst + k * 512 + lane * 16, rec + PIECE + k * 512 + lane * 16);
             }
         }
         cp_async_commit();
@@ -284,13 +310,17 @@ pages_split_kernel(const PagesDecodeParams p) {
 #pragma unroll
     for (int i = 0; i <= AHEAD; ++i) {
         place[i] = left > 0 ? look_up(block_of()) : Place{nullptr, 0};
-        if (i < AHEAD)
-#pragma unroll
-            for (int k = 0; k < 2 * KP; ++k) request(place[i].rec, i, k);
+        if (2 * i < NP) request(place[i].rec, i, 0, 2 * i);
+        if (2 * i + 1 < NP) request(place[i].rec, i, 1, 2 * i + 1);
     }
+    int slot = 0;                                                    // of the piece in work, which the one NP behind it takes over
+    auto pass_on = [&](int u, int i) {
+        request(place[(i + NP) / 2].rec, u + (i + NP) / 2, (i + NP) % 2, slot);
+        slot = slot + 1 == NP ? 0 : slot + 1;
+    };
 
     uint32_t qf[KP][8];                                              // this lane's features of head g, f16
-    float q_scale;                                                   // their power of two, times scale log2(e)
+    float q_scale[2];                                                // scale log2(e) over the power of two of heads 2 t, 2 t + 1
     auto load_q = [&]() {
         uint4 v[KP][2];
         float most = 0.f;
@@ -313,7 +343,9 @@ pages_split_kernel(const PagesDecodeParams p) {
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
         const int e = max(int(__float_as_uint(most) >> 23), 20) - 127;          // most < 2^(e + 1): times 2^(14 - e), below 2^15
         const float up = __uint_as_float(uint32_t(127 + 14 - e) << 23);
-        q_scale = p.scale_log2 * __uint_as_float(uint32_t(127 - 14 + e) << 23);
+        const float down = p.scale_log2 * __uint_as_float(uint32_t(127 - 14 + e) << 23);
+        q_scale[0] = __shfl_sync(0xffffffffu, down, 8 * t);
+        q_scale[1] = __shfl_sync(0xffffffffu, down, 8 * t + 4);
 #pragma unroll
         for (int i = 0; i < KP; ++i)
 #pragma unroll
@@ -325,124 +357,135 @@ pages_split_kernel(const PagesDecodeParams p) {
     };
     load_q();
 
-    float m = -INFINITY, mw = -INFINITY, sum = 0.f;                  // of head g: maxima of the scores and of the weights' exponents, row sum (this lane's keys)
+    // of heads 2 t, 2 t + 1: maxima of the scores and of the weights' exponents, row sums (this lane's keys)
+    float m[2] = {-INFINITY, -INFINITY}, mw[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
     float o[FB][4];                                                  // features 16 f + g (c0 c1) and + 8 (c2 c3) of heads 2 t, 2 t + 1
 #pragma unroll
     for (int f = 0; f < FB; ++f) { o[f][0] = 0.f; o[f][1] = 0.f; o[f][2] = 0.f; o[f][3] = 0.f; }
 #pragma unroll 1
     for (int u = 0; u < n_unit; ++u) {
         const int rows = place[0].rows;
-        const uint8_t* then = place[AHEAD].rec;                      // of unit u + AHEAD
-        const int blk = left > 0 ? block_of() : 0;                   // of the one behind it
-        const uint8_t* mine = ring + u % AHEAD * 2 * KP * kPagesPiece;
-        float* own = scales + u % kPagesScaleSets * 128;
-        float c[8][4];                                               // eight products side by side: each waits for the one before it in its sum
+        const int blk = left > 0 ? block_of() : 0;                   // of unit u + AHEAD + 1
+        float* own = scales + u % L::kScaleSets * 128;
+        float c[4][4];                                               // of keys a = 16 (g / 2) + 4 j + g % 2 and a + 2: heads 2 t, 2 t + 1 of either
 #pragma unroll
-        for (int n = 0; n < 8; ++n) { c[n][0] = 0.f; c[n][1] = 0.f; c[n][2] = 0.f; c[n][3] = 0.f; }
-#pragma unroll
-        for (int i = 0; i < KP; ++i) {
-            cp_async_wait<kPagesPieces - 1>();
-            __syncwarp();
-            if (rows > 0) {
-                if (i == 0) {
-                    const float2 v = *reinterpret_cast<const float2*>(own + kPageBlock + 2 * lane);
-                    *reinterpret_cast<float2*>(own + kPageBlock + 2 * lane) = make_float2(__log2f(v.x), __log2f(v.y));
-                }
-#pragma unroll
-                for (int n0 = 0; n0 < 8; n0 += 4) {
-                    uint4 x[4];
-#pragma unroll
-                    for (int n = 0; n < 4; ++n) x[n] = *reinterpret_cast<const uint4*>(mine + i * kPagesPiece + (16 * (g >> 1) + 2 * (n0 + n) + (g & 1)) * 64 + 16 * t);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-#pragma unroll
-                        for (int n = 0; n < 4; ++n) {
-                            uint32_t b0, b1;
-                            e4m3x4_to_f16(k == 0 ? x[n].x : k == 1 ? x[n].y : k == 2 ? x[n].z : x[n].w, b0, b1);
-                            mma_f16_16x8x16(c[n0 + n], qf[i][2 * k], 0u, qf[i][2 * k + 1], 0u, b0, b1);
-                        }
-                }
-            }
-            __syncwarp();                                            // everyone has read the piece; the logarithms are there
-            request(then, u + AHEAD, i);
-        }
-        uint32_t pw[8];                                              // weights of keys 16 t + 2 n, + 1
+        for (int j = 0; j < 4; ++j) { c[j][0] = 0.f; c[j][1] = 0.f; c[j][2] = 0.f; c[j][3] = 0.f; }
+        cp_async_wait<NP - 1>();
+        __syncwarp();
         if (rows > 0) {
-            float s[8][2], x[8][2];                                  // scores over q_scale; log2 of the values' scales, then the weights' exponents
+            {
+                // scales in the order in which the lanes have the keys: [2 (key / 16) + key % 2][key % 16 / 2]; of the values, their logarithms
+                const float2 k = *reinterpret_cast<const float2*>(own + 2 * lane), v = *reinterpret_cast<const float2*>(own + kPageBlock + 2 * lane);
+                __syncwarp();
+                float* to = own + (lane >> 3) * 16 + (lane & 7);
+                to[0] = k.x;
+                to[8] = k.y;
+                to[kPageBlock] = __log2f(v.x);
+                to[kPageBlock + 8] = __log2f(v.y);
+            }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float4 a = *reinterpret_cast<const float4*>(own + 16 * t + 4 * i);
-                const float4 y = *reinterpret_cast<const float4*>(own + kPageBlock + 16 * t + 4 * i);
-                s[2 * i][0] = c[2 * i][0] * a.x; s[2 * i][1] = c[2 * i][1] * a.y;
-                s[2 * i + 1][0] = c[2 * i + 1][0] * a.z; s[2 * i + 1][1] = c[2 * i + 1][1] * a.w;
-                x[2 * i][0] = y.x; x[2 * i][1] = y.y; x[2 * i + 1][0] = y.z; x[2 * i + 1][1] = y.w;
+            for (int i = 0; i < KP; ++i) {
+                const uint8_t* row = ring + slot * PIECE + (16 * (g >> 1) + (g & 1)) * D + 16 * (D == 128 ? (4 * i + t) ^ ((g & 1) << 2) : t);
+                uint4 x[4], y[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    x[j] = *reinterpret_cast<const uint4*>(row + 4 * j * D);
+                    y[j] = *reinterpret_cast<const uint4*>(row + (4 * j + 2) * D);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t a0, a1, a2, a3;
+                        e4m3x4_to_f16(k == 0 ? x[j].x : k == 1 ? x[j].y : k == 2 ? x[j].z : x[j].w, a0, a2);
+                        e4m3x4_to_f16(k == 0 ? y[j].x : k == 1 ? y[j].y : k == 2 ? y[j].z : y[j].w, a1, a3);
+                        mma_f16_16x8x16(c[j], a0, a1, a2, a3, qf[i][2 * k], qf[i][2 * k + 1]);
+                    }
+            }
+        }
+        __syncwarp();                                                // everyone has read the keys; the scales are in order
+        pass_on(u, 0);
+        uint32_t pw[8];                                              // weights of keys 16 t + 4 j, + 1 (and + 2, + 3) of head g
+        if (rows > 0) {
+            float s[8][2], x[8];                                     // scores of this lane's keys a, a + 2, ..; log2 of the values' scales
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float4 a = *reinterpret_cast<const float4*>(own + 8 * g + 4 * i);
+                const float4 y = *reinterpret_cast<const float4*>(own + kPageBlock + 8 * g + 4 * i);
+                const float sk[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    s[4 * i + j][0] = c[2 * i + j / 2][2 * (j & 1)] * sk[j] * q_scale[0];
+                    s[4 * i + j][1] = c[2 * i + j / 2][2 * (j & 1) + 1] * sk[j] * q_scale[1];
+                }
+                x[4 * i] = y.x; x[4 * i + 1] = y.y; x[4 * i + 2] = y.z; x[4 * i + 3] = y.w;
             }
             if (rows < kPageBlock) {                                 // what lies past the last key may hold anything
 #pragma unroll
-                for (int n = 0; n < 8; ++n)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        if (16 * t + 2 * n + i >= rows) { s[n][i] = -INFINITY; x[n][i] = 0.f; }
+                for (int j = 0; j < 8; ++j)
+                    if (16 * (g >> 1) + (g & 1) + 2 * j >= rows) { s[j][0] = s[j][1] = -INFINITY; x[j] = 0.f; }
             }
-            float mx = -INFINITY, mxw = -INFINITY;
+            float f[2], base[2], base_w[2], part[2] = {0.f, 0.f};
+            bool moved = false;
 #pragma unroll
-            for (int n = 0; n < 8; ++n)
+            for (int h = 0; h < 2; ++h) {
+                float mx = s[0][h], mxw = s[0][h] + x[0];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    s[n][i] *= q_scale;
-                    x[n][i] += s[n][i];
-                    mx = fmaxf(mx, s[n][i]);
-                    mxw = fmaxf(mxw, x[n][i]);
+                for (int j = 1; j < 8; ++j) { mx = fmaxf(mx, s[j][h]); mxw = fmaxf(mxw, s[j][h] + x[j]); }
+#pragma unroll
+                for (int off = 4; off < 32; off <<= 1) {
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+                    mxw = fmaxf(mxw, __shfl_xor_sync(0xffffffffu, mxw, off));
                 }
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-            mxw = fmaxf(mxw, __shfl_xor_sync(0xffffffffu, mxw, 1));
-            mx = fmaxf(m, fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2)));
-            mxw = fmaxf(mw, fmaxf(mxw, __shfl_xor_sync(0xffffffffu, mxw, 2)));
-            const float base = mx == -INFINITY ? 0.f : mx, alpha = fast_exp2(m - base);
-            const float base_w = mxw == -INFINITY ? 0.f : mxw - 14.f, alpha_w = fast_exp2(mw - mxw);
-            float part = 0.f;
-#pragma unroll
-            for (int n = 0; n < 8; ++n) {
-                part += fast_exp2(s[n][0] - base) + fast_exp2(s[n][1] - base);
-                pw[n] = pack_f16x2(fast_exp2(x[n][0] - base_w), fast_exp2(x[n][1] - base_w));
+                mx = fmaxf(m[h], mx);
+                mxw = fmaxf(mw[h], mxw);
+                base[h] = mx == -INFINITY ? 0.f : mx;
+                base_w[h] = mxw == -INFINITY ? 0.f : mxw - 14.f;
+                sum[h] *= fast_exp2(m[h] - base[h]);
+                f[h] = mw[h] != mxw && mw[h] != -INFINITY ? fast_exp2(mw[h] - mxw) : 1.f;
+                moved |= f[h] != 1.f;
+                m[h] = mx;
+                mw[h] = mxw;
             }
-            sum = sum * alpha + part;
-            const bool moved = mw != mxw && mw != -INFINITY;
-            m = mx;
-            mw = mxw;
-            if (__any_sync(0xffffffffu, moved)) {
-                const float f = moved ? alpha_w : 1.f;
-                const float a0 = __shfl_sync(0xffffffffu, f, 8 * t), a1 = __shfl_sync(0xffffffffu, f, 8 * t + 4);
 #pragma unroll
-                for (int i = 0; i < FB; ++i) { o[i][0] *= a0; o[i][1] *= a1; o[i][2] *= a0; o[i][3] *= a1; }
+            for (int j = 0; j < 8; ++j) {
+                part[0] += fast_exp2(s[j][0] - base[0]);
+                part[1] += fast_exp2(s[j][1] - base[1]);
+                pw[j] = transpose_8x8(pack_f16x2(fast_exp2(s[j][0] + x[j] - base_w[0]), fast_exp2(s[j][1] + x[j] - base_w[1])));
+            }
+            sum[0] += part[0];
+            sum[1] += part[1];
+            if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+                for (int i = 0; i < FB; ++i) { o[i][0] *= f[0]; o[i][1] *= f[1]; o[i][2] *= f[0]; o[i][3] *= f[1]; }
             }
         }
         const bool leaves = u + 1 < n_unit && at.j + 1 == at.n;
         Place behind = left > 0 ? look_up(blk) : Place{nullptr, 0};
+        cp_async_wait<NP - 1>();
+        __syncwarp();
+        if (rows > 0) {
+            uint8_t* sv = ring + slot * PIECE;
+            if (rows < kPageBlock) {                                 // value codes past the last key: zero, their weights are 0
+                for (int e = lane; e < PIECE / 16; e += 32) {
+                    uint4* at16 = reinterpret_cast<uint4*>(sv) + e;
+                    uint32_t word[4] = {at16->x, at16->y, at16->z, at16->w};
 #pragma unroll
-        for (int i = 0; i < KP; ++i) {
-            cp_async_wait<kPagesPieces - 1>();
-            __syncwarp();
-            uint8_t* sv = ring + (u % AHEAD * 2 * KP + KP + i) * kPagesPiece;
-            if (rows > 0) {
-                if (rows < kPageBlock) {                             // value codes past the last key: zero, their weights are 0
-                    for (int e = lane; e < kPagesPiece / 16; e += 32) {
-                        uint4* at16 = reinterpret_cast<uint4*>(sv) + e;
-                        uint32_t word[4] = {at16->x, at16->y, at16->z, at16->w};
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const int some = min(max(rows - 16 * (e & 3) - 4 * k, 0), 4);
-                            word[k] = some == 4 ? word[k] : word[k] & ((1u << (8 * some)) - 1u);
-                        }
-                        *at16 = make_uint4(word[0], word[1], word[2], word[3]);
+                    for (int k = 0; k < 4; ++k) {
+                        const int some = min(max(rows - 16 * (e & 3) - 4 * k, 0), 4);
+                        word[k] = some == 4 ? word[k] : word[k] & ((1u << (8 * some)) - 1u);
                     }
-                    __syncwarp();
+                    *at16 = make_uint4(word[0], word[1], word[2], word[3]);
                 }
+                __syncwarp();
+            }
+#pragma unroll
+            for (int f0 = 0; f0 < FB; f0 += 4) {
                 uint4 x[4], y[4];
 #pragma unroll
                 for (int f = 0; f < 4; ++f) {
-                    x[f] = *reinterpret_cast<const uint4*>(sv + (16 * f + g) * kPageBlock + 16 * t);
-                    y[f] = *reinterpret_cast<const uint4*>(sv + (16 * f + 8 + g) * kPageBlock + 16 * t);
+                    x[f] = *reinterpret_cast<const uint4*>(sv + (16 * (f0 + f) + g) * kPageBlock + 16 * t);
+                    y[f] = *reinterpret_cast<const uint4*>(sv + (16 * (f0 + f) + 8 + g) * kPageBlock + 16 * t);
                 }
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
@@ -451,39 +494,39 @@ pages_split_kernel(const PagesDecodeParams p) {
                         uint32_t a0, a1, a2, a3;
                         e4m3x4_to_f16(k == 0 ? x[f].x : k == 1 ? x[f].y : k == 2 ? x[f].z : x[f].w, a0, a2);
                         e4m3x4_to_f16(k == 0 ? y[f].x : k == 1 ? y[f].y : k == 2 ? y[f].z : y[f].w, a1, a3);
-                        mma_f16_16x8x16(o[4 * i + f], a0, a1, a2, a3, pw[2 * k], pw[2 * k + 1]);
+                        mma_f16_16x8x16(o[f0 + f], a0, a1, a2, a3, pw[2 * k], pw[2 * k + 1]);
                     }
             }
-            __syncwarp();                                            // everyone has read the piece
-            request(then, u + AHEAD, KP + i);
         }
+        __syncwarp();                                                // everyone has read the values
+        pass_on(u, 1);
         if (u + AHEAD + 1 >= n_unit) grid_launch_dependents();       // all loads are on their way: the merge may come up
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) place[i] = place[i + 1];
         place[AHEAD] = behind;
         if (leaves || u + 1 == n_unit) {
             // ---- the group's partial result of this warp ----
-            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
             float* out = p.part + (size_t(w) + size_t(at.b) * p.Hk + at.r) * p.G * (D + 2);
-            // the weighted sums are relative to 2^(mw - 14), the row sum to 2^m
-            const float f = mw == -INFINITY ? 0.f : fast_exp2(mw - 14.f - m);
-            const float a0 = __shfl_sync(0xffffffffu, f, 8 * t), a1 = __shfl_sync(0xffffffffu, f, 8 * t + 4);
-            if (t == 0 && g < p.G) *reinterpret_cast<float2*>(out + g * (D + 2)) = make_float2(m, sum);
 #pragma unroll
-            for (int i = 0; i < FB; ++i) {
-                if (2 * t < p.G) {
-                    out[2 * t * (D + 2) + 2 + 16 * i + g] = o[i][0] * a0;
-                    out[2 * t * (D + 2) + 2 + 16 * i + 8 + g] = o[i][2] * a0;
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int off = 4; off < 32; off <<= 1) sum[h] += __shfl_xor_sync(0xffffffffu, sum[h], off);
+                if (2 * t + h < p.G) {
+                    float* to = out + (2 * t + h) * (D + 2);
+                    if (g == 0) *reinterpret_cast<float2*>(to) = make_float2(m[h], sum[h]);
+                    // the weighted sums are relative to 2^(mw - 14), the row sum to 2^m
+                    const float f = mw[h] == -INFINITY ? 0.f : fast_exp2(mw[h] - 14.f - m[h]);
+#pragma unroll
+                    for (int i = 0; i < FB; ++i) {
+                        to[2 + 16 * i + g] = o[i][h] * f;
+                        to[2 + 16 * i + 8 + g] = o[i][2 + h] * f;
+                    }
                 }
-                if (2 * t + 1 < p.G) {
-                    out[(2 * t + 1) * (D + 2) + 2 + 16 * i + g] = o[i][1] * a1;
-                    out[(2 * t + 1) * (D + 2) + 2 + 16 * i + 8 + g] = o[i][3] * a1;
-                }
-                o[i][0] = 0.f; o[i][1] = 0.f; o[i][2] = 0.f; o[i][3] = 0.f;
+                m[h] = mw[h] = -INFINITY;
+                sum[h] = 0.f;
             }
-            m = mw = -INFINITY;
-            sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < FB; ++i) { o[i][0] = 0.f; o[i][1] = 0.f; o[i][2] = 0.f; o[i][3] = 0.f; }
         }
         if (u + 1 < n_unit) {
             at.next(s_before, p.Hk);
