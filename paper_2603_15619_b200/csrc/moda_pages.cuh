@@ -67,11 +67,27 @@ __device__ __forceinline__ void turn4x4(uint32_t& a, uint32_t& b, uint32_t& c, u
     d = __byte_perm(ab1, cd1, 0x7632);
 }
 
-// The correctly rounded x / d, but for the sign of a zero, with r = RN(1 / d): q = RN(x r) corrected by its exact remainder (Markstein's theorem, as div_rn in
-// moda_cache.cuh).  Nothing may underflow on the way, and d's significand must not be all ones.
-__device__ __forceinline__ float div_by(float x, float d, float r) {
-    const float q = x * r;
-    return fmaf(fmaf(-q, d, x), r, q);
+// Instructions that take two fp32 numbers in a 64-bit register (pair_f32), or three: the write kernel is bound by the instructions that it issues.
+__device__ __forceinline__ void unpair_f32(uint64_t x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
+__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {           // NaN if one of them is
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float min3(float a, float b, float c) {
+    float r;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
 }
 __device__ __forceinline__ uint32_t times_bf16x2(uint32_t a, uint32_t b) {
     uint32_t r;
@@ -79,22 +95,24 @@ __device__ __forceinline__ uint32_t times_bf16x2(uint32_t a, uint32_t b) {
     return r;
 }
 
-// 16 features of a row that LANES adjacent lanes hold: their codes and the row's scale.  The depth cache's rule and bytes, in fewer instructions, of which the
-// write kernel is made (quantise a prompt of 65536 rows of 8 heads, d = 128: 129 us with div_rn and its slow path for every element): no element has a branch, as
-// rows of which it would need one are brought into range first (exactly, by a power of two; or by 0, which makes of a row with an infinite element what the division
-// by infinity would), and signs come from the input's words.  A scale's significand, m / 7 of 128 <= m < 256, is never all ones.
+// 16 features of a row that LANES adjacent lanes hold: their codes and the row's scale.  The depth cache's rule and bytes, in fewer instructions: quotients two at a
+// time, q = RN(x r) with r = RN(1 / d) corrected by its exact remainder (Markstein's theorem, as div_rn in moda_cache.cuh; a scale's significand, m / 7 of 128 <= m < 256, is
+// never all ones); no element has a branch, as rows of which it would need one are brought into range first (exactly, by a power of two; or by 0, which makes of a row
+// with an infinite element what the division by infinity would), and signs come from the input's words.
 template <int LANES>
 __device__ __forceinline__ uint4 quantise_row16(const uint4& lo, const uint4& hi, float& scale) {
     uint32_t w8[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-    uint32_t most2 = 0u, sign[4];                                    // largest of either half; NaN counts for nothing
+    uint32_t most2 = w8[0], sign[4];                                 // largest magnitude of either half; NaN counts for nothing
 #pragma unroll
-    for (int k = 0; k < 8; ++k) asm("max.bf16x2 %0, %0, %1;" : "+r"(most2) : "r"(w8[k] & 0x7fff7fffu));
+    for (int k = 1; k < 8; ++k) asm("max.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(most2) : "r"(w8[k]));
 #pragma unroll
-    for (int k = 0; k < 4; ++k) sign[k] = __byte_perm(w8[2 * k], w8[2 * k + 1], 0x7531) & 0x80808080u;
-    float am = fmaxf(bf16_lo_to_f32(most2), bf16_hi_to_f32(most2));
+    for (int k = 0; k < 4; ++k) sign[k] = __byte_perm(w8[2 * k], w8[2 * k + 1], 0x7531);
+    float am = fmaxf(fabsf(bf16_lo_to_f32(most2)), fabsf(bf16_hi_to_f32(most2)));
+    am = fmaxf(am, 0.f);                                             // 0 where all are NaN
 #pragma unroll
     for (int off = 1; off < LANES; off <<= 1) am = fmaxf(am, __shfl_xor_sync(0xffffffffu, am, off));
-    scale = div_by(am, 448.f, 1.f / 448.f);
+    const float q0 = am * (1.f / 448.f);
+    scale = fmaf(fmaf(-q0, 448.f, am), 1.f / 448.f, q0);
     float d = scale;
     constexpr float kTiny = 8.271806125530277e-25f;                  // 2^-80
     if (__any_sync(0xffffffffu, !(am >= kTiny && am < INFINITY))) {
@@ -108,15 +126,19 @@ __device__ __forceinline__ uint4 quantise_row16(const uint4& lo, const uint4& hi
         for (int k = 0; k < 8; ++k) w8[k] = times_bf16x2(w8[k], factor);
     }
     const float r = __frcp_rn(d);
+    const uint64_t r2 = pair_f32(r, r), d2 = pair_f32(-d, -d);
     uint32_t w[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        uint32_t a, b;
-        asm("{\n.reg .b16 t;\ncvt.rn.satfinite.e4m3x2.f32 t, %1, %2;\nmov.b32 %0, {t, 0};\n}\n"
-            : "=r"(a) : "f"(div_by(bf16_hi_to_f32(w8[2 * k]), d, r)), "f"(div_by(bf16_lo_to_f32(w8[2 * k]), d, r)));
-        asm("{\n.reg .b16 t;\ncvt.rn.satfinite.e4m3x2.f32 t, %1, %2;\nmov.b32 %0, {t, 0};\n}\n"
-            : "=r"(b) : "f"(div_by(bf16_hi_to_f32(w8[2 * k + 1]), d, r)), "f"(div_by(bf16_lo_to_f32(w8[2 * k + 1]), d, r)));
-        w[k] = __byte_perm(a, b, 0x5410) | sign[k];
+        uint32_t half[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint64_t x = pair_f32(bf16_lo_to_f32(w8[2 * k + i]), bf16_hi_to_f32(w8[2 * k + i])), q = mul_f32x2(x, r2);
+            float a, b;
+            unpair_f32(fma_f32x2(fma_f32x2(q, d2, x), r2, q), a, b);
+            asm("{\n.reg .b16 t;\ncvt.rn.satfinite.e4m3x2.f32 t, %1, %2;\nmov.b32 %0, {t, 0};\n}\n" : "=r"(half[i]) : "f"(b), "f"(a));
+        }
+        w[k] = (__byte_perm(half[0], half[1], 0x5410) & 0x7f7f7f7fu) | (sign[k] & 0x80808080u);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
@@ -161,8 +183,8 @@ pages_write_kernel(const PagesRowsParams p) {
     constexpr int KW = D / 4 + 4;                                    // words of a row of codes in shared memory, padded by 16 bytes
     constexpr int SETS = kPagesThreads / (D / 4);                    // threads that share four features of the bounds
     __shared__ __align__(16) uint32_t s_k[kPageBlock][KW], s_v[kPageBlock][KW];
-    __shared__ float s_scale[kPageBlock], s_hi[SETS][D], s_lo[SETS][D], s_most[kPagesThreads / 32];
-    __shared__ int s_bad;
+    __shared__ __align__(16) float s_scale[kPageBlock], s_ext[2][SETS][D];   // largest and smallest of a set of rows
+    __shared__ uint32_t s_most[kPagesThreads / 32];
     const int b = blockIdx.z, hk = blockIdx.y, tid = threadIdx.x;
     PagesRows w;
     if (!pages_rows<false>(p, b, w)) return;
@@ -171,7 +193,6 @@ pages_write_kernel(const PagesRowsParams p) {
     uint8_t* rec = p.pages + (size_t(tile) * p.Hk + hk) * page_block_bytes(D);
     float* scales = reinterpret_cast<float*>(rec + 2 * kPageBlock * D);
     const int c = tid % LPR, row0 = tid / LPR;                       // 16 features; first row
-    if (tid == 0) s_bad = 0;
     // the block's earlier keys
     if (p.bounds) {
         for (int e = tid; e < w.r0 * LPR; e += kPagesThreads)
@@ -239,51 +260,52 @@ pages_write_kernel(const PagesRowsParams p) {
     float hi[4], lo[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) { hi[j] = -INFINITY; lo[j] = INFINITY; }
-    uint32_t worst = 0u;                                             // largest code, or NaN
-    bool bad = false;
-#pragma unroll 4
-    for (int row = set; row < w.r1; row += SETS) {
-        uint32_t a, e;
-        e4m3x4_to_f16(s_k[row][f], a, e);
-        asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(worst) : "r"(a));
-        asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(worst) : "r"(e));
-        const float2 x = f16x2_to_f32(a), y = f16x2_to_f32(e);
-        const float scale = s_scale[row];
-        bad |= !(scale < INFINITY);
-        const float v[4] = {x.x * scale, x.y * scale, y.x * scale, y.y * scale};
+    for (int row = 2 * set; row < w.r1; row += 2 * SETS) {           // two rows at a time: the last one twice where it is alone
+        const int other = min(row + 1, w.r1 - 1);
+        uint32_t a0, a1, b0, b1;
+        e4m3x4_to_f16(s_k[row][f], a0, a1);
+        e4m3x4_to_f16(s_k[other][f], b0, b1);
+        const float sa = s_scale[row], sb = s_scale[other];
+        const uint64_t sa2 = pair_f32(sa, sa), sb2 = pair_f32(sb, sb);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            hi[j] = fmaxf(hi[j], v[j]);
-            lo[j] = fminf(lo[j], v[j]);
+        for (int j = 0; j < 2; ++j) {
+            const float2 x = f16x2_to_f32(j ? a1 : a0), y = f16x2_to_f32(j ? b1 : b0);
+            float x0, x1, y0, y1;
+            unpair_f32(mul_f32x2(pair_f32(x.x, x.y), sa2), x0, x1);
+            unpair_f32(mul_f32x2(pair_f32(y.x, y.y), sb2), y0, y1);
+            hi[2 * j] = max3_nan(hi[2 * j], x0, y0);
+            hi[2 * j + 1] = max3_nan(hi[2 * j + 1], x1, y1);
+            lo[2 * j] = min3(lo[2 * j], x0, y0);
+            lo[2 * j + 1] = min3(lo[2 * j + 1], x1, y1);
         }
     }
-    {
-        const float2 x = f16x2_to_f32(worst);
-        bad |= x.x != x.x || x.y != x.y;
-    }
-    if (bad) s_bad = 1;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) { s_hi[set][4 * f + j] = hi[j]; s_lo[set][4 * f + j] = lo[j]; }
+    *reinterpret_cast<float4*>(&s_ext[0][set][4 * f]) = make_float4(hi[0], hi[1], hi[2], hi[3]);
+    *reinterpret_cast<float4*>(&s_ext[1][set][4 * f]) = make_float4(lo[0], lo[1], lo[2], lo[3]);
     __syncthreads();
-    float h = -INFINITY, l = INFINITY, most = 0.f;
-    if (tid < D) {
+    // a thread per feature for the largest, and one for the smallest
+    const bool low = tid >= D;
+    float x = 0.f;
+    if (tid < 2 * D) {
+        const float* of = &s_ext[low][0][low ? tid - D : tid];
+        x = of[0];
 #pragma unroll
-        for (int s = 0; s < SETS; ++s) { h = fmaxf(h, s_hi[s][tid]); l = fminf(l, s_lo[s][tid]); }
-        most = fmaxf(fabsf(h), fabsf(l));
+        for (int s = 1; s + 1 < SETS; s += 2) x = low ? min3(x, of[s * D], of[(s + 1) * D]) : max3_nan(x, of[s * D], of[(s + 1) * D]);
+        x = low ? fminf(x, of[(SETS - 1) * D]) : max3_nan(x, of[(SETS - 1) * D], x);
     }
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
+    // bits of magnitudes are in the order of the numbers, and those of NaN are the largest
+    const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(x) & 0x7fffffffu);
     if (tid % 32 == 0) s_most[tid / 32] = most;
     __syncthreads();
-    if (tid < D) {
-        most = s_most[0];
+    if (tid < 2 * D) {
+        uint32_t all = s_most[0];
 #pragma unroll
-        for (int i = 1; i < D / 32; ++i) most = fmaxf(most, s_most[i]);
-        const float scale = s_bad ? INFINITY : __fdiv_rn(most, 127.f);
+        for (int i = 1; i < 2 * D / 32; ++i) all = max(all, s_most[i]);
+        const bool bad = all >= 0x7f800000u;
+        const float scale = bad ? INFINITY : __fdiv_rn(__uint_as_float(all), 127.f);
         uint8_t* to = p.bounds + (size_t(tile) * p.Hk + hk) * page_bounds_bytes(D);
-        const bool flat = s_bad || !(scale > 0.f);
-        to[tid] = uint8_t(flat ? 0 : int(fminf(ceilf(__fdiv_rn(h, scale)), 127.f)));
-        to[D + tid] = uint8_t(flat ? 0 : int(fmaxf(floorf(__fdiv_rn(l, scale)), -127.f)));
+        const float over = __fdiv_rn(x, scale);
+        const int code = bad || !(scale > 0.f) ? 0 : int(low ? fmaxf(floorf(over), -127.f) : fminf(ceilf(over), 127.f));
+        to[tid] = uint8_t(code);
         if (tid == 0) *reinterpret_cast<float*>(to + 2 * D) = scale;
     }
 }
