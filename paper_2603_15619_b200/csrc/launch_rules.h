@@ -101,11 +101,11 @@ inline EvictForm evict_form(int T, long long rows, int sms) {
     return {ranks, 0, 512, 1};
 }
 
-// CTAs of a cluster that rate the blocks of a (sequence, head) (moda_pages.cuh): 256 blocks are one round of a CTA's loads.
+// CTAs of a cluster that rate the blocks of a (sequence, head) (moda_pages.cuh): 128 blocks are one round of a CTA's loads.
 constexpr int kSelectMostBlocks = 32768;                   // of a sequence: their ratings are held in shared memory
 inline int select_ranks(int blocks, long long rows, int sms) {
     int ranks = 1;
-    while (ranks < 8 && blocks > 256 * ranks && rows * ranks * 2 <= sms) ranks *= 2;
+    while (ranks < 8 && blocks > 128 * ranks && rows * ranks * 2 <= 8ll * sms) ranks *= 2;
     return ranks;
 }
 

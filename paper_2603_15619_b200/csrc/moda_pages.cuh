@@ -31,7 +31,7 @@ struct PagesParams {
     int B, Hk, sub, num_pages, max_blocks;   // sub: blocks of a page
     // Number of block `blk` of a sequence, over all pages; -1 where the table has no page for it.
     __device__ __forceinline__ int tile(int b, int blk) const {
-        const int at = blk / sub;
+        const int at = sub == 1 ? blk : blk / sub;
         const int page = at < max_blocks ? table[size_t(b) * max_blocks + at] : -1;
         return unsigned(page) < unsigned(num_pages) ? page * sub + (blk - at * sub) : -1;
     }
@@ -398,7 +398,7 @@ struct PagesSelectParams : PagesParams {
     int G, max_len, n_keep, n_recent;
 };
 
-constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
+constexpr int kSelectThreads = 256, kSelectWarps = kSelectThreads / 32;
 constexpr int kSelectSets = 4;                                       // blocks that a group of lanes has on its way
 constexpr int kSelectMostGroup = 32;
 
@@ -410,7 +410,7 @@ __device__ __forceinline__ void st_cluster_u32(uint32_t addr, uint32_t v) {
 }
 
 template <int D>
-__global__ void __launch_bounds__(kSelectThreads)
+__global__ void __launch_bounds__(kSelectThreads, 4)
 pages_select_kernel(const PagesSelectParams p) {
     constexpr int LPB = D / 16, GPW = 32 / LPB;                      // lanes of a block (16 features each), blocks of a warp at a time
     extern __shared__ __align__(16) uint8_t select_smem_raw[];
@@ -429,6 +429,7 @@ pages_select_kernel(const PagesSelectParams p) {
     const bool some = want > 0 && want < old;
 
     if (some) {
+        if (ranks > 1) cluster_arrive();                             // this CTA has started
         // ---- the queries in 8 bits ----
         const __nv_bfloat16* q = p.q + (size_t(b) * p.Hk + hk) * p.G * D;
         float most = 0.f;
@@ -460,32 +461,33 @@ pages_select_kernel(const PagesSelectParams p) {
         }
         __syncthreads();
         // ---- ratings ----
-        if (ranks > 1) cluster_sync_all();                           // the first CTA has started
+        if (ranks > 1) cluster_wait();                               // and so has the first one
         const uint32_t keys = ranks > 1 ? cluster_map_shared(smem_u32(s_key), 0u) : smem_u32(s_key);
         const int grp = lane / LPB, sub = lane % LPB;
         constexpr int STEP = GPW * kSelectSets;                      // blocks of a warp's iteration
         const int mine = (LPB == 8 ? (sub >> 1) : sub);              // which set this lane ends up with
+        const uint8_t* head = p.bounds + size_t(hk) * page_bounds_bytes(D);
+        const size_t stride = size_t(p.Hk) * page_bounds_bytes(D);
         for (int i0 = (rank * kSelectWarps + warp) * STEP; i0 < old; i0 += ranks * kSelectWarps * STEP) {
-            const uint8_t* rec[kSelectSets];
+            int tile[kSelectSets];
             uint4 hi[kSelectSets], lo[kSelectSets];
 #pragma unroll
             for (int s = 0; s < kSelectSets; ++s) {
                 const int blk = i0 + s * GPW + grp;
-                const int tile = blk < old ? p.tile(b, blk) : -1;
-                rec[s] = tile >= 0 ? p.bounds + (size_t(tile) * p.Hk + hk) * page_bounds_bytes(D) : nullptr;
+                tile[s] = blk < old ? p.tile(b, blk) : -1;
             }
+            int own = tile[0];
 #pragma unroll
             for (int s = 0; s < kSelectSets; ++s) {
+                if (mine == s) own = tile[s];
                 hi[s] = lo[s] = make_uint4(0u, 0u, 0u, 0u);
-                if (rec[s]) {
-                    hi[s] = *reinterpret_cast<const uint4*>(rec[s] + 16 * sub);
-                    lo[s] = *reinterpret_cast<const uint4*>(rec[s] + D + 16 * sub);
+                if (tile[s] >= 0) {
+                    const uint8_t* rec = head + size_t(tile[s]) * stride + 16 * sub;
+                    hi[s] = *reinterpret_cast<const uint4*>(rec);
+                    lo[s] = *reinterpret_cast<const uint4*>(rec + D);
                 }
             }
-            const uint8_t* own = rec[0];
-#pragma unroll
-            for (int s = 1; s < kSelectSets; ++s) own = mine == s ? rec[s] : own;
-            const float scale = own ? *reinterpret_cast<const float*>(own + 2 * D) : 0.f;
+            const float scale = own >= 0 ? *reinterpret_cast<const float*>(head + size_t(own) * stride + 2 * D) : 0.f;
             int best = INT_MIN;
             for (int h = 0; h < p.G; ++h) {
                 const uint4 qp = *reinterpret_cast<const uint4*>(s_qp + h * (D / 4) + 4 * sub), qn = *reinterpret_cast<const uint4*>(s_qn + h * (D / 4) + 4 * sub);
@@ -513,7 +515,7 @@ pages_select_kernel(const PagesSelectParams p) {
             const int blk = i0 + mine * GPW + grp;
             if ((LPB == 4 || (sub & 1) == 0) && blk < old) {
                 // a block without a page is the last to be taken, one with keys that are not finite the first
-                const float r = own ? (scale < INFINITY ? float(best) * scale : INFINITY) : -INFINITY;
+                const float r = own >= 0 ? (scale < INFINITY ? float(best) * scale : INFINITY) : -INFINITY;
                 st_cluster_u32(keys + 4u * uint32_t(blk), evict_key(r));
             }
         }
@@ -539,9 +541,9 @@ pages_select_kernel(const PagesSelectParams p) {
         __syncthreads();
         mn = s_min; mx = s_max;
         int shift = mn == mx ? 0 : 32 - __clz(mn ^ mx);              // bits below `shift` are still to be found
-        uint32_t left = uint32_t(want);
+        uint32_t left = uint32_t(want), count = uint32_t(old);       // keys still to take among those that agree so far, and how many agree
         thr = shift < 32 ? mx >> shift << shift : 0u;
-        for (int pass = 0; shift > 0; ++pass) {
+        for (int pass = 0; shift > 0 && count > left; ++pass) {
             const int bits = min(shift, 8), agree = shift;
             shift -= bits;
             uint32_t* hist = s_hist[pass];
@@ -572,8 +574,13 @@ pages_select_kernel(const PagesSelectParams p) {
             }
             thr |= __shfl_sync(0xffffffffu, bin, at) << shift;
             left -= __shfl_sync(0xffffffffu, over, at);
+            count = hist[__shfl_sync(0xffffffffu, bin, at)];
         }
         ties = left;
+        if (shift > 0) {                                             // all that agree stay: key >= thr, whose lower bits are 0
+            ties = thr == 0u ? uint32_t(old) : 0u;
+            thr = thr == 0u ? 0u : thr - 1u;
+        }
     }
     // ---- the blocks in their order ----
     uint32_t gt = 0, eq = 0;

@@ -153,9 +153,9 @@ def test_cluster_of_a_selection(tmp_path):
     src.write_text(RULES)
     subprocess.run(["g++", "-std=c++17", "-shared", "-fPIC", f"-I{build.CSRC}", "-o", str(so), str(src)], check=True)
     ranks = ctypes.CDLL(str(so)).select_ranks
-    for blocks in (0, 1, 256, 257, 1000, 5000, 32768):
-        for rows in (1, 8, 18, 19, 74, 75, 300, 10000):
+    for blocks in (0, 1, 128, 129, 1000, 5000, 32768):
+        for rows in (1, 8, 147, 148, 149, 592, 593, 10000):
             r = ranks(blocks, rows, 148)
-            assert r in (1, 2, 4, 8) and (r == 1 or rows * r <= 148)
-            assert blocks > 256 or r == 1
+            assert r in (1, 2, 4, 8) and (r == 1 or rows * r <= 8 * 148)
+            assert blocks > 128 or r == 1
     assert ranks(32768, 8, 148) == 8
