@@ -615,7 +615,8 @@ int moda_attn_decode_shared(const void* q, const void* K_prefix, const void* V_p
  *                             rating = scale * max_{h in group} sum_f max(q8[h, f] smallest[f], q8[h, f] largest[f])
  *
  *                         (what a key within the bounds could score at most; the sums are of whole numbers).  index : int32 [B][H_kv][n_blocks], ascending, -1 behind them.
- *                         A block without a page is rated last, one whose bounds have scale inf first.  max_seq_len <= 64 * 32768.  One launch.
+ *                         A block without a page is rated last, one whose bounds have scale inf first.  max_seq_len <= 64 * 32768.
+ *                         workspace : moda_kv_select_workspace_bytes.  Two launches.
  * moda_attn_decode_e4m3   the decode step: O, LSE, depth_kv_token, groups and scale as for moda_attn_decode_paged, with seq_lens[b] in 0 .. max_seq_len.  index (int32
  *                         [B][H_kv][n_blocks]) NULL: all blocks; else the blocks of the first min(n_blocks, ceil(seq_lens[b] / 64)) entries of a row, an entry that is no block
  *                         of the sequence being passed over (one that comes twice counts twice).  A token without any key has O = 0 and LSE = -inf.
@@ -631,9 +632,10 @@ int moda_kv_write_e4m3(void* pages, void* bounds, const void* K, const void* V, 
                        int B, int T, int page_size, int num_pages, int max_blocks_per_seq, int H_kv, int d, void* stream);
 int moda_kv_read_e4m3(const void* pages, const int* block_table, const int* seq_lens, const int* start,
                       int B, int T, int page_size, int num_pages, int max_blocks_per_seq, int H_kv, int d, void* K_out, void* V_out, void* stream);
+size_t moda_kv_select_workspace_bytes(int B, int max_seq_len, int H_kv);
 int moda_kv_select_blocks(const void* q, const void* bounds, const int* block_table, const int* seq_lens,
                           int B, int max_seq_len, int page_size, int num_pages, int max_blocks_per_seq, int H, int H_kv, int d,
-                          int n_blocks, int n_recent, int* index, void* stream);
+                          int n_blocks, int n_recent, int* index, void* workspace, size_t workspace_bytes, void* stream);
 size_t moda_decode_e4m3_workspace_bytes(int B, int H, int H_kv, int d);
 int moda_attn_decode_e4m3(const void* q, const void* pages, const int* block_table, const int* seq_lens, const int* index, int n_blocks,
                           const void* depth_kv_token,

@@ -42,7 +42,7 @@ SYMBOLS = (
     "moda_kv_evict",
     "moda_decode_shared_workspace_bytes", "moda_attn_decode_shared",
     "moda_kv_page_e4m3_bytes", "moda_kv_page_bounds_bytes",
-    "moda_kv_write_e4m3", "moda_kv_read_e4m3", "moda_kv_select_blocks",
+    "moda_kv_write_e4m3", "moda_kv_read_e4m3", "moda_kv_select_workspace_bytes", "moda_kv_select_blocks",
     "moda_decode_e4m3_workspace_bytes", "moda_attn_decode_e4m3",
 )
 MODA_STATIC_SCRATCH_ROWS = 1 << 20
@@ -170,7 +170,9 @@ def load() -> ctypes.CDLL:
     lib.moda_kv_read_e4m3.restype = ci
     lib.moda_kv_read_e4m3.argtypes = [vp] * 4 + [ci] * 7 + [vp] * 3
     lib.moda_kv_select_blocks.restype = ci
-    lib.moda_kv_select_blocks.argtypes = [vp] * 4 + [ci] * 10 + [vp] * 2
+    lib.moda_kv_select_blocks.argtypes = [vp] * 4 + [ci] * 10 + [vp] * 2 + [sz, vp]
+    lib.moda_kv_select_workspace_bytes.restype = sz
+    lib.moda_kv_select_workspace_bytes.argtypes = [ci] * 3
     lib.moda_decode_e4m3_workspace_bytes.restype = sz
     lib.moda_decode_e4m3_workspace_bytes.argtypes = [ci] * 4
     lib.moda_attn_decode_e4m3.restype = ci
@@ -1023,10 +1025,14 @@ def moda_kv_read_e4m3(pages, block_table, seq_lens, T, start=None, K_out=None, V
     return tuple(outs)
 
 
-def moda_kv_select_blocks(q, bounds, block_table, seq_lens, max_seq_len, n_blocks, n_recent=1, index=None, stream=None):
+def moda_kv_select_workspace_bytes(B, max_seq_len, H_kv) -> int:
+    return int(load().moda_kv_select_workspace_bytes(B, max_seq_len, H_kv))
+
+
+def moda_kv_select_blocks(q, bounds, block_table, seq_lens, max_seq_len, n_blocks, n_recent=1, index=None, workspace=None, stream=None):
     """The blocks of 64 positions that a token's queries q [B,H,d] attend to: per (sequence, key/value head) the last ``n_recent`` and those that the bounds of their
     keys rate highest, ``n_blocks`` in all: index int32 [B,H_kv,n_blocks], ascending, -1 behind the last one."""
-    if stream is None and (out := host().kv_select(q, bounds, block_table, seq_lens, max_seq_len, n_blocks, n_recent, index)) is not None:
+    if stream is None and (out := host().kv_select(q, bounds, block_table, seq_lens, max_seq_len, n_blocks, n_recent, index, workspace)) is not None:
         return out
     page_size, num_pages, Hk, d, B, most = _paged(bounds, block_table, bounds=True)
     if q.dtype != torch.bfloat16 or q.dim() != 3 or (q.shape[0], q.shape[2]) != (B, d):
@@ -1035,8 +1041,11 @@ def moda_kv_select_blocks(q, bounds, block_table, seq_lens, max_seq_len, n_block
     n_blocks = int(n_blocks)
     shape = (B, Hk, max(n_blocks, 1))
     index = _new(shape, torch.int32, q.device, stream) if index is None else _int32(index, "index", shape)
+    if workspace is None:
+        workspace = _new((max(moda_kv_select_workspace_bytes(B, int(max_seq_len), Hk), 16),), torch.uint8, q.device, stream)
     _check(load().moda_kv_select_blocks(_ptr(q), _ptr(bounds), _ptr(block_table), _ptr(seq_lens), B, int(max_seq_len), page_size, num_pages, most,
-                                        q.shape[1], Hk, d, n_blocks, int(n_recent), _ptr(index), _stream(stream)), "moda_kv_select_blocks")
+                                        q.shape[1], Hk, d, n_blocks, int(n_recent), _ptr(index), _ptr(workspace),
+                                        workspace.numel() * workspace.element_size(), _stream(stream)), "moda_kv_select_blocks")
     return index
 
 

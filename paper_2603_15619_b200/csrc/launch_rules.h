@@ -101,12 +101,19 @@ inline EvictForm evict_form(int T, long long rows, int sms) {
     return {ranks, 0, 512, 1};
 }
 
-// CTAs of a cluster that rate the blocks of a (sequence, head) (moda_pages.cuh): 128 blocks are one round of a CTA's loads.
+// The selection of blocks (moda_pages.cuh).
 constexpr int kSelectMostBlocks = 32768;                   // of a sequence: their ratings are held in shared memory
+// CTAs of a cluster that rates and selects the blocks of a row (sequence, head), 128 blocks being one round of a CTA's loads; 0: rate in one kernel, select in another.
 inline int select_ranks(int blocks, long long rows, int sms) {
     int ranks = 1;
-    while (ranks < 8 && blocks > 128 * ranks && rows * ranks * 2 <= 8ll * sms) ranks *= 2;
-    return ranks;
+    while (ranks < 8 && blocks > 128 * ranks && rows * ranks * 2 <= 4ll * sms) ranks *= 2;
+    return rows * ranks <= 4ll * sms && blocks <= 512 * ranks ? ranks : 0;
+}
+// Rounds of `step` blocks that a CTA of the first of the two takes: one while there are few CTAs, then more, as every CTA has queries to prepare first.
+inline int rate_rounds(int blocks, int step, long long rows, int sms) {
+    int rounds = 1;
+    while (rounds < 8 && rows * ((blocks + step * rounds - 1) / (step * rounds)) > 8ll * sms) rounds *= 2;
+    return rounds;
 }
 
 }  // namespace moda

@@ -55,19 +55,37 @@ int launch_pages(void (*kernel)(P), dim3 grid, int threads, size_t smem, bool be
     return cuda_ok(cudaLaunchKernelEx(&cfg, kernel, p)) ? MODA_OK : MODA_ERR_CUDA;
 }
 
-template <int D>
-int launch_select(const PagesSelectParams& p, int ranks, cudaStream_t stream) {
-    const int smem = select_smem(p.G, D, pages_blocks(p.max_len));
-    if (smem > 44000) {                           // beside the static part
-        static thread_local int configured_dev = -1;
-        int dev = 0;
-        if (!cuda_ok(cudaGetDevice(&dev))) return MODA_ERR_CUDA;
-        if (configured_dev != dev) {
-            if (!set_smem_limit(pages_select_kernel<D>, select_smem(kSelectMostGroup, D, kSelectMostBlocks))) return MODA_ERR_CUDA;
-            configured_dev = dev;
-        }
+// A kernel's limit of dynamic shared memory, raised to `most` on a thread's first call on a device that needs more than a kernel may have without asking.
+template <typename Kernel>
+int raise_smem(Kernel kernel, size_t need, int most, int* configured_dev) {
+    if (need <= 40000) return MODA_OK;            // beside the static part
+    int dev = 0;
+    if (!cuda_ok(cudaGetDevice(&dev))) return MODA_ERR_CUDA;
+    if (*configured_dev != dev) {
+        if (!set_smem_limit(kernel, most)) return MODA_ERR_CUDA;
+        *configured_dev = dev;
     }
-    return launch_pages(pages_select_kernel<D>, dim3(unsigned(ranks), unsigned(p.Hk), unsigned(p.B)), kSelectThreads, size_t(smem), false, p, stream, ranks);
+    return MODA_OK;
+}
+
+template <int D>
+int launch_select(PagesSelectParams& p, int sms, cudaStream_t stream) {
+    static thread_local int one_dev = -1, rate_dev = -1, select_dev = -1;
+    const long long rows = (long long)p.B * p.Hk;
+    const size_t ratings = size_t(p.most) * 4, queries = size_t(2) * p.G * D;
+    const int ranks = select_ranks(p.most, rows, sms);
+    if (ranks > 0) {
+        if (int rc = raise_smem(pages_select_one_kernel<D>, queries + ratings, 2 * MODA_MAX_GROUP * D + kSelectMostBlocks * 4, &one_dev)) return rc;
+        return launch_pages(pages_select_one_kernel<D>, dim3(unsigned(ranks), unsigned(p.Hk), unsigned(p.B)), kSelectThreads, queries + ratings, false, p, stream, ranks);
+    }
+    const int heads = std::min(p.Hk, kSelectWarps), eights = (p.Hk + kSelectWarps - 1) / kSelectWarps;
+    const int step = kSelectWarps / heads * select_step(D);
+    p.rounds = rate_rounds(p.most, step, (long long)p.B * eights, sms);
+    const unsigned parts = unsigned((p.most + step * p.rounds - 1) / (step * p.rounds));
+    if (int rc = raise_smem(pages_rate_kernel<D>, heads * queries, kSelectWarps * 2 * MODA_MAX_GROUP * D, &rate_dev)) return rc;
+    if (int rc = launch_pages(pages_rate_kernel<D>, dim3(parts, unsigned(eights), unsigned(p.B)), kSelectThreads, heads * queries, false, p, stream)) return rc;
+    if (int rc = raise_smem(pages_select_kernel, ratings, kSelectMostBlocks * 4, &select_dev)) return rc;
+    return launch_pages(pages_select_kernel, dim3(unsigned(p.Hk), unsigned(p.B)), kSelectThreads, ratings, true, p, stream);
 }
 
 template <int D>
@@ -132,25 +150,32 @@ int moda_kv_read_e4m3(const void* pages, const int* block_table, const int* seq_
     return launch_pages(d == 128 ? pages_read_kernel<128> : pages_read_kernel<64>, grid, kPagesThreads, 0, false, p, static_cast<cudaStream_t>(stream));
 }
 
+size_t moda_kv_select_workspace_bytes(int B, int max_seq_len, int H_kv) {
+    if (B < 1 || H_kv < 1 || max_seq_len < 0 || pages_blocks(max_seq_len) > kSelectMostBlocks) return 0;
+    return (size_t(B) * H_kv * std::max(pages_blocks(max_seq_len), 1) * 4 + 15) / 16 * 16;
+}
+
 int moda_kv_select_blocks(const void* q, const void* bounds, const int* block_table, const int* seq_lens,
                           int B, int max_seq_len, int page_size, int num_pages, int max_blocks_per_seq, int H, int H_kv, int d,
-                          int n_blocks, int n_recent, int* index, void* stream) {
+                          int n_blocks, int n_recent, int* index, void* workspace, size_t workspace_bytes, void* stream) {
     if (int rc = check_pages(B, page_size, num_pages, max_blocks_per_seq, H_kv, d)) return rc;
     if (H < 1 || max_seq_len < 0 || max_seq_len > max_blocks_per_seq * page_size || pages_blocks(max_seq_len) > kSelectMostBlocks) return MODA_ERR_BAD_SHAPE;
     if (n_blocks < 1 || n_recent < 0 || n_recent > n_blocks || (long long)B * H_kv > 0x7fffffffLL / n_blocks) return MODA_ERR_BAD_SHAPE;
     if (int rc = check_groups(H, H_kv)) return rc;
     if (!q || !bounds || !block_table || !seq_lens || !index) return MODA_ERR_NULL_POINTER;
     if (!aligned16(q) || !aligned16(bounds) || !aligned4(block_table) || !aligned4(seq_lens) || !aligned4(index)) return MODA_ERR_MISALIGNED;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < moda_kv_select_workspace_bytes(B, max_seq_len, H_kv)) return MODA_ERR_WORKSPACE;
     if (int rc = check_device()) return rc;
     int sms = 0;
     if (int rc = device_sm_count(&sms)) return rc;
     PagesSelectParams p = {};
     set_pages(p, block_table, B, H_kv, page_size, num_pages, max_blocks_per_seq);
     p.q = static_cast<const __nv_bfloat16*>(q); p.bounds = static_cast<const uint8_t*>(bounds); p.lens = seq_lens; p.index = index;
+    p.rating = static_cast<uint32_t*>(workspace);
     p.G = H / H_kv; p.max_len = max_seq_len; p.n_keep = n_blocks; p.n_recent = n_recent;
-    const int ranks = select_ranks(pages_blocks(max_seq_len), (long long)B * H_kv, sms);
+    p.most = pages_blocks(max_seq_len);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return d == 128 ? launch_select<128>(p, ranks, st) : launch_select<64>(p, ranks, st);
+    return d == 128 ? launch_select<128>(p, sms, st) : launch_select<64>(p, sms, st);
 }
 
 size_t moda_decode_e4m3_workspace_bytes(int B, int H, int H_kv, int d) {

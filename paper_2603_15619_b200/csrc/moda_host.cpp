@@ -40,7 +40,8 @@ using at::Tensor;
     X(moda_attn_decode_paged) X(moda_decode_workspace_bytes)                                                            \
     X(moda_attn_key_mass) X(moda_key_mass_workspace_bytes) X(moda_attn_decode_mass) X(moda_decode_mass_workspace_bytes) \
     X(moda_kv_evict) X(moda_attn_decode_shared) X(moda_decode_shared_workspace_bytes)                                   \
-    X(moda_kv_write_e4m3) X(moda_kv_read_e4m3) X(moda_kv_select_blocks) X(moda_attn_decode_e4m3) X(moda_decode_e4m3_workspace_bytes)
+    X(moda_kv_write_e4m3) X(moda_kv_read_e4m3) X(moda_kv_select_blocks) X(moda_kv_select_workspace_bytes) \
+    X(moda_attn_decode_e4m3) X(moda_decode_e4m3_workspace_bytes)
 struct Library {
 #define X(name) decltype(&::name) name = nullptr;
     MODA_HOST_CALLS(X)
@@ -556,22 +557,23 @@ PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// kv_select(q, bounds, table, seq_lens, max_seq_len, n_blocks, n_recent, index) -> index
+// kv_select(q, bounds, table, seq_lens, max_seq_len, n_blocks, n_recent, index, workspace) -> index
 PyObject* kv_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     Paged s;
     int T, keep, recent;
-    const Tensor *lens, *index, *q;
-    if (n != 8 || !plain_thread() || !paged_args(a[1], a[2], 2, 16, s) || a[3] == Py_None || !lens_arg(a[3], s.B, lens) || !int_arg(a[4], T) ||
+    const Tensor *lens, *index, *q, *ws;
+    if (n != 9 || !plain_thread() || !paged_args(a[1], a[2], 2, 16, s) || a[3] == Py_None || !lens_arg(a[3], s.B, lens) || !int_arg(a[4], T) ||
         !int_arg(a[5], keep) || !int_arg(a[6], recent) || keep < 1) return none();
     if ((q = dense(a[0], at::kBFloat16, 3)) == nullptr || !small(*q) || q->size(0) != s.B || q->size(2) != s.d || !optional_dense(a[7], index) ||
-        !tensor_of(index, at::kInt, {s.B, s.Hk, keep})) return none();
+        !tensor_of(index, at::kInt, {s.B, s.Hk, keep}) || !optional_dense(a[8], ws)) return none();
     Tensor t = index != nullptr ? *index : Tensor();
     {
         NoGil nogil;
         if (!t.defined()) t = fresh({s.B, s.Hk, keep}, at::kInt, *q);
+        const Tensor w = scratch(ws, ws != nullptr ? 0 : lib.moda_kv_select_workspace_bytes(s.B, T, s.Hk), *q);
         const int rc = lib.moda_kv_select_blocks(q->data_ptr(), s.data->data_ptr(), i32(s.table), i32(lens), s.B, T, s.page, s.pages, s.most, int(q->size(1)), s.Hk, s.d,
-                                                 keep, recent, static_cast<int*>(t.data_ptr()), stream());
+                                                 keep, recent, static_cast<int*>(t.data_ptr()), w.data_ptr(), bytes_of(w), stream());
         if (rc != 0) fail(rc, "moda_kv_select_blocks");
     }
     return out(a[7], t);

@@ -387,174 +387,164 @@ pages_read_kernel(const PagesRowsParams p) {
 // which is what a key within the block's bounds could score at most.  The sums are of whole numbers (dp4a), so that a rating has one value whatever the order, and
 // ties are ties.
 //
-// A cluster of `ranks` CTAs per (sequence, head), each rating a share of the blocks; all ratings go to the first one's shared memory, which finds the
-// lowest that stays digit by digit (8 bits, from the highest bit in which any two differ) and writes the blocks in their order.
+//   pages_select_one_kernel  a cluster of up to 8 CTAs per (sequence, head): each rates a share of the blocks into the first one's shared memory, which selects.  For few
+//                            rows: one launch.
+//   pages_rate_kernel        for many: a CTA per (sequence, up to 8 heads, some of its blocks) rates, bound by HBM where sequences are long (2 d + 16 bytes a block),
+//   pages_select_kernel      and a CTA per (sequence, head) selects.  (32 x 131072 positions, 8 heads: 26.2 us; in one kernel 31.0, as the CTAs that select hold the place of
+//                            others that would rate; one sequence of 65536 8.6 and 7.3.)
+//
+// The selection is a chain of short phases, some 4 us whatever the length is: the lowest rating that stays digit by digit (8 bits, from the highest bit in which any two
+// differ, until all that are left stay), then the blocks in their order.  The second kernel may come up when the first one's CTAs have ended, not before: 24.9 against 29.6 us.
 // ---------------------------------------------------------------------------------------------------------------------
 struct PagesSelectParams : PagesParams {
     const __nv_bfloat16* q;       // [B][Hk * G][d]
     const uint8_t* bounds;
     const int* lens;              // [B]
     int* index;                   // [B][Hk][n_keep]
-    int G, max_len, n_keep, n_recent;
+    uint32_t* rating;             // [B][Hk][most]: integers in the order of the ratings
+    int G, max_len, n_keep, n_recent, most, rounds;   // most: blocks of a sequence; rounds: that a warp of pages_rate_kernel takes
 };
 
 constexpr int kSelectThreads = 256, kSelectWarps = kSelectThreads / 32;
 constexpr int kSelectSets = 4;                                       // blocks that a group of lanes has on its way
-constexpr int kSelectMostGroup = 32;
+__host__ __device__ constexpr int select_step(int d) { return 32 / (d / 16) * kSelectSets; }    // blocks of a warp's round
 
 __host__ __device__ inline int pages_blocks(int len) { return len / kPageBlock + (len % kPageBlock != 0); }
-inline int select_smem(int G, int d, int blocks) { return 2 * G * d + 4 * blocks; }
 
-__device__ __forceinline__ void st_cluster_u32(uint32_t addr, uint32_t v) {
-    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+// Of the blocks of a sequence: `old` that are rated, `want` of which stay, and the recent ones.
+struct SelectParts {
+    int old, want, recent;
+    __device__ __forceinline__ SelectParts(const PagesSelectParams& p, int b) {
+        const int n = pages_blocks(min(max(p.lens[b], 0), p.max_len)), kept = min(p.n_keep, n);
+        recent = min(p.n_recent, kept);
+        old = n - recent;
+        want = kept - recent;
+    }
+    __device__ __forceinline__ bool some() const { return want > 0 && want < old; }      // not all and not none of the old ones
+};
+
+// The queries of a group in 8 bits by a warp: positive parts and negative parts, [2][G][D / 4] words of four features.
+template <int D>
+__device__ __forceinline__ void queries_in_8_bits(const PagesSelectParams& p, int b, int hk, uint32_t* to, int lane) {
+    const int words = p.G * (D / 4);
+    const uint2* q = reinterpret_cast<const uint2*>(p.q + (size_t(b) * p.Hk + hk) * p.G * D);
+    float most = 0.f;
+#pragma unroll 4
+    for (int e = lane; e < words; e += 32) {
+        const uint2 v = q[e];
+        most = fmaxf(most, fmaxf(fmaxf(fabsf(bf16_lo_to_f32(v.x)), fabsf(bf16_hi_to_f32(v.x))), fmaxf(fabsf(bf16_lo_to_f32(v.y)), fabsf(bf16_hi_to_f32(v.y)))));
+    }
+    most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
+    const float inv = most > 0.f ? __fdiv_rn(127.f, most) : 0.f;
+#pragma unroll 4
+    for (int e = lane; e < words; e += 32) {
+        const uint2 v = q[e];
+        const float x[4] = {bf16_lo_to_f32(v.x), bf16_hi_to_f32(v.x), bf16_lo_to_f32(v.y), bf16_hi_to_f32(v.y)};
+        uint32_t pos = 0u, neg = 0u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = min(max(__float2int_rn(x[j] * inv), -127), 127);
+            pos |= uint32_t(max(i, 0)) << (8 * j);
+            neg |= (uint32_t(min(i, 0)) & 0xffu) << (8 * j);
+        }
+        to[e] = pos;
+        to[words + e] = neg;
+    }
 }
 
-template <int D>
-__global__ void __launch_bounds__(kSelectThreads, 4)
-pages_select_kernel(const PagesSelectParams p) {
-    constexpr int LPB = D / 16, GPW = 32 / LPB;                      // lanes of a block (16 features each), blocks of a warp at a time
-    extern __shared__ __align__(16) uint8_t select_smem_raw[];
-    uint32_t* s_qp = reinterpret_cast<uint32_t*>(select_smem_raw);   // [G][D / 4] positive parts of the queries
-    uint32_t* s_qn = s_qp + p.G * (D / 4);                           // negative parts
-    uint32_t* s_key = s_qn + p.G * (D / 4);                          // [blocks], of the first CTA
-    __shared__ uint32_t s_hist[4][256], s_gt[kSelectWarps], s_eq[kSelectWarps], s_min, s_max;
-    __shared__ float s_most[kSelectWarps];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int ranks = gridDim.x, rank = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
-    const int len = min(max(p.lens[b], 0), p.max_len), n = pages_blocks(len);
-    const int kept = min(p.n_keep, n), recent = min(p.n_recent, kept);
-    const int old = n - recent, want = kept - recent;
-    int* index = p.index + (size_t(b) * p.Hk + hk) * p.n_keep;
-    grid_launch_dependents();
-    const bool some = want > 0 && want < old;
-
-    if (some) {
-        if (ranks > 1) cluster_arrive();                             // this CTA has started
-        // ---- the queries in 8 bits ----
-        const __nv_bfloat16* q = p.q + (size_t(b) * p.Hk + hk) * p.G * D;
-        float most = 0.f;
-        for (int e = tid; e < p.G * (D / 4); e += kSelectThreads) {
-            const uint2 v = reinterpret_cast<const uint2*>(q)[e];
-            most = fmaxf(most, fmaxf(fmaxf(fabsf(bf16_lo_to_f32(v.x)), fabsf(bf16_hi_to_f32(v.x))), fmaxf(fabsf(bf16_lo_to_f32(v.y)), fabsf(bf16_hi_to_f32(v.y)))));
-        }
+// Ratings of blocks i0 .. i0 + select_step(D) - 1 of a head (below `old`) by a warp, d / 16 lanes a block: put(block, integer in the order of the ratings).
+template <int D, class Put>
+__device__ __forceinline__ void rate_blocks(const PagesSelectParams& p, int b, int hk, int i0, int old, const uint32_t* s_qp, int lane, const Put& put) {
+    constexpr int LPB = D / 16, GPW = 32 / LPB;                      // lanes of a block (16 features each), blocks at a time
+    const uint32_t* s_qn = s_qp + p.G * (D / 4);
+    const int grp = lane / LPB, sub = lane % LPB;
+    const int mine = (LPB == 8 ? (sub >> 1) : sub);                  // which set this lane ends up with
+    const uint8_t* head = p.bounds + size_t(hk) * page_bounds_bytes(D);
+    const size_t stride = size_t(p.Hk) * page_bounds_bytes(D);
+    int tile[kSelectSets];
+    uint4 hi[kSelectSets], lo[kSelectSets];
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
-        if (lane == 0) s_most[warp] = most;
-        for (int i = tid; i < 4 * 256; i += kSelectThreads) s_hist[0][i] = 0u;
-        if (tid == 0) { s_min = 0xffffffffu; s_max = 0u; }
-        __syncthreads();
+    for (int s = 0; s < kSelectSets; ++s) {
+        const int blk = i0 + s * GPW + grp;
+        tile[s] = blk < old ? p.tile(b, blk) : -1;
+    }
+    int own = tile[0];
 #pragma unroll
-        for (int i = 0; i < kSelectWarps; ++i) most = fmaxf(most, s_most[i]);
-        const float inv = most > 0.f ? __fdiv_rn(127.f, most) : 0.f;
-        for (int e = tid; e < p.G * (D / 4); e += kSelectThreads) {
-            const uint2 v = reinterpret_cast<const uint2*>(q)[e];
-            const float x[4] = {bf16_lo_to_f32(v.x), bf16_hi_to_f32(v.x), bf16_lo_to_f32(v.y), bf16_hi_to_f32(v.y)};
-            uint32_t pos = 0u, neg = 0u;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int i = min(max(__float2int_rn(x[j] * inv), -127), 127);
-                pos |= uint32_t(max(i, 0)) << (8 * j);
-                neg |= (uint32_t(min(i, 0)) & 0xffu) << (8 * j);
-            }
-            s_qp[e] = pos;
-            s_qn[e] = neg;
-        }
-        __syncthreads();
-        // ---- ratings ----
-        if (ranks > 1) cluster_wait();                               // and so has the first one
-        const uint32_t keys = ranks > 1 ? cluster_map_shared(smem_u32(s_key), 0u) : smem_u32(s_key);
-        const int grp = lane / LPB, sub = lane % LPB;
-        constexpr int STEP = GPW * kSelectSets;                      // blocks of a warp's iteration
-        const int mine = (LPB == 8 ? (sub >> 1) : sub);              // which set this lane ends up with
-        const uint8_t* head = p.bounds + size_t(hk) * page_bounds_bytes(D);
-        const size_t stride = size_t(p.Hk) * page_bounds_bytes(D);
-        for (int i0 = (rank * kSelectWarps + warp) * STEP; i0 < old; i0 += ranks * kSelectWarps * STEP) {
-            int tile[kSelectSets];
-            uint4 hi[kSelectSets], lo[kSelectSets];
-#pragma unroll
-            for (int s = 0; s < kSelectSets; ++s) {
-                const int blk = i0 + s * GPW + grp;
-                tile[s] = blk < old ? p.tile(b, blk) : -1;
-            }
-            int own = tile[0];
-#pragma unroll
-            for (int s = 0; s < kSelectSets; ++s) {
-                if (mine == s) own = tile[s];
-                hi[s] = lo[s] = make_uint4(0u, 0u, 0u, 0u);
-                if (tile[s] >= 0) {
-                    const uint8_t* rec = head + size_t(tile[s]) * stride + 16 * sub;
-                    hi[s] = *reinterpret_cast<const uint4*>(rec);
-                    lo[s] = *reinterpret_cast<const uint4*>(rec + D);
-                }
-            }
-            const float scale = own >= 0 ? *reinterpret_cast<const float*>(head + size_t(own) * stride + 2 * D) : 0.f;
-            int best = INT_MIN;
-            for (int h = 0; h < p.G; ++h) {
-                const uint4 qp = *reinterpret_cast<const uint4*>(s_qp + h * (D / 4) + 4 * sub), qn = *reinterpret_cast<const uint4*>(s_qn + h * (D / 4) + 4 * sub);
-                int a[kSelectSets];
-#pragma unroll
-                for (int s = 0; s < kSelectSets; ++s) {
-                    int v = __dp4a(int(qp.x), int(hi[s].x), 0);
-                    v = __dp4a(int(qp.y), int(hi[s].y), v);
-                    v = __dp4a(int(qp.z), int(hi[s].z), v);
-                    v = __dp4a(int(qp.w), int(hi[s].w), v);
-                    v = __dp4a(int(qn.x), int(lo[s].x), v);
-                    v = __dp4a(int(qn.y), int(lo[s].y), v);
-                    v = __dp4a(int(qn.z), int(lo[s].z), v);
-                    a[s] = __dp4a(int(qn.w), int(lo[s].w), v);
-                }
-                // sums over the lanes of a block; each lane keeps one of the four sets
-                constexpr int O2 = LPB / 2, O1 = LPB / 4;
-                const bool up2 = sub & O2, up1 = sub & O1;
-                const int g0 = __shfl_xor_sync(0xffffffffu, up2 ? a[0] : a[2], O2), g1 = __shfl_xor_sync(0xffffffffu, up2 ? a[1] : a[3], O2);
-                const int c0 = (up2 ? a[2] : a[0]) + g0, c1 = (up2 ? a[3] : a[1]) + g1;
-                int v = (up1 ? c1 : c0) + __shfl_xor_sync(0xffffffffu, up1 ? c0 : c1, O1);
-                if (LPB == 8) v += __shfl_xor_sync(0xffffffffu, v, 1);
-                best = max(best, v);
-            }
-            const int blk = i0 + mine * GPW + grp;
-            if ((LPB == 4 || (sub & 1) == 0) && blk < old) {
-                // a block without a page is the last to be taken, one with keys that are not finite the first
-                const float r = own >= 0 ? (scale < INFINITY ? float(best) * scale : INFINITY) : -INFINITY;
-                st_cluster_u32(keys + 4u * uint32_t(blk), evict_key(r));
-            }
-        }
-        if (ranks > 1) {
-            cluster_sync_all();
-            if (rank != 0) return;
-        } else {
-            __syncthreads();
+    for (int s = 0; s < kSelectSets; ++s) {
+        if (mine == s) own = tile[s];
+        hi[s] = lo[s] = make_uint4(0u, 0u, 0u, 0u);
+        if (tile[s] >= 0) {
+            const uint8_t* rec = head + size_t(tile[s]) * stride + 16 * sub;
+            hi[s] = *reinterpret_cast<const uint4*>(rec);
+            lo[s] = *reinterpret_cast<const uint4*>(rec + D);
         }
     }
-    if (rank != 0) return;
+    const float scale = own >= 0 ? *reinterpret_cast<const float*>(head + size_t(own) * stride + 2 * D) : 0.f;
+    int best = INT_MIN;
+    for (int h = 0; h < p.G; ++h) {
+        const uint4 qp = *reinterpret_cast<const uint4*>(s_qp + h * (D / 4) + 4 * sub), qn = *reinterpret_cast<const uint4*>(s_qn + h * (D / 4) + 4 * sub);
+        int a[kSelectSets];
+#pragma unroll
+        for (int s = 0; s < kSelectSets; ++s) {
+            int v = __dp4a(int(qp.x), int(hi[s].x), 0);
+            v = __dp4a(int(qp.y), int(hi[s].y), v);
+            v = __dp4a(int(qp.z), int(hi[s].z), v);
+            v = __dp4a(int(qp.w), int(hi[s].w), v);
+            v = __dp4a(int(qn.x), int(lo[s].x), v);
+            v = __dp4a(int(qn.y), int(lo[s].y), v);
+            v = __dp4a(int(qn.z), int(lo[s].z), v);
+            a[s] = __dp4a(int(qn.w), int(lo[s].w), v);
+        }
+        // sums over the lanes of a block; each lane keeps one of the four sets
+        constexpr int O2 = LPB / 2, O1 = LPB / 4;
+        const bool up2 = sub & O2, up1 = sub & O1;
+        const int g0 = __shfl_xor_sync(0xffffffffu, up2 ? a[0] : a[2], O2), g1 = __shfl_xor_sync(0xffffffffu, up2 ? a[1] : a[3], O2);
+        const int c0 = (up2 ? a[2] : a[0]) + g0, c1 = (up2 ? a[3] : a[1]) + g1;
+        int v = (up1 ? c1 : c0) + __shfl_xor_sync(0xffffffffu, up1 ? c0 : c1, O1);
+        if (LPB == 8) v += __shfl_xor_sync(0xffffffffu, v, 1);
+        best = max(best, v);
+    }
+    const int blk = i0 + mine * GPW + grp;
+    if ((LPB == 4 || (sub & 1) == 0) && blk < old)
+        // a block without a page is the last to be taken, one with keys that are not finite the first
+        put(blk, evict_key(own >= 0 ? (scale < INFINITY ? float(best) * scale : INFINITY) : -INFINITY));
+}
 
-    // ---- the lowest key that stays: keys > thr do, and the first `ties` that equal it ----
-    const int run = ((old + kSelectThreads - 1) / kSelectThreads) | 1;   // keys of a thread: adjacent ones, an odd number for the banks
+struct SelectShared {
+    __align__(16) uint32_t hist[4][256];          // all 0 at the start
+    uint32_t gt[kSelectWarps], eq[kSelectWarps], mn[kSelectWarps], mx[kSelectWarps];
+};
+
+// The blocks that stay, by a CTA with their ratings in shared memory (mn, mx: least and largest that this thread has seen of them): those above the lowest that
+// stays, and the first `ties` that equal it, in their order; then the recent ones, and -1.
+__device__ __forceinline__ void select_blocks(const PagesSelectParams& p, const SelectParts& x, int* index, const uint32_t* s_key, uint32_t mn, uint32_t mx, SelectShared& s) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int old = x.old, want = x.want;
+    const int run = ((old + kSelectThreads - 1) / kSelectThreads) | 1;   // ratings of a thread: adjacent ones, an odd number for the banks
     const int r0 = min(tid * run, old), r1 = min(r0 + run, old);
     uint32_t thr = 0u, ties = 0u;
-    if (some) {
-        uint32_t mn = 0xffffffffu, mx = 0u;
-        for (int i = r0; i < r1; ++i) { const uint32_t k = s_key[i]; mn = min(mn, k); mx = max(mx, k); }
+    if (x.some()) {
         mn = __reduce_min_sync(0xffffffffu, mn);
         mx = __reduce_max_sync(0xffffffffu, mx);
-        if (lane == 0) { atomicMin(&s_min, mn); atomicMax(&s_max, mx); }
+        if (lane == 0) { s.mn[warp] = mn; s.mx[warp] = mx; }
         __syncthreads();
-        mn = s_min; mx = s_max;
+#pragma unroll
+        for (int i = 0; i < kSelectWarps; ++i) { mn = min(mn, s.mn[i]); mx = max(mx, s.mx[i]); }
         int shift = mn == mx ? 0 : 32 - __clz(mn ^ mx);              // bits below `shift` are still to be found
-        uint32_t left = uint32_t(want), count = uint32_t(old);       // keys still to take among those that agree so far, and how many agree
+        uint32_t left = uint32_t(want), count = uint32_t(old);       // still to take among those that agree so far, and how many agree
         thr = shift < 32 ? mx >> shift << shift : 0u;
         for (int pass = 0; shift > 0 && count > left; ++pass) {
             const int bits = min(shift, 8), agree = shift;
             shift -= bits;
-            uint32_t* hist = s_hist[pass];
+            uint32_t* hist = s.hist[pass];
             for (int i = r0; i < r1; ++i) {
                 const uint32_t k = s_key[i];
                 if (agree == 32 || ((k ^ thr) >> agree) == 0u) atomicAdd(&hist[(k >> shift) & ((1u << bits) - 1u)], 1u);
             }
             __syncthreads();
             // every warp for itself: 8 bins a lane
-            const uint4 x = *reinterpret_cast<const uint4*>(&hist[8 * lane]), y = *reinterpret_cast<const uint4*>(&hist[8 * lane + 4]);
-            const uint32_t c[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+            const uint4 u = *reinterpret_cast<const uint4*>(&hist[8 * lane]), v = *reinterpret_cast<const uint4*>(&hist[8 * lane + 4]);
+            const uint32_t c[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
             uint32_t sum = 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum += c[j];
@@ -564,7 +554,7 @@ pages_select_kernel(const PagesSelectParams p) {
                 const uint32_t up = __shfl_down_sync(0xffffffffu, incl, off);
                 if (lane + off < 32) incl += up;
             }
-            uint32_t over = incl - sum;                              // keys in bins above this lane's
+            uint32_t over = incl - sum;                              // in bins above this lane's
             const int at = __ffs(__ballot_sync(0xffffffffu, over < left && incl >= left)) - 1;
             uint32_t bin = 8u * lane;
 #pragma unroll
@@ -572,19 +562,19 @@ pages_select_kernel(const PagesSelectParams p) {
                 if (over + c[j] >= left) { bin += uint32_t(j); break; }
                 over += c[j];
             }
-            thr |= __shfl_sync(0xffffffffu, bin, at) << shift;
+            bin = __shfl_sync(0xffffffffu, bin, at);
+            thr |= bin << shift;
             left -= __shfl_sync(0xffffffffu, over, at);
-            count = hist[__shfl_sync(0xffffffffu, bin, at)];
+            count = hist[bin];
         }
         ties = left;
-        if (shift > 0) {                                             // all that agree stay: key >= thr, whose lower bits are 0
+        if (shift > 0) {                                             // all that agree stay: rating >= thr, whose lower bits are 0
             ties = thr == 0u ? uint32_t(old) : 0u;
             thr = thr == 0u ? 0u : thr - 1u;
         }
     }
-    // ---- the blocks in their order ----
     uint32_t gt = 0, eq = 0;
-    if (some) {
+    if (x.some()) {
         for (int i = r0; i < r1; ++i) { const uint32_t k = s_key[i]; gt += k > thr; eq += k == thr; }
     } else if (want > 0) {
         gt = uint32_t(r1 - r0);
@@ -592,15 +582,15 @@ pages_select_kernel(const PagesSelectParams p) {
     uint32_t gt_incl = gt, eq_incl = eq;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-        const uint32_t x = __shfl_up_sync(0xffffffffu, gt_incl, off), y = __shfl_up_sync(0xffffffffu, eq_incl, off);
-        if (lane >= off) { gt_incl += x; eq_incl += y; }
+        const uint32_t a = __shfl_up_sync(0xffffffffu, gt_incl, off), e = __shfl_up_sync(0xffffffffu, eq_incl, off);
+        if (lane >= off) { gt_incl += a; eq_incl += e; }
     }
-    if (lane == 31) { s_gt[warp] = gt_incl; s_eq[warp] = eq_incl; }
+    if (lane == 31) { s.gt[warp] = gt_incl; s.eq[warp] = eq_incl; }
     __syncthreads();
-    uint32_t gt_before = __reduce_add_sync(0xffffffffu, lane < warp ? s_gt[lane] : 0u) + gt_incl - gt;
-    uint32_t eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? s_eq[lane] : 0u) + eq_incl - eq;
+    const uint32_t gt_before = __reduce_add_sync(0xffffffffu, lane < warp ? s.gt[lane] : 0u) + gt_incl - gt;
+    uint32_t eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? s.eq[lane] : 0u) + eq_incl - eq;
     uint32_t at = gt_before + min(eq_before, ties);
-    if (some) {
+    if (x.some()) {
         for (int i = r0; i < r1; ++i) {
             const uint32_t k = s_key[i];
             const bool tie = k == thr;
@@ -610,7 +600,87 @@ pages_select_kernel(const PagesSelectParams p) {
     } else if (want > 0) {
         for (int i = r0; i < r1; ++i) index[at++] = i;
     }
-    for (int i = tid; i < p.n_keep - want; i += kSelectThreads) index[want + i] = i < recent ? old + i : -1;
+    for (int i = tid; i < p.n_keep - want; i += kSelectThreads) index[want + i] = i < x.recent ? old + i : -1;
+}
+
+__device__ __forceinline__ void st_cluster_u32(uint32_t addr, uint32_t v) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
+// grid (cluster, Hk, B)
+template <int D>
+__global__ void __launch_bounds__(kSelectThreads, 4)
+pages_select_one_kernel(const PagesSelectParams p) {
+    extern __shared__ __align__(16) uint32_t s_one[];                // [2][G][D / 4] queries, [most] ratings of the first CTA
+    __shared__ SelectShared s;
+    uint32_t* s_key = s_one + 2 * p.G * (D / 4);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int ranks = gridDim.x, rank = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
+    const SelectParts x(p, b);
+    uint32_t mn = 0xffffffffu, mx = 0u;
+    if (x.some()) {
+        if (ranks > 1) cluster_arrive();                             // this CTA has started
+        if (warp == 0) queries_in_8_bits<D>(p, b, hk, s_one, lane);
+        else if (rank == 0)
+            for (int i = tid - 32; i < 4 * 256; i += kSelectThreads - 32) s.hist[0][i] = 0u;
+        __syncthreads();
+        if (ranks > 1) cluster_wait();                               // and so has the first one
+        const uint32_t keys = ranks > 1 ? cluster_map_shared(smem_u32(s_key), 0u) : smem_u32(s_key);
+        constexpr int STEP = select_step(D);
+        for (int i0 = (rank * kSelectWarps + warp) * STEP; i0 < x.old; i0 += ranks * kSelectWarps * STEP)
+            rate_blocks<D>(p, b, hk, i0, x.old, s_one, lane, [&](int blk, uint32_t k) { st_cluster_u32(keys + 4u * uint32_t(blk), k); });
+        if (ranks > 1) cluster_sync_all();
+        else __syncthreads();
+        if (rank == 0)
+            for (int i = tid; i < x.old; i += kSelectThreads) { const uint32_t k = s_key[i]; mn = min(mn, k); mx = max(mx, k); }
+    }
+    if (rank == 0) select_blocks(p, x, p.index + (size_t(b) * p.Hk + hk) * p.n_keep, s_key, mn, mx, s);
+}
+
+// grid (parts of a sequence, eights of the key/value heads, B).  The warps of a CTA take adjacent heads, whose bounds are adjacent in memory.
+template <int D>
+__global__ void __launch_bounds__(kSelectThreads, 4)
+pages_rate_kernel(const PagesSelectParams p) {
+    constexpr int STEP = select_step(D);
+    extern __shared__ __align__(16) uint32_t s_q[];                  // [heads][2][G][D / 4]
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int hk0 = int(blockIdx.y) * kSelectWarps, heads = min(p.Hk - hk0, kSelectWarps), b = blockIdx.z;
+    const int at_once = kSelectWarps / heads;                        // steps that the warps take side by side
+    const SelectParts x(p, b);
+    const int first = int(blockIdx.x) * at_once * p.rounds * STEP;
+    if (!x.some() || first >= x.old) return;
+    const uint32_t* queries = s_q + warp % heads * 2 * p.G * (D / 4);
+    if (warp < heads) queries_in_8_bits<D>(p, b, hk0 + warp, s_q + warp * 2 * p.G * (D / 4), lane);
+    __syncthreads();
+    if (warp >= at_once * heads) return;
+    const int hk = hk0 + warp % heads;
+    uint32_t* rating = p.rating + (size_t(b) * p.Hk + hk) * p.most;
+    int i0 = first + warp / heads * STEP;
+    for (int round = 0; round < p.rounds && i0 < x.old; ++round, i0 += at_once * STEP)
+        rate_blocks<D>(p, b, hk, i0, x.old, queries, lane, [&](int blk, uint32_t k) { rating[blk] = k; });
+}
+
+// grid (Hk, B)
+__global__ void __launch_bounds__(kSelectThreads)
+pages_select_kernel(const PagesSelectParams p) {
+    extern __shared__ __align__(16) uint32_t s_key[];                // [most]
+    __shared__ SelectShared s;
+    const int tid = threadIdx.x, hk = blockIdx.x, b = blockIdx.y;
+    const SelectParts x(p, b);
+    for (int i = tid; i < 4 * 256; i += kSelectThreads) s.hist[0][i] = 0u;
+    grid_dependency_wait();                                          // the ratings
+    uint32_t mn = 0xffffffffu, mx = 0u;
+    if (x.some()) {
+        const uint32_t* rating = p.rating + (size_t(b) * p.Hk + hk) * p.most;
+#pragma unroll 4
+        for (int i = tid; i < x.old; i += kSelectThreads) {
+            const uint32_t k = __ldcg(rating + i);
+            s_key[i] = k;
+            mn = min(mn, k);
+            mx = max(mx, k);
+        }
+    }
+    select_blocks(p, x, p.index + (size_t(b) * p.Hk + hk) * p.n_keep, s_key, mn, mx, s);
 }
 
 }  // namespace moda

@@ -59,8 +59,13 @@ def test_rows_validation(f):
 
 
 def test_select_validation():
-    def call(q=P, bounds=P, table=P, lens=P, B=2, T=200, page=64, pages_n=10, most=4, H=4, Hk=2, d=64, n=3, recent=1, index=P):
-        return binding.load().moda_kv_select_blocks(q, bounds, table, lens, B, T, page, pages_n, most, H, Hk, d, n, recent, index, None)
+    need = moda.moda_kv_select_workspace_bytes(2, 200, 2)
+    assert need >= 2 * 2 * 4 * 4 and moda.moda_kv_select_workspace_bytes(1, 64 * 32768 + 1, 1) == 0 and moda.moda_kv_select_workspace_bytes(0, 5, 1) == 0
+
+    def call(q=P, bounds=P, table=P, lens=P, B=2, T=200, page=64, pages_n=10, most=4, H=4, Hk=2, d=64, n=3, recent=1, index=P, work=P, wb=need):
+        return binding.load().moda_kv_select_blocks(q, bounds, table, lens, B, T, page, pages_n, most, H, Hk, d, n, recent, index, work, ctypes.c_size_t(wb), None)
+
+    assert call(work=None) == -7 and call(work=ODD) == -7 and call(wb=need - 1) == -7
 
     for bad in (dict(B=0), dict(T=-1), dict(T=257), dict(page=65), dict(pages_n=0), dict(n=0), dict(recent=-1), dict(recent=4), dict(H=0), dict(n=1 << 30),
                 dict(T=64 * 32768 + 1, most=1 << 20)):
@@ -143,19 +148,22 @@ def test_plain_forms_agree_with_themselves():
 
 RULES = r"""
 #include "launch_rules.h"
+extern "C" int rate_rounds(int blocks, int step, int rows, int sms) { return moda::rate_rounds(blocks, step, rows, sms); }
 extern "C" int select_ranks(int blocks, int rows, int sms) { return moda::select_ranks(blocks, rows, sms); }
-extern "C" int most_blocks() { return moda::kSelectMostBlocks; }
 """
 
 
-def test_cluster_of_a_selection(tmp_path):
+def test_forms_of_a_selection(tmp_path):
     src, so = tmp_path / "rules.cpp", tmp_path / "rules.so"
     src.write_text(RULES)
     subprocess.run(["g++", "-std=c++17", "-shared", "-fPIC", f"-I{build.CSRC}", "-o", str(so), str(src)], check=True)
-    ranks = ctypes.CDLL(str(so)).select_ranks
+    lib = ctypes.CDLL(str(so))
     for blocks in (0, 1, 128, 129, 1000, 5000, 32768):
         for rows in (1, 8, 147, 148, 149, 592, 593, 10000):
-            r = ranks(blocks, rows, 148)
-            assert r in (1, 2, 4, 8) and (r == 1 or rows * r <= 8 * 148)
-            assert blocks > 128 or r == 1
-    assert ranks(32768, 8, 148) == 8
+            r = lib.rate_rounds(blocks, 128, rows, 148)
+            ctas = lambda n: rows * -(-blocks // (128 * n))
+            assert r in (1, 2, 4, 8) and (r == 8 or ctas(r) <= 8 * 148) and (r == 1 or ctas(r // 2) > 8 * 148)
+            n = lib.select_ranks(blocks, rows, 148)
+            assert n in (0, 1, 2, 4, 8) and rows * n <= 4 * 148 and (n < 2 or blocks > 64 * n)
+            assert n > 0 or rows > 4 * 148 // 8 or blocks > 4096
+    assert lib.select_ranks(1024, 8, 148) == 8 and lib.select_ranks(2048, 256, 148) == 0 and lib.select_ranks(32768, 1, 148) == 0
