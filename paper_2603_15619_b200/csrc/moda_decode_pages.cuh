@@ -273,9 +273,49 @@ pages_split_kernel(const PagesDecodeParams p) {
     float* scales = reinterpret_cast<float*>(ring + NP * PIECE);     // [kScaleSets][128], of consecutive units
     PagesWalk ahead;                                                 // the unit that is looked up next
     ahead.begin(s_before, p.B, p.Hk, first);
-    PagesWalk at = ahead;                                            // the one in work
     int left = n_unit;                                               // units not yet looked up
-    struct Place { const uint8_t* rec; int rows; };                  // where a unit lies (null: nowhere), its keys
+    uint32_t qf[KP][8];                                              // this lane's features of head g, f16
+    float q_scale[2];                                                // scale log2(e) over the power of two of heads 2 t, 2 t + 1
+    auto load_q = [&](uint4 (&v)[KP][2], int group) {
+#pragma unroll
+        for (int i = 0; i < KP; ++i) {
+            v[i][0] = v[i][1] = make_uint4(0u, 0u, 0u, 0u);
+            if (g < p.G) {
+                const uint4* src = reinterpret_cast<const uint4*>(p.q + (size_t(group) * p.G + g) * D + 64 * i + 16 * t);
+                v[i][0] = src[0];
+                v[i][1] = src[1];
+            }
+        }
+    };
+    auto take_q = [&](const uint4 (&v)[KP][2]) {
+        float most = 0.f;
+#pragma unroll
+        for (int i = 0; i < KP; ++i)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const uint32_t words[4] = {v[i][k].x, v[i][k].y, v[i][k].z, v[i][k].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) most = fmaxf(most, fmaxf(fabsf(bf16_lo_to_f32(words[j])), fabsf(bf16_hi_to_f32(words[j]))));
+            }
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+        const int e = max(int(__float_as_uint(most) >> 23), 20) - 127;          // most < 2^(e + 1): times 2^(14 - e), below 2^15
+        const float up = __uint_as_float(uint32_t(127 + 14 - e) << 23);
+        const float down = p.scale_log2 * __uint_as_float(uint32_t(127 - 14 + e) << 23);
+        q_scale[0] = __shfl_sync(0xffffffffu, down, 8 * t);
+        q_scale[1] = __shfl_sync(0xffffffffu, down, 8 * t + 4);
+#pragma unroll
+        for (int i = 0; i < KP; ++i)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const uint32_t words[4] = {v[i][k].x, v[i][k].y, v[i][k].z, v[i][k].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) qf[i][4 * k + j] = pack_f16x2(bf16_lo_to_f32(words[j]) * up, bf16_hi_to_f32(words[j]) * up);
+            }
+    };
+    uint4 raw[KP][2];
+    load_q(raw, ahead.b * p.Hk + ahead.r);                                 // ahead of the pieces, behind which it would wait
+    struct Place { const uint8_t* rec; int rows, group; };           // where a unit lies (null: nowhere), its keys; sequence Hk + group
     auto block_of = [&]() -> int {
         return p.index ? p.index[(size_t(ahead.b) * (p.Hk / p.kv_rep) + ahead.r / p.kv_rep) * p.n_index + ahead.j] : ahead.j;
     };
@@ -285,6 +325,7 @@ pages_split_kernel(const PagesDecodeParams p) {
         Place x;
         x.rec = tile >= 0 ? p.pages + (size_t(tile) * (p.Hk / p.kv_rep) + ahead.r / p.kv_rep) * page_block_bytes(D) : nullptr;
         x.rows = tile >= 0 ? min(len - blk * kPageBlock, kPageBlock) : 0;
+        x.group = ahead.b * p.Hk + ahead.r;
         if (--left > 0) ahead.next(s_before, p.Hk);
         return x;
     };
@@ -308,54 +349,19 @@ pages_split_kernel(const PagesDecodeParams p) {
     };
     Place place[AHEAD + 1];                                          // of units u .. u + AHEAD
 #pragma unroll
+    for (int i = 0; i <= AHEAD; ++i) place[i] = left > 0 ? look_up(block_of()) : Place{nullptr, 0, -1};
+#pragma unroll
     for (int i = 0; i <= AHEAD; ++i) {
-        place[i] = left > 0 ? look_up(block_of()) : Place{nullptr, 0};
         if (2 * i < NP) request(place[i].rec, i, 0, 2 * i);
         if (2 * i + 1 < NP) request(place[i].rec, i, 1, 2 * i + 1);
     }
+    take_q(raw);
+    if (place[1].group != place[0].group && place[1].group >= 0) load_q(raw, place[1].group);
     int slot = 0;                                                    // of the piece in work, which the one NP behind it takes over
     auto pass_on = [&](int u, int i) {
         request(place[(i + NP) / 2].rec, u + (i + NP) / 2, (i + NP) % 2, slot);
         slot = slot + 1 == NP ? 0 : slot + 1;
     };
-
-    uint32_t qf[KP][8];                                              // this lane's features of head g, f16
-    float q_scale[2];                                                // scale log2(e) over the power of two of heads 2 t, 2 t + 1
-    auto load_q = [&]() {
-        uint4 v[KP][2];
-        float most = 0.f;
-#pragma unroll
-        for (int i = 0; i < KP; ++i) {
-            v[i][0] = v[i][1] = make_uint4(0u, 0u, 0u, 0u);
-            if (g < p.G) {
-                const uint4* src = reinterpret_cast<const uint4*>(p.q + (size_t(at.b) * p.H + at.r * p.G + g) * D + 64 * i + 16 * t);
-                v[i][0] = src[0];
-                v[i][1] = src[1];
-            }
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const uint32_t words[4] = {v[i][k].x, v[i][k].y, v[i][k].z, v[i][k].w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) most = fmaxf(most, fmaxf(fabsf(bf16_lo_to_f32(words[j])), fabsf(bf16_hi_to_f32(words[j]))));
-            }
-        }
-        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-        const int e = max(int(__float_as_uint(most) >> 23), 20) - 127;          // most < 2^(e + 1): times 2^(14 - e), below 2^15
-        const float up = __uint_as_float(uint32_t(127 + 14 - e) << 23);
-        const float down = p.scale_log2 * __uint_as_float(uint32_t(127 - 14 + e) << 23);
-        q_scale[0] = __shfl_sync(0xffffffffu, down, 8 * t);
-        q_scale[1] = __shfl_sync(0xffffffffu, down, 8 * t + 4);
-#pragma unroll
-        for (int i = 0; i < KP; ++i)
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const uint32_t words[4] = {v[i][k].x, v[i][k].y, v[i][k].z, v[i][k].w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) qf[i][4 * k + j] = pack_f16x2(bf16_lo_to_f32(words[j]) * up, bf16_hi_to_f32(words[j]) * up);
-            }
-    };
-    load_q();
 
     // of heads 2 t, 2 t + 1: maxima of the scores and of the weights' exponents, row sums (this lane's keys)
     float m[2] = {-INFINITY, -INFINITY}, mw[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
@@ -460,8 +466,7 @@ pages_split_kernel(const PagesDecodeParams p) {
                 for (int i = 0; i < FB; ++i) { o[i][0] *= f[0]; o[i][1] *= f[1]; o[i][2] *= f[0]; o[i][3] *= f[1]; }
             }
         }
-        const bool leaves = u + 1 < n_unit && at.j + 1 == at.n;
-        Place behind = left > 0 ? look_up(blk) : Place{nullptr, 0};
+        Place behind = left > 0 ? look_up(blk) : Place{nullptr, 0, -1};
         cp_async_wait<NP - 1>();
         __syncwarp();
         if (rows > 0) {
@@ -501,12 +506,13 @@ pages_split_kernel(const PagesDecodeParams p) {
         __syncwarp();                                                // everyone has read the values
         pass_on(u, 1);
         if (u + AHEAD + 1 >= n_unit) grid_launch_dependents();       // all loads are on their way: the merge may come up
+        const int group = place[0].group;
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) place[i] = place[i + 1];
         place[AHEAD] = behind;
-        if (leaves || u + 1 == n_unit) {
+        if (place[0].group != group) {
             // ---- the group's partial result of this warp ----
-            float* out = p.part + (size_t(w) + size_t(at.b) * p.Hk + at.r) * p.G * (D + 2);
+            float* out = p.part + (size_t(w) + group) * p.G * (D + 2);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -528,10 +534,9 @@ pages_split_kernel(const PagesDecodeParams p) {
 #pragma unroll
             for (int i = 0; i < FB; ++i) { o[i][0] = 0.f; o[i][1] = 0.f; o[i][2] = 0.f; o[i][3] = 0.f; }
         }
-        if (u + 1 < n_unit) {
-            at.next(s_before, p.Hk);
-            if (leaves) load_q();
-        }
+        // the queries of the next unit's group; those of the one behind it are on their way for a unit's time
+        if (place[0].group != group && place[0].group >= 0) take_q(raw);
+        if (place[1].group != place[0].group && place[1].group >= 0) load_q(raw, place[1].group);
     }
 }
 
