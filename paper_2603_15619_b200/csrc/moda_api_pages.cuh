@@ -204,10 +204,10 @@ int moda_attn_decode_e4m3(const void* q, const void* pages, const int* block_tab
     if (int rc = device_sm_count(&sms)) return rc;
     PagesDecodeParams p = {};
     p.kv_rep = H / H_kv > 8 ? H / H_kv / 8 : 1;
-    set_pages(p, block_table, B, H_kv * p.kv_rep, page_size, num_pages, max_blocks_per_seq);
+    set_pages(p, block_table, B, H_kv, page_size, num_pages, max_blocks_per_seq);
     p.q = static_cast<const __nv_bfloat16*>(q); p.pages = static_cast<const uint8_t*>(pages); p.lens = seq_lens; p.index = index;
     p.depth = static_cast<const __nv_bfloat16*>(depth_kv_token); p.O = static_cast<__nv_bfloat16*>(O); p.LSE = LSE;
-    p.G = H / p.Hk; p.H = H; p.l = l; p.max_len = max_seq_len; p.n_index = n_blocks;
+    p.G = H / H_kv / p.kv_rep; p.H = H; p.l = l; p.max_len = max_seq_len; p.n_index = n_blocks;
     p.part = static_cast<float*>(workspace);
     p.before = reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + pages_part_bytes(B, H, p.G, d));
     p.warps = std::min(sms, kPagesMostCtas) * pages_split_warps(d);

@@ -31,18 +31,19 @@
 namespace moda {
 
 struct PagesDecodeParams : PagesParams {
-    // Hk counts groups of at most 8 query heads; kv_rep of them read one key/value head
+    // The query heads of a key/value head in kv_rep sets of at most 8; set s of head hk of sequence b is number (b Hk + hk) kv_rep + s, heads number * G ..
     const __nv_bfloat16* q;       // [B][H][d]
     const uint8_t* pages;
     const int* lens;              // [B], each 0 .. max_len
-    const int* index;             // [B][Hk / kv_rep][n_index]: blocks, or null: all
-    const __nv_bfloat16* depth;   // [l][B][Hk / kv_rep][2][d]
+    const int* index;             // [B][Hk][n_index]: blocks, or null: all
+    const __nv_bfloat16* depth;   // [l][B][Hk][2][d]
     __nv_bfloat16* O;             // [B][H][d]
     float* LSE;                   // [B][H]
-    float* part;                  // [warps + B Hk][G][d + 2]: m (log2 domain), l, o[d]
+    float* part;                  // [warps + sets][G][d + 2], then [sets][G][d + 2] of the depth pairs: m (log2 domain), l, o[d]
     int* before;                  // [B + 1]: blocks of the sequences before each
     int G, H, l, kv_rep, max_len, n_index, warps;
     float scale_log2;
+    __device__ __forceinline__ int sets() const { return B * Hk * kv_rep; }
     __device__ __forceinline__ int len(int b) const { return min(max(lens[b], 0), max_len); }
     // Blocks of a sequence that a group takes.
     __device__ __forceinline__ int units(int b) const {
@@ -111,17 +112,16 @@ struct PagesWalk {
 // The depth pairs of a group's token by one warp: a partial result like those of the cached keys.  Scores by m16n8k16 products of bf16 (heads as rows, slots as
 // columns), weights in fp32 through shared memory, and the weighted values on the CUDA cores, each lane D / 32 features of all heads.
 template <int D>
-__device__ __forceinline__ void pages_depth(const PagesDecodeParams& p, int b, int r, float (*s_w)[8], float* out, int lane) {
+__device__ __forceinline__ void pages_depth(const PagesDecodeParams& p, int set, float (*s_w)[8], float* out, int lane) {
     constexpr int FPL = D / 32, SLOTS = 32;
     const int g = lane >> 2, t = lane & 3;
-    const int heads = p.Hk / p.kv_rep;
-    const size_t stride = size_t(p.B) * heads * 2 * D;               // elements between depth slots
-    const __nv_bfloat16* depth0 = p.depth + (size_t(b) * heads + r / p.kv_rep) * 2 * D;
+    const size_t stride = size_t(p.B) * p.Hk * 2 * D;                // elements between depth slots
+    const __nv_bfloat16* depth0 = p.depth + size_t(set / p.kv_rep) * 2 * D;
     uint4 q[D / 32];
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
         q[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (g < p.G) q[i] = *reinterpret_cast<const uint4*>(p.q + (size_t(b) * p.H + r * p.G + g) * D + 32 * i + 8 * t);
+        if (g < p.G) q[i] = *reinterpret_cast<const uint4*>(p.q + (size_t(set) * p.G + g) * D + 32 * i + 8 * t);
     }
     float m = -INFINITY, sum = 0.f, acc[8][FPL];
 #pragma unroll
@@ -232,9 +232,9 @@ pages_split_kernel(const PagesDecodeParams p) {
     if (p.index) grid_dependency_wait();                             // launched beside what comes before it in the stream
     if (warp >= NW) {
         // ---- warps for the depth pairs ----
-        const int groups = p.l > 0 ? p.B * p.Hk : 0;
-        for (int i = (warp - NW) * gridDim.x + blockIdx.x; i < groups; i += L::kDepthWarps * gridDim.x)
-            pages_depth<D>(p, i / p.Hk, i % p.Hk, s_w[warp - NW], p.part + (size_t(p.warps) + size_t(p.B) * p.Hk + i) * p.G * (D + 2), lane);
+        const int sets = p.l > 0 ? p.sets() : 0;
+        for (int i = (warp - NW) * gridDim.x + blockIdx.x; i < sets; i += L::kDepthWarps * gridDim.x)
+            pages_depth<D>(p, i, s_w[warp - NW], p.part + (size_t(p.warps) + p.sets() + i) * p.G * (D + 2), lane);
         return;
     }
     // ---- blocks of the sequences before each ----
@@ -262,10 +262,11 @@ pages_split_kernel(const PagesDecodeParams p) {
         if (blockIdx.x == 0)
             for (int b = tid; b <= p.B; b += NW * 32) p.before[b] = s_before[b];
     }
-    const long long total = (long long)s_before[p.B] * p.Hk, runs = min(total, (long long)p.warps);
-    const int w = warp * gridDim.x + blockIdx.x;                     // neighbours in the order are on different SMs
-    if (w >= runs) return;
-    const int first = int(total * w / runs), n_unit = int(total * (w + 1) / runs) - first;
+    // neighbours in the order are on different SMs; the sets of a head take the same blocks at the same time, so that one of them finds them in L2
+    const long long total = (long long)s_before[p.B] * p.Hk, runs = min(total, (long long)(p.warps / p.kv_rep));
+    const int w = warp * gridDim.x + blockIdx.x, run = w / p.kv_rep, set = w - run * p.kv_rep;
+    if (run >= runs) return;
+    const int first = int(total * run / runs), n_unit = int(total * (run + 1) / runs) - first;
 
     // ---- the ring: pieces (a unit's keys, then its values) in order, the next ones on their way while one is worked on ----
     uint8_t* ring = split_smem + warp * L::kWarpBytes;
@@ -314,18 +315,18 @@ pages_split_kernel(const PagesDecodeParams p) {
             }
     };
     uint4 raw[KP][2];
-    load_q(raw, ahead.b * p.Hk + ahead.r);                                 // ahead of the pieces, behind which it would wait
-    struct Place { const uint8_t* rec; int rows, group; };           // where a unit lies (null: nowhere), its keys; sequence Hk + group
+    load_q(raw, (ahead.b * p.Hk + ahead.r) * p.kv_rep + set);                                 // ahead of the pieces, behind which it would wait
+    struct Place { const uint8_t* rec; int rows, group; };           // where a unit lies (null: nowhere), its keys, its set of heads
     auto block_of = [&]() -> int {
-        return p.index ? p.index[(size_t(ahead.b) * (p.Hk / p.kv_rep) + ahead.r / p.kv_rep) * p.n_index + ahead.j] : ahead.j;
+        return p.index ? p.index[(size_t(ahead.b) * p.Hk + ahead.r) * p.n_index + ahead.j] : ahead.j;
     };
     auto look_up = [&](int blk) -> Place {
         const int len = p.len(ahead.b);
         const int tile = blk >= 0 && blk < pages_blocks(len) ? p.tile(ahead.b, blk) : -1;
         Place x;
-        x.rec = tile >= 0 ? p.pages + (size_t(tile) * (p.Hk / p.kv_rep) + ahead.r / p.kv_rep) * page_block_bytes(D) : nullptr;
+        x.rec = tile >= 0 ? p.pages + (size_t(tile) * p.Hk + ahead.r) * page_block_bytes(D) : nullptr;
         x.rows = tile >= 0 ? min(len - blk * kPageBlock, kPageBlock) : 0;
-        x.group = ahead.b * p.Hk + ahead.r;
+        x.group = (ahead.b * p.Hk + ahead.r) * p.kv_rep + set;
         if (--left > 0) ahead.next(s_before, p.Hk);
         return x;
     };
@@ -512,7 +513,7 @@ pages_split_kernel(const PagesDecodeParams p) {
         place[AHEAD] = behind;
         if (place[0].group != group) {
             // ---- the group's partial result of this warp ----
-            float* out = p.part + (size_t(w) + group) * p.G * (D + 2);
+            float* out = p.part + (size_t(run) * p.kv_rep + group) * p.G * (D + 2);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -572,14 +573,14 @@ pages_merge_kernel(const PagesDecodeParams p) {
         own = __ldcg(p.before + b + 1) - before;
         all = __ldcg(p.before + p.B);
     }
-    const long long total = (long long)all * p.Hk, first = (long long)before * p.Hk + (long long)r * own;
-    // warp of a unit: the one whose run holds it
-    const long long runs = min(total, (long long)p.warps);
+    const long long total = (long long)all * p.Hk, first = (long long)before * p.Hk + (long long)(r / p.kv_rep) * own;
+    // run of a unit
+    const long long runs = min(total, (long long)(p.warps / p.kv_rep));
     const int w0 = own > 0 ? int(((first + 1) * runs - 1) / total) : 0, w1 = own > 0 ? int(((first + own) * runs - 1) / total) : -1;
     const int S = w1 - w0 + 1, n = S + (p.l > 0 ? 1 : 0);            // the last one is that of the depth pairs
-    const size_t stride = size_t(p.G) * (D + 2), group = size_t(b) * p.Hk + r;
-    const float* part = p.part + (size_t(w0) + group) * stride + g * (D + 2);
-    const float* depth = p.part + (size_t(p.warps) + size_t(p.B) * p.Hk + group) * stride + g * (D + 2);
+    const size_t stride = size_t(p.kv_rep) * p.G * (D + 2), group = size_t(b) * p.Hk * p.kv_rep + r;
+    const float* part = p.part + (size_t(w0) * p.kv_rep + group) * p.G * (D + 2) + g * (D + 2);
+    const float* depth = p.part + (size_t(p.warps) + p.sets() + group) * p.G * (D + 2) + g * (D + 2);
     float m = -INFINITY, lt = 0.f, acc[FPL];
 #pragma unroll
     for (int c = 0; c < FPL; ++c) acc[c] = 0.f;
