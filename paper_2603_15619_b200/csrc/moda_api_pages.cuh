@@ -70,14 +70,12 @@ int raise_smem(Kernel kernel, size_t need, int most, int* configured_dev) {
 
 template <int D>
 int launch_select(PagesSelectParams& p, int sms, cudaStream_t stream) {
-    static thread_local int one_dev = -1, rate_dev = -1, select_dev = -1;
+    static thread_local int rate_dev = -1, select_dev = -1;
     const long long rows = (long long)p.B * p.Hk;
     const size_t ratings = size_t(p.most) * 4, queries = size_t(2) * p.G * D;
     const int ranks = select_ranks(p.most, rows, sms);
-    if (ranks > 0) {
-        if (int rc = raise_smem(pages_select_one_kernel<D>, queries + ratings, 2 * MODA_MAX_GROUP * D + kSelectMostBlocks * 4, &one_dev)) return rc;
+    if (ranks > 0)                                // at most 4096 blocks: within what a kernel may have without asking
         return launch_pages(pages_select_one_kernel<D>, dim3(unsigned(ranks), unsigned(p.Hk), unsigned(p.B)), kSelectThreads, queries + ratings, false, p, stream, ranks);
-    }
     const int heads = std::min(p.Hk, kSelectWarps), eights = (p.Hk + kSelectWarps - 1) / kSelectWarps;
     const int step = kSelectWarps / heads * select_step(D);
     p.rounds = rate_rounds(p.most, step, (long long)p.B * eights, sms);

@@ -95,7 +95,8 @@ __device__ __forceinline__ uint32_t times_bf16x2(uint32_t a, uint32_t b) {
     return r;
 }
 
-// 16 features of a row that LANES adjacent lanes hold: their codes and the row's scale.  The depth cache's rule and bytes, in fewer instructions: quotients two at a
+// 16 features of a row that LANES adjacent lanes hold: their codes and the row's scale.  The depth cache's rule and bytes (but for the sign of a NaN), in fewer
+// instructions, which bound the write kernel: quotients two at a
 // time, q = RN(x r) with r = RN(1 / d) corrected by its exact remainder (Markstein's theorem, as div_rn in moda_cache.cuh; a scale's significand, m / 7 of 128 <= m < 256, is
 // never all ones); no element has a branch, as rows of which it would need one are brought into range first (exactly, by a power of two; or by 0, which makes of a row
 // with an infinite element what the division by infinity would), and signs come from the input's words.

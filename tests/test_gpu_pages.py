@@ -43,6 +43,30 @@ def test_write_gives_the_bytes_of_the_definition(B, T, Hk, d, page, start, n_new
 
 
 @pytest.mark.parametrize("d", [64, 128])
+def test_rows_of_every_size_have_the_depth_caches_codes(d):
+    # from bf16's smallest numbers to its largest, rows of one element, quotients that are ties: the oracle's codes and scales, and the bytes of the depth cache
+    rng = np.random.default_rng(d)
+    T = 261
+    X = rng.standard_normal((1, T, 1, d)) * 2.0 ** (np.linspace(-138, 125, T)[None, :, None, None])
+    X[0, ::7, 0, 1:] = 0.0
+    X[0, 1::7] = rng.integers(-255, 256, X[0, 1::7].shape) * 2.0 ** rng.integers(-20, 20, X[0, 1::7].shape[:2] + (1,))
+    X = ref.bf16(np.clip(X, -3e38, 3e38))
+    dev = moda.alloc_kv_pages_e4m3(5, 64, 1, d)
+    table = torch.arange(5, dtype=torch.int32, device="cuda")[None].contiguous()
+    moda.moda_kv_write_e4m3(dev, ref.put(X), ref.put(-X), table)
+    codes, scale = ref.orc.quantize_e4m3_rows(X[0, :, 0])
+    negated, _ = ref.orc.quantize_e4m3_rows(-X[0, :, 0])
+    kc, vc, ks, vs = ref.split(dev.cpu().numpy()[:, 0, 0], d)
+    rows = lambda a: a.reshape(-1, *a.shape[2:])[:T]
+    assert np.array_equal(rows(ks), scale) and np.array_equal(rows(vs), scale)
+    assert np.array_equal(rows(kc), codes) and np.array_equal(rows(vc.swapaxes(-1, -2)), negated)
+    cache = moda.alloc_depth_cache_e4m3(1, T, 1, d, 1)
+    moda.moda_depth_cache_append_e4m3(cache, 0, ref.put(X), ref.put(-X))
+    block = cache.cpu().numpy()[:3 * 2 * (128 * d + 512)].reshape(3, 2, -1)[:, 0]
+    assert np.array_equal(block[:, :128 * d].reshape(3, d // 16, 128, 16).swapaxes(1, 2).reshape(-1, d)[:T], codes)
+
+
+@pytest.mark.parametrize("d", [64, 128])
 def test_rows_that_are_not_finite(d):
     pages, bounds, table, dev = ref.make(1, 100, 2, d, 64, [100], seed=3)
     K, V = (ref.bf16(np.random.default_rng(i).standard_normal((1, 3, 2, d))) for i in range(2))
@@ -113,6 +137,21 @@ def test_selection_is_the_definition(B, lens, H, Hk, d, page, keep, recent, few)
     assert np.array_equal(index.cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("B,blocks,H,Hk,d,keep", [(40, 20, 32, 16, 64, 7), (20, 40, 160, 10, 128, 9), (2, 4200, 2, 1, 64, 33), (1, 11000, 3, 1, 128, 500), (9, 300, 256, 8, 128, 5),
+                                                  (1, 4000, 6, 3, 64, 4)])
+def test_selection_in_both_forms(B, blocks, H, Hk, d, keep):
+    # many rows, very long ones, more heads than a CTA's warps, queries that take more shared memory than a kernel has without asking
+    rng = np.random.default_rng(blocks)
+    lens = [max(64 * blocks - 97 * b * b, 1) for b in range(B)]
+    table = rng.permutation(B * blocks).astype(np.int32).reshape(B, blocks)
+    bounds = _bounds(B * blocks, 1, Hk, d, 2, False)
+    q = ref.bf16(rng.standard_normal((B, H, d)))
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    index = moda.moda_kv_select_blocks(ref.put(q), torch.from_numpy(bounds).cuda(), torch.from_numpy(table).cuda(), n, 64 * blocks, keep, 2).cpu().numpy()
+    some = sorted({0, 1, B // 2, B - 1} & set(range(B)))
+    assert np.array_equal(index[some], ref.select(q[some], bounds, table[some], [lens[b] for b in some], 64, keep, 2))
+
+
 def test_selection_of_blocks_without_a_page_or_with_values_that_are_not_finite():
     d, n = 64, 50
     bounds = _bounds(n, 1, 1, d, 1, False)
@@ -159,7 +198,8 @@ def _check(O, LSE, want):
     empty = np.isneginf(lse)
     assert np.array_equal(np.isneginf(LSE), empty) and (O[empty] == 0).all()
     assert (np.abs(O - o) <= o_tol).all(), float((np.abs(O - o) / np.maximum(o_tol, 1e-30)).max())
-    assert (np.abs(LSE - lse)[~empty] <= lse_tol[~empty]).all(), float((np.abs(LSE - lse)[~empty] / lse_tol[~empty]).max())
+    off = np.abs(LSE[~empty] - lse[~empty]) / lse_tol[~empty]
+    assert (off <= 1).all(), float(off.max())
 
 
 @pytest.mark.parametrize("sharp", [1.0, 30.0])
@@ -258,3 +298,46 @@ def test_same_bits_again_on_another_stream_and_captured():
     torch.cuda.synchronize()
     for got in (second, third, fourth):
         assert all(torch.equal(x, y) for x, y in zip(first, got))
+
+
+def test_pages_far_from_the_first():
+    # more than 2^32 bytes into the pages
+    d, Hk, page = 128, 8, 256
+    num = (1 << 32) // moda.moda_kv_page_e4m3_bytes(page, Hk, d) + 40
+    pages, bounds = moda.alloc_kv_pages_e4m3(num, page, Hk, d), moda.alloc_kv_bounds(num, page, Hk, d)
+    n = 700
+    table = torch.tensor([[num - 1, num - 30, num - 2]], dtype=torch.int32, device="cuda")
+    rng = np.random.default_rng(0)
+    K, V = (ref.bf16(rng.standard_normal((1, n, Hk, d))) for _ in range(2))
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    moda.moda_kv_write_e4m3(pages, ref.put(K), ref.put(V), table, bounds=bounds)
+    small, few = moda.alloc_kv_pages_e4m3(3, page, Hk, d), moda.alloc_kv_bounds(3, page, Hk, d)
+    near = torch.tensor([[1, 0, 2]], dtype=torch.int32, device="cuda")
+    moda.moda_kv_write_e4m3(small, ref.put(K), ref.put(V), near, bounds=few)
+    q = ref.put(ref.bf16(rng.standard_normal((1, 16, d))))
+    for a, b in zip(moda.moda_kv_read_e4m3(pages, table, lens, n), moda.moda_kv_read_e4m3(small, near, lens, n)):
+        assert torch.equal(a, b) and a.any()
+    index = moda.moda_kv_select_blocks(q, bounds, table, lens, n, 4, 1)
+    assert torch.equal(index, moda.moda_kv_select_blocks(q, few, near, lens, n, 4, 1))
+    for i in (None, index):
+        got, want = (moda.moda_attn_decode_e4m3(q, x, t, lens, None, n, 0, 0.1, index=i) for x, t in ((pages, table), (small, near)))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_nothing_is_written_beside_the_outputs():
+    B, H, Hk, d, l, lens = 3, 6, 2, 64, 2, [130, 0, 65]
+    pages, bounds, table, dev = ref.make(B, 130, Hk, d, 64, lens, seed=11)
+    rng = np.random.default_rng(3)
+    q, depth = ref.put(ref.bf16(rng.standard_normal((B, H, d)))), ref.put(ref.bf16(rng.standard_normal((l, B, Hk, 2, d))))
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    band = lambda count, dtype: torch.full((count + 128,), 77, dtype=dtype, device="cuda")
+    Ob, Lb, Ib = band(B * H * d, torch.bfloat16), band(B * H, torch.float32), band(B * Hk * 3, torch.int32)
+    Wb = band(moda.moda_decode_e4m3_workspace_bytes(B, H, Hk, d), torch.uint8)
+    Sb = band(moda.moda_kv_select_workspace_bytes(B, 130, Hk), torch.uint8)
+    cut = lambda t, *s: t[64:-64].view(*s)
+    moda.moda_kv_select_blocks(q, dev[1], dev[2], n, 130, 3, 1, index=cut(Ib, B, Hk, 3), workspace=cut(Sb, -1))
+    moda.moda_attn_decode_e4m3(q, dev[0], dev[2], n, depth, 130, l, 0.1, O=cut(Ob, B, H, d), LSE=cut(Lb, B, H), workspace=cut(Wb, -1))
+    torch.cuda.synchronize()
+    for t in (Ob, Lb, Ib, Wb, Sb):
+        assert (t[:64] == 77).all() and (t[-64:] == 77).all()
+    assert np.array_equal(dev[0].cpu().numpy(), pages) and np.array_equal(dev[1].cpu().numpy(), bounds)
