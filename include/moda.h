@@ -602,7 +602,7 @@ int moda_attn_decode_shared(const void* q, const void* K_prefix, const void* V_p
  *     block_table : device int32 [B][max_blocks_per_seq] as for moda_attn_decode_paged (a "block" there is a page).  An entry outside [0, num_pages) is no page:
  *                   nothing is written there, its rows read as zeros, its keys have no weight.
  *
- * moda_kv_write_e4m3      row i of K, V (bf16 [B][T][H_kv][d]), i < n_new[b] (device int32 [B], 0 .. T; NULL: T), becomes position start[b] + i (device int32 [B]; NULL: 0)
+ * moda_kv_write_e4m3      row i of K, V (bf16 [B][T][H_kv][d]), i < n_new[b] (device int32 [B], 0 .. T; NULL: T), becomes position start[b] + i (device int32 [B], not negative; NULL: 0)
  *                         of sequence b.  Positions behind the table's end are dropped.  Of the blocks that it touches, other positions' codes and scales stay as they are.
  *                         bounds (may be NULL): those of every touched block are set anew, over its positions before start[b] + n_new[b]: per feature the largest and the
  *                         smallest dequantised key, over scale = max / 127, rounded up and down (a block with a value that is not finite: codes 0, scale inf).
@@ -616,7 +616,7 @@ int moda_attn_decode_shared(const void* q, const void* K_prefix, const void* V_p
  *
  *                         (what a key within the bounds could score at most; the sums are of whole numbers).  index : int32 [B][H_kv][n_blocks], ascending, -1 behind them.
  *                         A block without a page is rated last, one whose bounds have scale inf first.  max_seq_len <= 64 * 32768.
- *                         workspace : moda_kv_select_workspace_bytes.  Two launches.
+ *                         workspace : moda_kv_select_workspace_bytes.  One launch or two.
  * moda_attn_decode_e4m3   the decode step: O, LSE, depth_kv_token, groups and scale as for moda_attn_decode_paged, with seq_lens[b] in 0 .. max_seq_len.  index (int32
  *                         [B][H_kv][n_blocks]) NULL: all blocks; else the blocks of the first min(n_blocks, ceil(seq_lens[b] / 64)) entries of a row, an entry that is no block
  *                         of the sequence being passed over (one that comes twice counts twice).  A token without any key has O = 0 and LSE = -inf.

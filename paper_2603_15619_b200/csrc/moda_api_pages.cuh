@@ -171,7 +171,7 @@ int moda_kv_select_blocks(const void* q, const void* bounds, const int* block_ta
     p.q = static_cast<const __nv_bfloat16*>(q); p.bounds = static_cast<const uint8_t*>(bounds); p.lens = seq_lens; p.index = index;
     p.rating = static_cast<uint32_t*>(workspace);
     p.G = H / H_kv; p.max_len = max_seq_len; p.n_keep = n_blocks; p.n_recent = n_recent;
-    p.most = pages_blocks(max_seq_len);
+    p.most = std::max(pages_blocks(max_seq_len), 1);                                    // a grid has a part, also where no sequence has a block
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return d == 128 ? launch_select<128>(p, sms, st) : launch_select<64>(p, sms, st);
 }

@@ -152,6 +152,17 @@ def test_selection_in_both_forms(B, blocks, H, Hk, d, keep):
     assert np.array_equal(index[some], ref.select(q[some], bounds, table[some], [lens[b] for b in some], 64, keep, 2))
 
 
+@pytest.mark.parametrize("B,Hk", [(1, 1), (2, 300), (400, 8)])
+def test_selection_where_no_sequence_has_a_block(B, Hk):
+    d = 64
+    bounds = torch.zeros((1, 1, Hk, 2 * d + 16), dtype=torch.uint8, device="cuda")
+    table, lens = torch.zeros((B, 1), dtype=torch.int32, device="cuda"), torch.zeros((B,), dtype=torch.int32, device="cuda")
+    q = torch.ones((B, Hk, d), dtype=torch.bfloat16, device="cuda")
+    for most in (0, 64):
+        assert moda.moda_kv_select_blocks(q, bounds, table, lens, most, 3, 1).eq(-1).all()
+    assert moda.moda_last_status() == 0
+
+
 def test_selection_of_blocks_without_a_page_or_with_values_that_are_not_finite():
     d, n = 64, 50
     bounds = _bounds(n, 1, 1, d, 1, False)
