@@ -453,33 +453,33 @@ __device__ __forceinline__ void queries_in_8_bits(const PagesSelectParams& p, in
     }
 }
 
-// Ratings of blocks i0 .. i0 + select_step(D) - 1 of a head (below `old`) by a warp, d / 16 lanes a block: put(block, integer in the order of the ratings).
+// Numbers of blocks i0 .. i0 + select_step(D) - 1 of a sequence (below `old`), one a lane.
+template <int D>
+__device__ __forceinline__ int tiles_of(const PagesSelectParams& p, int b, int i0, int old, int lane) {
+    return lane < select_step(D) && i0 + lane < old ? p.tile(b, i0 + lane) : -1;
+}
+
+// Their ratings for a head by a warp, d / 16 lanes a block: put(block, integer in the order of the ratings).
 template <int D, class Put>
-__device__ __forceinline__ void rate_blocks(const PagesSelectParams& p, int b, int hk, int i0, int old, const uint32_t* s_qp, int lane, const Put& put) {
+__device__ __forceinline__ void rate_blocks(const PagesSelectParams& p, int tiles, int hk, int i0, int old, const uint32_t* s_qp, int lane, const Put& put) {
     constexpr int LPB = D / 16, GPW = 32 / LPB;                      // lanes of a block (16 features each), blocks at a time
     const uint32_t* s_qn = s_qp + p.G * (D / 4);
     const int grp = lane / LPB, sub = lane % LPB;
     const int mine = (LPB == 8 ? (sub >> 1) : sub);                  // which set this lane ends up with
     const uint8_t* head = p.bounds + size_t(hk) * page_bounds_bytes(D);
     const size_t stride = size_t(p.Hk) * page_bounds_bytes(D);
-    int tile[kSelectSets];
     uint4 hi[kSelectSets], lo[kSelectSets];
 #pragma unroll
     for (int s = 0; s < kSelectSets; ++s) {
-        const int blk = i0 + s * GPW + grp;
-        tile[s] = blk < old ? p.tile(b, blk) : -1;
-    }
-    int own = tile[0];
-#pragma unroll
-    for (int s = 0; s < kSelectSets; ++s) {
-        if (mine == s) own = tile[s];
+        const int tile = __shfl_sync(0xffffffffu, tiles, s * GPW + grp);
         hi[s] = lo[s] = make_uint4(0u, 0u, 0u, 0u);
-        if (tile[s] >= 0) {
-            const uint8_t* rec = head + size_t(tile[s]) * stride + 16 * sub;
+        if (tile >= 0) {
+            const uint8_t* rec = head + size_t(tile) * stride + 16 * sub;
             hi[s] = *reinterpret_cast<const uint4*>(rec);
             lo[s] = *reinterpret_cast<const uint4*>(rec + D);
         }
     }
+    const int own = __shfl_sync(0xffffffffu, tiles, mine * GPW + grp);
     const float scale = own >= 0 ? *reinterpret_cast<const float*>(head + size_t(own) * stride + 2 * D) : 0.f;
     int best = INT_MIN;
     for (int h = 0; h < p.G; ++h) {
@@ -621,15 +621,20 @@ pages_select_one_kernel(const PagesSelectParams p) {
     uint32_t mn = 0xffffffffu, mx = 0u;
     if (x.some()) {
         if (ranks > 1) cluster_arrive();                             // this CTA has started
+        constexpr int STEP = select_step(D);
+        int i0 = (rank * kSelectWarps + warp) * STEP, tiles = tiles_of<D>(p, b, i0, x.old, lane);
         if (warp == 0) queries_in_8_bits<D>(p, b, hk, s_one, lane);
         else if (rank == 0)
             for (int i = tid - 32; i < 4 * 256; i += kSelectThreads - 32) s.hist[0][i] = 0u;
         __syncthreads();
         if (ranks > 1) cluster_wait();                               // and so has the first one
         const uint32_t keys = ranks > 1 ? cluster_map_shared(smem_u32(s_key), 0u) : smem_u32(s_key);
-        constexpr int STEP = select_step(D);
-        for (int i0 = (rank * kSelectWarps + warp) * STEP; i0 < x.old; i0 += ranks * kSelectWarps * STEP)
-            rate_blocks<D>(p, b, hk, i0, x.old, s_one, lane, [&](int blk, uint32_t k) { st_cluster_u32(keys + 4u * uint32_t(blk), k); });
+        while (i0 < x.old) {
+            const int next = i0 + ranks * kSelectWarps * STEP, behind = tiles_of<D>(p, b, next, x.old, lane);
+            rate_blocks<D>(p, tiles, hk, i0, x.old, s_one, lane, [&](int blk, uint32_t k) { st_cluster_u32(keys + 4u * uint32_t(blk), k); });
+            i0 = next;
+            tiles = behind;
+        }
         if (ranks > 1) cluster_sync_all();
         else __syncthreads();
         if (rank == 0)
@@ -650,15 +655,19 @@ pages_rate_kernel(const PagesSelectParams p) {
     const SelectParts x(p, b);
     const int first = int(blockIdx.x) * at_once * p.rounds * STEP;
     if (!x.some() || first >= x.old) return;
+    int i0 = first + warp / heads * STEP, tiles = tiles_of<D>(p, b, i0, x.old, lane);
     const uint32_t* queries = s_q + warp % heads * 2 * p.G * (D / 4);
     if (warp < heads) queries_in_8_bits<D>(p, b, hk0 + warp, s_q + warp * 2 * p.G * (D / 4), lane);
     __syncthreads();
     if (warp >= at_once * heads) return;
     const int hk = hk0 + warp % heads;
     uint32_t* rating = p.rating + (size_t(b) * p.Hk + hk) * p.most;
-    int i0 = first + warp / heads * STEP;
-    for (int round = 0; round < p.rounds && i0 < x.old; ++round, i0 += at_once * STEP)
-        rate_blocks<D>(p, b, hk, i0, x.old, queries, lane, [&](int blk, uint32_t k) { rating[blk] = k; });
+    for (int round = 0; round < p.rounds && i0 < x.old; ++round) {
+        const int next = i0 + at_once * STEP, behind = tiles_of<D>(p, b, next, x.old, lane);
+        rate_blocks<D>(p, tiles, hk, i0, x.old, queries, lane, [&](int blk, uint32_t k) { rating[blk] = k; });
+        i0 = next;
+        tiles = behind;
+    }
 }
 
 // grid (Hk, B)
