@@ -104,12 +104,15 @@ inline EvictForm evict_form(int T, long long rows, int sms) {
 // The selection of blocks (moda_pages.cuh).
 constexpr int kSelectMostBlocks = 32768;                   // of a sequence: their ratings are held in shared memory
 // CTAs of a cluster that rates and selects the blocks of a row (sequence, head), 128 blocks being one round of a CTA's loads; 0: rate in one kernel, select in another.
+// (d = 128.  8 rows of 1024 blocks: clusters of 1, 2, 4, 8 14.4, 10.5, 8.3, 7.2 us, two kernels 8.4; 64 rows of 512 at most: 10.6, 8.7, 7.4, 8.0 and 9.2; 256 of 1024 at most: clusters of
+// 2 18.0, two kernels 16.6.)
 inline int select_ranks(int blocks, long long rows, int sms) {
     int ranks = 1;
     while (ranks < 8 && blocks > 128 * ranks && rows * ranks * 2 <= 4ll * sms) ranks *= 2;
     return rows * ranks <= 4ll * sms && blocks <= 512 * ranks ? ranks : 0;
 }
 // Rounds of `step` blocks that a CTA of the first of the two takes: one while there are few CTAs, then more, as every CTA has queries to prepare first.
+// (256 rows of 2048 blocks at most: 1, 2, 4, 8 rounds 30.2, 26.7, 24.5, 31.2 us; the rule takes 4.)
 inline int rate_rounds(int blocks, int step, long long rows, int sms) {
     int rounds = 1;
     while (rounds < 8 && rows * ((blocks + step * rounds - 1) / (step * rounds)) > 8ll * sms) rounds *= 2;

@@ -22,7 +22,6 @@ int pages_rows_grid(int B, int T, int H_kv, dim3* grid) {
     return MODA_OK;
 }
 
-constexpr long long kPagesWideMerge = 592;
 constexpr int kPagesMostCtas = 148;               // partial results of that many fit the workspace
 
 inline int pages_split_warps(int d) { return d == 64 ? PagesSplit<64>::kWarps : PagesSplit<128>::kWarps; }
@@ -98,7 +97,9 @@ int launch_decode_pages(const PagesDecodeParams& p, cudaStream_t stream) {
     if (int rc = launch_pages(pages_split_kernel<D>, dim3(unsigned(p.warps / PagesSplit<D>::kWarps)), PagesSplit<D>::kThreads, size_t(PagesSplit<D>::smem(p.B)), p.index != nullptr, p, stream))
         return rc;
     const long long rows = (long long)p.B * p.H;
-    const bool wide = rows <= kPagesWideMerge;
+    // Four warps a row while the rows leave SMs idle and have more than two partial results each, else one.  In us, four and one: 16 rows 8.7 and 11.0, 512 25.2 and
+    // 30.5, 1024 37.3 and 38.2, 1536 48.2 and 47.9, 2048 61.2 and 58.7; 1024 with one to two results each 60.4 and 58.6.
+    const bool wide = rows <= 8 * kPagesMostCtas && 2ll * p.B * p.Hk <= p.warps;
     const long long per = kPagesMergeThreads / 32 / (wide ? 4 : 1);
     return launch_pages(wide ? pages_merge_kernel<D, 4> : pages_merge_kernel<D, 1>, dim3(unsigned((rows + per - 1) / per)), kPagesMergeThreads, 0, true, p, stream);
 }

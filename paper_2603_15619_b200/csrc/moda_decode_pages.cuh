@@ -4,19 +4,27 @@
 //   pages_split_kernel    a block of a (sequence, key/value head) is a unit; the units of all, in this order, are cut into equal runs, one per warp of the
 //                         device, and every warp works through its own: nothing waits for another warp.  A lane's share of a block's keys is the operand of its
 //                         matrix products as it lies in memory, and so is its share of the values: nothing is turned on the way.  A warp has a ring of
-//                         its own for three pieces (a block's keys, or its values) in shared memory, two on their way while one is worked on: 128 KiB an SM.
-//   pages_merge_kernel    a CTA per (sequence, query head): the depth pairs, then the partial results of the group's warps.
+//                         its own for three or four pieces (a block's keys, or its values) in shared memory, all but one on their way: 192 KiB an SM at d = 128.
+//                         Other warps of the CTA take the depth pairs, a partial result like the rest.  Groups of 16 or 32 query heads are sets of 8, whose runs
+//                         take the same blocks at the same time.
+//   pages_merge_kernel    one or four warps per (sequence, query head) join the partial results.
 //
-// One block, lane = (g, t) = (lane / 4, lane % 4), products m16n8k16 of f16 with fp32 sums:
+// One block, lane = (g, t) = (lane / 4, lane % 4), products m16n8k16 of f16 with fp32 sums, eight heads as columns:
 //
-//   S = Q K^T, heads as rows.  Column g of the n-th eight keys is key 16 (g / 2) + 2 n + g % 2 of the block, whose codes 64 i + 16 t .. + 15 the lane holds:
-//   a product pairs the same four of them with the same four of q, so that their order in it is no matter.  Thread t of a row then has the
-//   scores of keys 16 t + 2 n, + 1: in all, of keys 16 t .. 16 t + 15.
-//   O^T = V^T P^T, features as rows: the lane's value codes are those of feature g (and g + 8) of keys 16 t .. 16 t + 15, the keys whose weights it has.
+//   S^T = K Q^T, keys as rows.  Rows g and g + 8 of the j-th sixteen are keys a = 16 (g / 2) + g % 2 + 4 j and a + 2; the lane holds their codes 64 i + 16 t .. + 15, and a
+//   product pairs the same four of them with the same four of q, so that their order in it is no matter.  It ends up with the scores of those keys for heads 2 t, 2 t + 1.
+//   O^T = V^T P^T, features as rows: the lane's value codes are those of feature g (and g + 8) of keys 16 t .. 16 t + 15, whose weights for head g are what the scores'
+//   lanes have, turned 8 x 8 at a time.
 //
 // Codes are exact in f16 and so is q once a row is scaled by a power of two (below 2^-40 of its largest element it is rounded).  Keys' scales multiply scores, in fp32.
 // Values' scales go into the weights: w = exp2(s + log2(scale) - m'), with a running maximum m' of its own, 2^14 below the largest f16 power;
 // weights are rounded to f16 (2^-11) for the product, the row sum and both maxima are fp32.
+//
+// 32 sequences to 8192, 64 heads on 8, d = 128, 24 depth pairs: 59.2 us, of which the merge is 5; the bytes take 43.6 at the copy rate.  Read in this order by these warps
+// without any arithmetic they take 45 (5.97 TB/s); the rest is that SMs which share their path to L2 with more others stream up to 20 % slower (equal runs end
+// after 45 to 61 us).  Runs that others take over when they are done cost more in partial results and in queries that wait behind the stream than they win (63 us
+// and more).  96 sequences to 1500, 24 heads on 8, d = 64: 31 us against 13.2: a block of half the bytes has the same softmax, three heads in columns for eight.
+// Products of e4m3 codes as they are (m16n8k32) are no faster, 67.0 against 66.2 us at that stage.
 #pragma once
 
 #include <cstdint>
@@ -315,7 +323,7 @@ pages_split_kernel(const PagesDecodeParams p) {
             }
     };
     uint4 raw[KP][2];
-    load_q(raw, (ahead.b * p.Hk + ahead.r) * p.kv_rep + set);                                 // ahead of the pieces, behind which it would wait
+    load_q(raw, (ahead.b * p.Hk + ahead.r) * p.kv_rep + set);        // ahead of the pieces, behind which it would wait
     struct Place { const uint8_t* rec; int rows, group; };           // where a unit lies (null: nowhere), its keys, its set of heads
     auto block_of = [&]() -> int {
         return p.index ? p.index[(size_t(ahead.b) * p.Hk + ahead.r) * p.n_index + ahead.j] : ahead.j;
@@ -613,7 +621,7 @@ pages_merge_kernel(const PagesDecodeParams p) {
         for (int c = 0; c < FPL; ++c) acc[c] *= alpha;
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
-            const float f = fast_exp2(ml[u].x - base);               // 0 for a partial without keys, whose sums are 0 or NaN
+            const float f = fast_exp2(ml[u].x - base);               // 0 for a partial without keys, whose sums are 0 (or NaN: then so is the row)
             lt = fmaf(f, ml[u].y, lt);
 #pragma unroll
             for (int c = 0; c < FPL; ++c) acc[c] = fmaf(f, x[u][c], acc[c]);
