@@ -237,7 +237,7 @@ pages_split_kernel(const PagesDecodeParams p) {
     __shared__ __align__(16) float s_w[L::kDepthWarps][32][8];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int g = lane >> 2, t = lane & 3;
-    if (p.index) grid_dependency_wait();                             // launched beside what comes before it in the stream
+    grid_dependency_wait();
     if (warp >= NW) {
         // ---- warps for the depth pairs ----
         const int sets = p.l > 0 ? p.sets() : 0;

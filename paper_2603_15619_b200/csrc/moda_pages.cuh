@@ -189,6 +189,7 @@ pages_write_kernel(const PagesRowsParams p) {
     __shared__ __align__(16) float s_scale[kPageBlock], s_ext[2][SETS][D];   // largest and smallest of a set of rows
     __shared__ uint32_t s_most[kPagesThreads / 32];
     const int b = blockIdx.z, hk = blockIdx.y, tid = threadIdx.x;
+    grid_dependency_wait();
     PagesRows w;
     if (!pages_rows<false>(p, b, w)) return;
     const int tile = p.tile(b, w.blk);
@@ -322,6 +323,7 @@ pages_read_kernel(const PagesRowsParams p) {
     constexpr int KW = D / 4 + 4;
     __shared__ __align__(16) uint32_t s_v[kPageBlock][KW];
     const int b = blockIdx.z, hk = blockIdx.y, tid = threadIdx.x;
+    grid_dependency_wait();
     PagesRows w;
     if (!pages_rows<true>(p, b, w)) return;
     const int tile = p.tile(b, w.blk);
@@ -620,6 +622,7 @@ pages_select_one_kernel(const PagesSelectParams p) {
     uint32_t* s_key = s_one + 2 * p.G * (D / 4);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int ranks = gridDim.x, rank = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
+    grid_dependency_wait();
     const SelectParts x(p, b);
     uint32_t mn = 0xffffffffu, mx = 0u;
     if (x.some()) {
@@ -655,6 +658,7 @@ pages_rate_kernel(const PagesSelectParams p) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int hk0 = int(blockIdx.y) * kSelectWarps, heads = min(p.Hk - hk0, kSelectWarps), b = blockIdx.z;
     const int at_once = kSelectWarps / heads;                        // steps that the warps take side by side
+    grid_dependency_wait();
     const SelectParts x(p, b);
     const int first = int(blockIdx.x) * at_once * p.rounds * STEP;
     if (!x.some() || first >= x.old) return;

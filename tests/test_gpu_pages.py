@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2603_15619_b200 as moda
+from paper_2603_15619_b200 import synthetic
 
 import pages_ref as ref
 
@@ -309,6 +310,100 @@ def test_same_bits_again_on_another_stream_and_captured():
     torch.cuda.synchronize()
     for got in (second, third, fourth):
         assert all(torch.equal(x, y) for x, y in zip(first, got))
+
+
+def test_captured_behind_copies_and_other_streams():
+    # the calls as a graph's first node, behind a copy, and behind two streams at once: replays see what is in the buffers then
+    B, lens, H, Hk, d = 2, [400, 129], 4, 2, 64
+    pages, bounds, table, dev = ref.make(B, 400, Hk, d, 64, lens, seed=7)
+    rng = np.random.default_rng(3)
+    q = [ref.put(ref.bf16(rng.standard_normal((B, H, d)))) for _ in range(2)]
+    rows = [ref.put(ref.bf16(rng.standard_normal((B, 1, Hk, d)))) for _ in range(2)]
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    ends = n - 1
+    names = [torch.tensor([[[0, 2, 5], [1, 4, 6]], [[0, 1, 2], [1, 2, -1]]], dtype=torch.int32, device="cuda"),
+             torch.tensor([[[3, 4, 6], [0, 1, 2]], [[2, -1, -1], [0, 2, -1]]], dtype=torch.int32, device="cuda")]
+    own = [t.clone() for t in dev[:2]]
+    qs, row, index, ix2 = q[0].clone(), rows[0].clone(), names[0].clone(), torch.empty_like(names[0])
+
+    def first():
+        return moda.moda_attn_decode_e4m3(qs, own[0], dev[2], n, None, 400, 0, 0.2, index=index)
+
+    def copied():
+        ix2.copy_(index)
+        return moda.moda_attn_decode_e4m3(qs, own[0], dev[2], n, None, 400, 0, 0.2, index=ix2)
+
+    def joined():
+        here, beside = torch.cuda.current_stream(), torch.cuda.Stream()
+        beside.wait_stream(here)
+        with torch.cuda.stream(beside):
+            ix2.copy_(index)
+        moda.moda_kv_write_e4m3(own[0], row, row, dev[2], start=ends, bounds=own[1])
+        here.wait_stream(beside)
+        out = moda.moda_attn_decode_e4m3(qs, own[0], dev[2], n, None, 400, 0, 0.2, index=ix2)
+        return (*out, moda.moda_kv_select_blocks(qs, own[1], dev[2], n, 400, 3, 1), *moda.moda_kv_read_e4m3(own[0], dev[2], n, 400))
+
+    for step in (first, copied, joined):
+        step()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = step()
+        for i in (1, 0):
+            qs.copy_(q[i]), row.copy_(rows[i]), index.copy_(names[i])
+            for t, src in zip(own, dev[:2]):
+                t.copy_(src)
+            graph.replay()
+            got_i = [t.clone() for t in got]
+            for t, src in zip(own, dev[:2]):
+                t.copy_(src)
+            assert all(torch.equal(a, b) for a, b in zip(got_i, step()))
+        del graph
+    assert moda.moda_last_status() == 0
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_behind_calls_whose_kernels_start_early(d):
+    # what the calls over the pages read is written by calls that launch their own last kernels beside one another: the same bits with and without a wait on the host in between
+    B, T, H, l = 2, 700, 4, 3
+    x = synthetic.make(synthetic.Workload("chain", B=B, T=T, H=H, d=d, l=l), seed=3, device="cuda:0")
+    cache = moda.alloc_depth_cache(B, T, H, d, l, "cuda:0")
+    for i in range(l):
+        moda.moda_depth_cache_append(cache, i, x["Kd"][i].contiguous(), x["Vd"][i].contiguous())
+    n = torch.tensor([T, T - 130], dtype=torch.int32, device="cuda")
+    most = -(-T // 64)
+    table = torch.arange(B * most, dtype=torch.int32, device="cuda").reshape(B, most)
+    scale = d ** -0.5
+
+    def chain(wait):
+        pages, bounds = torch.zeros_like(moda.alloc_kv_pages_e4m3(B * most, 64, H, d)), torch.zeros_like(moda.alloc_kv_bounds(B * most, 64, H, d))
+        steps = []
+        def then(*out):
+            if wait:
+                torch.cuda.synchronize()
+            steps.extend(out)
+            return out
+        O, LSE = then(*moda.moda_attn_fwd(x["Q"], x["K"], x["V"], cache, l, scale))
+        _, dK, dV, _ = moda.moda_attn_bwd(x["Q"], x["K"], x["V"], cache, O, x["dO"], LSE, l, scale)
+        then(dK, dV)
+        moda.moda_kv_write_e4m3(pages, dK, dV, table, n_new=n, bounds=bounds)
+        then(pages, bounds)
+        q = dK[:, 5].contiguous()
+        index, = then(moda.moda_kv_select_blocks(q, bounds, table, n, T, 4, 1))
+        o, lse = then(*moda.moda_attn_decode_e4m3(q, pages, table, n, None, T, 0, scale, index=index))
+        moda.moda_kv_write_e4m3(pages, o[:, None], o[:, None], table, start=n - 1, bounds=bounds)
+        K, V = then(*moda.moda_kv_read_e4m3(pages, table, n, T))
+        then(*moda.moda_attn_decode(q, K, V, x["Kd"].new_zeros((1, B, H, 2, d)), T, 1, scale))
+        moda.moda_kv_write_e4m3(pages, K, V, table, n_new=n - 3, bounds=bounds)
+        then(*moda.moda_attn_decode_e4m3(o, pages, table, n, None, T, 0, scale))
+        return steps
+
+    want = [t.clone() for t in chain(True)]
+    for _ in range(20):
+        got = chain(False)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert moda.moda_last_status() == 0
 
 
 def test_pages_far_from_the_first():
