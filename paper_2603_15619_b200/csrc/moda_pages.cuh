@@ -177,8 +177,8 @@ constexpr int kPagesThreads = 256;
 
 // grid (blocks that T rows can touch, Hk, B): a CTA quantises the rows of one block of one head, and where `bounds` is given reads what the block's earlier
 // keys left and writes the bounds anew.  It is the only one that writes the block (a page belongs to one sequence).
-// 65536 rows of 8 heads, d = 128: 82.5 us, 5.0 TB/s (63.4 at the copy rate).  Bound by the instructions that it issues: 129 with a branch per element, 90.5 without, 83 with packed
-// products and three-operand extremes.  A token of 64 sequences: 7.3 us, a chain of loads, quantisation, extremes and three barriers.
+// 65536 rows of 8 heads, d = 128: 82 us, 5.0 TB/s (63.4 at the copy rate).  Bound by the instructions that it issues: 129 with a branch per element, 90.5 without, 83 with packed
+// products and three-operand extremes.  A token of 64 sequences: 6.9 us, a chain of loads, quantisation, extremes and three barriers.
 template <int D>
 __global__ void __launch_bounds__(kPagesThreads)
 pages_write_kernel(const PagesRowsParams p) {
@@ -314,7 +314,7 @@ pages_write_kernel(const PagesRowsParams p) {
     }
 }
 
-// grid (blocks that T rows can touch, Hk, B): rows of one block of one head, as bf16(scale * code).  65536 rows of 8 heads, d = 128: 78.4 us, 5.2 TB/s; two of three bytes
+// grid (blocks that T rows can touch, Hk, B): rows of one block of one head, as bf16(scale * code).  65536 rows of 8 heads, d = 128: 77.5 us, 5.2 TB/s; two of three bytes
 // are written, and a fill of the outputs alone takes 69 us.
 template <int D>
 __global__ void __launch_bounds__(kPagesThreads)

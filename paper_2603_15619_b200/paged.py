@@ -13,6 +13,7 @@ keeps the pages, which sequence has which, and the lengths.
     cache.release(b)                                     # sequence b has ended: its pages are free, its place is empty
 
 The host decides which page a sequence gets, so it knows every length: ``n_new`` is a list of numbers.  Positional information has to be in the keys.
+``attend`` and ``select`` can be captured into a CUDA graph: a replay takes the lengths and pages of its time, up to ``longest`` positions.  ``write`` and ``release`` cannot.
 """
 from __future__ import annotations
 
@@ -84,20 +85,22 @@ class PagedCache:
         """K, V bf16 [B,T,H_kv,d] of the first T (None: the longest sequence's) positions; zeros behind a sequence's last one."""
         return binding.moda_kv_read_e4m3(self.pages, self.table, self.lens, self.longest if T is None else T)
 
-    def select(self, q, n_blocks: int, n_recent: int = 1):
-        """The blocks that a token attends to, [B, H_kv, n_blocks]: also for the layers or steps that use them again (``attend(..., index=...)``)."""
+    def select(self, q, n_blocks: int, n_recent: int = 1, longest=None):
+        """The blocks that a token attends to, [B, H_kv, n_blocks]: also for the layers or steps that use them again (``attend(..., index=...)``).  ``longest``: positions of a
+        sequence that the call is for (None: of the longest now); ``max_len`` in a graph that is replayed while sequences grow."""
         if self.bounds is None:
             raise ValueError("this cache keeps no bounds")
-        self.index = binding.moda_kv_select_blocks(q, self.bounds, self.table, self.lens, self.longest, n_blocks, n_recent)
+        self.index = binding.moda_kv_select_blocks(q, self.bounds, self.table, self.lens, self.longest if longest is None else longest, n_blocks, n_recent)
         return self.index
 
-    def attend(self, q, depth_kv_token, l, scale, n_blocks=None, n_recent: int = 1, index=None, O=None, LSE=None, workspace=None):
-        """The step of the token written last: O [B,H,d], LSE [B,H].  With ``n_blocks`` over so many selected blocks of 64 positions, with ``index`` over those."""
+    def attend(self, q, depth_kv_token, l, scale, n_blocks=None, n_recent: int = 1, index=None, O=None, LSE=None, workspace=None, longest=None):
+        """The step of the token written last: O [B,H,d], LSE [B,H].  With ``n_blocks`` over so many selected blocks of 64 positions, with ``index`` over those.
+        ``longest`` as for ``select``."""
         if n_blocks is not None:
             if index is not None:
                 raise ValueError("n_blocks or index, not both")
-            index = self.select(q, n_blocks, n_recent)
-        return binding.moda_attn_decode_e4m3(q, self.pages, self.table, self.lens, depth_kv_token, self.longest, l, scale, index=index, O=O, LSE=LSE,
+            index = self.select(q, n_blocks, n_recent, longest)
+        return binding.moda_attn_decode_e4m3(q, self.pages, self.table, self.lens, depth_kv_token, self.longest if longest is None else longest, l, scale, index=index, O=O, LSE=LSE,
                                              workspace=workspace)
 
     def release(self, b: int):

@@ -69,6 +69,31 @@ def test_prompt_tokens_release_and_reuse(H, Hk, d, page):
     assert moda.moda_last_status() == 0
 
 
+def test_a_captured_step_takes_the_lengths_of_its_replay():
+    B, H, Hk, d, l, scale = 2, 8, 2, 128, 2, 0.1
+    g = torch.Generator(device="cuda").manual_seed(1)
+    new = lambda *n: torch.randn(n, generator=g, device="cuda", dtype=torch.bfloat16)
+    cache = moda.PagedCache(B, Hk, d, num_pages=20, max_len=600)
+    cache.write(new(B, 190, Hk, d), new(B, 190, Hk, d), n_new=[190, 40])
+    q, depth = new(B, H, d), new(l, B, Hk, 2, d)
+
+    def step(**kw):
+        return (*cache.attend(q, depth, l, scale, **kw), *cache.attend(q, depth, l, scale, n_blocks=3, n_recent=1, **kw), cache.index)
+
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(longest=cache.max_len)
+    for T in (1, 130, 64):
+        cache.write(new(B, T, Hk, d), new(B, T, Hk, d))
+        q.copy_(new(B, H, d))
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(got, step()))
+    cache.release(0)
+    graph.replay()
+    assert all(torch.equal(a, b) for a, b in zip(got, step())) and torch.isfinite(got[1][1]).all() and (got[0][0] != 0).any()
+
+
 def test_example_runs():
     spec = importlib.util.spec_from_file_location("paged_cache_example", os.path.join(ROOT, "examples", "paged_cache.py"))
     module = importlib.util.module_from_spec(spec)
