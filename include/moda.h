@@ -623,6 +623,8 @@ int moda_attn_decode_shared(const void* q, const void* K_prefix, const void* V_p
  *                         workspace : moda_decode_e4m3_workspace_bytes.  B <= 2048.  Two launches.
  *
  * The products take the codes as they are (exact in f16), q times a power of two, and weights rounded to f16; scales, maxima, sums and the accumulators are fp32.
+ * A weight of the value product is p_j scale_j, and W the largest of a query head's, rows of zeros (which add nothing) left out: it is off by 2^-11 of itself, or by
+ * up to 2^-39 W where it is below 2^-28 W.  That shows in a feature alone in which the rows of the largest weights have codes 0.
  * Sums in an order that depends on the lengths of all sequences and the device's SM count: the same call gives the same bits.
  * Ownership, asynchrony and error codes as for the other calls.
  */

@@ -17,8 +17,9 @@
 //   lanes have, turned 8 x 8 at a time.
 //
 // Codes are exact in f16 and so is q once a row is scaled by a power of two (below 2^-40 of its largest element it is rounded).  Keys' scales multiply scores, in fp32.
-// Values' scales go into the weights: w = exp2(s + log2(scale) - m'), with a running maximum m' of its own, 2^14 below the largest f16 power;
-// weights are rounded to f16 (2^-11) for the product, the row sum and both maxima are fp32.
+// Values' scales go into the weights: w = exp2(s + log2(scale) - m'), with a running maximum m' of its own, so that the largest weight is 2^14;
+// weights are rounded to f16 for the product (2^-11; below 2^-28 of the largest by up to 2^-39 of it), the row sum and both maxima are fp32.  A row of zeros, whose scale is 1
+// by the format, has weight 0 in the product and leaves m' alone: beside it, rows below 2^-28 of it would lose bits for nothing.
 //
 // 32 sequences to 8192, 64 heads on 8, d = 128, 24 depth pairs: 59.2 us, of which the merge is 5; the bytes take 43.6 at the copy rate.  Read in this order by these warps
 // without any arithmetic they take 45 (5.97 TB/s); the rest is that SMs which share their path to L2 with more others stream up to 20 % slower (equal runs end
@@ -387,10 +388,12 @@ pages_split_kernel(const PagesDecodeParams p) {
         for (int j = 0; j < 4; ++j) { c[j][0] = 0.f; c[j][1] = 0.f; c[j][2] = 0.f; c[j][3] = 0.f; }
         cp_async_wait<NP - 1>();
         __syncwarp();
+        bool one = false;                                            // a value row of this lane's has scale 1, so that it may be one of zeros
         if (rows > 0) {
             {
                 // scales in the order in which the lanes have the keys: [2 (key / 16) + key % 2][key % 16 / 2]; of the values, their logarithms
                 const float2 k = *reinterpret_cast<const float2*>(own + 2 * lane), v = *reinterpret_cast<const float2*>(own + kPageBlock + 2 * lane);
+                one = v.x == 1.f || v.y == 1.f;
                 __syncwarp();
                 float* to = own + (lane >> 3) * 16 + (lane & 7);
                 to[0] = k.x;
@@ -420,6 +423,28 @@ pages_split_kernel(const PagesDecodeParams p) {
         }
         __syncwarp();                                                // everyone has read the keys; the scales are in order
         pass_on(u, 0);
+        if (__any_sync(0xffffffffu, one)) {
+            // Rows of zeros add nothing to the weighted sum, and their scale is not of their size: weight 0 there, so that the others' keep their bits (in the row sum they count).
+            cp_async_wait<NP - 1>();
+            __syncwarp();
+            uint32_t some[4] = {0u, 0u, 0u, 0u};                     // a byte per position 16 (lane % 4) ..: not 0 where it has a code that is not
+#pragma unroll 4
+            for (int k = 0; k < PIECE / 512; ++k) {
+                const uint4 x = *reinterpret_cast<const uint4*>(ring + slot * PIECE + k * 512 + lane * 16);
+                some[0] |= x.x; some[1] |= x.y; some[2] |= x.z; some[3] |= x.w;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                for (int off = 4; off < 32; off <<= 1) some[i] |= __shfl_xor_sync(0xffffffffu, some[i], off);
+                if (lane < 4) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if ((some[i] >> (8 * k) & 0x7fu) == 0u) own[kPageBlock + 16 * lane + 8 * (k & 1) + 2 * i + (k >> 1)] = -INFINITY;
+                }
+            }
+            __syncwarp();
+        }
         uint32_t pw[8];                                              // weights of keys 16 t + 4 j, + 1 (and + 2, + 3) of head g
         if (rows > 0) {
             float s[8][2], x[8];                                     // scores of this lane's keys a, a + 2, ..; log2 of the values' scales
