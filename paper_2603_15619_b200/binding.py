@@ -1066,6 +1066,8 @@ def moda_attn_decode_e4m3(q, pages, block_table, seq_lens, depth_kv_token, max_s
     _int32(seq_lens, "seq_lens", (B,))
     if index is not None and (index.dtype != torch.int32 or index.dim() != 3 or tuple(index.shape[:2]) != (B, Hk)):
         raise ValueError("index must be an int32 [B, H_kv, n] tensor")
+    if index is not None and index.shape[2] < 1:                            # (its address is null, which to the C call means all blocks)
+        raise ValueError("index names no block")
     if l > 0 and depth_kv_token is None:
         raise ValueError("depth_kv_token must be a bf16 [l, B, H_kv, 2, d] tensor")
     O = _new_like(q, stream) if O is None else _given(O, B * H * d, torch.bfloat16)

@@ -592,7 +592,7 @@ PyObject* decode_e4m3(PyObject*, PyObject* const* a, Py_ssize_t n) {
         !int_arg(a[6], l) || l < 0 || !float_arg(a[7], scale)) return none();
     if ((q = dense(a[0], at::kBFloat16, 3)) == nullptr || !small(*q) || q->size(0) != s.B || q->size(2) != s.d) return none();
     if (l > 0 && ((depth = dense(a[4], at::kBFloat16, 5)) == nullptr || !shape_is(*depth, {l, s.B, s.Hk, 2, s.d}))) return none();
-    if (a[8] != Py_None && ((index = dense(a[8], at::kInt, 3)) == nullptr || !small(*index) || index->size(0) != s.B || index->size(1) != s.Hk)) return none();
+    if (a[8] != Py_None && ((index = dense(a[8], at::kInt, 3)) == nullptr || !small(*index) || index->size(0) != s.B || index->size(1) != s.Hk || index->size(2) < 1)) return none();
     const int H = int(q->size(1));
     if (!optional_dense(a[9], O) || !optional_dense(a[10], LSE) || !optional_dense(a[11], ws) || !holds(O, at::kBFloat16, q->numel()) ||
         !holds(LSE, at::kFloat, int64_t(s.B) * H)) return none();
