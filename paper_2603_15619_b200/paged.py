@@ -46,7 +46,7 @@ class PagedCache:
         return len(self._free)
 
     def _reserve(self, n_new):
-        """Pages for n_new[b] more positions of every sequence, or an error and nothing changed."""
+        """Pages for n_new[b] more positions of every sequence, as a list a sequence, or an error.  They are still free: ``_take`` them."""
         need = []
         for b, n in enumerate(n_new):
             end = self.lengths[b] + n
@@ -55,15 +55,20 @@ class PagedCache:
             need.append(max(-(-end // self.page_size) - len(self._owned[b]), 0))
         if sum(need) > len(self._free):
             raise ValueError(f"{sum(need)} pages required, {len(self._free)} are free")
-        at, pages = [], []
-        for b, n in enumerate(need):
-            for _ in range(n):
-                at.append(b * self.most + len(self._owned[b]))
-                self._owned[b].append(self._free.pop())
-                pages.append(self._owned[b][-1])
+        free = iter(reversed(self._free))
+        return [[next(free) for _ in range(n)] for n in need]
+
+    def _enter(self, pages, taken=True):
+        """Into the table, behind those of each sequence (or out of it again)."""
+        at = [b * self.most + len(self._owned[b]) + i for b, own in enumerate(pages) for i in range(len(own))]
         if at:
-            device = self.table.device
-            self.table.view(-1).index_copy_(0, torch.tensor(at, device=device), torch.tensor(pages, device=device, dtype=torch.int32))
+            device, number = self.table.device, [p if taken else -1 for own in pages for p in own]
+            self.table.view(-1).index_copy_(0, torch.tensor(at, device=device), torch.tensor(number, device=device, dtype=torch.int32))
+
+    def _take(self, pages):
+        for own, more in zip(self._owned, pages):
+            own.extend(more)
+            del self._free[len(self._free) - len(more):]
 
     def write(self, K, V, n_new=None):
         """Appends the first ``n_new[b]`` (None: all T) rows of K, V [B,T,H_kv,d] to every sequence."""
@@ -75,9 +80,15 @@ class PagedCache:
             raise ValueError("n_new must be B numbers from 0 to T")
         if K.shape != V.shape or K.dtype != torch.bfloat16 or V.dtype != torch.bfloat16 or not (K.is_contiguous() and V.is_contiguous()):
             raise ValueError("K and V must be contiguous bf16 tensors of one shape")
-        self._reserve(count)
-        more = None if n_new is None else torch.tensor(count, device=self.lens.device, dtype=torch.int32)
-        binding.moda_kv_write_e4m3(self.pages, K, V, self.table, start=self.lens, n_new=more, bounds=self.bounds)
+        pages = self._reserve(count)
+        self._enter(pages)
+        try:
+            more = None if n_new is None else torch.tensor(count, device=self.lens.device, dtype=torch.int32)
+            binding.moda_kv_write_e4m3(self.pages, K, V, self.table, start=self.lens, n_new=more, bounds=self.bounds)
+        except Exception:                                      # refused: nothing has happened
+            self._enter(pages, taken=False)
+            raise
+        self._take(pages)
         self.lens += T if more is None else more
         self.lengths = [a + n for a, n in zip(self.lengths, count)]
 

@@ -1,0 +1,55 @@
+"""PagedCache: what it does with calls that are refused late (on the CPU, with the kernels' calls left out)."""
+import pytest
+import torch
+
+import paper_2603_15619_b200 as moda
+from paper_2603_15619_b200 import binding
+
+BF16 = torch.bfloat16
+
+
+def cache(**kw):
+    return moda.PagedCache(**{**dict(B=3, H_kv=2, d=64, num_pages=7, max_len=300, page_size=128, device="cpu"), **kw})
+
+
+def rows(T, B=3):
+    return torch.zeros((B, T, 2, 64), dtype=BF16)
+
+
+@pytest.fixture
+def quiet(monkeypatch):
+    made = []
+    monkeypatch.setattr(binding, "moda_kv_write_e4m3", lambda *a, **k: made.append("write"))
+    monkeypatch.setattr(binding, "moda_kv_select_blocks", lambda q, bounds, table, lens, longest, n, recent: torch.zeros((3, 2, n), dtype=torch.int32))
+    monkeypatch.setattr(binding, "moda_attn_decode_e4m3", lambda *a, **k: made.append("attend"))
+    return made
+
+
+def state(c):
+    return c.table.tolist(), c.lens.tolist(), list(c.lengths), [list(x) for x in c._owned], list(c._free)
+
+
+def test_a_write_that_the_call_refuses_takes_no_pages(quiet, monkeypatch):
+    c = cache()
+    c.write(rows(100), rows(100), n_new=[100, 0, 128 - 28])
+    before = state(c)
+
+    def refuse(*a, **k):
+        raise moda.ModaError(-2, "moda_kv_write_e4m3")
+
+    for n_new in (None, [150, 130, 0], [0, 1, 0]):
+        with monkeypatch.context() as m:
+            m.setattr(binding, "moda_kv_write_e4m3", refuse)
+            with pytest.raises(moda.ModaError):
+                c.write(rows(150), rows(150), n_new=n_new)
+        assert state(c) == before
+    c.write(rows(1), rows(1))                                     # and the next one gets them
+    assert c.lengths == [101, 1, 101] and [len(x) for x in c._owned] == [1, 1, 1]
+
+
+def test_tensors_that_are_not_on_a_device_are_refused_without_effect():
+    c = cache()
+    before = state(c)
+    with pytest.raises(ValueError):
+        c.write(rows(200), rows(200))
+    assert state(c) == before
