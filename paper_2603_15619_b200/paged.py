@@ -80,6 +80,8 @@ class PagedCache:
             raise ValueError("n_new must be B numbers from 0 to T")
         if K.shape != V.shape or K.dtype != torch.bfloat16 or V.dtype != torch.bfloat16 or not (K.is_contiguous() and V.is_contiguous()):
             raise ValueError("K and V must be contiguous bf16 tensors of one shape")
+        if max(count) == 0:
+            return
         pages = self._reserve(count)
         self._enter(pages)
         try:
@@ -94,7 +96,12 @@ class PagedCache:
 
     def read(self, T=None):
         """K, V bf16 [B,T,H_kv,d] of the first T (None: the longest sequence's) positions; zeros behind a sequence's last one."""
-        return binding.moda_kv_read_e4m3(self.pages, self.table, self.lens, self.longest if T is None else T)
+        T = self.longest if T is None else int(T)
+        if T < 0:
+            raise ValueError("T >= 0 required")
+        if T == 0:
+            return tuple(torch.empty((self.B, 0, self.H_kv, self.d), device=self.pages.device, dtype=torch.bfloat16) for _ in range(2))
+        return binding.moda_kv_read_e4m3(self.pages, self.table, self.lens, T)
 
     def select(self, q, n_blocks: int, n_recent: int = 1, longest=None):
         """The blocks that a token attends to, [B, H_kv, n_blocks]: also for the layers or steps that use them again (``attend(..., index=...)``).  ``longest``: positions of a

@@ -1,4 +1,4 @@
-"""PagedCache: what it does with calls that are refused late (on the CPU, with the kernels' calls left out)."""
+"""PagedCache: calls that are refused late and calls with nothing to do (on the CPU, with the kernels' calls left out)."""
 import pytest
 import torch
 
@@ -53,3 +53,19 @@ def test_tensors_that_are_not_on_a_device_are_refused_without_effect():
     with pytest.raises(ValueError):
         c.write(rows(200), rows(200))
     assert state(c) == before
+
+
+def test_nothing_to_write_and_nothing_to_read(quiet):
+    c = cache()
+    K, V = c.read()
+    assert K.shape == V.shape == (3, 0, 2, 64) and K.dtype == V.dtype == BF16
+    c.write(rows(0), rows(0))
+    c.write(rows(0), rows(0), n_new=[0, 0, 0])
+    assert c.lengths == [0, 0, 0] and c.free_pages == 7 and quiet == []
+    for bad in (dict(K=rows(0).float(), V=rows(0)), dict(K=rows(0), V=rows(1)), dict(K=rows(0), V=rows(0), n_new=[0, 0, 1]), dict(K=rows(0, B=2), V=rows(0, B=2))):
+        with pytest.raises(ValueError):
+            c.write(**bad)
+    c.write(rows(5), rows(5))
+    assert c.read(0)[0].shape == (3, 0, 2, 64)
+    with pytest.raises(ValueError):
+        c.read(-1)
