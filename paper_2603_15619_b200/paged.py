@@ -35,6 +35,7 @@ class PagedCache:
         self.lengths = [0] * B                                 # what `lens` holds
         self._owned = [[] for _ in range(B)]
         self._free = list(range(num_pages - 1, -1, -1))
+        self._turns = [0] * B                                  # sequences that have had each place before
         self.index = None                                      # of the last selection
 
     @property
@@ -104,12 +105,20 @@ class PagedCache:
         return binding.moda_kv_read_e4m3(self.pages, self.table, self.lens, T)
 
     def select(self, q, n_blocks: int, n_recent: int = 1, longest=None):
-        """The blocks that a token attends to, [B, H_kv, n_blocks]: also for the layers or steps that use them again (``attend(..., index=...)``).  ``longest``: positions of a
-        sequence that the call is for (None: of the longest now); ``max_len`` in a graph that is replayed while sequences grow."""
+        """The blocks that a token attends to, [B, H_kv, n_blocks]: also for the layers or steps that use them again (``attend(..., index=...)``), until a sequence opens a
+        block or its place changes hands: an older index does not have the newest positions, whatever ``n_recent`` was, and ``attend`` refuses it (this tensor
+        itself: not a copy, and not one that a graph selects anew).  ``longest``: positions of a sequence that the call is for (None: of the longest now); ``max_len`` in a graph
+        that is replayed while sequences grow."""
         if self.bounds is None:
             raise ValueError("this cache keeps no bounds")
         self.index = binding.moda_kv_select_blocks(q, self.bounds, self.table, self.lens, self.longest if longest is None else longest, n_blocks, n_recent)
+        if not (self.index.is_cuda and torch.cuda.is_current_stream_capturing()):      # a graph's is made anew by every replay
+            self.index.selected_for = (self._turns, *self._held())
         return self.index
+
+    def _held(self):
+        """Blocks of every place, and whose they are."""
+        return [-(-n // 64) for n in self.lengths], list(self._turns)
 
     def attend(self, q, depth_kv_token, l, scale, n_blocks=None, n_recent: int = 1, index=None, O=None, LSE=None, workspace=None, longest=None):
         """The step of the token written last: O [B,H,d], LSE [B,H].  With ``n_blocks`` over so many selected blocks of 64 positions, with ``index`` over those.
@@ -118,6 +127,10 @@ class PagedCache:
             if index is not None:
                 raise ValueError("n_blocks or index, not both")
             index = self.select(q, n_blocks, n_recent, longest)
+        elif (made := getattr(index, "selected_for", None)) is not None:
+            blocks, turns = self._held()
+            if made[1] != blocks or (made[0] is self._turns and made[2] != turns):
+                raise ValueError("the index is older than a block that a sequence has opened since, or than a sequence: select again")
         return binding.moda_attn_decode_e4m3(q, self.pages, self.table, self.lens, depth_kv_token, self.longest if longest is None else longest, l, scale, index=index, O=O, LSE=LSE,
                                              workspace=workspace)
 
@@ -125,6 +138,7 @@ class PagedCache:
         """Sequence b has ended."""
         self._free.extend(reversed(self._owned[b]))
         self._owned[b] = []
+        self._turns[b] += 1
         self.lengths[b] = 0
         self.lens[b] = 0
         self.table[b] = -1

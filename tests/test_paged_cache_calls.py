@@ -1,4 +1,4 @@
-"""PagedCache: calls that are refused late and calls with nothing to do (on the CPU, with the kernels' calls left out)."""
+"""PagedCache: calls that are refused late, calls with nothing to do, an index that is older than a block (on the CPU, with the kernels' calls left out)."""
 import pytest
 import torch
 
@@ -69,3 +69,35 @@ def test_nothing_to_write_and_nothing_to_read(quiet):
     assert c.read(0)[0].shape == (3, 0, 2, 64)
     with pytest.raises(ValueError):
         c.read(-1)
+
+
+def test_an_index_is_refused_once_a_sequence_has_opened_a_block(quiet):
+    c, q = cache(), torch.zeros((3, 4, 64), dtype=BF16)
+    attend = lambda index, cache=c: cache.attend(q, None, 0, 0.1, index=index)
+    c.write(rows(100), rows(100), n_new=[63, 100, 0])
+    index = c.select(q, 2)
+    attend(index)
+    c.write(rows(1), rows(1), n_new=[1, 1, 0])                     # 64 and 101 positions: the same blocks
+    attend(index)
+    c.write(rows(1), rows(1), n_new=[1, 0, 0])                     # the 65th position is not in it, whatever n_recent was
+    with pytest.raises(ValueError, match="block"):
+        attend(index)
+    newer = c.select(q, 2)
+    attend(newer)
+    other = cache()                                                # a later layer's cache, with the same lengths and with others
+    other.write(rows(101), rows(101), n_new=[65, 101, 0])
+    attend(newer, other)
+    with pytest.raises(ValueError, match="block"):
+        attend(index, other)
+    c.release(1)
+    with pytest.raises(ValueError, match="block"):
+        attend(newer)
+    c.write(rows(100), rows(100), n_new=[0, 99, 0])
+    newest = c.select(q, 2)
+    c.release(1)
+    c.write(rows(100), rows(100), n_new=[0, 99, 0])                # as many positions, of another sequence
+    with pytest.raises(ValueError, match="sequence"):
+        attend(newest)
+    attend(torch.zeros((3, 2, 2), dtype=torch.int32))              # one of the caller's own making
+    c.attend(q, None, 0, 0.1, n_blocks=2)
+    assert quiet.count("attend") == 6
