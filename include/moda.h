@@ -619,10 +619,12 @@ int moda_attn_decode_shared(const void* q, const void* K_prefix, const void* V_p
  *                         workspace : moda_kv_select_workspace_bytes.  One launch or two.
  * moda_attn_decode_e4m3   the decode step: O, LSE, depth_kv_token, groups and scale as for moda_attn_decode_paged, with seq_lens[b] in 0 .. max_seq_len.  index (int32
  *                         [B][H_kv][n_blocks]) NULL: all blocks; else the blocks of the first min(n_blocks, ceil(seq_lens[b] / 64)) entries of a row, an entry that is no block
- *                         of the sequence being passed over (one that comes twice counts twice).  A token without any key has O = 0 and LSE = -inf.
+ *                         of the sequence being passed over (one that comes twice counts twice); blocks that it does not name, the newest among them, have no weight.
+ *                         A token without any key has O = 0 and LSE = -inf.
  *                         workspace : moda_decode_e4m3_workspace_bytes.  B <= 2048.  Two launches.
  *
- * The products take the codes as they are (exact in f16), q times a power of two, and weights rounded to f16; scales, maxima, sums and the accumulators are fp32.
+ * The products take the codes as they are (exact in f16), q times a power of two (exact in f16 above 2^-31 of a head's largest element, off by up to 2^-39 of that below),
+ * and weights rounded to f16; scales, maxima, sums and the accumulators are fp32.
  * A weight of the value product is p_j scale_j, and W the largest of a query head's, rows of zeros (which add nothing) left out: it is off by 2^-11 of itself, or by
  * up to 2^-39 W where it is below 2^-28 W.  That shows in a feature alone in which the rows of the largest weights have codes 0.
  * Sums in an order that depends on the lengths of all sequences and the device's SM count: the same call gives the same bits.

@@ -16,7 +16,8 @@
 //   O^T = V^T P^T, features as rows: the lane's value codes are those of feature g (and g + 8) of keys 16 t .. 16 t + 15, whose weights for head g are what the scores'
 //   lanes have, turned 8 x 8 at a time.
 //
-// Codes are exact in f16 and so is q once a row is scaled by a power of two (below 2^-40 of its largest element it is rounded).  Keys' scales multiply scores, in fp32.
+// Codes are exact in f16 and so is q once a row is scaled by a power of two, its elements above 2^-31 of the largest at least (those below by up to 2^-39 of it).  Keys'
+// scales multiply scores, in fp32.
 // Values' scales go into the weights: w = exp2(s + log2(scale) - m'), with a running maximum m' of its own, so that the largest weight is 2^14;
 // weights are rounded to f16 for the product (2^-11; below 2^-28 of the largest by up to 2^-39 of it), the row sum and both maxima are fp32.  A row of zeros, whose scale is 1
 // by the format, has weight 0 in the product and leaves m' alone: beside it, rows below 2^-28 of it would lose bits for nothing.

@@ -1,4 +1,4 @@
-"""Decode over pages in 8 bits where the value rows of a sequence differ most: rows of zeros, whose scale is 1 by the format, beside small ones, and rows of one feature."""
+"""Decode over pages in 8 bits where value rows differ most (rows of zeros, whose scale is 1 by the format, beside small ones, and rows of one feature), or elements of a query."""
 import numpy as np
 import pytest
 import torch
@@ -123,3 +123,26 @@ def test_a_row_of_one_feature_far_above_the_others(d, power):
     # the scales are 2^power / 448 and about 2 / 448, no weight is 2^16 below another: to 2^10 all are above 2^-28 of the largest and keep 2^-11
     if power <= 10:
         _check(O, LSE, want)
+
+
+@pytest.mark.parametrize("below", [20, 31, 33, 34])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_query_of_elements_of_very_different_sizes(d, below):
+    # the largest element of the query meets codes that are 0: the scores are those of elements 2^-below of it.  To 2^-31 they are exact, below they are off by half a step of
+    # f16 below its smallest normal number, 2^-25 where the largest is 2^14 or more: 2^-39 of the largest
+    n, H, Hk = 150, 8, 2
+    rng = np.random.default_rng(below)
+    K, V, q = rng.standard_normal((n, Hk, d)), rng.standard_normal((n, Hk, d)), rng.uniform(1.0, 2.0, (H, d)) * rng.choice([-1, 1], (H, d)) * 2.0 ** -below
+    K[:, :, 9], q[:, 9] = 0.0, 1.5
+    q, scale = ref.bf16(q), 2.0 ** below * d ** -0.5 * 0.5
+    O, LSE, (o, lse, o_tol, lse_tol), (pages, table) = _decode(ref.bf16(K), ref.bf16(V), q, scale)
+    if below > 31:
+        for k in range(Hk):
+            keys, values = ref.gather(pages, table, 0, k, n, 64, d)
+            ds = 1.5 * 2.0 ** -39 * np.abs(keys).sum(1).max() * scale          # of a score: all of its elements off by half a step
+            for h in range(k * (H // Hk), (k + 1) * (H // Hk)):
+                s = keys @ q[h].astype(np.float64) * scale
+                p = np.exp(s - lse[0, h])
+                lse_tol[0, h] += ds
+                o_tol[0, h] += np.expm1(2 * ds) * (p @ np.abs(values)) * 1.01      # a weight is off by a factor of exp(ds), the sum by as much; 1.01: their rounding on top
+    _check(O, LSE, (o, lse, o_tol, lse_tol))
