@@ -22,10 +22,10 @@
 // weights are rounded to f16 for the product (2^-11; below 2^-28 of the largest by up to 2^-39 of it), the row sum and both maxima are fp32.  A row of zeros, whose scale is 1
 // by the format, has weight 0 in the product and leaves m' alone: beside it, rows below 2^-28 of it would lose bits for nothing.
 //
-// 32 sequences to 8192, 64 heads on 8, d = 128, 24 depth pairs: 59.2 us, of which the merge is 5; the bytes take 43.6 at the copy rate.  Read in this order by these warps
+// 32 sequences to 8192, 64 heads on 8, d = 128, 24 depth pairs: 59.4 us, of which the merge is 5; the bytes take 43.6 at the copy rate.  Read in this order by these warps
 // without any arithmetic they take 45 (5.97 TB/s); the rest is that SMs which share their path to L2 with more others stream up to 20 % slower (equal runs end
 // after 45 to 61 us).  Runs that others take over when they are done cost more in partial results and in queries that wait behind the stream than they win (63 us
-// and more).  96 sequences to 1500, 24 heads on 8, d = 64: 31 us against 13.2: a block of half the bytes has the same softmax, three heads in columns for eight.
+// and more).  96 sequences to 1500, 24 heads on 8, d = 64: 31 to 32 us against 13.2: a block of half the bytes has the same softmax, three heads in columns for eight.
 // Products of e4m3 codes as they are (m16n8k32) are no faster, 67.0 against 66.2 us at that stage.
 #pragma once
 

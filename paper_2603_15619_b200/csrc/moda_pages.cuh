@@ -67,7 +67,7 @@ __device__ __forceinline__ void turn4x4(uint32_t& a, uint32_t& b, uint32_t& c, u
     d = __byte_perm(ab1, cd1, 0x7632);
 }
 
-// Instructions that take two fp32 numbers in a 64-bit register (pair_f32), or three: the write kernel is bound by the instructions that it issues.
+// Instructions that take two fp32 numbers in a 64-bit register (pair_f32), or three, for the write kernel, whose time went with the instructions that it issues.
 __device__ __forceinline__ void unpair_f32(uint64_t x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
 __device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
     uint64_t r;
@@ -96,10 +96,9 @@ __device__ __forceinline__ uint32_t times_bf16x2(uint32_t a, uint32_t b) {
 }
 
 // 16 features of a row that LANES adjacent lanes hold: their codes and the row's scale.  The depth cache's rule and bytes (but for the sign of a NaN), in fewer
-// instructions, which bound the write kernel: quotients two at a
-// time, q = RN(x r) with r = RN(1 / d) corrected by its exact remainder (Markstein's theorem, as div_rn in moda_cache.cuh; a scale's significand, m / 7 of 128 <= m < 256, is
-// never all ones); no element has a branch, as rows of which it would need one are brought into range first (exactly, by a power of two; or by 0, which makes of a row
-// with an infinite element what the division by infinity would), and signs come from the input's words.
+// instructions: quotients two at a time, q = RN(x r) with r = RN(1 / d) corrected by its exact remainder (Markstein's theorem, as div_rn in moda_cache.cuh; a scale's
+// significand, m / 7 of 128 <= m < 256, is never all ones); no element has a branch, as rows of which it would need one are brought into range first (exactly, by a power of
+// two; or by 0, which makes of a row with an infinite element what the division by infinity would), and signs come from the input's words.
 template <int LANES>
 __device__ __forceinline__ uint4 quantise_row16(const uint4& lo, const uint4& hi, float& scale) {
     uint32_t w8[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
@@ -177,8 +176,8 @@ constexpr int kPagesThreads = 256;
 
 // grid (blocks that T rows can touch, Hk, B): a CTA quantises the rows of one block of one head, and where `bounds` is given reads what the block's earlier
 // keys left and writes the bounds anew.  It is the only one that writes the block (a page belongs to one sequence).
-// 65536 rows of 8 heads, d = 128: 82 us, 5.0 TB/s (63.4 at the copy rate).  Bound by the instructions that it issues: 129 with a branch per element, 90.5 without, 83 with packed
-// products and three-operand extremes.  A token of 64 sequences: 6.9 us, a chain of loads, quantisation, extremes and three barriers.
+// 65536 rows of 8 heads, d = 128: 82 us, 5.0 TB/s (63.4 at the copy rate).  129 with a branch per element, 90.5 without, 83 with packed products
+// and three-operand extremes; now 71 % of the issue slots and 53 % of DRAM's peak (profiler): the CTAs of an SM load, compute and store in turn.  A token of 64 sequences: 6.9 us, a chain of loads, quantisation, extremes and three barriers.
 template <int D>
 __global__ void __launch_bounds__(kPagesThreads)
 pages_write_kernel(const PagesRowsParams p) {
